@@ -364,6 +364,70 @@ int mxq_slice_scale_tiled_batched(const mxq_ss_tiled_item *items, int count, int
 int mxq_slice_scale_batched_static(const mxq_ss_item *items, int count, int block,
                                    int src_fmt, int dst_fmt, mxq_stream stream);
 
+/*
+ * Products that read the codes (Sec. 3.5: W_t feeds the layer's matmul).
+ *
+ * mxq_matmul: D = A^ B^T, A^ [m, k] and B^ [n, k] the reconstructions of two MXFP8 E4M3 operands with their blocks along k,
+ *   D[i, j] = sum over blocks b of 2^(sa[i, b] + sb[j, b]) sum over k in b of Pa[i, k] Pb[j, k]
+ * as a linear layer takes it (activations times a weight's rows).  fmt must be MXQ_FP8_E4M3 (MXQ_ERR_FORMAT), block 32, 64
+ * or 128 (MXQ_ERR_BLOCK), k a multiple of block, m, n and k below 2^31 (MXQ_ERR_SIZE); m and n are any.  Sums are held in
+ * FP32 and rounded once to dst_dtype.  A poisoned block (scale byte 0xFF) makes its row or column of D quiet NaNs.  With
+ * m or n 0 nothing is done; with k 0 D is filled with zeros.  Results do not depend on timing.
+ *   a_codes, b_codes    [in]  device, m * k and n * k bytes, row-major, as mxq_quantize writes them
+ *   a_scales, b_scales  [in]  device, m * k / block and n * k / block bytes (plain order)
+ *   dst                 [out] device, [m, n] elements of dst_dtype, row-major; overlaps no input
+ */
+int mxq_matmul(const void *a_codes, const uint8_t *a_scales, const void *b_codes, const uint8_t *b_scales,
+               size_t m, size_t n, size_t k, int fmt, int block, void *dst, int dst_dtype, mxq_stream stream);
+
+/*
+ * Q_f (Eq. 1-3) of a row-major [rows, cols] matrix along its rows and of its transpose, from one read: what the three products
+ * of a linear layer's training step take.  Rows are padded with zeros to whole blocks in both results, so any shape goes:
+ *   codes    [out] device, [rows, cols rounded up to block], mxq_matrix_codes_bytes(rows, cols, block) bytes
+ *   scales   [out] device, [rows, that / block],            mxq_matrix_scales_bytes(rows, cols, block) bytes
+ *   codes_t  [out] device, [cols, rows rounded up to block], mxq_matrix_codes_bytes(cols, rows, block) bytes
+ *   scales_t [out] device, [cols, that / block],            mxq_matrix_scales_bytes(cols, rows, block) bytes
+ * codes and scales may both be null (only the transpose is wanted), or codes_t and scales_t.  fmt must be MXQ_FP8_E4M3, block
+ * 32, 64 or 128.  The bytes are those of mxq_quantize on the padded matrix and on its padded transpose.
+ */
+size_t mxq_matrix_codes_bytes(size_t rows, size_t cols, int block);
+size_t mxq_matrix_scales_bytes(size_t rows, size_t cols, int block);
+int mxq_quantize_matrix(const void *src, int src_dtype, size_t rows, size_t cols, int fmt, int block,
+                        void *codes, uint8_t *scales, void *codes_t, uint8_t *scales_t, mxq_stream stream);
+
+/*
+ * A mixture-of-experts layer for a few tokens (decoding) over experts held as codes: for each token t
+ *   choice   the top_k experts with the largest logits (equal ones: the lowest index; an expert whose logit is -inf is never
+ *            chosen, so a row of -inf alone chooses none and gives zeros); weights w = their softmax over the chosen experts
+ *            (renormalize != 0) or over all experts (renormalize == 0).  A NaN among a token's logits makes its output NaN.
+ *   out[t]   = sum over the chosen e of w[e] D_e (silu(G_e x[t]) * (U_e x[t])),  silu(v) = v / (1 + exp(-v))
+ * with G_e and U_e the first and the last `inner` rows of expert e's [2 * inner, hidden] up matrix and D_e its
+ * [hidden, inner] down matrix.  Weights enter as their reconstructions, x as it is; sums are held in FP32, the inner
+ * activations to 16 bits or more (24 for FP32 tokens).  Results do not depend on timing.  Only chosen experts are read.
+ *   layer     HOST struct, free to reuse when the call returns; fmt one of MXQ_FP8_E4M3, MXQ_FP4_E2M1, MXQ_INT8, MXQ_INT4
+ *             (MXQ_ERR_FORMAT), block 32, 64 or 128 (MXQ_ERR_BLOCK); hidden and inner non-zero multiples of block up to 2^20,
+ *             1 <= experts <= MXQ_MOE_EXPERTS_MAX (MXQ_ERR_SIZE)
+ *   x, out    device, [tokens, hidden] of dtype; no overlap.  tokens <= MXQ_MOE_TOKENS_MAX; 0 does nothing
+ *   logits    device, [tokens, experts] FP32, 16-byte aligned;  1 <= top_k <= min(experts, MXQ_MOE_TOP_K_MAX)
+ *   workspace device, 32-byte aligned, mxq_moe_workspace_bytes(tokens, top_k, inner, dtype) bytes or more (MXQ_ERR_SIZE); what
+ *             it holds before and after a call means nothing.  Calls whose work can overlap on the GPU must not share one
+ */
+#define MXQ_MOE_TOKENS_MAX 64
+#define MXQ_MOE_EXPERTS_MAX 512
+#define MXQ_MOE_TOP_K_MAX 16
+typedef struct mxq_moe_layer {
+    const void *up_codes;           /* [experts, 2 * inner, hidden] */
+    const uint8_t *up_scales;
+    const void *down_codes;         /* [experts, hidden, inner] */
+    const uint8_t *down_scales;
+    size_t hidden, inner;
+    int experts, fmt, block;
+} mxq_moe_layer;
+
+size_t mxq_moe_workspace_bytes(size_t tokens, int top_k, size_t inner, int dtype);   /* 0 for sizes that mxq_moe refuses */
+int mxq_moe(const mxq_moe_layer *layer, const void *x, int dtype, const float *logits, size_t tokens, int top_k,
+            int renormalize, void *out, void *workspace, size_t workspace_bytes, mxq_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -12,5 +12,6 @@ from .binding import (  # noqa: F401
     slice_scale_batched, slice_scale_batched_static, slice_scale_multi, quantize_tiled, slice_scale_tiled, slice_scale_tiled_batched, make_tiled_items, tile_scales, tiled_scales_bytes, status_string, STATIC_BATCH_MAX,
     slice_scale_pair_batched, make_pair_items,
     quantize_batched, make_q_items, dequantize_batched, make_dq_items,
+    matmul, quantize_matrix, linear_ste, moe, moe_workspace_bytes, MOE_TOKENS_MAX, MOE_EXPERTS_MAX, MOE_TOP_K_MAX,
     PreparedCall, prepare_quantize, prepare_slice_scale, prepare_dequantize, prepare_fake_quant, prepare_fake_quant_bwd,
 )

@@ -60,6 +60,12 @@ class _TiledItem(ctypes.Structure):
                 ("cols", ctypes.c_size_t), ("out_codes", ctypes.c_void_p), ("out_tiled_scales", ctypes.c_void_p)]
 
 
+class _MoeLayer(ctypes.Structure):
+    _fields_ = [("up_codes", ctypes.c_void_p), ("up_scales", ctypes.c_void_p), ("down_codes", ctypes.c_void_p),
+                ("down_scales", ctypes.c_void_p), ("hidden", ctypes.c_size_t), ("inner", ctypes.c_size_t),
+                ("experts", ctypes.c_int), ("fmt", ctypes.c_int), ("block", ctypes.c_int)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 _host = None            # the native module _mxq_host (csrc/host_calls.cpp): the plain case of the per-tensor calls
 
@@ -128,6 +134,18 @@ def load_library() -> ctypes.CDLL:
     L.mxq_slice_scale_pair_batched.restype = i
     L.mxq_slice_scale_batched_static.argtypes = [ctypes.POINTER(_Item), i, i, i, i, vp]
     L.mxq_slice_scale_batched_static.restype = i
+    L.mxq_matmul.argtypes = [vp, vp, vp, vp, sz, sz, sz, i, i, vp, i, vp]
+    L.mxq_matmul.restype = i
+    L.mxq_matrix_codes_bytes.argtypes = [sz, sz, i]
+    L.mxq_matrix_codes_bytes.restype = sz
+    L.mxq_matrix_scales_bytes.argtypes = [sz, sz, i]
+    L.mxq_matrix_scales_bytes.restype = sz
+    L.mxq_quantize_matrix.argtypes = [vp, i, sz, sz, i, i, vp, vp, vp, vp, vp]
+    L.mxq_quantize_matrix.restype = i
+    L.mxq_moe_workspace_bytes.argtypes = [sz, i, sz, i]
+    L.mxq_moe_workspace_bytes.restype = sz
+    L.mxq_moe.argtypes = [ctypes.POINTER(_MoeLayer), vp, i, vp, sz, i, i, vp, vp, sz, vp]
+    L.mxq_moe.restype = i
     for name in ("mxq_quantize", "mxq_slice_scale", "mxq_dequantize", "mxq_fake_quant", "mxq_fake_quant_bwd",
                  "mxq_slice_scale_batched"):
         getattr(L, name).restype = i
@@ -626,3 +644,178 @@ def slice_scale_batched_static(items: Sequence[Tuple[torch.Tensor, torch.Tensor,
         arr[k] = _Item(_dev(c, "codes"), _dev(s, "scales"), n, _dev(oc, "out_codes"), _dev(os_, "out_scales"))
     _check(L.mxq_slice_scale_batched_static(arr, len(items), block, FORMATS[src_fmt], FORMATS[dst_fmt],
                                             _stream(stream)), "mxq_slice_scale_batched_static")
+
+
+# ---- products that read the codes -----------------------------------------------------------------------------
+
+
+def _operand(t: torch.Tensor, what: str, nbytes: int, device: torch.device) -> int:
+    """The pointer of a code or scale buffer of at least `nbytes` bytes on `device`."""
+    if t.dtype != torch.uint8:
+        raise TypeError("%s must be uint8, got %s" % (what, t.dtype))
+    if t.numel() < nbytes:
+        raise ValueError("%s holds %d bytes, the operation takes %d" % (what, t.numel(), nbytes))
+    return _on(t, what, device)
+
+
+def _on(t: torch.Tensor, what: str, device: torch.device) -> int:
+    p = _dev(t, what)
+    if t.device != device:
+        raise ValueError("%s is on %s, the other tensors on %s" % (what, t.device, device))
+    return p
+
+
+class _Place:
+    """Makes `device` current and the work's stream (None: the device's current one) the allocator's while a call is put together:
+    temporary and result buffers then belong to the stream that uses them."""
+
+    __slots__ = ("device", "stream", "inner")
+
+    def __init__(self, device, stream):
+        self.device, self.stream, self.inner = device, stream, None
+
+    def __enter__(self):
+        if self.stream is not None:
+            s = self.stream if hasattr(self.stream, "cuda_stream") else torch.cuda.ExternalStream(int(self.stream), device=self.device)
+            if s.device != self.device:
+                raise ValueError("the stream is on %s, the tensors on %s" % (s.device, self.device))
+            self.inner = torch.cuda.stream(s)
+        elif self.device.index != torch.cuda.current_device():
+            self.inner = torch.cuda.device(self.device)
+        if self.inner is not None:
+            self.inner.__enter__()
+
+    def __exit__(self, *exc):
+        if self.inner is not None:
+            self.inner.__exit__(*exc)
+
+
+def matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor, b_scales: torch.Tensor, m: int, n: int, k: int,
+           fmt: str = "e4m3", block: int = 32, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+           stream=None) -> torch.Tensor:
+    """mxq_matmul: A^ B^T of two quantized operands [m, k] and [n, k] (``quantize``'s codes and scales), as [m, n] of
+    ``dtype`` (``out``'s where it is given)."""
+    L = _lib or load_library()
+    dev = a_codes.device
+    sizes = (m * k, m * k // block, n * k, n * k // block) if block > 0 and min(m, n, k) >= 0 else (0, 0, 0, 0)
+    if min(m, n, k) < 0:
+        raise ValueError("negative size")
+    ptrs = [_operand(t, what, size, dev) for t, what, size in zip((a_codes, a_scales, b_codes, b_scales),
+                                                                 ("a_codes", "a_scales", "b_codes", "b_scales"), sizes)]
+    with _Place(dev, stream):
+        if out is None:
+            out = torch.empty(m, n, dtype=dtype, device=dev)
+        elif out.numel() != m * n:
+            raise ValueError("out holds %d elements, the product %d" % (out.numel(), m * n))
+        _check(L.mxq_matmul(*ptrs, m, n, k, FORMATS[fmt], block, _on(out, "out", dev), _dtype_id(out), _stream(None)), "mxq_matmul")
+    return out
+
+
+def quantize_matrix(src: torch.Tensor, fmt: str = "e4m3", block: int = 32, rows: bool = True, cols: bool = True, stream=None):
+    """mxq_quantize_matrix: a 2-D tensor -> (codes, scales, codes_t, scales_t), its quantization along the rows and that of its
+    transpose, rows padded with zeros to whole blocks; ``rows=False`` / ``cols=False`` leave one of them out (None)."""
+    L = _lib or load_library()
+    if src.dim() != 2:
+        raise ValueError("quantize_matrix takes a [rows, cols] matrix")
+    r, c = src.shape
+    p, dt = _dev(src, "src"), _dtype_id(src)
+    with _Place(src.device, stream):
+        got = []
+        for wanted, x, y in ((rows, r, c), (cols, c, r)):
+            if wanted:
+                got += [torch.empty(L.mxq_matrix_codes_bytes(x, y, block), dtype=torch.uint8, device=src.device),
+                        torch.empty(L.mxq_matrix_scales_bytes(x, y, block), dtype=torch.uint8, device=src.device)]
+            else:
+                got += [None, None]
+        _check(L.mxq_quantize_matrix(p, dt, r, c, FORMATS[fmt], block, *[None if t is None else t.data_ptr() for t in got],
+                                     _stream(None)), "mxq_quantize_matrix")
+    return tuple(got)
+
+
+def _up(v: int, block: int) -> int:
+    return -(-v // block) * block
+
+
+class _LinearSTE(torch.autograd.Function):
+    """y = Q(x) Q(w)^T; backward dx = Q(dy) Q(w^T)^T and dw = Q(dy^T) Q(x^T)^T, the quantizers passed straight through."""
+
+    @staticmethod
+    def forward(ctx, x, w, block):
+        m, k, n = x.shape[0], x.shape[1], w.shape[0]
+        need_x, need_w = ctx.needs_input_grad[:2]
+        xc, xs, xct, xst = quantize_matrix(x, "e4m3", block, cols=need_w)
+        wc, ws, wct, wst = quantize_matrix(w, "e4m3", block, cols=need_x)
+        ctx.save_for_backward(xct, xst, wct, wst)
+        ctx.sizes, ctx.block, ctx.dtypes = (m, n, k), block, (x.dtype, w.dtype)
+        return matmul(xc, xs, wc, ws, m, n, _up(k, block), "e4m3", block, x.dtype)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        xct, xst, wct, wst = ctx.saved_tensors
+        (m, n, k), block = ctx.sizes, ctx.block
+        need_x, need_w = ctx.needs_input_grad[:2]
+        dc, ds, dct, dst = quantize_matrix(dy.contiguous(), "e4m3", block, rows=need_x, cols=need_w)
+        dx = matmul(dc, ds, wct, wst, m, k, _up(n, block), "e4m3", block, ctx.dtypes[0]) if need_x else None
+        dw = matmul(dct, dst, xct, xst, n, k, _up(m, block), "e4m3", block, ctx.dtypes[1]) if need_w else None
+        return dx, dw, None
+
+
+def linear_ste(x: torch.Tensor, w: torch.Tensor, block: int = 32) -> torch.Tensor:
+    """A linear layer whose three products run on MXFP8 E4M3 operands, differentiable: y = Q(x) Q(w)^T for x [..., k] and
+    w [n, k] (float32 or bfloat16), with dx = Q(dy) Q(w^T)^T and dw = Q(dy^T) Q(x^T)^T, each operand quantized in blocks
+    along the dimension that its product sums over and the quantizers passed straight through.  Any sizes; y and dx have x's type,
+    dw has w's.  The backward pass keeps the transposes' codes (a byte per element), not x and w."""
+    if _lib is None:
+        load_library()
+    if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
+        raise ValueError("linear_ste takes x [..., k] and w [n, k], got %s and %s" % (tuple(x.shape), tuple(w.shape)))
+    if block not in (32, 64, 128):
+        raise MxqError(-3, "linear_ste")
+    for t, what in ((x, "x"), (w, "w")):
+        _dtype_id(t)
+        if not t.is_cuda or t.device != x.device:
+            raise ValueError("%s must be a CUDA tensor on x's device (libmxq has no CPU path)" % what)
+    y = _LinearSTE.apply(x.reshape(-1, x.shape[-1]).contiguous(), w.contiguous(), block)
+    return y.view(*x.shape[:-1], w.shape[0])
+
+
+#: limits of ``moe`` (MXQ_MOE_*_MAX in include/mxq.h)
+MOE_TOKENS_MAX, MOE_EXPERTS_MAX, MOE_TOP_K_MAX = 64, 512, 16
+
+
+def moe_workspace_bytes(tokens: int, top_k: int, inner: int, dtype: torch.dtype = torch.bfloat16) -> int:
+    return load_library().mxq_moe_workspace_bytes(tokens, top_k, inner, F32 if dtype == torch.float32 else BF16)
+
+
+def moe(x: torch.Tensor, logits: torch.Tensor, up_codes: torch.Tensor, up_scales: torch.Tensor, down_codes: torch.Tensor,
+        down_scales: torch.Tensor, inner: int, top_k: int, fmt: str, block: int = 32, renormalize: bool = True,
+        out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """mxq_moe: a mixture-of-experts layer for up to MOE_TOKENS_MAX tokens x [tokens, hidden] with the router's float32 logits
+    [tokens, experts] over experts held as codes: up matrices [experts, 2 * inner, hidden] (gate rows first) and
+    down matrices [experts, hidden, inner], as ``quantize`` writes them.  ``workspace`` (uint8, ``moe_workspace_bytes``) saves
+    the allocation of one per call; calls that can overlap on the GPU must not share it."""
+    L = _lib or load_library()
+    if x.dim() != 2 or logits.dim() != 2 or logits.shape[0] != x.shape[0]:
+        raise ValueError("moe takes x [tokens, hidden] and logits [tokens, experts]")
+    if logits.dtype != torch.float32:
+        raise TypeError("logits are float32, got %s" % logits.dtype)
+    (tokens, hidden), experts, dev, dt = x.shape, logits.shape[1], x.device, _dtype_id(x)
+    weights = experts * hidden * max(inner, 0)
+    per = block if block > 0 else 1
+    ptrs = [_operand(t, what, size, dev) for t, what, size in
+            ((up_codes, "up_codes", codes_bytes(2 * weights, fmt)), (up_scales, "up_scales", 2 * weights // per),
+             (down_codes, "down_codes", codes_bytes(weights, fmt)), (down_scales, "down_scales", weights // per))]
+    if inner < 0:
+        raise ValueError("negative size")
+    layer = _MoeLayer(*ptrs, hidden, inner, experts, FORMATS[fmt], block)
+    with _Place(dev, stream):
+        if out is None:
+            out = torch.empty_like(x)
+        elif out.shape != x.shape or out.dtype != x.dtype:
+            raise ValueError("out must have x's shape and type")
+        if workspace is None:
+            workspace = torch.empty(L.mxq_moe_workspace_bytes(tokens, top_k, inner, dt), dtype=torch.uint8, device=dev)
+        _check(L.mxq_moe(ctypes.byref(layer), _dev(x, "x"), dt, _on(logits, "logits", dev), tokens, top_k, int(bool(renormalize)),
+                         _on(out, "out", dev), _operand(workspace, "workspace", 0, dev), workspace.numel(), _stream(None)), "mxq_moe")
+    return out

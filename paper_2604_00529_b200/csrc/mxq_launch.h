@@ -1,6 +1,7 @@
 // Internal interface between the C ABI (argument checks, mxq_api.cu) and the per-operation
 // translation units that instantiate and launch the kernels.  Arguments are already validated.
 #pragma once
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 #include <type_traits>
@@ -85,6 +86,14 @@ int launch_dequantize_batched(const DqDeviceItem* items_host, int count, size_t 
 size_t q_batched_tiles(size_t nunits);
 size_t dq_batched_tiles(size_t nunits);
 
+// D = A^ B^T, A [m, k], B [n, k], D [m, n] row-major; codes E4M3, plain scale bytes [rows, k / block].
+struct MatmulArgs {
+    const uint8_t *a, *as, *b, *bs;
+    size_t m, n, k;
+    int block;
+    uint8_t* dst;
+};
+
 // Batched Slice-and-Scale over a device-resident item table and its coarse tile index (see
 // mxq_kernels.cuh: SsDeviceItem, TileIndex); used by the fixed-table entry point.
 struct SsDeviceItem;
@@ -150,10 +159,11 @@ inline void fill_item_block(BLK& blk, const ITEM* items, int count, size_t total
 
 // Launches `kern` on `stream` with programmatic stream serialization allowed (see pdl_release /
 // pdl_acquire in mxq_access.cuh).  Returns MXQ_OK or MXQ_ERR_CUDA.
+//   smem     dynamic shared memory; more than 48 KB needs allow_smem() for the kernel first
+//   cluster  CTAs per thread-block cluster along the grid's first dimension
 template <class... KArgs, class... Args>
-inline int launch_kernel(void (*kern)(KArgs...), int grid, int threads, cudaStream_t stream, const Args&... args)
+inline int launch_grid(void (*kern)(KArgs...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t stream, const Args&... args)
 {
-    if (grid <= 0) return MXQ_ERR_SIZE;
 #ifdef MXQ_DEBUG
     if (debug_upload(stream) != 0) {                      // the byte ranges this launch may touch
         (void)cudaGetLastError();
@@ -161,15 +171,19 @@ inline int launch_kernel(void (*kern)(KArgs...), int grid, int threads, cudaStre
     }
 #endif
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = 0;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     // (the arguments go by address: an item table is copied once, into the launch itself)
     auto launch = [&](const KArgs&... a) {
         void* p[] = {const_cast<void*>(static_cast<const void*>(&a))...};
@@ -179,6 +193,32 @@ inline int launch_kernel(void (*kern)(KArgs...), int grid, int threads, cudaStre
         (void)cudaGetLastError();
         return MXQ_ERR_CUDA;
     }
+    return MXQ_OK;
+}
+
+template <class... KArgs, class... Args>
+inline int launch_kernel(void (*kern)(KArgs...), int grid, int threads, cudaStream_t stream, const Args&... args)
+{
+    if (grid <= 0) return MXQ_ERR_SIZE;
+    return launch_grid(kern, dim3((unsigned)grid), threads, 0, 1, stream, args...);
+}
+
+// Lets `kern` have `smem` bytes of dynamic shared memory on the current device.  `done` is the kernel's own: the devices that
+// know already, one bit each (devices beyond 63 are told every time).
+inline int allow_smem(const void* kern, size_t smem, std::atomic<uint64_t>& done)
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return MXQ_ERR_CUDA;
+    }
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0ull;
+    if (done.load(std::memory_order_relaxed) & bit) return MXQ_OK;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return MXQ_ERR_CUDA;
+    }
+    done.fetch_or(bit, std::memory_order_relaxed);
     return MXQ_OK;
 }
 

@@ -1,0 +1,224 @@
+// Q_f (Eq. 1-3) of a matrix along its rows and of its transpose, from one read: the operands of a linear layer's three products
+// (y = x w^T takes x and w along k, dx = dy w takes dy along n and w^T along n, dw = dy^T x takes both transposes along m).
+//
+// A CTA of 256 threads holds a tile of 128 x 128 elements in registers, eight columns of four consecutive rows, twice, per
+// thread.  Blocks of 32, 64 or 128 elements never cross a tile.  Along the rows the block maximum is a shuffle over 4, 8 or
+// 16 lanes; along the columns each thread's four rows meet in shared memory.  The transposed codes go through shared memory
+// four rows to a word, words exchanged so that neither side has bank conflicts, and leave as whole 128-byte lines.
+// Rows beyond the matrix, up to a whole block, are zeros: they add nothing to a product.
+#include "mxq_kernels.cuh"
+#include "mxq_launch.h"
+
+namespace mxq {
+namespace {
+
+constexpr int kTile = 128;
+constexpr int kMatThreads = 256;
+
+// eight consecutive elements of row r from column c on, as FP32; zeros outside the matrix
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const uint8_t* __restrict__ src, size_t rows, size_t cols, size_t r, size_t c, float (&v)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    if (r >= rows) return;
+    if constexpr (VEC) {                                     // cols % 8 == 0: a piece is inside or outside as a whole
+        if (c >= cols) return;
+        const uint8_t* p = src + (r * cols + c) * T::size;
+        if constexpr (T::size == 4) {
+            MXQ_CHECKED(p, 32, return)
+            const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            MXQ_CHECKED(p, 16, return)
+            const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float((j & 1) ? (w[j / 2] & 0xFFFF0000u) : (w[j / 2] << 16));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (c + j >= cols) continue;
+            const uint8_t* p = src + (r * cols + c + j) * T::size;
+            MXQ_CHECKED(p, T::size, continue)
+            if constexpr (T::size == 4) v[j] = __ldg(reinterpret_cast<const float*>(p));
+            else v[j] = __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p)) << 16);
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t upper_abs(float v) { return (__float_as_uint(v) >> 16) & 0x7FFFu; }
+
+// FP32 bit patterns are ordered like the values, and only the exponent field of a maximum is used (0xFF: the block is
+// poisoned): the patterns' upper halves are enough, two columns to a word.
+template <class T, class F, int BLOCK, bool VEC>
+__global__ void __launch_bounds__(kMatThreads)
+quantize_matrix_kernel(const uint8_t* __restrict__ src, size_t rows, size_t cols, uint8_t* __restrict__ codes,
+                       uint8_t* __restrict__ scales, uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t, uint32_t col_tiles)
+{
+    constexpr int LPB = BLOCK / 8;                           // lanes per block along a row
+    constexpr int G = BLOCK / 32;                            // groups of 32 rows per block along a column
+    __shared__ uint32_t s_max[2][8][kTile / 2];              // [rows / 64][warp][column pair]
+    __shared__ uint8_t s_byte[4][kTile];                     // scale byte per group of 32 rows and column
+    __shared__ uint32_t s_codes[kTile][32];                  // [column][four rows], exchanged
+    pdl_release();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, l = lane & 15, rg = warp * 2 + (lane >> 4);
+    const size_t tr = blockIdx.x / col_tiles, tc = blockIdx.x % col_tiles;
+    const size_t r0 = tr * kTile, c0 = tc * kTile;
+    const size_t rows_p = (rows + BLOCK - 1) / BLOCK * BLOCK, cols_p = (cols + BLOCK - 1) / BLOCK * BLOCK;
+    pdl_acquire();
+
+    float v[2][4][8];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load8<T, VEC>(src, rows, cols, r0 + s * 64 + rg * 4 + i, c0 + l * 8, v[s][i]);
+
+    if (codes) {                                             // along the rows
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) m = max(m, upper_abs(v[s][i][j]));
+                m = group_max<LPB>(m);
+                const BlockScale sc = block_scale<F>(m << 16);
+                const size_t r = r0 + s * 64 + rg * 4 + i, c = c0 + l * 8;
+                if (r >= rows || c >= cols_p) continue;
+                uint2 q = make_uint2(0, 0);
+                if (sc.byte != 255u) {
+                    const float (&e)[8] = v[s][i];
+                    q.x = quantize_fp_hw_quad<F>(e[0] * sc.inv, e[1] * sc.inv, e[2] * sc.inv, e[3] * sc.inv);
+                    q.y = quantize_fp_hw_quad<F>(e[4] * sc.inv, e[5] * sc.inv, e[6] * sc.inv, e[7] * sc.inv);
+                }
+                uint8_t* p = codes + r * cols_p + c;
+                MXQ_CHECKED(p, 8, continue)
+                *reinterpret_cast<uint2*>(p) = q;
+                if (l % LPB == 0) st_u8(scales + r * (cols_p / BLOCK) + c / BLOCK, sc.byte);
+            }
+    }
+    if (!codes_t) return;
+
+    // along the columns: the thread's four rows, the two halves of the warp, then the four warps of a group of 32 rows
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = __vmaxu2(m, upper_abs(v[s][i][2 * j]) | upper_abs(v[s][i][2 * j + 1]) << 16);
+            m = __vmaxu2(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+            if (lane < 16) s_max[s][warp][l * 4 + j] = m;
+        }
+    __syncthreads();
+    {
+        const int c = tid & 127, s = tid >> 7;               // one column's 64 rows
+        uint32_t g[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) m = max(m, (s_max[k >> 1][(k & 1) * 4 + w][c >> 1] >> (16 * (c & 1))) & 0xFFFFu);
+            g[k] = m;
+        }
+        if constexpr (G == 2) { g[0] = g[1] = max(g[0], g[1]); g[2] = g[3] = max(g[2], g[3]); }
+        if constexpr (G == 4) g[0] = g[1] = g[2] = g[3] = max(max(g[0], g[1]), max(g[2], g[3]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t gm = s ? g[2 + h] : g[h];
+            const BlockScale sc = block_scale<F>(gm << 16);
+            const int k = s * 2 + h;
+            s_byte[k][c] = (uint8_t)sc.byte;
+            const size_t row = r0 + (size_t)k * 32;
+            if (k % G == 0 && row < rows_p && c0 + c < cols) st_u8(scales_t + (c0 + c) * (rows_p / BLOCK) + row / BLOCK, sc.byte);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = l * 8 + j;
+            const uint32_t byte = s_byte[s * 2 + (rg >> 3)][c];
+            const float inv = __uint_as_float((254u - byte) << 23);          // E4M3: byte <= 246 unless poisoned
+            const uint32_t q = byte == 255u ? 0u : quantize_fp_hw_quad<F>(v[s][0][j] * inv, v[s][1][j] * inv, v[s][2][j] * inv, v[s][3][j] * inv);
+            s_codes[c][(rg + 16 * s) ^ (2 * l)] = q;
+        }
+    __syncthreads();
+    const size_t row = r0 + (size_t)lane * 4;
+#pragma unroll 4
+    for (int c = warp; c < kTile; c += kMatThreads / 32) {
+        if (c0 + c >= cols || row >= rows_p) continue;
+        st_u32(codes_t + (c0 + c) * rows_p + row, s_codes[c][lane ^ (2 * (c >> 3))]);
+    }
+}
+
+template <class T, int BLOCK>
+int run(const void* src, size_t rows, size_t cols, void* codes, uint8_t* scales, void* codes_t, uint8_t* scales_t, cudaStream_t stream)
+{
+    using F = Fmt<MXQ_FP8_E4M3>;
+    const size_t rt = (rows + kTile - 1) / kTile, ct = (cols + kTile - 1) / kTile;
+    if (ct > 0x7FFFFFFF || rt > 0x7FFFFFFF / ct) return MXQ_ERR_SIZE;
+    auto go = [&](auto kern) {
+        return launch_kernel(kern, (int)(rt * ct), kMatThreads, stream, static_cast<const uint8_t*>(src), rows, cols,
+                             static_cast<uint8_t*>(codes), scales, static_cast<uint8_t*>(codes_t), scales_t, (uint32_t)ct);
+    };
+    return cols % 8 == 0 ? go(quantize_matrix_kernel<T, F, BLOCK, true>) : go(quantize_matrix_kernel<T, F, BLOCK, false>);
+}
+
+template <class T>
+int by_block(int block, const void* src, size_t rows, size_t cols, void* codes, uint8_t* scales, void* codes_t, uint8_t* scales_t,
+             cudaStream_t stream)
+{
+    switch (block) {
+    case 32: return run<T, 32>(src, rows, cols, codes, scales, codes_t, scales_t, stream);
+    case 64: return run<T, 64>(src, rows, cols, codes, scales, codes_t, scales_t, stream);
+    default: return run<T, 128>(src, rows, cols, codes, scales, codes_t, scales_t, stream);
+    }
+}
+
+inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+}  // namespace
+
+}  // namespace mxq
+
+using namespace mxq;
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+size_t mxq_matrix_codes_bytes(size_t rows, size_t cols, int block)
+{
+    return block > 0 ? rows * ((cols + (size_t)block - 1) / (size_t)block) * (size_t)block : 0;
+}
+
+size_t mxq_matrix_scales_bytes(size_t rows, size_t cols, int block)
+{
+    return block > 0 ? rows * ((cols + (size_t)block - 1) / (size_t)block) : 0;
+}
+
+int mxq_quantize_matrix(const void* src, int src_dtype, size_t rows, size_t cols, int fmt, int block, void* codes, uint8_t* scales,
+                        void* codes_t, uint8_t* scales_t, mxq_stream stream)
+{
+    if (fmt != MXQ_FP8_E4M3 || (src_dtype != MXQ_F32 && src_dtype != MXQ_BF16)) return MXQ_ERR_FORMAT;
+    if (block != 32 && block != 64 && block != 128) return MXQ_ERR_BLOCK;
+    if (rows == 0 || cols == 0) return MXQ_OK;
+    if (rows > (SIZE_MAX / 8) / cols) return MXQ_ERR_SIZE;
+    if (!src || (!codes && !codes_t) || !codes != !scales || !codes_t != !scales_t) return MXQ_ERR_NULL;
+    if (!aligned(src, 32) || !aligned(codes, 32) || !aligned(codes_t, 32) || !aligned(scales, 16) || !aligned(scales_t, 16)) return MXQ_ERR_ALIGN;
+    MXQ_DEBUG_SCOPE();
+    MXQ_DEBUG_EXPECT(src, rows * cols * (src_dtype == MXQ_F32 ? 4u : 2u));
+    MXQ_DEBUG_EXPECT(codes, mxq_matrix_codes_bytes(rows, cols, block));
+    MXQ_DEBUG_EXPECT(scales, mxq_matrix_scales_bytes(rows, cols, block));
+    MXQ_DEBUG_EXPECT(codes_t, mxq_matrix_codes_bytes(cols, rows, block));
+    MXQ_DEBUG_EXPECT(scales_t, mxq_matrix_scales_bytes(cols, rows, block));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (src_dtype == MXQ_F32) return by_block<F32>(block, src, rows, cols, codes, scales, codes_t, scales_t, s);
+    return by_block<BF16>(block, src, rows, cols, codes, scales, codes_t, scales_t, s);
+}
+
+}  // extern "C"
+#pragma GCC visibility pop
