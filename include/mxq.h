@@ -82,7 +82,7 @@ typedef enum {
     MXQ_ERR_ALIGN = -5,   /* a pointer is not aligned as required (32 bytes data, 16 bytes scales) */
     MXQ_ERR_PAIR = -6,    /* (src_fmt, dst_fmt) is not a same-family high-to-low pair */
     MXQ_ERR_CUDA = -7,    /* a CUDA call or launch failed */
-    MXQ_ERR_TIMEOUT = -8  /* reserved: a bounded device-side wait gave up */
+    MXQ_ERR_TIMEOUT = -8  /* a bounded device-side wait gave up (mxq_wait_status) */
 } mxq_status;
 
 /* Human-readable name of a status code (static storage, never null). */
@@ -379,6 +379,13 @@ int mxq_slice_scale_batched_static(const mxq_ss_item *items, int count, int bloc
  */
 int mxq_matmul(const void *a_codes, const uint8_t *a_scales, const void *b_codes, const uint8_t *b_scales,
                size_t m, size_t n, size_t k, int fmt, int block, void *dst, int dst_dtype, mxq_stream stream);
+
+/*
+ * The kernels of mxq_matmul wait inside the device for their own copies and matrix instructions, ten seconds at most.  A wait
+ * that runs out (it cannot, unless the GPU is failing) ends the kernel with an unfinished D and is remembered per device:
+ * mxq_wait_status waits for the current device and returns MXQ_ERR_TIMEOUT if that happened since the last reset.
+ */
+int mxq_wait_status(int reset);
 
 /*
  * Q_f (Eq. 1-3) of a row-major [rows, cols] matrix along its rows and of its transpose, from one read: what the three products

@@ -136,6 +136,8 @@ def load_library() -> ctypes.CDLL:
     L.mxq_slice_scale_batched_static.restype = i
     L.mxq_matmul.argtypes = [vp, vp, vp, vp, sz, sz, sz, i, i, vp, i, vp]
     L.mxq_matmul.restype = i
+    L.mxq_wait_status.argtypes = [i]
+    L.mxq_wait_status.restype = i
     L.mxq_matrix_codes_bytes.argtypes = [sz, sz, i]
     L.mxq_matrix_codes_bytes.restype = sz
     L.mxq_matrix_scales_bytes.argtypes = [sz, sz, i]

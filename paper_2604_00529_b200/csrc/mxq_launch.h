@@ -93,6 +93,9 @@ struct MatmulArgs {
     int block;
     uint8_t* dst;
 };
+int launch_matmul_few(const MatmulArgs& p, int dst_dtype, cudaStream_t stream);     // few rows of A: bound by reading B
+int launch_matmul_tc(const MatmulArgs& p, int dst_dtype, cudaStream_t stream);      // on the tensor cores
+int tc_status(int reset);
 
 // Batched Slice-and-Scale over a device-resident item table and its coarse tile index (see
 // mxq_kernels.cuh: SsDeviceItem, TileIndex); used by the fixed-table entry point.

@@ -6,8 +6,6 @@
 
 namespace mxq {
 
-int launch_matmul_few(const MatmulArgs& p, int dst_dtype, cudaStream_t stream);
-
 namespace {
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -226,8 +224,10 @@ int mxq_matmul(const void* a_codes, const uint8_t* a_scales, const void* b_codes
     MXQ_DEBUG_EXPECT(dst, m * n * size);
     const MatmulArgs p{static_cast<const uint8_t*>(a_codes), a_scales, static_cast<const uint8_t*>(b_codes), b_scales, m, n, k, block,
                        static_cast<uint8_t*>(dst)};
-    return launch_matmul_few(p, dst_dtype, s);
+    return m <= 16 ? launch_matmul_few(p, dst_dtype, s) : launch_matmul_tc(p, dst_dtype, s);
 }
+
+int mxq_wait_status(int reset) { return tc_status(reset); }
 
 }  // extern "C"
 #pragma GCC visibility pop

@@ -1,0 +1,363 @@
+// D = L^ R^T on the fifth-generation tensor cores (block-scaled E4M3 matrix instructions): the product of mxq_matmul for more
+// rows than a few.  L's rows go to the accumulator's lanes, R's rows to its columns; which operand is which is the launcher's choice.
+//
+// The instruction takes one scale byte per row and 32 values of k, multiplied in by the hardware; a block of 64 or 128
+// repeats its byte.  Scales therefore come in as plain bytes and are spread by the warps that bring them to shared memory
+// (four bytes per row and k tile of 128), from where they are copied to tensor memory in front of the tile's four instructions.
+//
+// Warps of a CTA: 0 loads operand tiles (TMA), 1 issues the matrix instructions (of the pair: the first CTA's), 4 - 7 bring the
+// scales, 8 - 11 write results.  A CTA pair (CG = 2) works on 256 rows of L, 128 per CTA, and shares the tile of R half and half.
+#include <cuda.h>
+
+#include "mxq_kernels.cuh"
+#include "mxq_launch.h"
+#include "mxq_tensor.cuh"
+
+namespace mxq {
+namespace {
+
+__device__ unsigned int g_status;                            // a bounded wait gave up
+
+constexpr int kRowsL = 128;                                  // rows of L per CTA
+constexpr int kTileK = 128;                                  // bytes = elements of k per stage
+constexpr int kThreads = 384;
+
+template <int CG, int BN>
+struct Shape {
+    static constexpr int rows_r = BN / CG;                   // rows of R that a CTA loads
+    static constexpr int sf_r = (BN + 127) / 128;            // 512-byte scale tiles of R
+    static constexpr int bytes_l = kRowsL * kTileK, bytes_r = rows_r * kTileK;
+    static constexpr int bytes_sf = 512 * (1 + sf_r);
+    static constexpr int stage = bytes_l + bytes_r + (bytes_sf + 1023) / 1024 * 1024;
+    static constexpr int stages = 200 * 1024 / stage < 8 ? 200 * 1024 / stage : 8;
+    static constexpr int sf_cols = 4 * (1 + sf_r);           // columns of tensor memory per stage
+    static constexpr int buffers = 2 * BN + stages * sf_cols <= 512 ? 2 : 1;
+    static constexpr int tmem_used = buffers * BN + stages * sf_cols;
+    static constexpr int tmem_cols = tmem_used <= 64 ? 64 : tmem_used <= 128 ? 128 : tmem_used <= 256 ? 256 : 512;
+    static constexpr int smem = stages * stage + 1024;       // (the base is aligned up to 1024)
+    static_assert(tmem_used <= 512, "tensor memory");
+};
+
+struct TcArgs {
+    const uint8_t *ls, *rs;                                  // scale bytes
+    uint8_t* dst;
+    size_t rows_l, rows_r;
+    uint32_t kblocks, k, tiles_l, tiles_r, ktiles;
+    int block_shift;
+    size_t ld;                                               // elements between rows of dst
+};
+
+// Where tile number t lies: groups of eight tile rows of L, so that the tiles in flight share operands in L2.
+__device__ __forceinline__ void tile_at(uint32_t t, uint32_t tiles_l, uint32_t tiles_r, uint32_t& tl, uint32_t& tr)
+{
+    constexpr uint32_t G = 8;
+    const uint32_t group = t / (G * tiles_r), first = group * G, height = min(G, tiles_l - first), in = t - group * G * tiles_r;
+    tl = first + in % height;
+    tr = in / height;
+}
+
+// The four scale bytes of a row for a k tile.  Bytes beyond k, or of a row beyond the matrix, are 1.0: what they scale is 0.
+__device__ __forceinline__ uint32_t scale_word(const uint8_t* s, size_t row, size_t rows, uint32_t kt, const TcArgs& p)
+{
+    if (row >= rows) return 0x7F7F7F7Fu;
+    const uint8_t* at = s + row * p.kblocks;
+    if (p.block_shift == 7) return ld_u8(at + kt) * 0x01010101u;           // k is a multiple of the block
+    if (p.block_shift == 6) {
+        const uint32_t i = kt * 2, lo = ld_u8(at + i), hi = i + 1 < p.kblocks ? ld_u8(at + i + 1) : 127u;
+        return lo * 0x0101u | hi * 0x01010000u;
+    }
+    const uint32_t i = kt * 4;
+    if ((p.kblocks & 3u) == 0) return ld_u32(at + i);
+    uint32_t w = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) w |= (i + j < p.kblocks ? ld_u8(at + i + j) : 127u) << (8 * j);
+    return w;
+}
+
+template <class OUT>
+__device__ __forceinline__ void put(uint8_t* dst, size_t i, float v)
+{
+    if constexpr (OUT::size == 4) {
+        MXQ_CHECKED(dst + i * 4, 4, return)
+        reinterpret_cast<float*>(dst)[i] = v;
+    } else {
+        st_u16(dst + i * 2, pack_bf16x2(v, 0.f) & 0xFFFFu);
+    }
+}
+
+// 32 columns of one row per lane to memory.  T: D's rows are the accumulator's columns.
+template <class OUT, bool T>
+__device__ __forceinline__ void store_block(const TcArgs& p, const uint32_t (&v)[32], size_t row, size_t col, float* stage, int lane)
+{
+    if constexpr (T) {                                       // a warp's 32 lanes are consecutive elements of a row of D
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (row < p.rows_l && col + j < p.rows_r) put<OUT>(p.dst, (col + j) * p.ld + row, __uint_as_float(v[j]));
+    } else if (p.ld % (32 / OUT::size) == 0) {               // whole 32-byte sectors
+        constexpr int PER = 32 / OUT::size;
+        if (row >= p.rows_l) return;
+#pragma unroll
+        for (int s = 0; s < 32 / PER; ++s) {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (OUT::size == 4) w[j] = v[s * 8 + j];
+                else w[j] = pack_bf16x2(__uint_as_float(v[s * 16 + 2 * j]), __uint_as_float(v[s * 16 + 2 * j + 1]));
+            }
+            if (col + s * PER < p.rows_r) st256(p.dst + (row * p.ld + col + s * PER) * OUT::size, w);
+        }
+    } else {                                                 // any alignment: through shared memory, lanes along the row
+        const size_t row0 = row - lane;
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) stage[lane * 33 + j] = __uint_as_float(v[j]);
+        __syncwarp();
+        for (int r = 0; r < 32; ++r)
+            if (row0 + r < p.rows_l && col + lane < p.rows_r) put<OUT>(p.dst, (row0 + r) * p.ld + col + lane, stage[r * 33 + lane]);
+    }
+}
+
+template <class OUT, int CG, int BN, bool T>
+__global__ void __launch_bounds__(kThreads, 1)
+matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_r, const TcArgs p)
+{
+    using S = Shape<CG, BN>;
+    extern __shared__ uint8_t s_raw[];
+    __shared__ __align__(8) uint64_t s_full[S::stages], s_empty[S::stages], s_acc_full[2], s_acc_empty[2];
+    __shared__ uint32_t s_tmem, s_gave_up;
+    __shared__ float s_out[T ? 1 : 4 * 32 * 33];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
+    const uint32_t base = (smem_addr(s_raw) + 1023u) & ~1023u;
+    uint8_t* const base_p = s_raw + (base - smem_addr(s_raw));
+    pdl_release();
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::stages; ++i) {
+            mbar_init(smem_addr(&s_full[i]), 1 + 4 * CG);    // the loader's bytes, four scale warps of each CTA
+            mbar_init(smem_addr(&s_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_addr(&s_acc_full[i]), 1);
+            mbar_init(smem_addr(&s_acc_empty[i]), 4 * CG);
+        }
+        s_gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        tmem_alloc<CG>(smem_addr(&s_tmem), S::tmem_cols);
+        if (lane == 0) {
+            tma_prefetch_map(&map_l);
+            tma_prefetch_map(&map_r);
+        }
+    }
+    tc_fence_before();
+    if constexpr (CG == 2) cluster_sync();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    pdl_acquire();
+
+    const uint32_t tiles = p.tiles_l * p.tiles_r, step = gridDim.x / CG, first = blockIdx.x / CG;
+    auto wait = [&](uint64_t& bar, uint32_t parity) { return mbar_wait(smem_addr(&bar), parity, &s_gave_up, &g_status); };
+    uint32_t stage = 0, phase = 0;
+    auto advance = [&] {
+        if (++stage == (uint32_t)S::stages) {
+            stage = 0;
+            phase ^= 1;
+        }
+    };
+
+    if (warp == 0 && lane == 0) {                            // operand tiles
+        bool ok = true;
+        for (uint32_t t = first; ok && t < tiles; t += step) {
+            uint32_t tl, tr;
+            tile_at(t, p.tiles_l, p.tiles_r, tl, tr);
+            const int yl = (int)(tl * (kRowsL * CG) + rank * kRowsL), yr = (int)(tr * BN + rank * S::rows_r);
+            for (uint32_t kt = 0; ok && kt < p.ktiles; ++kt, advance()) {
+                if (!(ok = wait(s_empty[stage], phase ^ 1))) break;
+                uint32_t bar = smem_addr(&s_full[stage]);
+                const uint32_t at = base + stage * S::stage;
+                if (rank == 0) mbar_expect(bar, CG * (S::bytes_l + S::bytes_r));
+                if constexpr (CG == 2) bar = peer_addr(bar, 0);
+                tma_tile<CG>(at, &map_l, (int)(kt * kTileK), yl, bar);
+                tma_tile<CG>(at + S::bytes_l, &map_r, (int)(kt * kTileK), yr, bar);
+            }
+        }
+    } else if (warp == 1 && lane == 0 && rank == 0) {        // matrix instructions
+        bool ok = true;
+        uint32_t n = 0;
+        for (uint32_t t = first; ok && t < tiles; t += step, ++n) {
+            const uint32_t buf = S::buffers == 2 ? n & 1 : 0, use = S::buffers == 2 ? n >> 1 : n;
+            if (!(ok = wait(s_acc_empty[buf], (use & 1) ^ 1))) break;
+            tc_fence_after();
+            const uint32_t d = tmem + buf * BN;
+            for (uint32_t kt = 0; kt < p.ktiles; ++kt, advance()) {
+                if (!(ok = wait(s_full[stage], phase))) break;
+                tc_fence_after();
+                const uint32_t at = base + stage * S::stage, sf = at + S::bytes_l + S::bytes_r;
+                const uint32_t tsf = tmem + S::buffers * BN + stage * S::sf_cols;
+#pragma unroll
+                for (int i = 0; i < 1 + S::sf_r; ++i) scales_to_tmem<CG>(tsf + 4 * i, scales_desc(sf + 512 * i));
+                const uint64_t a = operand_desc(at), b = operand_desc(at + S::bytes_l);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)                  // 32 bytes of k further inside the swizzled rows
+                    mma_scaled<CG>(d, a + 2 * j, b + 2 * j, instr_desc(kRowsL * CG, BN, j), tsf, tsf + 4, kt > 0 || j > 0);
+                mma_commit<CG>(smem_addr(&s_empty[stage]));
+            }
+            if (ok) mma_commit<CG>(smem_addr(&s_acc_full[buf]));
+        }
+    } else if (warp >= 4 && warp < 8) {                      // scales
+        const uint32_t r = (warp - 4) * 32 + lane;
+        bool ok = true;
+        for (uint32_t t = first; ok && t < tiles; t += step) {
+            uint32_t tl, tr;
+            tile_at(t, p.tiles_l, p.tiles_r, tl, tr);
+            const size_t row_l = (size_t)tl * (kRowsL * CG) + rank * kRowsL + r, row_r = (size_t)tr * BN + r;
+            uint32_t w[1 + S::sf_r];
+            auto load = [&](uint32_t kt) {
+                w[0] = scale_word(p.ls, row_l, p.rows_l, kt, p);
+#pragma unroll
+                for (int i = 0; i < S::sf_r; ++i)
+                    w[1 + i] = (int)r + 128 * i < BN ? scale_word(p.rs, row_r + 128 * i, p.rows_r, kt, p) : 0x7F7F7F7Fu;
+            };
+            load(0);
+            for (uint32_t kt = 0; kt < p.ktiles; ++kt, advance()) {
+                ok = wait(s_empty[stage], phase ^ 1);
+                if (!__all_sync(0xFFFFFFFFu, ok)) {
+                    ok = false;
+                    break;
+                }
+                uint32_t* sf = reinterpret_cast<uint32_t*>(base_p + stage * S::stage + S::bytes_l + S::bytes_r);
+#pragma unroll
+                for (int i = 0; i < 1 + S::sf_r; ++i) sf[128 * i + (r & 31) * 4 + (r >> 5)] = w[i];
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_full[stage]), CG == 2 ? 0 : cluster_rank()));
+                if (kt + 1 < p.ktiles) load(kt + 1);
+            }
+        }
+    } else if (warp >= 8) {                                  // results
+        bool ok = true;
+        uint32_t n = 0;
+        const int q = warp & 3;
+        for (uint32_t t = first; ok && t < tiles; t += step, ++n) {
+            uint32_t tl, tr;
+            tile_at(t, p.tiles_l, p.tiles_r, tl, tr);
+            const uint32_t buf = S::buffers == 2 ? n & 1 : 0, use = S::buffers == 2 ? n >> 1 : n;
+            ok = wait(s_acc_full[buf], use & 1);
+            if (!__all_sync(0xFFFFFFFFu, ok)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            const size_t row = (size_t)tl * (kRowsL * CG) + rank * kRowsL + q * 32 + lane;
+#pragma unroll 1
+            for (int c = 0; c < BN; c += 32) {
+                uint32_t v[32];
+                tmem_ld32(v, tmem + buf * BN + c + ((uint32_t)(q * 32) << 16));
+                tmem_ld_wait();
+                store_block<OUT, T>(p, v, row, (size_t)tr * BN + c, s_out + (T ? 0 : q * 32 * 33), lane);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_acc_empty[buf]), CG == 2 ? 0 : cluster_rank()));
+        }
+    }
+    __syncwarp();
+    // A wait that gave up may have left copies under way: let those of this CTA land before its memory goes.
+    if (s_gave_up && threadIdx.x == 0) {
+        const uint64_t began = global_ns();
+        while (global_ns() - began < 1000ull * 1000) {}
+    }
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();
+    if (warp == 0) tmem_free<CG>(tmem, S::tmem_cols);
+}
+
+// ---- launchers --------------------------------------------------------------------------------------------
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encoder()
+{
+    static const EncodeFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeFn>(p);
+    }();
+    return fn;
+}
+
+// [rows, k] bytes in boxes of `box_rows` x 128, zeros beyond the matrix
+bool make_map(CUtensorMap* map, const uint8_t* p, size_t rows, size_t k, int box_rows)
+{
+    const EncodeFn enc = encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)k};
+    const cuuint32_t box[2] = {kTileK, (cuuint32_t)box_rows}, elem[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class OUT, int CG, int BN, bool T>
+int run(const MatmulArgs& m, cudaStream_t stream)
+{
+    using S = Shape<CG, BN>;
+    static std::atomic<uint64_t> done{0};
+    auto kern = matmul_tc_kernel<OUT, CG, BN, T>;
+    if (int rc = allow_smem(reinterpret_cast<const void*>(kern), S::smem, done)) return rc;
+    TcArgs p;
+    p.ls = T ? m.bs : m.as;
+    p.rs = T ? m.as : m.bs;
+    p.rows_l = T ? m.n : m.m;
+    p.rows_r = T ? m.m : m.n;
+    p.dst = m.dst;
+    p.ld = m.n;
+    p.k = (uint32_t)m.k;
+    p.kblocks = (uint32_t)(m.k / (size_t)m.block);
+    p.block_shift = m.block == 32 ? 5 : m.block == 64 ? 6 : 7;
+    p.ktiles = (uint32_t)((m.k + kTileK - 1) / kTileK);
+    p.tiles_l = (uint32_t)((p.rows_l + kRowsL * CG - 1) / (kRowsL * CG));
+    p.tiles_r = (uint32_t)((p.rows_r + BN - 1) / BN);
+    if ((uint64_t)p.tiles_l * p.tiles_r > 0x7FFFFFFFull) return MXQ_ERR_SIZE;
+    CUtensorMap ml, mr;
+    if (!make_map(&ml, T ? m.b : m.a, p.rows_l, m.k, kRowsL) || !make_map(&mr, T ? m.a : m.b, p.rows_r, m.k, S::rows_r)) return MXQ_ERR_CUDA;
+    const uint32_t tiles = p.tiles_l * p.tiles_r, most = 148 / CG;
+    const unsigned grid = (tiles < most ? tiles : most) * CG;
+    return launch_grid(kern, dim3(grid), kThreads, S::smem, CG, stream, ml, mr, p);
+}
+
+}  // namespace
+
+int launch_matmul_tc(const MatmulArgs& p, int dst_dtype, cudaStream_t stream)
+{
+    if (dst_dtype == MXQ_F32) return run<F32, 2, 256, false>(p, stream);
+    return run<BF16, 2, 256, false>(p, stream);
+}
+
+// Whether a bounded wait of these kernels gave up on the current device; waits for the device.
+int tc_status(int reset)
+{
+    unsigned int v = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&v, g_status, sizeof v) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return MXQ_ERR_CUDA;
+    }
+    if (v && reset) {
+        const unsigned int zero = 0;
+        if (cudaMemcpyToSymbol(g_status, &zero, sizeof zero) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return MXQ_ERR_CUDA;
+        }
+    }
+    return v ? MXQ_ERR_TIMEOUT : MXQ_OK;
+}
+
+}  // namespace mxq
