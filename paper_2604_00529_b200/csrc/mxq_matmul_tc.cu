@@ -31,8 +31,12 @@ struct Shape {
     static constexpr int stage = bytes_l + bytes_r + (bytes_sf + 1023) / 1024 * 1024;
     static constexpr int stages = 200 * 1024 / stage < 8 ? 200 * 1024 / stage : 8;
     static constexpr int sf_cols = 4 * (1 + sf_r);           // columns of tensor memory per stage
-    static constexpr int buffers = 2 * BN + stages * sf_cols <= 512 ? 2 : 1;
-    static constexpr int tmem_used = buffers * BN + stages * sf_cols;
+    // Two accumulators, so that one tile's results leave while the next is computed.  Where tensor memory does not hold both
+    // (BN = 256), the second begins inside the first; the columns that they share are read first.
+    static constexpr int over = 2 * BN + stages * sf_cols <= 512 ? 0 : (2 * BN + stages * sf_cols - 512 + 31) / 32 * 32;
+    static constexpr int second = BN - over;                 // where the second one begins
+    static constexpr int sf_at = 2 * BN - over;
+    static constexpr int tmem_used = sf_at + stages * sf_cols;
     static constexpr int tmem_cols = tmem_used <= 64 ? 64 : tmem_used <= 128 ? 128 : tmem_used <= 256 ? 256 : 512;
     static constexpr int smem = stages * stage + 1024;       // (the base is aligned up to 1024)
     static_assert(tmem_used <= 512, "tensor memory");
@@ -42,8 +46,7 @@ struct TcArgs {
     const uint8_t *ls, *rs;                                  // scale bytes
     uint8_t* dst;
     size_t rows_l, rows_r;
-    uint32_t kblocks, k, tiles_l, tiles_r, ktiles;
-    int block_shift;
+    uint32_t kblocks, tiles_l, tiles_r, ktiles;
     size_t ld;                                               // elements between rows of dst
 };
 
@@ -56,23 +59,41 @@ __device__ __forceinline__ void tile_at(uint32_t t, uint32_t tiles_l, uint32_t t
     tr = in / height;
 }
 
-// The four scale bytes of a row for a k tile.  Bytes beyond k, or of a row beyond the matrix, are 1.0: what they scale is 0.
-__device__ __forceinline__ uint32_t scale_word(const uint8_t* s, size_t row, size_t rows, uint32_t kt, const TcArgs& p)
-{
-    if (row >= rows) return 0x7F7F7F7Fu;
-    const uint8_t* at = s + row * p.kblocks;
-    if (p.block_shift == 7) return ld_u8(at + kt) * 0x01010101u;           // k is a multiple of the block
-    if (p.block_shift == 6) {
-        const uint32_t i = kt * 2, lo = ld_u8(at + i), hi = i + 1 < p.kblocks ? ld_u8(at + i + 1) : 127u;
-        return lo * 0x0101u | hi * 0x01010000u;
-    }
-    const uint32_t i = kt * 4;
-    if ((p.kblocks & 3u) == 0) return ld_u32(at + i);
-    uint32_t w = 0;
+// The scale bytes of a row for eight k tiles, as they lie in memory.  They are fetched that far ahead because one k tile takes
+// the tensor cores less time than one load takes: fetched tile by tile, the loads' latency was the kernel's time (8192 x 14336 x
+// 4096 in 1222 us).  Bytes beyond k, or of a row beyond the matrix, are 1.0: what they scale is 0.
+constexpr int kAhead = 8;
+template <int BLOCK>
+struct RowScales {
+    static constexpr int PER = kTileK / BLOCK;               // bytes per k tile
+    static constexpr int NW = kAhead * PER / 4;
+    uint32_t w[NW];
+
+    __device__ __forceinline__ void load(const uint8_t* s, size_t row, size_t rows, uint32_t kt, uint32_t kblocks)
+    {
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) w |= (i + j < p.kblocks ? ld_u8(at + i + j) : 127u) << (8 * j);
-    return w;
-}
+        for (int j = 0; j < NW; ++j) w[j] = 0x7F7F7F7Fu;
+        if (row >= rows) return;
+        const uint8_t* at = s + row * kblocks;
+        const uint32_t first = kt * PER;
+        if ((kblocks & 3u) == 0) {
+#pragma unroll
+            for (int j = 0; j < NW; ++j)
+                if (first + 4 * j < kblocks) w[j] = ld_u32(at + first + 4 * j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4 * NW; ++j)
+                if (first + j < kblocks) w[j / 4] = __byte_perm(w[j / 4], ld_u8(at + first + j), (0x3210u & ~(0xFu << 4 * (j % 4))) | 4u << 4 * (j % 4));
+        }
+    }
+    // the four bytes of k tile i, one per 32 values of k
+    __device__ __forceinline__ uint32_t word(int i) const
+    {
+        if constexpr (BLOCK == 32) return w[i];
+        else if constexpr (BLOCK == 64) return __byte_perm(w[i / 2], 0, i % 2 ? 0x3322 : 0x1100);
+        else return __byte_perm(w[i / 4], 0, 0x1111u * (i % 4));
+    }
+};
 
 template <class OUT>
 __device__ __forceinline__ void put(uint8_t* dst, size_t i, float v)
@@ -117,13 +138,13 @@ __device__ __forceinline__ void store_block(const TcArgs& p, const uint32_t (&v)
     }
 }
 
-template <class OUT, int CG, int BN, bool T>
+template <class OUT, int CG, int BN, bool T, int BLOCK>
 __global__ void __launch_bounds__(kThreads, 1)
 matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_r, const TcArgs p)
 {
     using S = Shape<CG, BN>;
     extern __shared__ uint8_t s_raw[];
-    __shared__ __align__(8) uint64_t s_full[S::stages], s_empty[S::stages], s_acc_full[2], s_acc_empty[2];
+    __shared__ __align__(8) uint64_t s_full[S::stages], s_empty[S::stages], s_acc_full[2], s_acc_free;
     __shared__ uint32_t s_tmem, s_gave_up;
     __shared__ float s_out[T ? 1 : 4 * 32 * 33];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -136,10 +157,8 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
             mbar_init(smem_addr(&s_full[i]), 1 + 4 * CG);    // the loader's bytes, four scale warps of each CTA
             mbar_init(smem_addr(&s_empty[i]), 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_addr(&s_acc_full[i]), 1);
-            mbar_init(smem_addr(&s_acc_empty[i]), 4 * CG);
-        }
+        for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&s_acc_full[i]), 1);
+        mbar_init(smem_addr(&s_acc_free), 4 * CG);
         s_gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -187,15 +206,16 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
         bool ok = true;
         uint32_t n = 0;
         for (uint32_t t = first; ok && t < tiles; t += step, ++n) {
-            const uint32_t buf = S::buffers == 2 ? n & 1 : 0, use = S::buffers == 2 ? n >> 1 : n;
-            if (!(ok = wait(s_acc_empty[buf], (use & 1) ^ 1))) break;
+            // The last tile's shared columns have been read; and since whoever read them had done with the tile before, so has
+            // the accumulator that this tile goes to.
+            if (n > 0 && !(ok = wait(s_acc_free, (n - 1) & 1))) break;
             tc_fence_after();
-            const uint32_t d = tmem + buf * BN;
+            const uint32_t buf = n & 1, d = tmem + buf * S::second;
             for (uint32_t kt = 0; kt < p.ktiles; ++kt, advance()) {
                 if (!(ok = wait(s_full[stage], phase))) break;
                 tc_fence_after();
                 const uint32_t at = base + stage * S::stage, sf = at + S::bytes_l + S::bytes_r;
-                const uint32_t tsf = tmem + S::buffers * BN + stage * S::sf_cols;
+                const uint32_t tsf = tmem + S::sf_at + stage * S::sf_cols;
 #pragma unroll
                 for (int i = 0; i < 1 + S::sf_r; ++i) scales_to_tmem<CG>(tsf + 4 * i, scales_desc(sf + 512 * i));
                 const uint64_t a = operand_desc(at), b = operand_desc(at + S::bytes_l);
@@ -213,27 +233,31 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
             uint32_t tl, tr;
             tile_at(t, p.tiles_l, p.tiles_r, tl, tr);
             const size_t row_l = (size_t)tl * (kRowsL * CG) + rank * kRowsL + r, row_r = (size_t)tr * BN + r;
-            uint32_t w[1 + S::sf_r];
+            RowScales<BLOCK> now[1 + S::sf_r], next[1 + S::sf_r];
             auto load = [&](uint32_t kt) {
-                w[0] = scale_word(p.ls, row_l, p.rows_l, kt, p);
+                next[0].load(p.ls, row_l, p.rows_l, kt, p.kblocks);
 #pragma unroll
                 for (int i = 0; i < S::sf_r; ++i)
-                    w[1 + i] = (int)r + 128 * i < BN ? scale_word(p.rs, row_r + 128 * i, p.rows_r, kt, p) : 0x7F7F7F7Fu;
+                    next[1 + i].load(p.rs, row_r + 128 * i, (int)r + 128 * i < BN ? p.rows_r : 0, kt, p.kblocks);
             };
             load(0);
-            for (uint32_t kt = 0; kt < p.ktiles; ++kt, advance()) {
-                ok = wait(s_empty[stage], phase ^ 1);
-                if (!__all_sync(0xFFFFFFFFu, ok)) {
-                    ok = false;
-                    break;
-                }
-                uint32_t* sf = reinterpret_cast<uint32_t*>(base_p + stage * S::stage + S::bytes_l + S::bytes_r);
+            for (uint32_t k0 = 0; ok && k0 < p.ktiles; k0 += kAhead) {
 #pragma unroll
-                for (int i = 0; i < 1 + S::sf_r; ++i) sf[128 * i + (r & 31) * 4 + (r >> 5)] = w[i];
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_full[stage]), CG == 2 ? 0 : cluster_rank()));
-                if (kt + 1 < p.ktiles) load(kt + 1);
+                for (int i = 0; i < 1 + S::sf_r; ++i) now[i] = next[i];
+                if (k0 + kAhead < p.ktiles) load(k0 + kAhead);
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) {
+                    if (k0 + j >= p.ktiles) break;
+                    ok = __all_sync(0xFFFFFFFFu, wait(s_empty[stage], phase ^ 1));
+                    if (!ok) break;
+                    uint32_t* sf = reinterpret_cast<uint32_t*>(base_p + stage * S::stage + S::bytes_l + S::bytes_r);
+#pragma unroll
+                    for (int i = 0; i < 1 + S::sf_r; ++i) sf[128 * i + (r & 31) * 4 + (r >> 5)] = now[i].word(j);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_full[stage]), CG == 2 ? 0 : cluster_rank()));
+                    advance();
+                }
             }
         }
     } else if (warp >= 8) {                                  // results
@@ -243,24 +267,27 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
         for (uint32_t t = first; ok && t < tiles; t += step, ++n) {
             uint32_t tl, tr;
             tile_at(t, p.tiles_l, p.tiles_r, tl, tr);
-            const uint32_t buf = S::buffers == 2 ? n & 1 : 0, use = S::buffers == 2 ? n >> 1 : n;
-            ok = wait(s_acc_full[buf], use & 1);
-            if (!__all_sync(0xFFFFFFFFu, ok)) {
-                ok = false;
-                break;
-            }
+            const uint32_t buf = n & 1;
+            ok = __all_sync(0xFFFFFFFFu, wait(s_acc_full[buf], (n >> 1) & 1));
+            if (!ok) break;
             tc_fence_after();
             const size_t row = (size_t)tl * (kRowsL * CG) + rank * kRowsL + q * 32 + lane;
+            auto release = [&] {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_acc_free), CG == 2 ? 0 : cluster_rank()));
+            };
+            if (S::over == 0) release();
 #pragma unroll 1
-            for (int c = 0; c < BN; c += 32) {
+            for (int i = 0; i < BN; i += 32) {
+                // the shared columns are the first accumulator's last ones and the second one's first
+                const int c = buf == 0 && S::over ? (i + S::second) % BN : i;
                 uint32_t v[32];
-                tmem_ld32(v, tmem + buf * BN + c + ((uint32_t)(q * 32) << 16));
+                tmem_ld32(v, tmem + buf * S::second + c + ((uint32_t)(q * 32) << 16));
                 tmem_ld_wait();
+                if (S::over && i + 32 == S::over) release();
                 store_block<OUT, T>(p, v, row, (size_t)tr * BN + c, s_out + (T ? 0 : q * 32 * 33), lane);
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_acc_empty[buf]), CG == 2 ? 0 : cluster_rank()));
         }
     }
     __syncwarp();
@@ -306,12 +333,12 @@ bool make_map(CUtensorMap* map, const uint8_t* p, size_t rows, size_t k, int box
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class OUT, int CG, int BN, bool T>
-int run(const MatmulArgs& m, cudaStream_t stream)
+template <class OUT, int CG, int BN, bool T, int BLOCK>
+int run_block(const MatmulArgs& m, cudaStream_t stream)
 {
     using S = Shape<CG, BN>;
     static std::atomic<uint64_t> done{0};
-    auto kern = matmul_tc_kernel<OUT, CG, BN, T>;
+    auto kern = matmul_tc_kernel<OUT, CG, BN, T, BLOCK>;
     if (int rc = allow_smem(reinterpret_cast<const void*>(kern), S::smem, done)) return rc;
     TcArgs p;
     p.ls = T ? m.bs : m.as;
@@ -320,9 +347,7 @@ int run(const MatmulArgs& m, cudaStream_t stream)
     p.rows_r = T ? m.m : m.n;
     p.dst = m.dst;
     p.ld = m.n;
-    p.k = (uint32_t)m.k;
     p.kblocks = (uint32_t)(m.k / (size_t)m.block);
-    p.block_shift = m.block == 32 ? 5 : m.block == 64 ? 6 : 7;
     p.ktiles = (uint32_t)((m.k + kTileK - 1) / kTileK);
     p.tiles_l = (uint32_t)((p.rows_l + kRowsL * CG - 1) / (kRowsL * CG));
     p.tiles_r = (uint32_t)((p.rows_r + BN - 1) / BN);
@@ -332,6 +357,14 @@ int run(const MatmulArgs& m, cudaStream_t stream)
     const uint32_t tiles = p.tiles_l * p.tiles_r, most = 148 / CG;
     const unsigned grid = (tiles < most ? tiles : most) * CG;
     return launch_grid(kern, dim3(grid), kThreads, S::smem, CG, stream, ml, mr, p);
+}
+
+template <class OUT, int CG, int BN, bool T>
+int run(const MatmulArgs& m, cudaStream_t stream)
+{
+    if (m.block == 32) return run_block<OUT, CG, BN, T, 32>(m, stream);
+    if (m.block == 64) return run_block<OUT, CG, BN, T, 64>(m, stream);
+    return run_block<OUT, CG, BN, T, 128>(m, stream);
 }
 
 }  // namespace
