@@ -4,9 +4,11 @@
 // The instruction takes one scale byte per row and 32 values of k, multiplied in by the hardware; a block of 64 or 128
 // repeats its byte.  Scales therefore come in as plain bytes and are spread by the warps that bring them to shared memory
 // (four bytes per row and k tile of 128), from where they are copied to tensor memory in front of the tile's four instructions.
+// They are brought for eight k tiles at a time: a hand-over (a fence between the two memory proxies, an arrival across the pair)
+// takes longer than the tensor cores take for one.
 //
-// Warps of a CTA: 0 loads operand tiles (TMA), 1 issues the matrix instructions (of the pair: the first CTA's), 4 - 7 bring the
-// scales, 8 - 11 write results.  A CTA pair (CG = 2) works on 256 rows of L, 128 per CTA, and shares the tile of R half and half.
+// Warps of a CTA: 0 loads operand tiles (TMA), 1 issues the matrix instructions (of the pair: the first CTA's), 4 - 6 bring the
+// scales, 128 rows each, 8 - 11 write results.  A CTA pair (CG = 2) works on 256 rows of L, 128 per CTA, and shares the tile of R half and half.
 #include <cuda.h>
 
 #include "mxq_kernels.cuh"
@@ -21,16 +23,18 @@ __device__ unsigned int g_status;                            // a bounded wait g
 constexpr int kRowsL = 128;                                  // rows of L per CTA
 constexpr int kTileK = 128;                                  // bytes = elements of k per stage
 constexpr int kThreads = 384;
+constexpr int kAhead = 8;                                   // k tiles whose scales are brought together
 
 template <int CG, int BN>
 struct Shape {
     static constexpr int rows_r = BN / CG;                   // rows of R that a CTA loads
     static constexpr int sf_r = (BN + 127) / 128;            // 512-byte scale tiles of R
     static constexpr int bytes_l = kRowsL * kTileK, bytes_r = rows_r * kTileK;
-    static constexpr int bytes_sf = 512 * (1 + sf_r);
-    static constexpr int stage = bytes_l + bytes_r + (bytes_sf + 1023) / 1024 * 1024;
-    static constexpr int stages = 200 * 1024 / stage < 8 ? 200 * 1024 / stage : 8;
-    static constexpr int sf_cols = 4 * (1 + sf_r);           // columns of tensor memory per stage
+    static constexpr int sets = 1 + sf_r;                    // groups of 128 rows that have scales
+    static constexpr int slot = kAhead * sets * 512;         // the scale words of kAhead k tiles
+    static constexpr int stage = bytes_l + bytes_r;
+    static constexpr int stages = (205 * 1024 - 2 * slot) / stage < 8 ? (205 * 1024 - 2 * slot) / stage : 8;
+    static constexpr int sf_cols = 4 * sets;                 // columns of tensor memory per stage
     // Two accumulators, so that one tile's results leave while the next is computed.  Where tensor memory does not hold both
     // (BN = 256), the second begins inside the first; the columns that they share are read first.
     static constexpr int over = 2 * BN + stages * sf_cols <= 512 ? 0 : (2 * BN + stages * sf_cols - 512 + 31) / 32 * 32;
@@ -38,7 +42,7 @@ struct Shape {
     static constexpr int sf_at = 2 * BN - over;
     static constexpr int tmem_used = sf_at + stages * sf_cols;
     static constexpr int tmem_cols = tmem_used <= 64 ? 64 : tmem_used <= 128 ? 128 : tmem_used <= 256 ? 256 : 512;
-    static constexpr int smem = stages * stage + 1024;       // (the base is aligned up to 1024)
+    static constexpr int smem = stages * stage + 2 * slot + 1024;       // (the base is aligned up to 1024)
     static_assert(tmem_used <= 512, "tensor memory");
 };
 
@@ -59,10 +63,8 @@ __device__ __forceinline__ void tile_at(uint32_t t, uint32_t tiles_l, uint32_t t
     tr = in / height;
 }
 
-// The scale bytes of a row for eight k tiles, as they lie in memory.  They are fetched that far ahead because one k tile takes
-// the tensor cores less time than one load takes: fetched tile by tile, the loads' latency was the kernel's time (8192 x 14336 x
-// 4096 in 1222 us).  Bytes beyond k, or of a row beyond the matrix, are 1.0: what they scale is 0.
-constexpr int kAhead = 8;
+// The scale bytes of a row for eight k tiles, as they lie in memory.  Bytes beyond k, or of a row beyond the matrix, are 1.0:
+// what they scale is 0.
 template <int BLOCK>
 struct RowScales {
     static constexpr int PER = kTileK / BLOCK;               // bytes per k tile
@@ -144,7 +146,7 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
 {
     using S = Shape<CG, BN>;
     extern __shared__ uint8_t s_raw[];
-    __shared__ __align__(8) uint64_t s_full[S::stages], s_empty[S::stages], s_acc_full[2], s_acc_free;
+    __shared__ __align__(8) uint64_t s_full[S::stages], s_empty[S::stages], s_sf_full[2], s_sf_empty[2], s_acc_full[2], s_acc_free;
     __shared__ uint32_t s_tmem, s_gave_up;
     __shared__ float s_out[T ? 1 : 4 * 32 * 33];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -154,10 +156,14 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
     pdl_release();
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::stages; ++i) {
-            mbar_init(smem_addr(&s_full[i]), 1 + 4 * CG);    // the loader's bytes, four scale warps of each CTA
+            mbar_init(smem_addr(&s_full[i]), 1);
             mbar_init(smem_addr(&s_empty[i]), 1);
         }
-        for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&s_acc_full[i]), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_addr(&s_sf_full[i]), S::sets * CG);
+            mbar_init(smem_addr(&s_sf_empty[i]), 1);
+            mbar_init(smem_addr(&s_acc_full[i]), 1);
+        }
         mbar_init(smem_addr(&s_acc_free), 4 * CG);
         s_gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -178,7 +184,8 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
 
     const uint32_t tiles = p.tiles_l * p.tiles_r, step = gridDim.x / CG, first = blockIdx.x / CG;
     auto wait = [&](uint64_t& bar, uint32_t parity) { return mbar_wait(smem_addr(&bar), parity, &s_gave_up, &g_status); };
-    uint32_t stage = 0, phase = 0;
+    uint32_t stage = 0, phase = 0, slot = 0;                 // slots are numbered through: slot & 1, parity (slot >> 1) & 1
+    const uint32_t slots = base + S::stages * S::stage;
     auto advance = [&] {
         if (++stage == (uint32_t)S::stages) {
             stage = 0;
@@ -213,51 +220,50 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
             const uint32_t buf = n & 1, d = tmem + buf * S::second;
             for (uint32_t kt = 0; kt < p.ktiles; ++kt, advance()) {
                 if (!(ok = wait(s_full[stage], phase))) break;
+                if (kt % kAhead == 0 && !(ok = wait(s_sf_full[slot & 1], (slot >> 1) & 1))) break;
                 tc_fence_after();
-                const uint32_t at = base + stage * S::stage, sf = at + S::bytes_l + S::bytes_r;
+                const uint32_t at = base + stage * S::stage, sf = slots + (slot & 1) * S::slot + kt % kAhead * (S::sets * 512);
                 const uint32_t tsf = tmem + S::sf_at + stage * S::sf_cols;
 #pragma unroll
-                for (int i = 0; i < 1 + S::sf_r; ++i) scales_to_tmem<CG>(tsf + 4 * i, scales_desc(sf + 512 * i));
+                for (int i = 0; i < S::sets; ++i) scales_to_tmem<CG>(tsf + 4 * i, scales_desc(sf + 512 * i));
                 const uint64_t a = operand_desc(at), b = operand_desc(at + S::bytes_l);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)                  // 32 bytes of k further inside the swizzled rows
                     mma_scaled<CG>(d, a + 2 * j, b + 2 * j, instr_desc(kRowsL * CG, BN, j), tsf, tsf + 4, kt > 0 || j > 0);
                 mma_commit<CG>(smem_addr(&s_empty[stage]));
+                if (kt % kAhead == kAhead - 1 || kt + 1 == p.ktiles) mma_commit<CG>(smem_addr(&s_sf_empty[slot++ & 1]));
             }
             if (ok) mma_commit<CG>(smem_addr(&s_acc_full[buf]));
         }
-    } else if (warp >= 4 && warp < 8) {                      // scales
-        const uint32_t r = (warp - 4) * 32 + lane;
+    } else if (warp >= 4 && warp < 4 + S::sets) {            // scales: rows lane, lane + 32, + 64 and + 96 of the warp's 128
+        const int set = warp - 4;
         bool ok = true;
         for (uint32_t t = first; ok && t < tiles; t += step) {
             uint32_t tl, tr;
             tile_at(t, p.tiles_l, p.tiles_r, tl, tr);
-            const size_t row_l = (size_t)tl * (kRowsL * CG) + rank * kRowsL + r, row_r = (size_t)tr * BN + r;
-            RowScales<BLOCK> now[1 + S::sf_r], next[1 + S::sf_r];
+            const uint8_t* s = set == 0 ? p.ls : p.rs;
+            const size_t row0 = set == 0 ? (size_t)tl * (kRowsL * CG) + rank * kRowsL : (size_t)tr * BN + 128 * (set - 1);
+            const size_t rows = set == 0 ? p.rows_l : min(p.rows_r, (size_t)(tr + 1) * BN);
+            RowScales<BLOCK> next[4];
             auto load = [&](uint32_t kt) {
-                next[0].load(p.ls, row_l, p.rows_l, kt, p.kblocks);
 #pragma unroll
-                for (int i = 0; i < S::sf_r; ++i)
-                    next[1 + i].load(p.rs, row_r + 128 * i, (int)r + 128 * i < BN ? p.rows_r : 0, kt, p.kblocks);
+                for (int i = 0; i < 4; ++i) next[i].load(s, row0 + lane + 32 * i, rows, kt, p.kblocks);
             };
             load(0);
-            for (uint32_t k0 = 0; ok && k0 < p.ktiles; k0 += kAhead) {
+            for (uint32_t k0 = 0; k0 < p.ktiles; k0 += kAhead, ++slot) {
+                RowScales<BLOCK> now[4];
 #pragma unroll
-                for (int i = 0; i < 1 + S::sf_r; ++i) now[i] = next[i];
+                for (int i = 0; i < 4; ++i) now[i] = next[i];
                 if (k0 + kAhead < p.ktiles) load(k0 + kAhead);
+                ok = __all_sync(0xFFFFFFFFu, wait(s_sf_empty[slot & 1], ((slot >> 1) & 1) ^ 1));
+                if (!ok) break;
+                uint4* to = reinterpret_cast<uint4*>(base_p + S::stages * S::stage + (slot & 1) * S::slot + set * 512) + lane;
 #pragma unroll
-                for (int j = 0; j < kAhead; ++j) {
-                    if (k0 + j >= p.ktiles) break;
-                    ok = __all_sync(0xFFFFFFFFu, wait(s_empty[stage], phase ^ 1));
-                    if (!ok) break;
-                    uint32_t* sf = reinterpret_cast<uint32_t*>(base_p + stage * S::stage + S::bytes_l + S::bytes_r);
-#pragma unroll
-                    for (int i = 0; i < 1 + S::sf_r; ++i) sf[128 * i + (r & 31) * 4 + (r >> 5)] = now[i].word(j);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_full[stage]), CG == 2 ? 0 : cluster_rank()));
-                    advance();
-                }
+                for (int j = 0; j < kAhead; ++j)
+                    to[j * (S::sets * 32)] = make_uint4(now[0].word(j), now[1].word(j), now[2].word(j), now[3].word(j));
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_sf_full[slot & 1]), CG == 2 ? 0 : cluster_rank()));
             }
         }
     } else if (warp >= 8) {                                  // results
