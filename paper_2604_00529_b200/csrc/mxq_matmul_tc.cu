@@ -149,7 +149,7 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
     __shared__ __align__(8) uint64_t s_full[S::stages], s_empty[S::stages], s_sf_full[2], s_sf_empty[2], s_acc_full[2], s_acc_free;
     __shared__ uint32_t s_tmem, s_gave_up;
     __shared__ float s_out[T ? 1 : 4 * 32 * 33];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
     const uint32_t base = (smem_addr(s_raw) + 1023u) & ~1023u;
     uint8_t* const base_p = s_raw + (base - smem_addr(s_raw));
@@ -193,7 +193,7 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
         }
     };
 
-    if (warp == 0 && lane == 0) {                            // operand tiles
+    if (warp == 0) {                                         // operand tiles
         bool ok = true;
         for (uint32_t t = first; ok && t < tiles; t += step) {
             uint32_t tl, tr;
@@ -201,15 +201,18 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
             const int yl = (int)(tl * (kRowsL * CG) + rank * kRowsL), yr = (int)(tr * BN + rank * S::rows_r);
             for (uint32_t kt = 0; ok && kt < p.ktiles; ++kt, advance()) {
                 if (!(ok = wait(s_empty[stage], phase ^ 1))) break;
-                uint32_t bar = smem_addr(&s_full[stage]);
-                const uint32_t at = base + stage * S::stage;
-                if (rank == 0) mbar_expect(bar, CG * (S::bytes_l + S::bytes_r));
-                if constexpr (CG == 2) bar = peer_addr(bar, 0);
-                tma_tile<CG>(at, &map_l, (int)(kt * kTileK), yl, bar);
-                tma_tile<CG>(at + S::bytes_l, &map_r, (int)(kt * kTileK), yr, bar);
+                if (elect_one()) {
+                    uint32_t bar = smem_addr(&s_full[stage]);
+                    const uint32_t at = base + stage * S::stage;
+                    if (rank == 0) mbar_expect(bar, CG * (S::bytes_l + S::bytes_r));
+                    if constexpr (CG == 2) bar = peer_addr(bar, 0);
+                    tma_tile<CG>(at, &map_l, (int)(kt * kTileK), yl, bar);
+                    tma_tile<CG>(at + S::bytes_l, &map_r, (int)(kt * kTileK), yr, bar);
+                }
+                __syncwarp();
             }
         }
-    } else if (warp == 1 && lane == 0 && rank == 0) {        // matrix instructions
+    } else if (warp == 1 && rank == 0) {                     // matrix instructions
         bool ok = true;
         uint32_t n = 0;
         for (uint32_t t = first; ok && t < tiles; t += step, ++n) {
@@ -224,16 +227,21 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
                 tc_fence_after();
                 const uint32_t at = base + stage * S::stage, sf = slots + (slot & 1) * S::slot + kt % kAhead * (S::sets * 512);
                 const uint32_t tsf = tmem + S::sf_at + stage * S::sf_cols;
-#pragma unroll
-                for (int i = 0; i < S::sets; ++i) scales_to_tmem<CG>(tsf + 4 * i, scales_desc(sf + 512 * i));
                 const uint64_t a = operand_desc(at), b = operand_desc(at + S::bytes_l);
+                const bool last = kt % kAhead == kAhead - 1 || kt + 1 == p.ktiles;
+                if (elect_one()) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)                  // 32 bytes of k further inside the swizzled rows
-                    mma_scaled<CG>(d, a + 2 * j, b + 2 * j, instr_desc(kRowsL * CG, BN, j), tsf, tsf + 4, kt > 0 || j > 0);
-                mma_commit<CG>(smem_addr(&s_empty[stage]));
-                if (kt % kAhead == kAhead - 1 || kt + 1 == p.ktiles) mma_commit<CG>(smem_addr(&s_sf_empty[slot++ & 1]));
+                    for (int i = 0; i < S::sets; ++i) scales_to_tmem<CG>(tsf + 4 * i, scales_desc(sf + 512 * i));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)              // 32 bytes of k further inside the swizzled rows
+                        mma_scaled<CG>(d, a + 2 * j, b + 2 * j, instr_desc(kRowsL * CG, BN, j), tsf, tsf + 4, kt > 0 || j > 0);
+                    mma_commit<CG>(smem_addr(&s_empty[stage]));
+                    if (last) mma_commit<CG>(smem_addr(&s_sf_empty[slot & 1]));
+                    if (kt + 1 == p.ktiles) mma_commit<CG>(smem_addr(&s_acc_full[buf]));
+                }
+                __syncwarp();
+                slot += last;
             }
-            if (ok) mma_commit<CG>(smem_addr(&s_acc_full[buf]));
         }
     } else if (warp >= 4 && warp < 4 + S::sets) {            // scales: rows lane, lane + 32, + 64 and + 96 of the warp's 128
         const int set = warp - 4;
@@ -251,19 +259,16 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
             };
             load(0);
             for (uint32_t k0 = 0; k0 < p.ktiles; k0 += kAhead, ++slot) {
-                RowScales<BLOCK> now[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) now[i] = next[i];
-                if (k0 + kAhead < p.ktiles) load(k0 + kAhead);
                 ok = __all_sync(0xFFFFFFFFu, wait(s_sf_empty[slot & 1], ((slot >> 1) & 1) ^ 1));
                 if (!ok) break;
                 uint4* to = reinterpret_cast<uint4*>(base_p + S::stages * S::stage + (slot & 1) * S::slot + set * 512) + lane;
 #pragma unroll
                 for (int j = 0; j < kAhead; ++j)
-                    to[j * (S::sets * 32)] = make_uint4(now[0].word(j), now[1].word(j), now[2].word(j), now[3].word(j));
+                    to[j * (S::sets * 32)] = make_uint4(next[0].word(j), next[1].word(j), next[2].word(j), next[3].word(j));
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_sf_full[slot & 1]), CG == 2 ? 0 : cluster_rank()));
+                if (k0 + kAhead < p.ktiles) load(k0 + kAhead);      // behind the fence, which waits for loads under way
             }
         }
     } else if (warp >= 8) {                                  // results

@@ -29,6 +29,15 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// One lane of the warp, the same every time.  The warps that feed the tensor cores run their loops with all lanes, so that what
+// they compute is uniform for the compiler, and let this lane alone issue.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(one));
+    return one != 0;
+}
+
 // ---- mbarriers --------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
@@ -49,7 +58,7 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
@@ -67,13 +76,14 @@ constexpr uint64_t kWaitLimitNs = 10ull * 1000 * 1000 * 1000;
 
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, unsigned int* status)
 {
-    if (mbar_try(bar, parity)) return true;
-    const uint64_t began = global_ns();
+    uint64_t began = 0;                                      // (the timer is slow to read: not before many tries)
     for (uint32_t i = 1;; ++i) {
         if (mbar_try(bar, parity)) return true;
-        if ((i & 63u) == 0) {
+        if ((i & 1023u) == 0) {
             if (*gave_up) return false;
-            if (global_ns() - began > kWaitLimitNs) {
+            const uint64_t now = global_ns();
+            if (began == 0) began = now;
+            if (now - began > kWaitLimitNs) {
                 *gave_up = 1;
                 atomicOr(status, 1u);
                 return false;
