@@ -224,7 +224,7 @@ int mxq_matmul(const void* a_codes, const uint8_t* a_scales, const void* b_codes
     MXQ_DEBUG_EXPECT(dst, m * n * size);
     const MatmulArgs p{static_cast<const uint8_t*>(a_codes), a_scales, static_cast<const uint8_t*>(b_codes), b_scales, m, n, k, block,
                        static_cast<uint8_t*>(dst)};
-    return m <= 16 ? launch_matmul_few(p, dst_dtype, s) : launch_matmul_tc(p, dst_dtype, s);
+    return m <= 4 ? launch_matmul_few(p, dst_dtype, s) : launch_matmul_tc(p, dst_dtype, s);
 }
 
 int mxq_wait_status(int reset) { return tc_status(reset); }

@@ -7,8 +7,10 @@
 // They are brought for eight k tiles at a time: a hand-over (a fence between the two memory proxies, an arrival across the pair)
 // takes longer than the tensor cores take for one.
 //
-// Warps of a CTA: 0 loads operand tiles (TMA), 1 issues the matrix instructions (of the pair: the first CTA's), 4 - 6 bring the
-// scales, 128 rows each, 8 - 11 write results.  A CTA pair (CG = 2) works on 256 rows of L, 128 per CTA, and shares the tile of R half and half.
+// Warps of a CTA: 0 loads operand tiles (TMA), 1 issues the matrix instructions (of the pair: the first CTA's), 2 - 7 bring the
+// scales, 8 - 11 write results.  Tiles are worked on one after another by a CTA (pair) per SM (pair of SMs); or,
+// where there are too few of them for that (SPLIT), a cluster shares one tile's k out and adds its parts through distributed
+// shared memory, in a fixed order.  A CTA pair (CG = 2) works on 256 rows of L, 128 per CTA, and shares the tile of R half and half.
 #include <cuda.h>
 
 #include "mxq_kernels.cuh"
@@ -23,17 +25,18 @@ __device__ unsigned int g_status;                            // a bounded wait g
 constexpr int kRowsL = 128;                                  // rows of L per CTA
 constexpr int kTileK = 128;                                  // bytes = elements of k per stage
 constexpr int kThreads = 384;
-constexpr int kAhead = 8;                                   // k tiles whose scales are brought together
 
 template <int CG, int BN>
 struct Shape {
+    static constexpr int ahead = 8;                          // k tiles whose scales are brought together
+    static constexpr int budget = 205 * 1024;
     static constexpr int rows_r = BN / CG;                   // rows of R that a CTA loads
     static constexpr int sf_r = (BN + 127) / 128;            // 512-byte scale tiles of R
     static constexpr int bytes_l = kRowsL * kTileK, bytes_r = rows_r * kTileK;
     static constexpr int sets = 1 + sf_r;                    // groups of 128 rows that have scales
-    static constexpr int slot = kAhead * sets * 512;         // the scale words of kAhead k tiles
+    static constexpr int slot = ahead * sets * 512;          // the scale words of `ahead` k tiles
     static constexpr int stage = bytes_l + bytes_r;
-    static constexpr int stages = (205 * 1024 - 2 * slot) / stage < 8 ? (205 * 1024 - 2 * slot) / stage : 8;
+    static constexpr int stages = (budget - 2 * slot) / stage < 8 ? (budget - 2 * slot) / stage : 8;
     static constexpr int sf_cols = 4 * sets;                 // columns of tensor memory per stage
     // Two accumulators, so that one tile's results leave while the next is computed.  Where tensor memory does not hold both
     // (BN = 256), the second begins inside the first; the columns that they share are read first.
@@ -50,7 +53,7 @@ struct TcArgs {
     const uint8_t *ls, *rs;                                  // scale bytes
     uint8_t* dst;
     size_t rows_l, rows_r;
-    uint32_t kblocks, tiles_l, tiles_r, ktiles;
+    uint32_t kblocks, tiles_l, tiles_r, ktiles, split;
     size_t ld;                                               // elements between rows of dst
 };
 
@@ -63,12 +66,12 @@ __device__ __forceinline__ void tile_at(uint32_t t, uint32_t tiles_l, uint32_t t
     tr = in / height;
 }
 
-// The scale bytes of a row for eight k tiles, as they lie in memory.  Bytes beyond k, or of a row beyond the matrix, are 1.0:
+// The scale bytes of a row for AHEAD k tiles, as they lie in memory.  Bytes beyond k, or of a row beyond the matrix, are 1.0:
 // what they scale is 0.
-template <int BLOCK>
+template <int BLOCK, int AHEAD>
 struct RowScales {
     static constexpr int PER = kTileK / BLOCK;               // bytes per k tile
-    static constexpr int NW = kAhead * PER / 4;
+    static constexpr int NW = AHEAD * PER / 4;
     uint32_t w[NW];
 
     __device__ __forceinline__ void load(const uint8_t* s, size_t row, size_t rows, uint32_t kt, uint32_t kblocks)
@@ -78,7 +81,7 @@ struct RowScales {
         if (row >= rows) return;
         const uint8_t* at = s + row * kblocks;
         const uint32_t first = kt * PER;
-        if ((kblocks & 3u) == 0) {
+        if (((kblocks | first) & 3u) == 0) {
 #pragma unroll
             for (int j = 0; j < NW; ++j)
                 if (first + 4 * j < kblocks) w[j] = ld_u32(at + first + 4 * j);
@@ -140,7 +143,7 @@ __device__ __forceinline__ void store_block(const TcArgs& p, const uint32_t (&v)
     }
 }
 
-template <class OUT, int CG, int BN, bool T, int BLOCK>
+template <class OUT, int CG, int BN, bool T, int BLOCK, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
 matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_r, const TcArgs p)
 {
@@ -148,9 +151,10 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
     extern __shared__ uint8_t s_raw[];
     __shared__ __align__(8) uint64_t s_full[S::stages], s_empty[S::stages], s_sf_full[2], s_sf_empty[2], s_acc_full[2], s_acc_free;
     __shared__ uint32_t s_tmem, s_gave_up;
+    static_assert(!SPLIT || T, "parts are added along D's rows");
     __shared__ float s_out[T ? 1 : 4 * 32 * 33];
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
+    const uint32_t in_cluster = CG == 2 || SPLIT ? cluster_rank() : 0u, rank = in_cluster % CG, leader = in_cluster - rank;
     const uint32_t base = (smem_addr(s_raw) + 1023u) & ~1023u;
     uint8_t* const base_p = s_raw + (base - smem_addr(s_raw));
     pdl_release();
@@ -176,13 +180,20 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
         }
     }
     tc_fence_before();
-    if constexpr (CG == 2) cluster_sync();
+    if constexpr (CG == 2 || SPLIT) cluster_sync();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     pdl_acquire();
 
-    const uint32_t tiles = p.tiles_l * p.tiles_r, step = gridDim.x / CG, first = blockIdx.x / CG;
+    // the tiles of this CTA (pair) and its k tiles of each: all of them, or a part that begins at a whole word of scale bytes
+    const uint32_t tiles = p.tiles_l * p.tiles_r, step = SPLIT ? tiles : gridDim.x / CG, first = blockIdx.x / (SPLIT ? CG * p.split : CG);
+    uint32_t k_lo = 0, k_hi = p.ktiles;
+    if constexpr (SPLIT) {
+        const uint32_t unit = p.ktiles >= 8 * p.split ? 4 : 1, units = (p.ktiles + unit - 1) / unit, part = in_cluster / CG;
+        k_lo = min(units * part / p.split * unit, p.ktiles);
+        k_hi = min(units * (part + 1) / p.split * unit, p.ktiles);
+    }
     auto wait = [&](uint64_t& bar, uint32_t parity) { return mbar_wait(smem_addr(&bar), parity, &s_gave_up, &g_status); };
     uint32_t stage = 0, phase = 0, slot = 0;                 // slots are numbered through: slot & 1, parity (slot >> 1) & 1
     const uint32_t slots = base + S::stages * S::stage;
@@ -199,13 +210,13 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
             uint32_t tl, tr;
             tile_at(t, p.tiles_l, p.tiles_r, tl, tr);
             const int yl = (int)(tl * (kRowsL * CG) + rank * kRowsL), yr = (int)(tr * BN + rank * S::rows_r);
-            for (uint32_t kt = 0; ok && kt < p.ktiles; ++kt, advance()) {
+            for (uint32_t kt = k_lo; ok && kt < k_hi; ++kt, advance()) {
                 if (!(ok = wait(s_empty[stage], phase ^ 1))) break;
                 if (elect_one()) {
                     uint32_t bar = smem_addr(&s_full[stage]);
                     const uint32_t at = base + stage * S::stage;
                     if (rank == 0) mbar_expect(bar, CG * (S::bytes_l + S::bytes_r));
-                    if constexpr (CG == 2) bar = peer_addr(bar, 0);
+                    if constexpr (CG == 2) bar = peer_addr(bar, leader);
                     tma_tile<CG>(at, &map_l, (int)(kt * kTileK), yl, bar);
                     tma_tile<CG>(at + S::bytes_l, &map_r, (int)(kt * kTileK), yr, bar);
                 }
@@ -221,55 +232,58 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
             if (n > 0 && !(ok = wait(s_acc_free, (n - 1) & 1))) break;
             tc_fence_after();
             const uint32_t buf = n & 1, d = tmem + buf * S::second;
-            for (uint32_t kt = 0; kt < p.ktiles; ++kt, advance()) {
+            for (uint32_t kt = 0; kt < k_hi - k_lo; ++kt, advance()) {
                 if (!(ok = wait(s_full[stage], phase))) break;
-                if (kt % kAhead == 0 && !(ok = wait(s_sf_full[slot & 1], (slot >> 1) & 1))) break;
+                if (kt % S::ahead == 0 && !(ok = wait(s_sf_full[slot & 1], (slot >> 1) & 1))) break;
                 tc_fence_after();
-                const uint32_t at = base + stage * S::stage, sf = slots + (slot & 1) * S::slot + kt % kAhead * (S::sets * 512);
+                const uint32_t at = base + stage * S::stage, sf = slots + (slot & 1) * S::slot + kt % S::ahead * (S::sets * 512);
                 const uint32_t tsf = tmem + S::sf_at + stage * S::sf_cols;
                 const uint64_t a = operand_desc(at), b = operand_desc(at + S::bytes_l);
-                const bool last = kt % kAhead == kAhead - 1 || kt + 1 == p.ktiles;
+                const bool end = kt + 1 == k_hi - k_lo, last = kt % S::ahead == S::ahead - 1 || end;
                 if (elect_one()) {
 #pragma unroll
                     for (int i = 0; i < S::sets; ++i) scales_to_tmem<CG>(tsf + 4 * i, scales_desc(sf + 512 * i));
 #pragma unroll
                     for (int j = 0; j < 4; ++j)              // 32 bytes of k further inside the swizzled rows
                         mma_scaled<CG>(d, a + 2 * j, b + 2 * j, instr_desc(kRowsL * CG, BN, j), tsf, tsf + 4, kt > 0 || j > 0);
-                    mma_commit<CG>(smem_addr(&s_empty[stage]));
-                    if (last) mma_commit<CG>(smem_addr(&s_sf_empty[slot & 1]));
-                    if (kt + 1 == p.ktiles) mma_commit<CG>(smem_addr(&s_acc_full[buf]));
+                    mma_commit<CG>(smem_addr(&s_empty[stage]), leader);
+                    if (last) mma_commit<CG>(smem_addr(&s_sf_empty[slot & 1]), leader);
+                    if (end) mma_commit<CG>(smem_addr(&s_acc_full[buf]), leader);
                 }
                 __syncwarp();
                 slot += last;
             }
         }
-    } else if (warp >= 4 && warp < 4 + S::sets) {            // scales: rows lane, lane + 32, + 64 and + 96 of the warp's 128
-        const int set = warp - 4;
-        bool ok = true;
-        for (uint32_t t = first; ok && t < tiles; t += step) {
+    } else if (warp >= 2 && warp < 8 && (warp - 2) % 3 < S::sets) {
+        // Scales: rows lane, lane + 32, + 64 and + 96 of a group of 128, for every other slot: two warps take turns, since filling one
+        // (loads, a fence that waits for them, an arrival) takes longer than the tensor cores take for its k tiles.
+        const int set = (warp - 2) % 3;
+        const uint32_t turn = (warp - 2) / 3, chunks = (k_hi - k_lo + S::ahead - 1) / S::ahead;
+        const uint8_t* s = set == 0 ? p.ls : p.rs;
+        uint32_t t = first, c = turn;
+        RowScales<BLOCK, S::ahead> w[4];
+        auto load = [&] {                                    // the warp's next chunk, which may lie in a later tile
+            for (; t < tiles && c >= chunks; t += step) c -= chunks;
+            if (t >= tiles) return;
             uint32_t tl, tr;
             tile_at(t, p.tiles_l, p.tiles_r, tl, tr);
-            const uint8_t* s = set == 0 ? p.ls : p.rs;
             const size_t row0 = set == 0 ? (size_t)tl * (kRowsL * CG) + rank * kRowsL : (size_t)tr * BN + 128 * (set - 1);
             const size_t rows = set == 0 ? p.rows_l : min(p.rows_r, (size_t)(tr + 1) * BN);
-            RowScales<BLOCK> next[4];
-            auto load = [&](uint32_t kt) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) next[i].load(s, row0 + lane + 32 * i, rows, kt, p.kblocks);
-            };
-            load(0);
-            for (uint32_t k0 = 0; k0 < p.ktiles; k0 += kAhead, ++slot) {
-                ok = __all_sync(0xFFFFFFFFu, wait(s_sf_empty[slot & 1], ((slot >> 1) & 1) ^ 1));
-                if (!ok) break;
-                uint4* to = reinterpret_cast<uint4*>(base_p + S::stages * S::stage + (slot & 1) * S::slot + set * 512) + lane;
+            for (int i = 0; i < 4; ++i) w[i].load(s, row0 + lane + 32 * i, rows, k_lo + c * S::ahead, p.kblocks);
+        };
+        load();
+        for (slot = turn; t < tiles; slot += 2) {
+            if (!__all_sync(0xFFFFFFFFu, wait(s_sf_empty[turn], ((slot >> 1) & 1) ^ 1))) break;
+            uint4* to = reinterpret_cast<uint4*>(base_p + S::stages * S::stage + turn * S::slot + set * 512) + lane;
 #pragma unroll
-                for (int j = 0; j < kAhead; ++j)
-                    to[j * (S::sets * 32)] = make_uint4(next[0].word(j), next[1].word(j), next[2].word(j), next[3].word(j));
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_sf_full[slot & 1]), CG == 2 ? 0 : cluster_rank()));
-                if (k0 + kAhead < p.ktiles) load(k0 + kAhead);      // behind the fence, which waits for loads under way
-            }
+            for (int j = 0; j < S::ahead; ++j)
+                to[j * (S::sets * 32)] = make_uint4(w[0].word(j), w[1].word(j), w[2].word(j), w[3].word(j));
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_sf_full[turn]), leader));
+            c += 2;
+            load();                                          // behind the fence
         }
     } else if (warp >= 8) {                                  // results
         bool ok = true;
@@ -286,7 +300,7 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
             auto release = [&] {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_acc_free), CG == 2 ? 0 : cluster_rank()));
+                if (lane == 0) mbar_arrive_cluster(peer_addr(smem_addr(&s_acc_free), leader));
             };
             if (S::over == 0) release();
 #pragma unroll 1
@@ -297,6 +311,12 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
                 tmem_ld32(v, tmem + buf * S::second + c + ((uint32_t)(q * 32) << 16));
                 tmem_ld_wait();
                 if (S::over && i + 32 == S::over) release();
+                if constexpr (SPLIT) {                       // the stages are free: every product of theirs is done
+                    float* part = reinterpret_cast<float*>(base_p) + q * 32 + lane;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) part[(c + j) * kRowsL] = __uint_as_float(v[j]);
+                    continue;
+                }
                 store_block<OUT, T>(p, v, row, (size_t)tr * BN + c, s_out + (T ? 0 : q * 32 * 33), lane);
             }
         }
@@ -309,7 +329,40 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
     }
     tc_fence_before();
     __syncthreads();
-    if constexpr (CG == 2) cluster_sync();
+    if constexpr (SPLIT) {                                   // this CTA's share of the columns, the parts in order
+        static_assert(S::stages * S::stage >= BN * kRowsL * 4, "a part fits in the stages");
+        cluster_sync();
+        uint32_t tl, tr;
+        tile_at(first, p.tiles_l, p.tiles_r, tl, tr);
+        const size_t row = (size_t)tl * (kRowsL * CG) + rank * kRowsL + lane * 4;
+        const uint32_t part = in_cluster / CG, c_hi = BN * (part + 1) / p.split;
+        for (uint32_t c = BN * part / p.split + warp; c < c_hi; c += kThreads / 32) {
+            const size_t col = (size_t)tr * BN + c;
+            if (col >= p.rows_r) break;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (uint32_t i = 0; i < p.split; ++i) {
+                const float4 v = ld_peer4(peer_addr(base + (c * kRowsL + lane * 4) * 4, i * CG + rank));
+                sum.x += v.x;
+                sum.y += v.y;
+                sum.z += v.z;
+                sum.w += v.w;
+            }
+            const size_t at = col * p.ld + row;
+            if ((p.ld & 3) == 0) {
+                if (row >= p.rows_l) continue;
+                uint8_t* to = p.dst + at * OUT::size;
+                MXQ_CHECKED(to, 4 * OUT::size, continue)
+                if constexpr (OUT::size == 4) *reinterpret_cast<float4*>(to) = sum;
+                else *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
+            } else {
+                const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (row + j < p.rows_l) put<OUT>(p.dst, at + j, v[j]);
+            }
+        }
+    }
+    if constexpr (CG == 2 || SPLIT) cluster_sync();
     if (warp == 0) tmem_free<CG>(tmem, S::tmem_cols);
 }
 
@@ -344,12 +397,12 @@ bool make_map(CUtensorMap* map, const uint8_t* p, size_t rows, size_t k, int box
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class OUT, int CG, int BN, bool T, int BLOCK>
-int run_block(const MatmulArgs& m, cudaStream_t stream)
+template <class OUT, int CG, int BN, bool T, int BLOCK, bool SPLIT>
+int run_block(const MatmulArgs& m, uint32_t split, cudaStream_t stream)
 {
     using S = Shape<CG, BN>;
     static std::atomic<uint64_t> done{0};
-    auto kern = matmul_tc_kernel<OUT, CG, BN, T, BLOCK>;
+    auto kern = matmul_tc_kernel<OUT, CG, BN, T, BLOCK, SPLIT>;
     if (int rc = allow_smem(reinterpret_cast<const void*>(kern), S::smem, done)) return rc;
     TcArgs p;
     p.ls = T ? m.bs : m.as;
@@ -358,32 +411,77 @@ int run_block(const MatmulArgs& m, cudaStream_t stream)
     p.rows_r = T ? m.m : m.n;
     p.dst = m.dst;
     p.ld = m.n;
+    p.split = split;
     p.kblocks = (uint32_t)(m.k / (size_t)m.block);
     p.ktiles = (uint32_t)((m.k + kTileK - 1) / kTileK);
     p.tiles_l = (uint32_t)((p.rows_l + kRowsL * CG - 1) / (kRowsL * CG));
     p.tiles_r = (uint32_t)((p.rows_r + BN - 1) / BN);
-    if ((uint64_t)p.tiles_l * p.tiles_r > 0x7FFFFFFFull) return MXQ_ERR_SIZE;
+    if ((uint64_t)p.tiles_l * p.tiles_r > 0x7FFFFFFFull / (CG * split)) return MXQ_ERR_SIZE;
     CUtensorMap ml, mr;
     if (!make_map(&ml, T ? m.b : m.a, p.rows_l, m.k, kRowsL) || !make_map(&mr, T ? m.a : m.b, p.rows_r, m.k, S::rows_r)) return MXQ_ERR_CUDA;
     const uint32_t tiles = p.tiles_l * p.tiles_r, most = 148 / CG;
-    const unsigned grid = (tiles < most ? tiles : most) * CG;
-    return launch_grid(kern, dim3(grid), kThreads, S::smem, CG, stream, ml, mr, p);
+    const unsigned grid = SPLIT ? tiles * split * CG : (tiles < most ? tiles : most) * CG;
+    return launch_grid(kern, dim3(grid), kThreads, S::smem, (int)(CG * split), stream, ml, mr, p);
 }
 
-template <class OUT, int CG, int BN, bool T>
-int run(const MatmulArgs& m, cudaStream_t stream)
+template <class OUT, int CG, int BN, bool T, bool SPLIT>
+int run(const MatmulArgs& m, uint32_t split, cudaStream_t stream)
 {
-    if (m.block == 32) return run_block<OUT, CG, BN, T, 32>(m, stream);
-    if (m.block == 64) return run_block<OUT, CG, BN, T, 64>(m, stream);
-    return run_block<OUT, CG, BN, T, 128>(m, stream);
+    if (m.block == 32) return run_block<OUT, CG, BN, T, 32, SPLIT>(m, split, stream);
+    if (m.block == 64) return run_block<OUT, CG, BN, T, 64, SPLIT>(m, split, stream);
+    return run_block<OUT, CG, BN, T, 128, SPLIT>(m, split, stream);
+}
+
+// What a launch is expected to take, in microseconds: a fixed part per wave of CTAs (start, first loads, sums and stores of the
+// results) and a time per k tile, as measured with blocks of 128 (device time, inputs of a few calls in turn):
+//   single CTAs, 32 columns, k in S parts    512 x 512 x 4096 S = 1, 2, 4: 12.7 10.2 9.6;   13 x 14336 x 4096 S = 1: 14.9
+//   single CTAs, 64 columns                  64 x 14336 x 4096 S = 1: 15.8 (32 columns 26.8: two waves);  1000 x 1111 x 1152: 8.8
+//   pairs, 128 columns, k in S parts         200 x 4096 x 14336 S = 1, 2: 31.0 21.1
+//   pairs, 128 columns, tiles in turn        512 x 4096 x 4096: 13.1 (256 columns 16.3);  4096 x 4096 x 4096: 67
+//   pairs, 256 columns, tiles in turn        512 x 4096 x 4096: 16.3;  4096 x 4096 x 4096: 56
+// The rule picks the smallest; beyond four CTAs a cluster finds too few free neighbours (S = 8: 17.7 against 7.9 us with S = 4 for
+// one row of 4096 x 4096), so more parts are not offered.
+struct Plan {
+    int cg, bn, split;                                       // split 0: tiles in turn
+    double us;
+};
+
+Plan plan(const MatmulArgs& m)
+{
+    auto tiles = [](size_t rows, size_t per) { return (double)((rows + per - 1) / per); };
+    const double kt = tiles(m.k, kTileK);
+    auto waves = [](double ctas) { return ctas <= 148 ? 1.0 : (double)(size_t)((ctas + 147) / 148); };
+    Plan best{2, 256, 0, 4.0 + waves(2 * tiles(m.m, 256) * tiles(m.n, 256)) * (kt * 0.36 + 1.6)};
+    auto offer = [&](int cg, int bn, int split, double us) {
+        if (us < best.us) best = Plan{cg, bn, split, us};
+    };
+    offer(2, 128, 0, 4.0 + waves(2 * tiles(m.m, 256) * tiles(m.n, 128)) * (kt * 0.25 + 1.2));
+    for (int s = 1; s <= 4; s *= 2) {
+        if (s > kt) break;
+        const double part = (double)(size_t)((kt + s - 1) / s);
+        offer(1, 32, s, waves(tiles(m.n, 128) * tiles(m.m, 32) * s) * (6.2 + part * 0.2));
+        offer(1, 64, s, waves(tiles(m.n, 128) * tiles(m.m, 64) * s) * (6.5 + part * 0.21));
+        if (s <= 2) offer(2, 128, s, waves(2 * tiles(m.n, 256) * tiles(m.m, 128) * s) * (6.6 + part * 0.22));
+    }
+    return best;
+}
+
+template <class OUT>
+int choose(const MatmulArgs& m, cudaStream_t stream)
+{
+    const Plan p = plan(m);
+    if (p.split && p.bn == 32) return run<OUT, 1, 32, true, true>(m, (uint32_t)p.split, stream);
+    if (p.split && p.bn == 64) return run<OUT, 1, 64, true, true>(m, (uint32_t)p.split, stream);
+    if (p.split) return run<OUT, 2, 128, true, true>(m, (uint32_t)p.split, stream);
+    if (p.bn == 128) return run<OUT, 2, 128, false, false>(m, 1, stream);
+    return run<OUT, 2, 256, false, false>(m, 1, stream);
 }
 
 }  // namespace
 
 int launch_matmul_tc(const MatmulArgs& p, int dst_dtype, cudaStream_t stream)
 {
-    if (dst_dtype == MXQ_F32) return run<F32, 2, 256, false>(p, stream);
-    return run<BF16, 2, 256, false>(p, stream);
+    return dst_dtype == MXQ_F32 ? choose<F32>(p, stream) : choose<BF16>(p, stream);
 }
 
 // Whether a bounded wait of these kernels gave up on the current device; waits for the device.

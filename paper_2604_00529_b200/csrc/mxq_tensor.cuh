@@ -190,15 +190,24 @@ __device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, u
                      :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)add) : "memory");
 }
 
-// One arrival at `bar` (of both CTAs of a pair) when all matrix instructions issued so far are done.
+// One arrival at `bar` (of both CTAs of a pair whose first one has rank `first` in the cluster) when all matrix instructions
+// issued so far are done.
 template <int CG>
-__device__ __forceinline__ void mma_commit(uint32_t bar)
+__device__ __forceinline__ void mma_commit(uint32_t bar, uint32_t first)
 {
     if constexpr (CG == 1)
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
     else
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                     :: "r"(bar), "h"((uint16_t)3) : "memory");
+                     :: "r"(bar), "h"((uint16_t)(3u << first)) : "memory");
+}
+
+// Four floats of another CTA's shared memory.
+__device__ __forceinline__ float4 ld_peer4(uint32_t cluster_addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
+    return v;
 }
 
 }  // namespace mxq

@@ -73,6 +73,21 @@ def test_matmul_scales_at_the_ends_of_their_range(m, block):
     pu.check(got, want, np.nan_to_num(pu.sum_bound(k, np.abs(a) @ np.abs(b).T)))
 
 
+@pytest.mark.parametrize("m,n,k,block,dtype", [(520, 4100, 640, 32, BF), (520, 4111, 1280, 128, FP), (2100, 4400, 512, 64, BF), (2100, 4401, 384, 128, BF),
+                                               (2100, 4401, 192, 64, FP), (4100, 2500, 1152, 32, FP), (8200, 300, 256, 128, BF)])
+def test_matmul_many_tiles(m, n, k, block, dtype):
+    """Sizes at which a CTA works on several tiles in turn, whole and cut off."""
+    rng = rng_of(m, n, k, block)
+    ac, as_, a = pu.quantized(rng, m, k, "e4m3", block)
+    bc, bs, b = pu.quantized(rng, n, k, "e4m3", block, 0.02)
+    out = Guarded(m * n * dtype.itemsize, dtype)
+    got = mxq.matmul(dev(ac), dev(as_), dev(bc), dev(bs), m, n, k, block=block, out=out.view)
+    out.check()
+    pu.check(got.view(m, n), a @ b.T, pu.sum_bound(k, np.abs(a) @ np.abs(b).T))
+    again = mxq.matmul(dev(ac), dev(as_), dev(bc), dev(bs), m, n, k, block=block, dtype=dtype)
+    assert torch.equal(got.view(m, n), again)
+
+
 def test_matmul_empty():
     c, s = torch.empty(0, dtype=torch.uint8, device="cuda"), torch.empty(0, dtype=torch.uint8, device="cuda")
     assert mxq.matmul(c, s, c, s, 0, 0, 128, block=128).shape == (0, 0)
