@@ -15,103 +15,142 @@ namespace {
 constexpr int kTile = 128;
 constexpr int kMatThreads = 256;
 
-// eight consecutive elements of row r from column c on, as FP32; zeros outside the matrix
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const uint8_t* __restrict__ src, size_t rows, size_t cols, size_t r, size_t c, float (&v)[8])
-{
+// Eight consecutive elements of one row: BF16 as they lie in memory, two to a word (half the registers of FP32 values).
+template <class T>
+struct Eight;
+template <>
+struct Eight<BF16> {
+    uint32_t w[4];
+    __device__ __forceinline__ float at(int j) const { return __uint_as_float((j & 1) ? (w[j / 2] & 0xFFFF0000u) : (w[j / 2] << 16)); }
+    __device__ __forceinline__ uint32_t upper2(int i) const { return w[i] & 0x7FFF7FFFu; }      // |patterns|' upper halves, elements 2 i, 2 i + 1
+    __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
+    __device__ __forceinline__ void load(const uint8_t* p)
+    {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+    }
+    __device__ __forceinline__ void put(int j, const uint8_t* p) { w[j / 2] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p)) << (16 * (j & 1)); }
+};
+template <>
+struct Eight<F32> {
+    uint32_t w[8];
+    __device__ __forceinline__ float at(int j) const { return __uint_as_float(w[j]); }
+    __device__ __forceinline__ uint32_t upper2(int i) const { return __byte_perm(w[2 * i], w[2 * i + 1], 0x7632) & 0x7FFF7FFFu; }
+    __device__ __forceinline__ void zero()
+    {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+        for (int j = 0; j < 8; ++j) w[j] = 0;
+    }
+    __device__ __forceinline__ void load(const uint8_t* p)
+    {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p)), b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    }
+    __device__ __forceinline__ void put(int j, const uint8_t* p) { w[j] = __ldg(reinterpret_cast<const uint32_t*>(p)); }
+};
+
+// elements c ... c + 7 of row r; zeros outside the matrix
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const uint8_t* __restrict__ src, size_t rows, size_t cols, size_t r, size_t c, Eight<T>& v)
+{
+    v.zero();
     if (r >= rows) return;
+    const uint8_t* p = src + (r * cols + c) * T::size;
     if constexpr (VEC) {                                     // cols % 8 == 0: a piece is inside or outside as a whole
         if (c >= cols) return;
-        const uint8_t* p = src + (r * cols + c) * T::size;
-        if constexpr (T::size == 4) {
-            MXQ_CHECKED(p, 32, return)
-            const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            MXQ_CHECKED(p, 16, return)
-            const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float((j & 1) ? (w[j / 2] & 0xFFFF0000u) : (w[j / 2] << 16));
-        }
+        MXQ_CHECKED(p, 8 * T::size, return)
+        v.load(p);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if (c + j >= cols) continue;
-            const uint8_t* p = src + (r * cols + c + j) * T::size;
-            MXQ_CHECKED(p, T::size, continue)
-            if constexpr (T::size == 4) v[j] = __ldg(reinterpret_cast<const float*>(p));
-            else v[j] = __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p)) << 16);
+            MXQ_CHECKED(p + j * T::size, T::size, continue)
+            v.put(j, p + j * T::size);
         }
     }
 }
 
-__device__ __forceinline__ uint32_t upper_abs(float v) { return (__float_as_uint(v) >> 16) & 0x7FFFu; }
-
 // FP32 bit patterns are ordered like the values, and only the exponent field of a maximum is used (0xFF: the block is
-// poisoned): the patterns' upper halves are enough, two columns to a word.
+// poisoned): the patterns' upper halves are enough, two to a word.
 template <class T, class F, int BLOCK, bool VEC>
-__global__ void __launch_bounds__(kMatThreads)
+__global__ void __launch_bounds__(kMatThreads, T::size == 2 ? 4 : 2)
 quantize_matrix_kernel(const uint8_t* __restrict__ src, size_t rows, size_t cols, uint8_t* __restrict__ codes,
-                       uint8_t* __restrict__ scales, uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t, uint32_t col_tiles)
+                       uint8_t* __restrict__ scales, uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t, uint32_t row_tiles, uint32_t col_tiles)
 {
     constexpr int LPB = BLOCK / 8;                           // lanes per block along a row
     constexpr int G = BLOCK / 32;                            // groups of 32 rows per block along a column
     __shared__ uint32_t s_max[2][8][kTile / 2];              // [rows / 64][warp][column pair]
-    __shared__ uint8_t s_byte[4][kTile];                     // scale byte per group of 32 rows and column
+    __shared__ __align__(8) uint8_t s_byte[4][kTile];        // scale byte per group of 32 rows and column
     __shared__ uint32_t s_codes[kTile][32];                  // [column][four rows], exchanged
     pdl_release();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, l = lane & 15, rg = warp * 2 + (lane >> 4);
-    const size_t tr = blockIdx.x / col_tiles, tc = blockIdx.x % col_tiles;
+    // eight tiles of a column one after another: the transpose's lines then meet in L2 as longer runs
+    const uint32_t band = blockIdx.x / (8 * col_tiles), height = min(8u, row_tiles - band * 8), in_band = blockIdx.x - band * 8 * col_tiles;
+    const size_t tr = band * 8 + in_band % height, tc = in_band / height;
     const size_t r0 = tr * kTile, c0 = tc * kTile;
     const size_t rows_p = (rows + BLOCK - 1) / BLOCK * BLOCK, cols_p = (cols + BLOCK - 1) / BLOCK * BLOCK;
     pdl_acquire();
 
-    float v[2][4][8];
+    Eight<T> v[2][4];                                        // rows 64 s + 4 rg + i
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int i = 0; i < 4; ++i) load8<T, VEC>(src, rows, cols, r0 + s * 64 + rg * 4 + i, c0 + l * 8, v[s][i]);
 
-    if (codes) {                                             // along the rows
+    // along the columns: the thread's four rows, the two halves of the warp, then (below) the four warps of a group of 32 rows
+    if (codes_t) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t m = __vmaxu2(__vmaxu2(v[s][0].upper2(j), v[s][1].upper2(j)), __vmaxu2(v[s][2].upper2(j), v[s][3].upper2(j)));
+                m = __vmaxu2(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+                if (lane < 16) s_max[s][warp][l * 4 + j] = m;
+            }
+    }
+
+    if (codes) {                                             // along the rows: the maxima of two rows to a word
+        uint32_t m[2][2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t a[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const Eight<T>& e = v[s][2 * h + i];
+                    a[i] = __vmaxu2(__vmaxu2(e.upper2(0), e.upper2(1)), __vmaxu2(e.upper2(2), e.upper2(3)));
+                }
+                m[s][h] = __vmaxu2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[0], a[1], 0x7632));
+            }
+#pragma unroll
+        for (int o = 1; o < LPB; o <<= 1)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) m[s][h] = __vmaxu2(m[s][h], __shfl_xor_sync(0xFFFFFFFFu, m[s][h], o));
+        const size_t c = c0 + l * 8;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                uint32_t m = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) m = max(m, upper_abs(v[s][i][j]));
-                m = group_max<LPB>(m);
-                const BlockScale sc = block_scale<F>(m << 16);
-                const size_t r = r0 + s * 64 + rg * 4 + i, c = c0 + l * 8;
-                if (r >= rows || c >= cols_p) continue;
-                uint2 q = make_uint2(0, 0);
-                if (sc.byte != 255u) {
-                    const float (&e)[8] = v[s][i];
-                    q.x = quantize_fp_hw_quad<F>(e[0] * sc.inv, e[1] * sc.inv, e[2] * sc.inv, e[3] * sc.inv);
-                    q.y = quantize_fp_hw_quad<F>(e[4] * sc.inv, e[5] * sc.inv, e[6] * sc.inv, e[7] * sc.inv);
+                const Eight<T>& e = v[s][i];
+                const BlockScale sc = block_scale<F>((i & 1) ? m[s][i / 2] & 0xFFFF0000u : m[s][i / 2] << 16);
+                uint2 q;
+                q.x = quantize_fp_hw_quad<F>(e.at(0) * sc.inv, e.at(1) * sc.inv, e.at(2) * sc.inv, e.at(3) * sc.inv);
+                q.y = quantize_fp_hw_quad<F>(e.at(4) * sc.inv, e.at(5) * sc.inv, e.at(6) * sc.inv, e.at(7) * sc.inv);
+                if (sc.byte == 255u) q = make_uint2(0, 0);
+                const size_t r = r0 + s * 64 + rg * 4 + i;
+                if (r < rows && c < cols_p) {
+                    uint8_t* p = codes + r * cols_p + c;
+                    bool ok = true;
+                    MXQ_CHECKED(p, 8, ok = false)
+                    if (ok) *reinterpret_cast<uint2*>(p) = q;
+                    if (l % LPB == 0) st_u8(scales + r * (cols_p / BLOCK) + c / BLOCK, sc.byte);
                 }
-                uint8_t* p = codes + r * cols_p + c;
-                MXQ_CHECKED(p, 8, continue)
-                *reinterpret_cast<uint2*>(p) = q;
-                if (l % LPB == 0) st_u8(scales + r * (cols_p / BLOCK) + c / BLOCK, sc.byte);
             }
     }
     if (!codes_t) return;
-
-    // along the columns: the thread's four rows, the two halves of the warp, then the four warps of a group of 32 rows
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) m = __vmaxu2(m, upper_abs(v[s][i][2 * j]) | upper_abs(v[s][i][2 * j + 1]) << 16);
-            m = __vmaxu2(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-            if (lane < 16) s_max[s][warp][l * 4 + j] = m;
-        }
     __syncthreads();
     {
         const int c = tid & 127, s = tid >> 7;               // one column's 64 rows
@@ -131,21 +170,36 @@ quantize_matrix_kernel(const uint8_t* __restrict__ src, size_t rows, size_t cols
             const BlockScale sc = block_scale<F>(gm << 16);
             const int k = s * 2 + h;
             s_byte[k][c] = (uint8_t)sc.byte;
-            const size_t row = r0 + (size_t)k * 32;
-            if (k % G == 0 && row < rows_p && c0 + c < cols) st_u8(scales_t + (c0 + c) * (rows_p / BLOCK) + row / BLOCK, sc.byte);
         }
     }
     __syncthreads();
+    if (tid < kTile && c0 + tid < cols) {                    // a column's scale bytes: one store where they are aligned
+        constexpr int N = 4 / G;
+        const size_t per_col = rows_p / BLOCK;
+        uint8_t* to = scales_t + (c0 + tid) * per_col + tr * N;
+        const uint32_t a = s_byte[0][tid], b = s_byte[G == 1 ? 1 : 2][tid];
+        if (N == 4 && per_col % 4 == 0) {
+            st_u32(to, a | b << 8 | (uint32_t)s_byte[2][tid] << 16 | (uint32_t)s_byte[3][tid] << 24);
+        } else if (N == 2 && per_col % 2 == 0) {
+            st_u16(to, a | b << 8);
+        } else {
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+            for (int k = 0; k < N; ++k)
+                if (r0 + k * BLOCK < rows_p) st_u8(to + k, s_byte[k * G][tid]);
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const uint2 b = *reinterpret_cast<const uint2*>(&s_byte[s * 2 + (rg >> 3)][l * 8]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int c = l * 8 + j;
-            const uint32_t byte = s_byte[s * 2 + (rg >> 3)][c];
+            const uint32_t byte = ((j < 4 ? b.x : b.y) >> (8 * (j & 3))) & 255u;
             const float inv = __uint_as_float((254u - byte) << 23);          // E4M3: byte <= 246 unless poisoned
-            const uint32_t q = byte == 255u ? 0u : quantize_fp_hw_quad<F>(v[s][0][j] * inv, v[s][1][j] * inv, v[s][2][j] * inv, v[s][3][j] * inv);
-            s_codes[c][(rg + 16 * s) ^ (2 * l)] = q;
+            uint32_t q = quantize_fp_hw_quad<F>(v[s][0].at(j) * inv, v[s][1].at(j) * inv, v[s][2].at(j) * inv, v[s][3].at(j) * inv);
+            if (byte == 255u) q = 0;
+            s_codes[l * 8 + j][(rg + 16 * s) ^ (2 * l)] = q;
         }
+    }
     __syncthreads();
     const size_t row = r0 + (size_t)lane * 4;
 #pragma unroll 4
@@ -163,7 +217,7 @@ int run(const void* src, size_t rows, size_t cols, void* codes, uint8_t* scales,
     if (ct > 0x7FFFFFFF || rt > 0x7FFFFFFF / ct) return MXQ_ERR_SIZE;
     auto go = [&](auto kern) {
         return launch_kernel(kern, (int)(rt * ct), kMatThreads, stream, static_cast<const uint8_t*>(src), rows, cols,
-                             static_cast<uint8_t*>(codes), scales, static_cast<uint8_t*>(codes_t), scales_t, (uint32_t)ct);
+                             static_cast<uint8_t*>(codes), scales, static_cast<uint8_t*>(codes_t), scales_t, (uint32_t)rt, (uint32_t)ct);
     };
     return cols % 8 == 0 ? go(quantize_matrix_kernel<T, F, BLOCK, true>) : go(quantize_matrix_kernel<T, F, BLOCK, false>);
 }
