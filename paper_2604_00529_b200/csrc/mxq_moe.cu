@@ -15,14 +15,14 @@
 #include "mxq_kernels.cuh"
 #include "mxq_launch.h"
 #include "mxq_product.cuh"
+#include "mxq_tensor.cuh"
 
 namespace mxq {
 namespace {
 
 constexpr int kMaxTokens = MXQ_MOE_TOKENS_MAX, kMaxExperts = MXQ_MOE_EXPERTS_MAX, kMaxTopK = MXQ_MOE_TOP_K_MAX;
-constexpr int kUpWarps = 4;             // warps per CTA of kernel 1
-constexpr int kUpTiles = 2;             // m16 tiles per CTA of kernel 1: eight rows of the gate and eight of the up half each
-constexpr int kDownWarps = 16;
+constexpr int kTeam = 4, kUpTeams = 4;  // kernel 1: warps of a team, teams of a CTA
+constexpr int kUpTiles = 2;             // 16-row tiles of a team's unit: eight rows of the gate and eight of the up half each
 
 struct MoeArgs {
     const uint8_t *x, *up, *up_s, *down, *down_s;
@@ -31,6 +31,8 @@ struct MoeArgs {
     size_t hidden, inner;
     int tokens, experts, top_k, renormalize, block_shift;
 };
+
+constexpr int kDownWarps = 16, kDownTiles = 2;     // kernel 2
 
 // ---- the choice -------------------------------------------------------------------------------------------
 
@@ -55,12 +57,10 @@ __device__ __forceinline__ uint32_t order_key(float v)
     return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-__device__ __forceinline__ void choose(const MoeArgs& p, Choice& ch)
+template <int PER>                                           // logits per lane: experts <= 32 PER
+__device__ __forceinline__ void choose_tokens(const MoeArgs& p, Choice& ch)
 {
-    constexpr int PER = kMaxExperts / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) ch.mask[e] = 0;
-    __syncthreads();
     const uint32_t none = order_key(-INFINITY);
     for (int t = warp; t < p.tokens; t += warps) {
         uint32_t key[PER];
@@ -71,7 +71,7 @@ __device__ __forceinline__ void choose(const MoeArgs& p, Choice& ch)
             const int e = j * 32 + lane;
             key[j] = 0;
             own[j] = -INFINITY;
-            if (j * 32 < p.experts && e < p.experts) {
+            if (e < p.experts) {
                 const float* at = p.logits + (size_t)t * p.experts + e;
                 bool ok = true;
                 MXQ_CHECKED(at, 4, ok = false)
@@ -84,19 +84,18 @@ __device__ __forceinline__ void choose(const MoeArgs& p, Choice& ch)
         for (int r = 0; r < p.top_k; ++r) {
             uint32_t best = 0;
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
-                if (j * 32 < p.experts) best = max(best, key[j]);
+            for (int j = 0; j < PER; ++j) best = max(best, key[j]);
             best = __reduce_max_sync(0xFFFFFFFFu, best);
             if (best <= none) break;                         // nothing but -inf is left
             uint32_t who = 0xFFFFFFFFu;
 #pragma unroll
             for (int j = PER - 1; j >= 0; --j)
-                if (j * 32 < p.experts && key[j] == best) who = (uint32_t)(j * 32 + lane);
+                if (key[j] == best) who = (uint32_t)(j * 32 + lane);
             who = __reduce_min_sync(0xFFFFFFFFu, who);
             float v = 0.f;
 #pragma unroll
             for (int j = 0; j < PER; ++j)
-                if (j * 32 < p.experts && (uint32_t)(j * 32 + lane) == who) {
+                if ((uint32_t)(j * 32 + lane) == who) {
                     v = own[j];
                     key[j] = 0;
                 }
@@ -112,8 +111,7 @@ __device__ __forceinline__ void choose(const MoeArgs& p, Choice& ch)
         if (!p.renormalize) {
             float s = 0.f;
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
-                if (j * 32 < p.experts) s += expf(own[j] - top);
+            for (int j = 0; j < PER; ++j) s += expf(own[j] - top);
 #pragma unroll
             for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
             total = s;
@@ -124,6 +122,16 @@ __device__ __forceinline__ void choose(const MoeArgs& p, Choice& ch)
             if (chosen >= 0) atomicOr(&ch.mask[chosen], 1ull << t);
         }
     }
+}
+
+__device__ __forceinline__ void choose(const MoeArgs& p, Choice& ch)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) ch.mask[e] = 0;
+    __syncthreads();
+    if (p.experts <= 64) choose_tokens<2>(p, ch);
+    else if (p.experts <= 128) choose_tokens<4>(p, ch);
+    else choose_tokens<kMaxExperts / 32>(p, ch);
     __syncthreads();
     if (warp == 0) {
         int active = 0, pairs = 0;
@@ -181,269 +189,475 @@ __device__ __forceinline__ void bf16_parts(float v, uint32_t (&o)[PARTS])
     }
 }
 
-// One row's consecutive elements for a lane's piece of codes, as BF16 pairs per part.
-template <class T, int N>
-struct TokenPiece;
-template <int N>
-struct TokenPiece<BF16, N> {
-    static constexpr int PARTS = 1;
-    uint32_t v[1][N / 2];
-    __device__ __forceinline__ void load(const uint8_t* row, size_t at, bool in)
+// ---- the pipeline of a warp -------------------------------------------------------------------------------
+// A warp's codes and token pieces of a few chunks are always under way to shared memory (asynchronous copies, each
+// lane's own 16 bytes in a slot of its own: no lane reads what another one copied, so waiting for the own copies is enough).
+// A chunk is 16 bytes of codes per lane and row: four lanes cover 64 (128) elements of k of an 8-bit (4-bit) row.
+
+__device__ __forceinline__ void copy16(uint32_t to, const uint8_t* from, bool in)      // zeros where `in` is false
+{
+    uint32_t size = in ? 16u : 0u;
+    MXQ_CHECKED(from, size, size = 0)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(from), "r"(size) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
+
+__device__ __forceinline__ uint4 lds16(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+// 16-row tiles of codes times eight tokens.  What a lane holds of a row lies at byte 16 t of the chunk's 64 bytes.
+template <int FMT, int TILES>
+struct Chunk {
+    using W = Widen<FMT>;
+    static constexpr int N = 128 / W::bits;                  // elements of k per lane
+    static constexpr int K = 4 * N;                          // and per chunk
+    static constexpr int bytes = TILES * 2 * 512;            // of a warp's slot
+
+    // The codes of rows g and g + 8 of each tile: `lo` and `hi` point to the first tile's rows 0 and 8, `next` bytes apart from the next
+    // tile's; `off` is the lane's byte from there (row g, byte 16 t of the chunk), `left` the row's bytes from the chunk on.
+    static __device__ __forceinline__ void fetch_codes(uint32_t slot, int lane, const uint8_t* lo, const uint8_t* hi, uint32_t next, uint32_t off,
+                                                       uint32_t left)
     {
+        const uint32_t to = slot + lane * 16;
+        const bool in = left >= 64u || (uint32_t)(lane & 3) * 16 < left;
+        if (!in) off = 0;
 #pragma unroll
-        for (int i = 0; i < N / 16; ++i) {
-            uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (in) ld256(w, row + (at + i * 16) * 2);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[0][i * 8 + j] = w[j];
+        for (int m = 0; m < TILES; ++m) {
+            copy16(to + m * 1024, lo + (in ? m * next : 0u) + off, in);
+            copy16(to + m * 1024 + 512, hi + (in ? m * next : 0u) + off, in);
         }
     }
-};
-template <int N>
-struct TokenPiece<F32, N> {
-    static constexpr int PARTS = 3;
-    uint32_t v[3][N / 2];
-    __device__ __forceinline__ void load(const uint8_t* row, size_t at, bool in)
+    // acc += the tiles times the token pieces.  ORDERED: the tokens' values lie in the order of the widened pairs already.
+    template <bool ORDERED, class X>
+    static __device__ __forceinline__ void multiply(float (&acc)[TILES][4], uint32_t slot, int lane, const X& x, const uint32_t (&byte)[TILES][2])
     {
+        uint32_t f[TILES][2], top = 0;
 #pragma unroll
-        for (int i = 0; i < N / 8; ++i) {
-            uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (in) ld256(w, row + (at + i * 8) * 4);
+        for (int m = 0; m < TILES; ++m)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t lo[3], hi[3];
-                bf16_parts<3>(__uint_as_float(w[2 * j]), lo);
-                bf16_parts<3>(__uint_as_float(w[2 * j + 1]), hi);
+            for (int h = 0; h < 2; ++h) {
+                f[m][h] = W::factor(byte[m][h]);
+                top = max(top, byte[m][h]);
+            }
+        if (W::fp && __any_sync(0xFFFFFFFFu, top > W::limit)) products<ORDERED, true>(acc, slot, lane, x, byte, f);
+        else products<ORDERED, false>(acc, slot, lane, x, byte, f);
+    }
+    // WIDE: some scale is beyond what one BF16 factor holds
+    template <bool ORDERED, bool WIDE, class X>
+    static __device__ __forceinline__ void products(float (&acc)[TILES][4], uint32_t slot, int lane, const X& x, const uint32_t (&byte)[TILES][2],
+                                                    const uint32_t (&f)[TILES][2])
+    {
+        constexpr int NP = W::NP;
+        uint4 c[TILES][2];
 #pragma unroll
-                for (int q = 0; q < 3; ++q) v[q][i * 4 + j] = lo[q] | hi[q] << 16;
+        for (int m = 0; m < TILES; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) c[m][h] = lds16(slot + (m * 2 + h) * 512 + lane * 16);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            uint32_t b[X::PARTS][NP];
+#pragma unroll
+            for (int q = 0; q < X::PARTS; ++q) {
+                uint32_t raw[NP];
+#pragma unroll
+                for (int i = 0; i < NP; ++i) raw[i] = x.v[q][w * NP + i];
+                if constexpr (ORDERED) {
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) b[q][i] = raw[i];
+                } else {
+                    order_pairs<NP>(raw, b[q]);
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < TILES; ++m) {
+                uint32_t a[2][NP];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    W::pairs(w == 0 ? c[m][h].x : w == 1 ? c[m][h].y : w == 2 ? c[m][h].z : c[m][h].w, f[m][h], a[h]);
+                    if constexpr (WIDE) {
+                        const uint32_t g = W::factor2(byte[m][h]);
+#pragma unroll
+                        for (int i = 0; i < NP; ++i) a[h][i] = W::mul(a[h][i], g);
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < X::PARTS; ++q)
+#pragma unroll
+                    for (int i = 0; i < NP; i += 2) Bf16Mma::mma(acc[m], a[0][i], a[1][i], a[0][i + 1], a[1][i + 1], b[q][i], b[q][i + 1]);
             }
         }
     }
 };
-// h as kernel 1 left it: PARTS planes of BF16 values, `plane` bytes apart
+
+// Where element i of h is stored: in the order of Widen's pairs, within its code word's elements.
+template <int FMT>
+__device__ __forceinline__ uint32_t ordered_index(uint32_t i)
+{
+    if constexpr (Widen<FMT>::NP == 2) return (i & ~3u) | (i & 1u) << 1 | (i >> 1 & 1u);
+    else return (i & ~7u) | (i & 3u) << 1 | (i >> 2 & 1u);
+}
+
+// A lane's BF16 pairs of a token's elements, per part.
 template <int P, int N>
-struct StoredPiece {
+struct TokenPiece {
     static constexpr int PARTS = P;
     uint32_t v[P][N / 2];
-    __device__ __forceinline__ void load(const uint8_t* row, size_t at, bool in, size_t plane)
+    __device__ __forceinline__ void zero()
     {
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) v[q][i] = 0;
+    }
+    // BF16 elements.  Lanes without a token keep what they have: finite values or not, their sums are not looked at.  Beyond k: zeros.
+    __device__ __forceinline__ void load(const uint8_t* at, bool live, bool in, size_t plane = 0)
+    {
+        if (!live) return;
 #pragma unroll
         for (int q = 0; q < P; ++q)
 #pragma unroll
             for (int i = 0; i < N / 16; ++i) {
                 uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (in) ld256(w, row + q * plane + (at + i * 16) * 2);
+                if (in) ld256(w, at + q * plane + i * 32);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[q][i * 8 + j] = w[j];
             }
     }
-};
-
-// Codes of rows g and g + 8 of a 16-row tile, one piece each, and their scale bytes.
-template <int FMT>
-struct CodePiece {
-    using W = Widen<FMT>;
-    static constexpr int N = 128 / W::bits;                  // elements of a piece
-    uint4 c[2];
-    uint32_t byte[2];
-
-    __device__ __forceinline__ void load(const uint8_t* r0, const uint8_t* r1, const uint8_t* s0, const uint8_t* s1, size_t at, size_t k,
-                                         int block_shift)
+    // FP32 elements from global memory, split into parts
+    __device__ __forceinline__ void load_f32(const uint8_t* at, bool in)
     {
-        c[0] = c[1] = make_uint4(0, 0, 0, 0);
-        byte[0] = byte[1] = 127;
-        if (at >= k) return;
-        c[0] = ld_once(r0 + at * W::bits / 8);
-        c[1] = ld_once(r1 + at * W::bits / 8);
-        byte[0] = ld_u8(s0 + (at >> block_shift));
-        byte[1] = ld_u8(s1 + (at >> block_shift));
-    }
-
-    // acc += the tile times the token pieces
-    template <class X>
-    __device__ __forceinline__ void multiply(float (&acc)[4], const X& x) const
-    {
-        constexpr int NP = W::NP;
-        const uint32_t f0 = W::factor(byte[0]), f1 = W::factor(byte[1]);
-        uint32_t g0 = 0, g1 = 0;
-        bool wide = false;                                   // a scale beyond what one BF16 factor holds
-        if constexpr (W::fp) {
-            wide = __any_sync(0xFFFFFFFFu, max(byte[0], byte[1]) > W::limit);
-            if (wide) {
-                g0 = W::factor2(byte[0]);
-                g1 = W::factor2(byte[1]);
-            }
-        }
-        const uint32_t w0[4] = {c[0].x, c[0].y, c[0].z, c[0].w}, w1[4] = {c[1].x, c[1].y, c[1].z, c[1].w};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            uint32_t a0[NP], a1[NP];
-            W::pairs(w0[w], f0, a0);
-            W::pairs(w1[w], f1, a1);
-            if (W::fp && wide) {
+        for (int i = 0; i < N / 8; ++i) {
+            uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (in) ld256(w, at + i * 32);
 #pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    a0[i] = W::mul(a0[i], g0);
-                    a1[i] = W::mul(a1[i], g1);
-                }
-            }
+            for (int j = 0; j < 4; ++j) {
+                uint32_t lo[P], hi[P];
+                bf16_parts<P>(__uint_as_float(w[2 * j]), lo);
+                bf16_parts<P>(__uint_as_float(w[2 * j + 1]), hi);
 #pragma unroll
-            for (int q = 0; q < X::PARTS; ++q) {
-                uint32_t raw[NP], b[NP];
-#pragma unroll
-                for (int i = 0; i < NP; ++i) raw[i] = x.v[q][w * NP + i];
-                order_pairs<NP>(raw, b);
-#pragma unroll
-                for (int i = 0; i < NP; i += 2) Bf16Mma::mma(acc, a0[i], a1[i], a0[i + 1], a1[i + 1], b[i], b[i + 1]);
+                for (int q = 0; q < P; ++q) v[q][i * 4 + j] = lo[q] | hi[q] << 16;
             }
         }
     }
 };
+
+constexpr int kSlots = 4;                                    // chunks under way per warp: two to four, as shared memory allows
+inline int slots_for(size_t shared, int warps, int bytes) { return (int)(shared / ((size_t)warps * bytes) < kSlots ? shared / ((size_t)warps * bytes) : kSlots); }
+
+__device__ __forceinline__ void wait_slot(int slots)         // all copies but those of the last slots - 1 groups
+{
+    if (slots == 4) wait_copies<3>();
+    else if (slots == 3) wait_copies<2>();
+    else wait_copies<1>();
+}
 
 // ---- kernel 1 ---------------------------------------------------------------------------------------------
-// A CTA of four warps works on units of 32 rows, 16 of the gate and the 16 of the up half that go with them, of one expert; the
-// warps share k out and meet in shared memory.  In a 16-row tile the first eight rows are the gate's and the last eight
-// the up half's.
+// One CTA per SM, of four teams of four warps.  A team works on units of 32 rows, 16 of the gate and the 16 of the up half that go
+// with them, of one expert, for eight of its tokens at a time; its warps share k out and meet in shared memory.  In a 16-row tile
+// the first eight rows are the gate's and the last eight the up half's.  A warp's copies run on into its next unit.
+
+template <class T, int FMT>
+using UpChunk = Chunk<FMT, kUpTiles>;
 
 template <class T, int FMT, int HPARTS>
-__global__ void __launch_bounds__(kUpWarps * 32, 4)
-moe_up_kernel(const MoeArgs p)
+__global__ void __launch_bounds__(kUpTeams * kTeam * 32, 1)
+moe_up_kernel(const MoeArgs p, const int slots)
 {
-    constexpr int TILES = kUpTiles, N = CodePiece<FMT>::N, CHUNK = 4 * N;
+    using C = UpChunk<T, FMT>;
+    constexpr int TILES = kUpTiles;
+    constexpr int bytes = C::bytes;
+    extern __shared__ __align__(16) uint8_t s_ring[];
     __shared__ Choice ch;
-    __shared__ float s_sum[kUpWarps][TILES][4][32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    __shared__ float s_sum[kUpTeams][kTeam][TILES][4][32];
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int team = warp / kTeam, part = warp % kTeam;
     pdl_acquire();
     pdl_release();                                           // after the wait: kernel 2 may read the logits at once
     choose(p, ch);
 
-    const size_t H = p.hidden, I = p.inner, hrow = H * CodePiece<FMT>::W::bits / 8, srow = H >> p.block_shift;
-    const size_t plane = (size_t)p.tokens * p.top_k * I * 2;
-    const int per_expert = (int)(I / (8 * TILES)), units = ch.active * per_expert;
-    for (int u = blockIdx.x; u < units; u += gridDim.x) {
-        const int pos = u / per_expert, e = ch.expert[pos], first = ch.first[pos], cnt = ch.first[pos + 1] - first;
-        const size_t i0 = (size_t)(u % per_expert) * (8 * TILES);
-        const uint8_t* codes = p.up + (size_t)e * 2 * I * hrow;
-        const uint8_t* scales = p.up_s + (size_t)e * 2 * I * srow;
-        for (int c0 = 0; c0 < cnt; c0 += 8) {                // eight tokens at a time
-            const bool live = c0 + g < cnt;
-            const uint8_t* xrow = p.x + (size_t)(live ? ch.token[first + c0 + g] : 0) * H * T::size;
-            float acc[TILES][4] = {}, sum[TILES][4] = {};
-#pragma unroll 2
-            for (size_t k0 = (size_t)warp * CHUNK; k0 < H; k0 += kUpWarps * CHUNK) {
-                const size_t at = k0 + (size_t)t * N;
-                CodePiece<FMT> cp[TILES];
-                TokenPiece<T, N> x;
-#pragma unroll
-                for (int m = 0; m < TILES; ++m) {
-                    const size_t r0 = i0 + m * 8 + g, r1 = I + r0;
-                    cp[m].load(codes + r0 * hrow, codes + r1 * hrow, scales + r0 * srow, scales + r1 * srow, at, H, p.block_shift);
-                }
-                x.load(xrow, at, live && at < H);
-#pragma unroll
-                for (int m = 0; m < TILES; ++m) {
-                    if constexpr (T::size == 4) {            // sums kept outside the matrix instruction, which truncates
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[m][j] = 0.f;
-                    }
-                    cp[m].multiply(T::size == 4 ? acc[m] : sum[m], x);
-                    if constexpr (T::size == 4) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) sum[m][j] += acc[m][j];
-                    }
-                }
-            }
-            __syncthreads();                                 // the last unit's sums have been read
-#pragma unroll
-            for (int m = 0; m < TILES; ++m)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s_sum[warp][m][j][lane] = sum[m][j];
-            __syncthreads();
-            // row r of the gate and of the up half, token c: elements (c & 1) and 2 + (c & 1) of lane r * 4 + c / 2
-            for (int o = threadIdx.x; o < TILES * 64; o += kUpWarps * 32) {
-                const int m = o >> 6, c = (o >> 3) & 7, r = o & 7, ln = r * 4 + (c >> 1);
-                if (c0 + c >= cnt) continue;
-                float gate = 0.f, lift = 0.f;
-#pragma unroll
-                for (int w = 0; w < kUpWarps; ++w) {
-                    gate += s_sum[w][m][c & 1][ln];
-                    lift += s_sum[w][m][2 + (c & 1)][ln];
-                }
-                const float h = gate / (1.f + expf(-gate)) * lift;
-                uint32_t part[HPARTS];
-                bf16_parts<HPARTS>(h, part);
-                uint8_t* at = p.h + ((size_t)(first + c0 + c) * I + i0 + m * 8 + r) * 2;
-#pragma unroll
-                for (int q = 0; q < HPARTS; ++q) st_u16(at + q * plane, part[q]);
-            }
+    const uint32_t H = (uint32_t)p.hidden, I = (uint32_t)p.inner, hrow = H * C::W::bits / 8, srow = H >> p.block_shift;
+    const size_t plane = (size_t)p.tokens * p.top_k * I * 2, half = (size_t)I * hrow, half_s = (size_t)I * srow;
+    const int per_expert = (int)(I / (8 * TILES)), units = ch.active * per_expert, stride = gridDim.x * kUpTeams;
+    const int turns = (int)((H + kTeam * C::K - 1) / (kTeam * C::K));    // chunks of a warp per unit and group of tokens
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + warp * slots * bytes;
+
+    // A warp's sequence of chunks: units, groups of eight of the unit's tokens, turns.  It is followed three times: where the copies
+    // are, one turn ahead where the scale bytes are, and where the products are.
+    struct At {
+        int unit, group, turn;
+    };
+    auto step = [&](At& a) {                                 // true: a new unit or group
+        if (++a.turn < turns) return false;
+        a.turn = 0;
+        a.group += 8;
+        const int pos = a.unit / per_expert;
+        if (a.group >= ch.first[pos + 1] - ch.first[pos]) {
+            a.group = 0;
+            a.unit += stride;
         }
+        return true;
+    };
+    auto row_of = [&](int unit) { return ((size_t)ch.expert[unit / per_expert] * 2) * I + (size_t)(unit % per_expert) * (8 * TILES); };
+
+    At ahead{team * (int)gridDim.x + (int)blockIdx.x, 0, 0};
+    const uint8_t* a_lo = nullptr;
+    auto enter_copies = [&] {
+        if (ahead.unit < units) a_lo = p.up + row_of(ahead.unit) * hrow;
+    };
+    auto fetch = [&](int slot) {
+        if (ahead.unit < units) {
+            const uint32_t kb = (uint32_t)(ahead.turn * kTeam + part) * 64, at = kb + t * 16;      // bytes of codes of a row
+            C::fetch_codes(ring + slot * bytes, lane, a_lo, a_lo + half, 8 * hrow, g * hrow + at, kb < hrow ? hrow - kb : 0);
+            if (step(ahead)) enter_copies();
+        }
+        copies_done();
+    };
+    At soon = ahead;
+    const uint8_t *s_lo = nullptr, *s_x = nullptr;
+    bool s_live = false;
+    auto enter_scales = [&] {
+        if (soon.unit >= units) return;
+        s_lo = p.up_s + row_of(soon.unit) * srow + (size_t)g * srow;
+        const int pos = soon.unit / per_expert, first = ch.first[pos], cnt = ch.first[pos + 1] - first;
+        s_live = soon.group + g < cnt;
+        s_x = p.x + (size_t)(s_live ? ch.token[first + soon.group + g] : 0) * H * T::size;
+    };
+    uint32_t byte[TILES][2];
+    TokenPiece<1, C::N> x_next;                              // (BF16 tokens)
+    x_next.zero();
+    auto fetch_scales = [&] {
+        if (soon.unit >= units) return;
+        const uint32_t at = ((uint32_t)(soon.turn * kTeam + part) * 64 + t * 16) * (8 / C::W::bits);
+        const uint8_t* s = s_lo + (at < H ? at >> p.block_shift : 0);
+#pragma unroll
+        for (int m = 0; m < TILES; ++m) {
+            byte[m][0] = ld_u8(s + m * 8 * srow);
+            byte[m][1] = ld_u8(s + half_s + m * 8 * srow);
+        }
+        if constexpr (T::size == 2) x_next.load(s_x + (at < H ? (size_t)at * 2 : 0), s_live, at < H);
+        if (step(soon)) enter_scales();
+    };
+    At now = ahead;
+    enter_copies();
+    enter_scales();
+    for (int i = 0; i < slots - 1; ++i) fetch(i);
+    fetch_scales();
+    int slot = 0;
+    while (now.unit < units) {
+        const int pos = now.unit / per_expert, first = ch.first[pos], cnt = ch.first[pos + 1] - first, unit = now.unit, group = now.group;
+        const bool live = group + g < cnt;
+        const uint8_t* xrow = p.x + (size_t)(T::size == 4 && live ? ch.token[first + group + g] : 0) * H * T::size;
+        float sum[TILES][4] = {};
+        for (int turn = 0; turn < turns; ++turn) {
+            fetch(slot == 0 ? slots - 1 : slot - 1);         // (that slot was read in the turn before)
+            wait_slot(slots);
+            const uint32_t at = ring + slot * bytes;
+            uint32_t scale[TILES][2];
+#pragma unroll
+            for (int m = 0; m < TILES; ++m) {
+                scale[m][0] = byte[m][0];
+                scale[m][1] = byte[m][1];
+            }
+            const TokenPiece<1, C::N> x_now = x_next;
+            fetch_scales();
+            if constexpr (T::size == 2) {
+                C::template multiply<false>(sum, at, lane, x_now, scale);
+            } else {                                         // sums kept outside the matrix instruction, which truncates
+                const uint32_t k = ((uint32_t)(turn * kTeam + part) * 64 + t * 16) * (8 / C::W::bits);
+                TokenPiece<3, C::N> x;
+                x.load_f32(xrow + (size_t)(k < H ? k : 0) * 4, live && k < H);
+                float acc[TILES][4] = {};
+                C::template multiply<false>(acc, at, lane, x, scale);
+#pragma unroll
+                for (int m = 0; m < TILES; ++m)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum[m][j] += acc[m][j];
+            }
+            slot = slot + 1 == slots ? 0 : slot + 1;
+        }
+#pragma unroll
+        for (int m = 0; m < TILES; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s_sum[team][part][m][j][lane] = sum[m][j];
+        asm volatile("bar.sync %0, %1;" :: "r"(1 + team), "n"(kTeam * 32) : "memory");
+        // row r of the gate and of the up half, token c: elements (c & 1) and 2 + (c & 1) of lane r * 4 + c / 2
+        for (int o = part * 32 + lane; o < TILES * 64; o += kTeam * 32) {
+            const int m = o >> 6, c = (o >> 3) & 7, r = o & 7, ln = r * 4 + (c >> 1);
+            if (group + c >= cnt) continue;
+            float gate = 0.f, lift = 0.f;
+#pragma unroll
+            for (int w = 0; w < kTeam; ++w) {
+                gate += s_sum[team][w][m][c & 1][ln];
+                lift += s_sum[team][w][m][2 + (c & 1)][ln];
+            }
+            const float h = gate / (1.f + expf(-gate)) * lift;
+            uint32_t hp[HPARTS];
+            bf16_parts<HPARTS>(h, hp);
+            uint8_t* to = p.h + ((size_t)(first + group + c) * I + ordered_index<FMT>((uint32_t)(unit % per_expert) * (8 * TILES) + m * 8 + r)) * 2;
+#pragma unroll
+            for (int q = 0; q < HPARTS; ++q) st_u16(to + q * plane, hp[q]);
+        }
+        asm volatile("bar.sync %0, %1;" :: "r"(1 + team), "n"(kTeam * 32) : "memory");
+        now.turn = turns - 1;
+        step(now);
     }
+    wait_copies<0>();
 }
 
 // ---- kernel 2 ---------------------------------------------------------------------------------------------
-// A CTA of 16 warps covers 16 rows of the output for all tokens.  The chunks of all active experts, laid end to end, are shared
-// out between the warps; a warp adds its weighted sums to its own copy of the tile, and the copies are added in order.
+// A CTA covers 32 rows of the output for all tokens; where that makes few CTAs, a cluster of them covers the same rows.  The chunks of
+// all active experts, laid end to end, are shared out between the warps; a warp adds its weighted sums to its own copy of the tile, and the copies are added in order.  The first
+// chunks' codes are fetched before the wait for kernel 1.
 
 template <class T, int FMT, int HPARTS>
 __global__ void __launch_bounds__(kDownWarps * 32, 1)
-moe_down_kernel(const MoeArgs p)
+moe_down_kernel(const MoeArgs p, const int slots, const int share)
 {
-    constexpr int N = CodePiece<FMT>::N, CHUNK = 4 * N;
+    constexpr int TILES = kDownTiles, WARPS = kDownWarps, ROWS = 16 * TILES;
+    using C = Chunk<FMT, TILES>;
+    constexpr int bytes = C::bytes;
     __shared__ Choice ch;
-    extern __shared__ float s_tile[];                        // [warp][token][16]
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    extern __shared__ __align__(16) uint8_t s_ring[];        // the warps' slots, then [warp][token][16] sums
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     pdl_release();
     choose(p, ch);                                           // (the logits were complete when kernel 1 let this one start)
-    const size_t H = p.hidden, I = p.inner, irow = I * CodePiece<FMT>::W::bits / 8, srow = I >> p.block_shift;
-    const size_t plane = (size_t)p.tokens * p.top_k * I * 2, j0 = (size_t)blockIdx.x * 16;
-    float* mine = s_tile + (size_t)warp * p.tokens * 16;
-    for (int i = lane; i < p.tokens * 16; i += 32) mine[i] = 0.f;
-    __syncwarp();
-    pdl_acquire();
+    const uint32_t H = (uint32_t)p.hidden, I = (uint32_t)p.inner, irow = I * C::W::bits / 8, srow = I >> p.block_shift;
+    const size_t plane = (size_t)p.tokens * p.top_k * I * 2, j0 = (size_t)(blockIdx.x / share) * ROWS;
+    const int rank = blockIdx.x % share;                     // of the cluster's CTAs, which share the chunks of one group of rows
+    float* const tile = reinterpret_cast<float*>(s_ring + WARPS * slots * bytes);
+    float* const mine = tile + (size_t)warp * p.tokens * ROWS;
+    for (int i = lane; i < p.tokens * ROWS; i += 32) mine[i] = 0.f;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + warp * slots * bytes;
 
-    const int per_expert = (int)((I + CHUNK - 1) / CHUNK), total = ch.active * per_expert;
-    int q = (int)((long long)total * warp / kDownWarps);
-    const int end = (int)((long long)total * (warp + 1) / kDownWarps);
-    while (q < end) {
-        const int pos = q / per_expert, e = ch.expert[pos], first = ch.first[pos], cnt = ch.first[pos + 1] - first;
-        const int lo = q - pos * per_expert, hi = min(per_expert, lo + end - q);
-        const size_t r0 = (size_t)e * H + j0 + g, r1 = r0 + 8;
-        for (int c0 = 0; c0 < cnt; c0 += 8) {
-            const bool live = c0 + g < cnt;
-            const uint8_t* hrow = p.h + (size_t)(first + c0 + (live ? g : 0)) * I * 2;
-            float acc[4] = {0.f, 0.f, 0.f, 0.f}, sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-            for (int c = lo; c < hi; ++c) {
-                const size_t at = (size_t)c * CHUNK + (size_t)t * N;
-                CodePiece<FMT> cp;
-                StoredPiece<HPARTS, N> x;
-                cp.load(p.down + r0 * irow, p.down + r1 * irow, p.down_s + r0 * srow, p.down_s + r1 * srow, at, I, p.block_shift);
-                x.load(hrow, at, live && at < I, plane);
-                if constexpr (T::size == 4) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[j] = 0.f;
-                }
-                cp.multiply(T::size == 4 ? acc : sum, x);
-                if constexpr (T::size == 4) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sum[j] += acc[j];
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {                    // row g + 8 (j >> 1), token 2 t + (j & 1) of the eight
-                const int c = c0 + 2 * t + (j & 1);
-                if (c < cnt) mine[ch.token[first + c] * 16 + g + 8 * (j >> 1)] += ch.weight[first + c] * sum[j];
-            }
-            __syncwarp();
+    // A warp's sequence of chunks: its part of each expert's, for eight of the expert's tokens at a time; followed three times as in
+    // kernel 1.
+    const int per_expert = (int)((irow + 63) / 64), total = ch.active * per_expert;
+    const int begin = (int)((long long)total * (rank * WARPS + warp) / (share * WARPS)), end = (int)((long long)total * (rank * WARPS + warp + 1) / (share * WARPS));
+    struct At {
+        int pos, lo, hi, group, c;                           // the expert, the warp's chunks [lo, hi) of it, ...; pos < 0: the end
+    };
+    auto start = [&](int q) {
+        if (q >= end) return At{-1, 0, 0, 0, 0};
+        const int pos = q / per_expert, lo = q - pos * per_expert;
+        return At{pos, lo, min(per_expert, lo + end - q), 0, lo};
+    };
+    auto step = [&](At& a) {                                 // true: another expert or group
+        if (++a.c < a.hi) return false;
+        a.group += 8;
+        a.c = a.lo;
+        if (a.group >= ch.first[a.pos + 1] - ch.first[a.pos]) a = start(a.pos * per_expert + a.hi);
+        return true;
+    };
+    At ahead = start(begin), soon = ahead, now = ahead;
+    const uint8_t *a_lo = nullptr, *s_lo = nullptr, *s_h = nullptr;
+    bool s_live = false;
+    auto enter_copies = [&] {
+        if (ahead.pos >= 0) a_lo = p.down + ((size_t)ch.expert[ahead.pos] * H + j0) * irow;
+    };
+    auto fetch = [&](int slot) {
+        if (ahead.pos >= 0) {
+            const uint32_t kb = (uint32_t)ahead.c * 64;
+            C::fetch_codes(ring + slot * bytes, lane, a_lo, a_lo + 8 * (size_t)irow, 16 * irow, g * irow + kb + t * 16, irow - kb);
+            if (step(ahead)) enter_copies();
         }
-        q += hi - lo;
-    }
-    __syncthreads();
-    for (int o = threadIdx.x; o < p.tokens * 16; o += kDownWarps * 32) {
-        float v = 0.f;
+        copies_done();
+    };
+    auto enter_scales = [&] {
+        if (soon.pos < 0) return;
+        s_lo = p.down_s + ((size_t)ch.expert[soon.pos] * H + j0 + g) * srow;
+        const int first = ch.first[soon.pos], cnt = ch.first[soon.pos + 1] - first;
+        s_live = soon.group + g < cnt;
+        s_h = p.h + (size_t)(first + soon.group + (s_live ? g : 0)) * I * 2;
+    };
+    uint32_t byte[TILES][2] = {};
+    TokenPiece<HPARTS, C::N> x_next;
+    x_next.zero();
+    auto fetch_scales = [&] {
+        if (soon.pos < 0) return;
+        const uint32_t at = ((uint32_t)soon.c * 64 + t * 16) * (8 / C::W::bits);
+        const uint8_t* s = s_lo + (at < I ? at >> p.block_shift : 0);
 #pragma unroll
-        for (int w = 0; w < kDownWarps; ++w) v += s_tile[(size_t)w * p.tokens * 16 + o];
-        const size_t i = (size_t)(o >> 4) * H + j0 + (o & 15);
+        for (int m = 0; m < TILES; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) byte[m][h] = ld_u8(s + (uint32_t)(m * 16 + h * 8) * srow);
+        x_next.load(s_h + (at < I ? (size_t)at * 2 : 0), s_live, at < I, plane);
+        if (step(soon)) enter_scales();
+    };
+    // the first slots' codes before the wait for kernel 1
+    enter_copies();
+    for (int i = 0; i < slots - 1; ++i) fetch(i);
+    pdl_acquire();
+    enter_scales();
+    fetch_scales();
+    int slot = 0;
+    while (now.pos >= 0) {
+        const int first = ch.first[now.pos], cnt = ch.first[now.pos + 1] - first, chunks = now.hi - now.lo, group = now.group;
+        float sum[TILES][4] = {};
+        for (int i = 0; i < chunks; ++i) {
+            fetch(slot == 0 ? slots - 1 : slot - 1);
+            wait_slot(slots);
+            const uint32_t at = ring + slot * bytes;
+            uint32_t scale[TILES][2];
+#pragma unroll
+            for (int m = 0; m < TILES; ++m) {
+                scale[m][0] = byte[m][0];
+                scale[m][1] = byte[m][1];
+            }
+            const TokenPiece<HPARTS, C::N> x = x_next;
+            fetch_scales();
+            if constexpr (T::size == 2) {
+                C::template multiply<true>(sum, at, lane, x, scale);
+            } else {
+                float acc[TILES][4] = {};
+                C::template multiply<true>(acc, at, lane, x, scale);
+#pragma unroll
+                for (int m = 0; m < TILES; ++m)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum[m][j] += acc[m][j];
+            }
+            slot = slot + 1 == slots ? 0 : slot + 1;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {                        // row g + 8 (j >> 1) of a tile, token 2 t + (j & 1) of the eight
+            const int c = group + 2 * t + (j & 1);
+            if (c >= cnt) continue;
+            float* const to = mine + ch.token[first + c] * ROWS + g + 8 * (j >> 1);
+            const float w = ch.weight[first + c];
+#pragma unroll
+            for (int m = 0; m < TILES; ++m) to[16 * m] += w * sum[m][j];
+        }
+        __syncwarp();
+        now.c = now.hi - 1;
+        step(now);
+    }
+    wait_copies<0>();
+    __syncthreads();
+    const int outs = p.tokens * ROWS;
+    if (share > 1) {                                         // the CTA's own sum into its first copy, then the cluster's in order of rank
+        for (int o = threadIdx.x; o < outs; o += WARPS * 32) {
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) v += tile[(size_t)w * outs + o];
+            tile[o] = v;
+        }
+        cluster_sync();
+    }
+    const uint32_t tile_at = smem_addr(tile);
+    for (int o = threadIdx.x + rank * WARPS * 32; o < outs; o += share * WARPS * 32) {
+        float v = 0.f;
+        if (share > 1) {
+            for (int r = 0; r < share; ++r) v += ld_peer(peer_addr(tile_at + o * 4, r));
+        } else {
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) v += tile[(size_t)w * outs + o];
+        }
+        const size_t i = (size_t)(o / ROWS) * H + j0 + o % ROWS;
         if constexpr (T::size == 4) {
             MXQ_CHECKED(p.out + i * 4, 4, continue)
             reinterpret_cast<float*>(p.out)[i] = v;
@@ -451,22 +665,38 @@ moe_down_kernel(const MoeArgs p)
             st_u16(p.out + i * 2, pack_bf16x2(v, 0.f) & 0xFFFFu);
         }
     }
+    if (share > 1) cluster_sync();                           // no CTA leaves while another one reads its sums
 }
 
 constexpr int h_parts(int dtype) { return dtype == MXQ_F32 ? 3 : 2; }
 
+constexpr size_t kShared = 226 * 1024;                       // what a CTA may use of an SM, less a little
+
 template <class T, int FMT>
 int run(const MoeArgs& p, cudaStream_t stream)
 {
-    constexpr int P = h_parts(T::id);
-    const size_t most = (size_t)p.tokens * p.top_k < (size_t)p.experts ? (size_t)p.tokens * p.top_k : (size_t)p.experts;
-    const size_t units = most * (p.inner / (8 * kUpTiles));
-    const unsigned grid = (unsigned)(units < 148 * 4 ? units : 148 * 4);
-    if (int rc = launch_grid(moe_up_kernel<T, FMT, P>, dim3(grid), kUpWarps * 32, 0, 1, stream, p)) return rc;
     static std::atomic<uint64_t> done{0};
-    auto down = moe_down_kernel<T, FMT, P>;
-    if (int rc = allow_smem(reinterpret_cast<const void*>(down), (size_t)kDownWarps * kMaxTokens * 64, done)) return rc;
-    return launch_grid(down, dim3((unsigned)(p.hidden / 16)), kDownWarps * 32, (size_t)kDownWarps * p.tokens * 64, 1, stream, p);
+    auto up = moe_up_kernel<T, FMT, h_parts(T::id)>;
+    constexpr int kUpWarps = kUpTeams * kTeam;
+    constexpr size_t kUpStatic = sizeof(Choice) + (size_t)kUpWarps * kUpTiles * 512 + 64;
+    constexpr int up_bytes = UpChunk<T, FMT>::bytes;
+    if (int rc = allow_smem(reinterpret_cast<const void*>(up), kShared - kUpStatic, done)) return rc;
+    const size_t most = (size_t)p.tokens * p.top_k < (size_t)p.experts ? (size_t)p.tokens * p.top_k : (size_t)p.experts;
+    const size_t units = most * (p.inner / (8 * kUpTiles)), ctas = (units + kUpTeams - 1) / kUpTeams;
+    const int up_slots = slots_for(kShared - kUpStatic, kUpWarps, up_bytes);
+    if (int rc = launch_grid(up, dim3((unsigned)(ctas < 148 ? ctas : 148)), kUpWarps * 32, (size_t)kUpWarps * up_slots * up_bytes, 1, stream, p, up_slots))
+        return rc;
+    static std::atomic<uint64_t> down_done{0};
+    auto down = moe_down_kernel<T, FMT, h_parts(T::id)>;
+    const size_t free = kShared - sizeof(Choice) - 64, sums = (size_t)kDownWarps * p.tokens * 64 * kDownTiles;
+    if (int rc = allow_smem(reinterpret_cast<const void*>(down), free, down_done)) return rc;
+    static_assert(kShared - sizeof(Choice) - 64 - (size_t)kDownWarps * kMaxTokens * 64 * kDownTiles >= 2 * kDownWarps * Chunk<FMT, kDownTiles>::bytes, "two slots at least");
+    const int slots = slots_for(free - sums, kDownWarps, Chunk<FMT, kDownTiles>::bytes);
+    const size_t groups = p.hidden / (16 * kDownTiles);
+    int share = 1;                                           // CTAs of a cluster: so many that there is about one CTA per SM
+    while (share < 8 && groups * share * 2 <= 148) share *= 2;
+    return launch_grid(down, dim3((unsigned)(groups * share)), kDownWarps * 32, (size_t)kDownWarps * slots * Chunk<FMT, kDownTiles>::bytes + sums, share, stream, p,
+                       slots, share);
 }
 
 template <class T>

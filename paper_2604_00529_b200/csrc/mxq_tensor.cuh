@@ -202,7 +202,13 @@ __device__ __forceinline__ void mma_commit(uint32_t bar, uint32_t first)
                      :: "r"(bar), "h"((uint16_t)(3u << first)) : "memory");
 }
 
-// Four floats of another CTA's shared memory.
+// A float, and four floats, of another CTA's shared memory.
+__device__ __forceinline__ float ld_peer(uint32_t cluster_addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ float4 ld_peer4(uint32_t cluster_addr)
 {
     float4 v;
