@@ -71,7 +71,9 @@ _host = None            # the native module _mxq_host (csrc/host_calls.cpp): the
 
 #: the entry points that _mxq_host calls
 _HOST_CALLS = ("mxq_quantize", "mxq_slice_scale", "mxq_slice_scale_multi", "mxq_dequantize", "mxq_tiled_scales_bytes",
-               "mxq_quantize_tiled", "mxq_slice_scale_tiled", "mxq_fake_quant", "mxq_fake_quant_bwd", "mxq_codes_bytes")
+               "mxq_quantize_tiled", "mxq_slice_scale_tiled", "mxq_fake_quant", "mxq_fake_quant_bwd", "mxq_codes_bytes",
+               "mxq_matmul", "mxq_quantize_matrix", "mxq_matrix_codes_bytes", "mxq_matrix_scales_bytes", "mxq_moe",
+               "mxq_moe_workspace_bytes")
 
 
 def library_path() -> str:
@@ -698,6 +700,9 @@ def matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, b_codes: torch.Tensor,
     """mxq_matmul: A^ B^T of two quantized operands [m, k] and [n, k] (``quantize``'s codes and scales), as [m, n] of
     ``dtype`` (``out``'s where it is given)."""
     L = _lib or load_library()
+    made = _host.matmul(a_codes, a_scales, b_codes, b_scales, m, n, k, fmt, block, dtype, out, stream)
+    if made is not None:
+        return made
     dev = a_codes.device
     sizes = (m * k, m * k // block, n * k, n * k // block) if block > 0 and min(m, n, k) >= 0 else (0, 0, 0, 0)
     if min(m, n, k) < 0:
@@ -717,6 +722,9 @@ def quantize_matrix(src: torch.Tensor, fmt: str = "e4m3", block: int = 32, rows:
     """mxq_quantize_matrix: a 2-D tensor -> (codes, scales, codes_t, scales_t), its quantization along the rows and that of its
     transpose, rows padded with zeros to whole blocks; ``rows=False`` / ``cols=False`` leave one of them out (None)."""
     L = _lib or load_library()
+    made = _host.quantize_matrix(src, fmt, block, rows, cols, stream)
+    if made is not None:
+        return made
     if src.dim() != 2:
         raise ValueError("quantize_matrix takes a [rows, cols] matrix")
     r, c = src.shape
@@ -770,6 +778,9 @@ def linear_ste(x: torch.Tensor, w: torch.Tensor, block: int = 32) -> torch.Tenso
     dw has w's.  The backward pass keeps the transposes' codes (a byte per element), not x and w."""
     if _lib is None:
         load_library()
+    made = _host.linear_ste(x, w, block)
+    if made is not None:
+        return made
     if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
         raise ValueError("linear_ste takes x [..., k] and w [n, k], got %s and %s" % (tuple(x.shape), tuple(w.shape)))
     if block not in (32, 64, 128):
@@ -798,6 +809,9 @@ def moe(x: torch.Tensor, logits: torch.Tensor, up_codes: torch.Tensor, up_scales
     down matrices [experts, hidden, inner], as ``quantize`` writes them.  ``workspace`` (uint8, ``moe_workspace_bytes``) saves
     the allocation of one per call; calls that can overlap on the GPU must not share it."""
     L = _lib or load_library()
+    made = _host.moe(x, logits, up_codes, up_scales, down_codes, down_scales, inner, top_k, fmt, block, renormalize, out, workspace, stream)
+    if made is not None:
+        return made
     if x.dim() != 2 or logits.dim() != 2 or logits.shape[0] != x.shape[0]:
         raise ValueError("moe takes x [tokens, hidden] and logits [tokens, experts]")
     if logits.dtype != torch.float32:

@@ -13,9 +13,11 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 
@@ -36,6 +38,12 @@ struct Api {
     decltype(&mxq_fake_quant) fake_quant;
     decltype(&mxq_fake_quant_bwd) fake_quant_bwd;
     decltype(&mxq_codes_bytes) codes_bytes;
+    decltype(&mxq_matmul) matmul;
+    decltype(&mxq_quantize_matrix) quantize_matrix;
+    decltype(&mxq_matrix_codes_bytes) matrix_codes_bytes;
+    decltype(&mxq_matrix_scales_bytes) matrix_scales_bytes;
+    decltype(&mxq_moe) moe;
+    decltype(&mxq_moe_workspace_bytes) moe_workspace_bytes;
 } api;
 
 PyObject* formats = nullptr;          // the binding's name -> id dict
@@ -468,6 +476,224 @@ PyObject* fake_quant_ste(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- products that read the codes -------------------------------------------------------------------------
+
+// Is the tensor on `device`, and is that the current one?
+bool here(const at::Tensor& t, c10::Device device) { return t.device() == device && device.index() == c10::cuda::current_device(); }
+
+// Codes or scales: at least `n` bytes on the current device.
+bool operand(const at::Tensor* t, int64_t n, c10::Device device) { return t && t->scalar_type() == at::kByte && t->numel() >= n && here(*t, device); }
+
+// matmul(a_codes, a_scales, b_codes, b_scales, m, n, k, fmt, block, dtype, out, stream)
+PyObject* matmul(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int fmt, block, dt;
+    int64_t m, n, k;
+    GENERAL_UNLESS(nargs == 12 && a[11] == Py_None && as_count(a[4], &m) && as_count(a[5], &n) && as_count(a[6], &k) && format_id(a[7], &fmt) &&
+                   as_int(a[8], &block) && block > 0 && m < (1ll << 31) && n < (1ll << 31) && k < (1ll << 31) && !modes_active());
+    const at::Tensor *ac = plain(a[0]), *as = plain(a[1]), *bc = plain(a[2]), *bs = plain(a[3]);
+    Output out;
+    GENERAL_UNLESS(ac && out.take(a[10]));
+    const c10::Device dev = ac->device();
+    GENERAL_UNLESS(operand(ac, m * k, dev) && operand(as, m * k / block, dev) && operand(bc, n * k, dev) && operand(bs, n * k / block, dev));
+    at::ScalarType type = at::kFloat;
+    if (out.tensor) {
+        GENERAL_UNLESS(dtype_id(*out.tensor, &dt) && out.tensor->numel() == m * n && here(*out.tensor, dev));
+    } else {
+        GENERAL_UNLESS(THPDtype_Check(a[9]));
+        type = reinterpret_cast<THPDtype*>(a[9])->scalar_type;
+        GENERAL_UNLESS(dtype_id(type, &dt));
+    }
+    const int rc = unlocked([&] {
+        out.make({m, n}, type, *ac);
+        return api.matmul(ac->data_ptr(), bytes(*as), bc->data_ptr(), bytes(*bs), (size_t)m, (size_t)n, (size_t)k, fmt, block, out.data(), dt,
+                          current_stream());
+    });
+    GENERAL_UNLESS(rc == MXQ_OK);
+    return out.result(a[10]);
+    END_HANDLE_TH_ERRORS
+}
+
+// The quantization of a matrix along its rows (codes, scales) and of its transpose (codes_t, scales_t); undefined where not wanted.
+struct MatrixCodes {
+    at::Tensor codes, scales, codes_t, scales_t;
+    int make(const at::Tensor& x, int dt, int64_t rows, int64_t cols, int fmt, int block, bool by_rows, bool by_cols)
+    {
+        const auto u8 = at::TensorOptions().dtype(at::kByte).device(x.device());
+        if (by_rows) {
+            codes = at::empty({(int64_t)api.matrix_codes_bytes((size_t)rows, (size_t)cols, block)}, u8);
+            scales = at::empty({(int64_t)api.matrix_scales_bytes((size_t)rows, (size_t)cols, block)}, u8);
+        }
+        if (by_cols) {
+            codes_t = at::empty({(int64_t)api.matrix_codes_bytes((size_t)cols, (size_t)rows, block)}, u8);
+            scales_t = at::empty({(int64_t)api.matrix_scales_bytes((size_t)cols, (size_t)rows, block)}, u8);
+        }
+        auto ptr = [](const at::Tensor& t) { return t.defined() ? static_cast<uint8_t*>(t.data_ptr()) : nullptr; };
+        return api.quantize_matrix(x.data_ptr(), dt, (size_t)rows, (size_t)cols, fmt, block, ptr(codes), ptr(scales), ptr(codes_t), ptr(scales_t),
+                                   current_stream());
+    }
+};
+
+// quantize_matrix(src, fmt, block, rows, cols, stream)
+PyObject* quantize_matrix(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int fmt, block, dt;
+    GENERAL_UNLESS(nargs == 6 && a[5] == Py_None && format_id(a[1], &fmt) && as_int(a[2], &block) && block > 0 && PyBool_Check(a[3]) &&
+                   PyBool_Check(a[4]) && !modes_active());
+    const at::Tensor* src = plain(a[0]);
+    GENERAL_UNLESS(src && dtype_id(*src, &dt) && src->dim() == 2 && here(*src, src->device()));
+    MatrixCodes q;
+    const int rc = unlocked([&] { return q.make(*src, dt, src->size(0), src->size(1), fmt, block, a[3] == Py_True, a[4] == Py_True); });
+    GENERAL_UNLESS(rc == MXQ_OK);
+    PyObject* t = PyTuple_New(4);
+    if (!t) return nullptr;
+    const at::Tensor* got[4] = {&q.codes, &q.scales, &q.codes_t, &q.scales_t};
+    for (int i = 0; i < 4; ++i) {
+        PyObject* o = got[i]->defined() ? THPVariable_Wrap(*got[i]) : Py_NewRef(Py_None);
+        if (!o) {
+            Py_DECREF(t);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(t, i, o);
+    }
+    return t;
+    END_HANDLE_TH_ERRORS
+}
+
+// moe(x, logits, up_codes, up_scales, down_codes, down_scales, inner, top_k, fmt, block, renormalize, out, workspace, stream)
+PyObject* moe(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int fmt, block, dt, top_k;
+    int64_t inner;
+    GENERAL_UNLESS(nargs == 14 && a[13] == Py_None && as_count(a[6], &inner) && inner > 0 && inner < (1ll << 31) && as_int(a[7], &top_k) && top_k > 0 &&
+                   format_id(a[8], &fmt) && as_int(a[9], &block) && block > 0 && PyBool_Check(a[10]) && !modes_active());
+    const at::Tensor *x = plain(a[0]), *logits = plain(a[1]), *uc = plain(a[2]), *us = plain(a[3]), *dc = plain(a[4]), *ds = plain(a[5]);
+    Output out, ws;
+    GENERAL_UNLESS(x && logits && dtype_id(*x, &dt) && x->dim() == 2 && logits->dim() == 2 && logits->scalar_type() == at::kFloat &&
+                   logits->size(0) == x->size(0) && out.take(a[11]) && ws.take(a[12]));
+    const c10::Device dev = x->device();
+    const int64_t tokens = x->size(0), hidden = x->size(1), experts = logits->size(1);
+    GENERAL_UNLESS(hidden > 0 && hidden < (1ll << 31) && experts > 0 && experts < (1 << 16) && inner * hidden < (1ll << 42));
+    const int64_t weights = experts * hidden * inner;
+    GENERAL_UNLESS(here(*x, dev) && here(*logits, dev) && operand(uc, (int64_t)api.codes_bytes((size_t)(2 * weights), fmt), dev) &&
+                   operand(us, 2 * weights / block, dev) && operand(dc, (int64_t)api.codes_bytes((size_t)weights, fmt), dev) &&
+                   operand(ds, weights / block, dev));
+    GENERAL_UNLESS(!out.tensor || (out.tensor->sizes() == x->sizes() && out.tensor->scalar_type() == x->scalar_type() && here(*out.tensor, dev)));
+    GENERAL_UNLESS(!ws.tensor || operand(ws.tensor, 0, dev));
+    const int rc = unlocked([&] {
+        out.make_like(*x);
+        ws.make({(int64_t)api.moe_workspace_bytes((size_t)tokens, top_k, (size_t)inner, dt)}, at::kByte, *x);
+        const mxq_moe_layer layer{uc->data_ptr(), bytes(*us), dc->data_ptr(), bytes(*ds), (size_t)hidden, (size_t)inner, (int)experts, fmt, block};
+        return api.moe(&layer, x->data_ptr(), dt, static_cast<const float*>(logits->data_ptr()), (size_t)tokens, top_k, a[10] == Py_True, out.data(),
+                       ws.data(), (size_t)ws.tensor->numel(), current_stream());
+    });
+    // (the first of the call's two launches may precede the one that failed)
+    if (rc == MXQ_ERR_CUDA) return raise_mxq_error(rc, "mxq_moe");
+    GENERAL_UNLESS(rc == MXQ_OK);
+    return out.result(a[11]);
+    END_HANDLE_TH_ERRORS
+}
+
+// y = Q(x) Q(w)^T with dx = Q(dy) Q(w^T)^T and dw = Q(dy^T) Q(x^T)^T: what _LinearSTE of binding.py does, for x [..., k] and w [n, k].
+struct LinearSTE : torch::autograd::Function<LinearSTE> {
+    static int64_t up(int64_t v, int64_t block) { return (v + block - 1) / block * block; }
+    static int product(const at::Tensor& a, const at::Tensor& as, const at::Tensor& b, const at::Tensor& bs, int64_t m, int64_t n, int64_t k, int64_t block,
+                       const at::Tensor& out)
+    {
+        int dt = 0;
+        dtype_id(out, &dt);
+        return api.matmul(a.data_ptr(), bytes(as), b.data_ptr(), bytes(bs), (size_t)m, (size_t)n, (size_t)k, MXQ_FP8_E4M3, (int)block, out.data_ptr(), dt,
+                          current_stream());
+    }
+
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& w, int64_t block, bool need_x, bool need_w)
+    {
+        const int64_t k = w.size(1), n = w.size(0), m = x.numel() / k;
+        int xt = 0, wt = 0;
+        dtype_id(x, &xt);
+        dtype_id(w, &wt);
+        MatrixCodes qx, qw;
+        if (qx.make(x, xt, m, k, MXQ_FP8_E4M3, (int)block, true, need_w) != MXQ_OK) throw NotPlain{};
+        if (qw.make(w, wt, n, k, MXQ_FP8_E4M3, (int)block, true, need_x) != MXQ_OK) throw NotPlain{};
+        std::vector<int64_t> sizes = x.sizes().vec();
+        sizes.back() = n;
+        at::Tensor y = at::empty(sizes, x.options());
+        if (product(qx.codes, qx.scales, qw.codes, qw.scales, m, n, up(k, block), block, y) != MXQ_OK) throw NotPlain{};
+        ctx->save_for_backward({qx.codes_t, qx.scales_t, qw.codes_t, qw.scales_t});
+        ctx->saved_data["block"] = block;
+        ctx->saved_data["sizes"] = x.sizes().vec();
+        ctx->saved_data["n"] = n;
+        ctx->saved_data["x_type"] = x.scalar_type();
+        ctx->saved_data["w_type"] = w.scalar_type();
+        return y;
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const auto saved = ctx->get_saved_variables();
+        const std::vector<int64_t> sizes = ctx->saved_data["sizes"].toIntVector();
+        const int64_t block = ctx->saved_data["block"].toInt(), n = ctx->saved_data["n"].toInt(), k = sizes.back();
+        int64_t m = 1;
+        for (size_t i = 0; i + 1 < sizes.size(); ++i) m *= sizes[i];
+        const bool need_x = saved[2].defined() && ctx->needs_input_grad(0), need_w = saved[0].defined() && ctx->needs_input_grad(1);
+        torch::autograd::variable_list out(5);
+        if (!grads[0].defined() || !(need_x || need_w)) return out;
+        const bool twice = at::GradMode::is_enabled() && grads[0].requires_grad();
+        {
+            at::NoGradGuard no_grad;
+            const at::Tensor dy = grads[0].contiguous();
+            int dt = 0;
+            TORCH_CHECK_TYPE(dtype_id(dy, &dt), "mxq tensors are float32 or bfloat16, got ", dy.scalar_type());
+            TORCH_CHECK_VALUE(dy.is_cuda(), "the gradient must be a CUDA tensor (libmxq has no CPU path)");
+            MatrixCodes q;
+            int rc = q.make(dy, dt, m, n, MXQ_FP8_E4M3, (int)block, need_x, need_w);
+            if (rc != MXQ_OK) throw_mxq_error(rc, "mxq_quantize_matrix");
+            if (need_x) {
+                out[0] = at::empty(sizes, dy.options().dtype(ctx->saved_data["x_type"].toScalarType()));
+                rc = product(q.codes, q.scales, saved[2], saved[3], m, k, up(n, block), block, out[0]);
+                if (rc != MXQ_OK) throw_mxq_error(rc, "mxq_matmul");
+            }
+            if (need_w) {
+                out[1] = at::empty({n, k}, dy.options().dtype(ctx->saved_data["w_type"].toScalarType()));
+                rc = product(q.codes_t, q.scales_t, saved[0], saved[1], n, k, up(m, block), block, out[1]);
+                if (rc != MXQ_OK) throw_mxq_error(rc, "mxq_matmul");
+            }
+        }
+        if (twice) {                       // the quantizers have no second derivative: say so where one is asked for
+            const auto refuse = std::make_shared<torch::autograd::DelayedError>("linear_ste can be differentiated once only", 5);
+            return (*refuse)(std::move(out));
+        }
+        return out;
+    }
+};
+
+// linear_ste(x, w, block)
+PyObject* linear_ste(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int block, dt;
+    GENERAL_UNLESS(nargs == 3 && as_int(a[2], &block) && (block == 32 || block == 64 || block == 128) && !modes_active() &&
+                   !torch::jit::tracer::isTracing());
+    const at::Tensor *x = plain(a[0]), *w = plain(a[1]);
+    const bool transforms = c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode);
+    GENERAL_UNLESS(x && w && dtype_id(*x, &dt) && dtype_id(*w, &dt) && x->dim() >= 1 && w->dim() == 2 && x->size(-1) == w->size(1) && x->numel() > 0 &&
+                   w->numel() > 0 && here(*x, x->device()) && here(*w, x->device()) && !x->_fw_grad(0).defined() && !w->_fw_grad(0).defined() &&
+                   !transforms);
+    const bool grad = at::GradMode::is_enabled();
+    at::Tensor y;
+    try {
+        Unlocked u;
+        y = LinearSTE::apply(*x, *w, (int64_t)block, grad && x->requires_grad(), grad && w->requires_grad());
+    } catch (const NotPlain&) {
+        Py_RETURN_NONE;
+    }
+    return THPVariable_Wrap(y);
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(addresses by name, formats, torch.nn.Parameter, MxqError)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs)
 {
@@ -493,6 +719,12 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     take("mxq_fake_quant", n.fake_quant);
     take("mxq_fake_quant_bwd", n.fake_quant_bwd);
     take("mxq_codes_bytes", n.codes_bytes);
+    take("mxq_matmul", n.matmul);
+    take("mxq_quantize_matrix", n.quantize_matrix);
+    take("mxq_matrix_codes_bytes", n.matrix_codes_bytes);
+    take("mxq_matrix_scales_bytes", n.matrix_scales_bytes);
+    take("mxq_moe", n.moe);
+    take("mxq_moe_workspace_bytes", n.moe_workspace_bytes);
     if (!ok) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "an entry point has no address");
         return nullptr;
@@ -510,7 +742,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs)
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bind),           FAST(quantize),          FAST(slice_scale), FAST(slice_scale_multi),
                          FAST(dequantize),     FAST(quantize_tiled),    FAST(slice_scale_tiled), FAST(fake_quant),
-                         FAST(fake_quant_bwd), FAST(run_prepared),      FAST(fake_quant_ste), {nullptr, nullptr, 0, nullptr}};
+                         FAST(fake_quant_bwd), FAST(run_prepared),      FAST(fake_quant_ste),
+                         FAST(matmul),         FAST(quantize_matrix),   FAST(moe),         FAST(linear_ste), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mxq_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -224,12 +224,12 @@ struct Chunk {
                                                        uint32_t left)
     {
         const uint32_t to = slot + lane * 16;
-        const bool in = left >= 64u || (uint32_t)(lane & 3) * 16 < left;
-        if (!in) off = 0;
+        const bool in = (uint32_t)(lane & 3) * 16 < left;
+        if (!in) off = next = 0;
 #pragma unroll
         for (int m = 0; m < TILES; ++m) {
-            copy16(to + m * 1024, lo + (in ? m * next : 0u) + off, in);
-            copy16(to + m * 1024 + 512, hi + (in ? m * next : 0u) + off, in);
+            copy16(to + m * 1024, lo + (m * next + off), in);
+            copy16(to + m * 1024 + 512, hi + (m * next + off), in);
         }
     }
     // acc += the tiles times the token pieces.  ORDERED: the tokens' values lie in the order of the widened pairs already.
@@ -454,6 +454,7 @@ moe_up_kernel(const MoeArgs p, const int slots)
         const bool live = group + g < cnt;
         const uint8_t* xrow = p.x + (size_t)(T::size == 4 && live ? ch.token[first + group + g] : 0) * H * T::size;
         float sum[TILES][4] = {};
+#pragma unroll 2
         for (int turn = 0; turn < turns; ++turn) {
             fetch(slot == 0 ? slots - 1 : slot - 1);         // (that slot was read in the turn before)
             wait_slot(slots);

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2604_00529_b200 as mxq
+import paper_2604_00529_b200.binding  # noqa: F401
 from oracle import mxq_oracle as orc
 
 import product_util as pu
@@ -275,6 +276,42 @@ def test_linear_ste_gradients_against_differences():
             lo[i, j] -= 1
             d = (f(hi, w) - f(lo, w)) / 2 if at is x else (f(x, hi) - f(x, lo)) / 2
             assert d == float(grad[i, j])
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_linear_ste_has_no_second_derivative(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(mxq.binding._host, "linear_ste", lambda *a: None)
+    x = torch.randn(4, 32, device="cuda", requires_grad=True)
+    w = torch.randn(8, 32, device="cuda", requires_grad=True)
+    (g,) = torch.autograd.grad(mxq.linear_ste(x, w).square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
+def test_native_and_general_path_agree(monkeypatch):
+    """The binding's native code and the Python code behind it: the same bits."""
+    rng = rng_of(81, 3)
+    ac, as_, _ = pu.quantized(rng, 40, 256, "e4m3", 64)
+    ops = [dev(t) for t in (ac, as_, ac, as_)]
+    x = torch.randn(5, 7, 96, device="cuda", dtype=BF, requires_grad=True)
+    w = torch.randn(50, 96, device="cuda", requires_grad=True)
+    xm, lg, up, down = moe_case(rng, 4, 6, 64, 96, "int4", 32, BF)
+
+    def everything():
+        y = mxq.linear_ste(x, w)
+        moe = mxq.moe(xm, dev(lg), up[0], up[1], down[0], down[1], 96, 2, "int4")
+        return [mxq.matmul(*ops, 40, 40, 256, block=64, dtype=FP), *mxq.quantize_matrix(x.detach().view(35, 96)), moe, y.detach(),
+                *torch.autograd.grad(y, (x, w), torch.ones_like(y))]
+
+    native = everything()
+    assert all(t.device.type == "cuda" for t in native)
+    host = mxq.binding._host
+    assert host.matmul(*ops, 40, 40, 256, "e4m3", 64, FP, None, None) is not None
+    for name in ("matmul", "quantize_matrix", "moe", "linear_ste"):
+        monkeypatch.setattr(host, name, lambda *a: None)
+    for a, b in zip(native, everything()):
+        assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)
 
 
 def test_linear_ste_empty_batch():
