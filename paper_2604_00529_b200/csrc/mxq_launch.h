@@ -95,6 +95,7 @@ struct MatmulArgs {
 };
 int launch_matmul_few(const MatmulArgs& p, int dst_dtype, cudaStream_t stream);     // few rows of A: bound by reading B
 int launch_matmul_tc(const MatmulArgs& p, int dst_dtype, cudaStream_t stream);      // on the tensor cores
+double matmul_tc_us(const MatmulArgs& p);                                            // what that is expected to take
 int tc_status(int reset);
 
 // Batched Slice-and-Scale over a device-resident item table and its coarse tile index (see

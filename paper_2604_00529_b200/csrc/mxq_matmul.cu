@@ -11,41 +11,44 @@ namespace {
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // ---- few rows of A ----------------------------------------------------------------------------------------
-// Bound by reading B once.  A CTA of eight warps covers 16 rows of B and 8 NG rows of A; the warps share k out in chunks of 64
-// and meet in shared memory at the end, in a fixed order.  Codes go from global memory straight into the fragments of the
-// warp's matrix instruction: widened to FP16, exactly, by the conversion instruction, and the block's two scales
-// multiply the FP32 sum of the block.
-//   BLK32: blocks of 32; a lane's piece is then 8 bytes, so that a matrix step stays within a block (16 bytes otherwise).
+// Bound by reading B once.  A CTA of 16 warps covers 32 rows of B and up to eight of A; the warps share k out in chunks of 64 and
+// meet in shared memory at the end, in a fixed order.  Codes go from global memory straight into the fragments of the warp's
+// matrix instruction: widened to FP16, exactly, by the conversion instruction, and the block's two scales multiply the
+// FP32 sum of the block.  (One row of A, B 4096 x 4096: 6.2 us; eight warps 9.7, 16 rows of B 8.6, one chunk under way per warp
+// instead of two 6.8.)
+//   BLK32: blocks of 32.  Two of the four lanes of a row then hold one block and two the other: a step is taken twice, with the other
+//   lanes' elements of A zero (the matrix instructions are the least of this kernel's time).
 
-constexpr int kFewWarps = 8;
-constexpr int kFewDepth = 4;                                // chunks in flight per warp
+constexpr int kFewWarps = 16;
+constexpr int kFewTiles = 2;                                // 16-row tiles of B per CTA
+constexpr int kFewDepth = 2;                                // chunks in flight per warp
 
-template <bool BLK32>
-struct Piece;                                               // the codes of one row in a chunk of 64: 16 bytes per lane
-template <>
-struct Piece<false> {
+struct Piece {                                              // a lane's 16 codes of one row in a chunk of 64; zeros beyond k
     uint32_t w[4];
-    __device__ __forceinline__ void load(const uint8_t* row, size_t k0, size_t k, int t)
+    __device__ __forceinline__ void load(const uint8_t* row, uint32_t k0, uint32_t k, int t)
     {
-        const size_t at = k0 + (size_t)t * 16;
+        const uint32_t at = k0 + t * 16;
         const uint4 v = at < k ? ld_once(row + at) : make_uint4(0, 0, 0, 0);
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
     }
 };
-template <>
-struct Piece<true> {
-    uint32_t w[4];
-    __device__ __forceinline__ void load(const uint8_t* row, size_t k0, size_t k, int t)
-    {
+
+// The scale bytes of a row for a chunk: one, or with blocks of 32 two (127, a factor of 1, beyond k: what they scale is 0).
+template <int SUB>
+__device__ __forceinline__ void chunk_scales(const uint8_t* row, uint32_t k0, uint32_t k, uint32_t kblocks, int block_shift, uint32_t (&x)[SUB])
+{
+    const uint32_t kb = k0 >> block_shift;
+    if constexpr (SUB == 1) {
+        x[0] = k0 < k ? ld_u8(row + kb) : 127u;
+    } else if ((kblocks & 1u) == 0) {                       // (the row then begins at an even address)
+        const uint32_t w = k0 < k ? ld_u16(row + kb) : 0x7F7Fu;
+        x[0] = w & 255u;
+        x[1] = w >> 8;
+    } else {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const size_t at = k0 + 32 * h + (size_t)t * 8;
-            const uint2 v = at < k ? ld_once8(row + at) : make_uint2(0, 0);
-            w[2 * h] = v.x;
-            w[2 * h + 1] = v.y;
-        }
+        for (int s = 0; s < SUB; ++s) x[s] = kb + s < kblocks ? ld_u8(row + kb + s) : 127u;
     }
-};
+}
 
 // sum += acc 2^(xb + xa - 254), element e of rows (e >> 1) of B and (e & 1) of A.  The exponents are added before they become
 // a factor, so that a large scale of one operand and a small one of the other do not overflow on the way.  A factor that
@@ -83,112 +86,125 @@ __device__ __forceinline__ void store_out(uint8_t* dst, size_t i, float v)
     }
 }
 
-template <class OUT, int NG, bool BLK32>
+constexpr int kFewRows = 8;                                 // rows of A: the columns of a matrix step
+
+template <class OUT, bool BLK32>
 __global__ void __launch_bounds__(kFewWarps * 32)
 matmul_few_kernel(const uint8_t* __restrict__ a, const uint8_t* __restrict__ as, const uint8_t* __restrict__ b,
-                  const uint8_t* __restrict__ bs, size_t m, size_t n, size_t k, uint32_t tiles_n, uint32_t kblocks, int block_shift,
-                  uint8_t* __restrict__ dst)
+                  const uint8_t* __restrict__ bs, size_t m, size_t n, uint32_t k, uint32_t kblocks, int block_shift, uint8_t* __restrict__ dst)
 {
     constexpr int SUB = BLK32 ? 2 : 1;                      // blocks that a chunk of 64 touches
-    __shared__ float s_sum[kFewWarps][NG][4][32];
+    __shared__ float s_sum[kFewWarps][kFewTiles][4][32];
     pdl_release();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const size_t j0 = (size_t)(blockIdx.x % tiles_n) * 16, i0 = (size_t)(blockIdx.x / tiles_n) * (8 * NG);
-    pdl_acquire();
-    // rows beyond the matrix read its last row; their results are not stored
-    const size_t jr[2] = {min(j0 + g, n - 1), min(j0 + g + 8, n - 1)};
-    size_t ir[NG], ic[NG][2];
+    const size_t j0 = (size_t)blockIdx.x * (16 * kFewTiles);
+    // rows beyond the matrices read their last row; their results are not stored
+    const uint8_t *br[kFewTiles][2], *bsr[kFewTiles][2], *ar = a + min((size_t)g, m - 1) * k, *asr[2];
 #pragma unroll
-    for (int q = 0; q < NG; ++q) {
-        ir[q] = min(i0 + q * 8 + g, m - 1);
-        ic[q][0] = min(i0 + q * 8 + 2 * t, m - 1);
-        ic[q][1] = min(i0 + q * 8 + 2 * t + 1, m - 1);
-    }
-    float sum[NG][4] = {};
-    const size_t chunks = (k + 63) / 64;
-    for (size_t c0 = warp; c0 < chunks; c0 += kFewWarps * kFewDepth) {
-        Piece<BLK32> pb[kFewDepth][2], pa[kFewDepth][NG];
-        uint32_t xb[kFewDepth][2][SUB], xa[kFewDepth][NG][2][SUB];
+    for (int u = 0; u < kFewTiles; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const size_t r = min(j0 + u * 16 + h * 8 + g, n - 1);
+            br[u][h] = b + r * k;
+            bsr[u][h] = bs + r * kblocks;
+        }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) asr[h] = as + min((size_t)(2 * t + h), m - 1) * kblocks;
+    pdl_acquire();
+    float sum[kFewTiles][4] = {};
+    const uint32_t chunks = (k + 63) / 64;
+    for (uint32_t c0 = warp; c0 < chunks; c0 += kFewWarps * kFewDepth) {
+        Piece pb[kFewDepth][kFewTiles][2], pa[kFewDepth];
+        uint32_t xb[kFewDepth][kFewTiles][2][SUB], xa[kFewDepth][2][SUB];
 #pragma unroll
         for (int d = 0; d < kFewDepth; ++d) {
-            const size_t c = c0 + d * kFewWarps, k0 = c * 64;       // a chunk beyond k loads nothing and adds zeros
+            const uint32_t k0 = (c0 + d * kFewWarps) * 64;         // a chunk beyond k loads nothing and adds zeros
 #pragma unroll
-            for (int h = 0; h < 2; ++h) pb[d][h].load(b + jr[h] * k, k0, k, t);
+            for (int u = 0; u < kFewTiles; ++u)
 #pragma unroll
-            for (int q = 0; q < NG; ++q) pa[d][q].load(a + ir[q] * k, k0, k, t);
+                for (int h = 0; h < 2; ++h) pb[d][u][h].load(br[u][h], k0, k, t);
+            pa[d].load(ar, k0, k, t);
 #pragma unroll
-            for (int s = 0; s < SUB; ++s) {
-                const size_t kk = k0 + 32 * s, kb = kk >> block_shift;
-                const bool in = kk < k;
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) xb[d][h][s] = in ? ld_u8(bs + jr[h] * kblocks + kb) : 127u;
-#pragma unroll
-                for (int q = 0; q < NG; ++q)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) xa[d][q][h][s] = in ? ld_u8(as + ic[q][h] * kblocks + kb) : 127u;
+                for (int u = 0; u < kFewTiles; ++u) chunk_scales<SUB>(bsr[u][h], k0, k, kblocks, block_shift, xb[d][u][h]);
+                chunk_scales<SUB>(asr[h], k0, k, kblocks, block_shift, xa[d][h]);
             }
         }
 #pragma unroll
         for (int d = 0; d < kFewDepth; ++d) {
-            uint32_t f0[8], f1[8];
+            uint32_t x[SUB][8];
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                e4m3_word_to_f16(pb[d][0].w[w], f0[2 * w], f0[2 * w + 1]);
-                e4m3_word_to_f16(pb[d][1].w[w], f1[2 * w], f1[2 * w + 1]);
+                uint32_t lo, hi;
+                e4m3_word_to_f16(pa[d].w[w], lo, hi);
+#pragma unroll
+                for (int s = 0; s < SUB; ++s) {
+                    const bool mine = !BLK32 || (t >> 1) == s;
+                    x[s][2 * w] = mine ? lo : 0u;
+                    x[s][2 * w + 1] = mine ? hi : 0u;
+                }
             }
 #pragma unroll
-            for (int q = 0; q < NG; ++q) {
-                uint32_t x[8];
+            for (int u = 0; u < kFewTiles; ++u) {
+                uint32_t f0[8], f1[8];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) e4m3_word_to_f16(pa[d][q].w[w], x[2 * w], x[2 * w + 1]);
+                for (int w = 0; w < 4; ++w) {
+                    e4m3_word_to_f16(pb[d][u][0].w[w], f0[2 * w], f0[2 * w + 1]);
+                    e4m3_word_to_f16(pb[d][u][1].w[w], f1[2 * w], f1[2 * w + 1]);
+                }
 #pragma unroll
                 for (int s = 0; s < SUB; ++s) {
                     float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int w = s * (4 / SUB); w < (s + 1) * (4 / SUB); ++w)
-                        F16Mma::mma(acc, f0[2 * w], f1[2 * w], f0[2 * w + 1], f1[2 * w + 1], x[2 * w], x[2 * w + 1]);
-                    add_scaled(sum[q], acc, xb[d][0][s], xb[d][1][s], xa[d][q][0][s], xa[d][q][1][s]);
+                    for (int w = 0; w < 4; ++w) F16Mma::mma(acc, f0[2 * w], f1[2 * w], f0[2 * w + 1], f1[2 * w + 1], x[s][2 * w], x[s][2 * w + 1]);
+                    add_scaled(sum[u], acc, xb[d][u][0][s], xb[d][u][1][s], xa[d][0][s], xa[d][1][s]);
                 }
             }
         }
     }
 #pragma unroll
-    for (int q = 0; q < NG; ++q)
+    for (int u = 0; u < kFewTiles; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s_sum[warp][q][e][lane] = sum[q][e];
+        for (int e = 0; e < 4; ++e) s_sum[warp][u][e][lane] = sum[u][e];
     __syncthreads();
-    // element (row g + 8 (e >> 1) of B, row 2 t + (e & 1) of A) of group q sits at [q][e][g * 4 + t]
-    for (int o = threadIdx.x; o < NG * 128; o += kFewWarps * 32) {
-        const int q = o >> 7, col = (o >> 4) & 7, row = o & 15;
-        const int e = (row >> 3) * 2 + (col & 1), ln = (row & 7) * 4 + (col >> 1);
-        float v = 0.f;
+    // element (row g + 8 (e >> 1) of a tile of B, row 2 t + (e & 1) of A) sits at [e][g * 4 + t]
+    if (threadIdx.x >= kFewTiles * 128) return;
+    const int row = threadIdx.x % (16 * kFewTiles), col = threadIdx.x / (16 * kFewTiles);
+    const int e = (row >> 3 & 1) * 2 + (col & 1), ln = (row & 7) * 4 + (col >> 1);
+    float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < kFewWarps; ++w) v += s_sum[w][q][e][ln];
-        const size_t i = i0 + q * 8 + col, j = j0 + row;
-        if (i < m && j < n) store_out<OUT>(dst, i * n + j, v);
-    }
+    for (int w = 0; w < kFewWarps; ++w) v += s_sum[w][row >> 4][e][ln];
+    const size_t j = j0 + row;
+    if ((size_t)col < m && j < n) store_out<OUT>(dst, (size_t)col * n + j, v);
 }
 
-template <class OUT, int NG>
+template <class OUT>
 int run_few(const MatmulArgs& p, cudaStream_t stream)
 {
-    const size_t gx = (p.n + 15) / 16, gy = (p.m + 8 * NG - 1) / (8 * NG);
-    if (gx * gy > 0x7FFFFFFF) return MXQ_ERR_SIZE;
+    const size_t ctas = (p.n + 16 * kFewTiles - 1) / (16 * kFewTiles);
     const uint32_t kblocks = (uint32_t)(p.k / (size_t)p.block);
     const int shift = p.block == 32 ? 5 : p.block == 64 ? 6 : 7;
     auto go = [&](auto kern) {
-        return launch_kernel(kern, (int)(gx * gy), kFewWarps * 32, stream, p.a, p.as, p.b, p.bs, p.m, p.n, p.k, (uint32_t)gx, kblocks, shift,
-                             p.dst);
+        return launch_kernel(kern, (int)ctas, kFewWarps * 32, stream, p.a, p.as, p.b, p.bs, p.m, p.n, (uint32_t)p.k, kblocks, shift, p.dst);
     };
-    return p.block == 32 ? go(matmul_few_kernel<OUT, NG, true>) : go(matmul_few_kernel<OUT, NG, false>);
+    return p.block == 32 ? go(matmul_few_kernel<OUT, true>) : go(matmul_few_kernel<OUT, false>);
+}
+
+// What a launch is expected to take, in microseconds: a time per wave of CTAs (one per SM) that grows with k.  As measured, one row of A:
+// B 1024 x 1024 3.4 (tensor cores 4.7), 4096 x 4096 6.2 (7.9), 6144 x 4096 11.6 (two waves; 10.0), 14336 x 4096 22 (15.5); with
+// blocks of 32, 4096 x 2048 5.7 (6.5) and 4096 x 4096 10.4 (8.0).
+double few_us(const MatmulArgs& p)
+{
+    const size_t ctas = (p.n + 16 * kFewTiles - 1) / (16 * kFewTiles);
+    return (double)((ctas + 147) / 148) * (2.1 + (p.block == 32 ? 0.002 : 0.001) * (double)p.k);
 }
 
 }  // namespace
 
 int launch_matmul_few(const MatmulArgs& p, int dst_dtype, cudaStream_t stream)
 {
-    if (p.m <= 8) return dst_dtype == MXQ_F32 ? run_few<F32, 1>(p, stream) : run_few<BF16, 1>(p, stream);
-    return dst_dtype == MXQ_F32 ? run_few<F32, 2>(p, stream) : run_few<BF16, 2>(p, stream);
+    return dst_dtype == MXQ_F32 ? run_few<F32>(p, stream) : run_few<BF16>(p, stream);
 }
 
 }  // namespace mxq
@@ -224,7 +240,7 @@ int mxq_matmul(const void* a_codes, const uint8_t* a_scales, const void* b_codes
     MXQ_DEBUG_EXPECT(dst, m * n * size);
     const MatmulArgs p{static_cast<const uint8_t*>(a_codes), a_scales, static_cast<const uint8_t*>(b_codes), b_scales, m, n, k, block,
                        static_cast<uint8_t*>(dst)};
-    return m <= 4 ? launch_matmul_few(p, dst_dtype, s) : launch_matmul_tc(p, dst_dtype, s);
+    return m <= (size_t)kFewRows && few_us(p) <= matmul_tc_us(p) ? launch_matmul_few(p, dst_dtype, s) : launch_matmul_tc(p, dst_dtype, s);
 }
 
 int mxq_wait_status(int reset) { return tc_status(reset); }

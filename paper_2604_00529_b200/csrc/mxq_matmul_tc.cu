@@ -81,14 +81,25 @@ struct RowScales {
         if (row >= rows) return;
         const uint8_t* at = s + row * kblocks;
         const uint32_t first = kt * PER;
-        if (((kblocks | first) & 3u) == 0) {
+        const uint32_t skip = (uint32_t)reinterpret_cast<uintptr_t>(at + first) & 3u, have = kblocks > first ? kblocks - first : 0;
+        const uint8_t* const from = at + first - skip;
+        if (skip == 0 && (kblocks & 3u) == 0) {
 #pragma unroll
             for (int j = 0; j < NW; ++j)
-                if (first + 4 * j < kblocks) w[j] = ld_u32(at + first + 4 * j);
-        } else {
+                if (4u * j < have) w[j] = ld_u32(at + first + 4 * j);
+        } else if (from + 4 * (NW + 1) <= s + rows * kblocks) {      // any alignment: the words that hold the bytes, shifted together
+            uint32_t v[NW + 1];
+#pragma unroll
+            for (int j = 0; j <= NW; ++j) v[j] = ld_u32(from + 4 * j);
+#pragma unroll
+            for (int j = 0; j < NW; ++j) {
+                const uint32_t left = have > 4u * j ? have - 4u * j : 0u, x = __funnelshift_r(v[j], v[j + 1], 8 * skip);
+                w[j] = left >= 4 ? x : left ? (x & ((1u << 8 * left) - 1u)) | (0x7F7F7F7Fu << 8 * left) : 0x7F7F7F7Fu;
+            }
+        } else {                                             // the last rows
 #pragma unroll
             for (int j = 0; j < 4 * NW; ++j)
-                if (first + j < kblocks) w[j / 4] = __byte_perm(w[j / 4], ld_u8(at + first + j), (0x3210u & ~(0xFu << 4 * (j % 4))) | 4u << 4 * (j % 4));
+                if (j < have) w[j / 4] = __byte_perm(w[j / 4], ld_u8(at + first + j), (0x3210u & ~(0xFu << 4 * (j % 4))) | 4u << 4 * (j % 4));
         }
     }
     // the four bytes of k tile i, one per 32 values of k
@@ -478,6 +489,8 @@ int choose(const MatmulArgs& m, cudaStream_t stream)
 }
 
 }  // namespace
+
+double matmul_tc_us(const MatmulArgs& p) { return plan(p).us; }
 
 int launch_matmul_tc(const MatmulArgs& p, int dst_dtype, cudaStream_t stream)
 {

@@ -37,15 +37,6 @@ __device__ __forceinline__ uint4 ld_once(const uint8_t* p)
     return v;
 }
 
-// 8 bytes of the same.
-__device__ __forceinline__ uint2 ld_once8(const uint8_t* p)
-{
-    uint2 v = make_uint2(0, 0);
-    MXQ_CHECKED(p, 8, return v)
-    asm volatile("ld.global.nc.L2::128B.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-    return v;
-}
-
 // ---- codes to BF16 pairs, the block's scale multiplied in -------------------------------------------------
 // Every element value of these formats has at most eight significant bits, and a scale is a power of two: the product is a BF16
 // number, exactly, unless it leaves BF16's range (FP32's range: it then over- or underflows as FP32 would, to within a
