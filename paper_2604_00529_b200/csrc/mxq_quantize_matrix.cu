@@ -49,53 +49,60 @@ struct Eight<F32> {
     __device__ __forceinline__ void put(int j, const uint8_t* p) { w[j] = __ldg(reinterpret_cast<const uint32_t*>(p)); }
 };
 
-// elements c ... c + 7 of row r; zeros outside the matrix
+// Eight elements at p, the first `left` columns of them inside the matrix; zeros outside.
 template <class T, bool VEC>
-__device__ __forceinline__ void load8(const uint8_t* __restrict__ src, size_t rows, size_t cols, size_t r, size_t c, Eight<T>& v)
+__device__ __forceinline__ void load8(const uint8_t* __restrict__ p, size_t left, Eight<T>& v)
 {
     v.zero();
-    if (r >= rows) return;
-    const uint8_t* p = src + (r * cols + c) * T::size;
     if constexpr (VEC) {                                     // cols % 8 == 0: a piece is inside or outside as a whole
-        if (c >= cols) return;
+        if (left == 0) return;
         MXQ_CHECKED(p, 8 * T::size, return)
         v.load(p);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (c + j >= cols) continue;
+            if ((size_t)j >= left) continue;
             MXQ_CHECKED(p + j * T::size, T::size, continue)
             v.put(j, p + j * T::size);
         }
     }
 }
 
+struct MatrixShared {
+    uint32_t max[2][8][kTile / 2];                           // [rows / 64][warp][column pair]
+    uint8_t byte[4][kTile];                                  // scale byte per group of 32 rows and column
+    alignas(16) float inv[4][kTile];                         // its multiplier
+    alignas(16) uint32_t codes[kTile][32];                   // [column][four rows], exchanged
+};
+
 // FP32 bit patterns are ordered like the values, and only the exponent field of a maximum is used (0xFF: the block is
 // poisoned): the patterns' upper halves are enough, two to a word.
-template <class T, class F, int BLOCK, bool VEC>
-__global__ void __launch_bounds__(kMatThreads, T::size == 2 ? 4 : 2)
-quantize_matrix_kernel(const uint8_t* __restrict__ src, size_t rows, size_t cols, uint8_t* __restrict__ codes,
-                       uint8_t* __restrict__ scales, uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t, uint32_t row_tiles, uint32_t col_tiles)
+//   WHOLE: the tile lies inside the matrix; nothing is compared with its edges.  (The kernel is bound by instructions: 14336 x 4096 BF16
+//   took 25 per element and 55 us with every access compared and addressed for itself, 45 us like this: 5.2 TB/s.)
+template <class T, class F, int BLOCK, bool VEC, bool WHOLE>
+__device__ __forceinline__ void matrix_tile(const uint8_t* __restrict__ src, size_t rows, size_t cols, uint8_t* __restrict__ codes,
+                                            uint8_t* __restrict__ scales, uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t, size_t tr, size_t tc, MatrixShared& sh)
 {
     constexpr int LPB = BLOCK / 8;                           // lanes per block along a row
     constexpr int G = BLOCK / 32;                            // groups of 32 rows per block along a column
-    __shared__ uint32_t s_max[2][8][kTile / 2];              // [rows / 64][warp][column pair]
-    __shared__ __align__(8) uint8_t s_byte[4][kTile];        // scale byte per group of 32 rows and column
-    __shared__ uint32_t s_codes[kTile][32];                  // [column][four rows], exchanged
-    pdl_release();
+    auto& s_max = sh.max;
+    auto& s_byte = sh.byte;
+    auto& s_inv = sh.inv;
+    auto& s_codes = sh.codes;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, l = lane & 15, rg = warp * 2 + (lane >> 4);
-    // eight tiles of a column one after another: the transpose's lines then meet in L2 as longer runs
-    const uint32_t band = blockIdx.x / (8 * col_tiles), height = min(8u, row_tiles - band * 8), in_band = blockIdx.x - band * 8 * col_tiles;
-    const size_t tr = band * 8 + in_band % height, tc = in_band / height;
-    const size_t r0 = tr * kTile, c0 = tc * kTile;
+    const size_t r0 = tr * kTile, c0 = tc * kTile, c = c0 + l * 8;
     const size_t rows_p = (rows + BLOCK - 1) / BLOCK * BLOCK, cols_p = (cols + BLOCK - 1) / BLOCK * BLOCK;
-    pdl_acquire();
+    const size_t row = r0 + rg * 4;                          // the thread's rows: row + i and row + 64 + i
 
-    Eight<T> v[2][4];                                        // rows 64 s + 4 rg + i
+    Eight<T> v[2][4];
+    {
+        const size_t pitch = cols * T::size, left = WHOLE ? 8 : cols > c ? cols - c : 0;
+        const uint8_t* p = src + row * pitch + c * T::size;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load8<T, VEC>(src, rows, cols, r0 + s * 64 + rg * 4 + i, c0 + l * 8, v[s][i]);
+            for (int i = 0; i < 4; ++i) load8<T, VEC>(p + (s * 64 + i) * pitch, WHOLE || row + s * 64 + i < rows ? left : 0, v[s][i]);
+    }
 
     // along the columns: the thread's four rows, the two halves of the warp, then (below) the four warps of a group of 32 rows
     if (codes_t) {
@@ -129,7 +136,8 @@ quantize_matrix_kernel(const uint8_t* __restrict__ src, size_t rows, size_t cols
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) m[s][h] = __vmaxu2(m[s][h], __shfl_xor_sync(0xFFFFFFFFu, m[s][h], o));
-        const size_t c = c0 + l * 8;
+        uint8_t* const pc = codes + row * cols_p + c;
+        uint8_t* const ps = scales + row * (cols_p / BLOCK) + c / BLOCK;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -140,40 +148,42 @@ quantize_matrix_kernel(const uint8_t* __restrict__ src, size_t rows, size_t cols
                 q.x = quantize_fp_hw_quad<F>(e.at(0) * sc.inv, e.at(1) * sc.inv, e.at(2) * sc.inv, e.at(3) * sc.inv);
                 q.y = quantize_fp_hw_quad<F>(e.at(4) * sc.inv, e.at(5) * sc.inv, e.at(6) * sc.inv, e.at(7) * sc.inv);
                 if (sc.byte == 255u) q = make_uint2(0, 0);
-                const size_t r = r0 + s * 64 + rg * 4 + i;
-                if (r < rows && c < cols_p) {
-                    uint8_t* p = codes + r * cols_p + c;
+                if (WHOLE || (row + s * 64 + i < rows && c < cols_p)) {
+                    uint8_t* p = pc + (s * 64 + i) * cols_p;
                     bool ok = true;
                     MXQ_CHECKED(p, 8, ok = false)
                     if (ok) *reinterpret_cast<uint2*>(p) = q;
-                    if (l % LPB == 0) st_u8(scales + r * (cols_p / BLOCK) + c / BLOCK, sc.byte);
+                    if (l % LPB == 0) st_u8(ps + (s * 64 + i) * (cols_p / BLOCK), sc.byte);
                 }
             }
     }
     if (!codes_t) return;
     __syncthreads();
+    bool poison = false;
     {
-        const int c = tid & 127, s = tid >> 7;               // one column's 64 rows
+        const int k0 = (tid >> 7) * 2, col = tid & 127;      // two groups of 32 rows of one column
         uint32_t g[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
+            if (G < 4 && (k >> 1) != (k0 >> 1)) continue;
             uint32_t m = 0;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) m = max(m, (s_max[k >> 1][(k & 1) * 4 + w][c >> 1] >> (16 * (c & 1))) & 0xFFFFu);
+            for (int w = 0; w < 4; ++w) m = max(m, (s_max[k >> 1][(k & 1) * 4 + w][col >> 1] >> (16 * (col & 1))) & 0xFFFFu);
             g[k] = m;
         }
-        if constexpr (G == 2) { g[0] = g[1] = max(g[0], g[1]); g[2] = g[3] = max(g[2], g[3]); }
-        if constexpr (G == 4) g[0] = g[1] = g[2] = g[3] = max(max(g[0], g[1]), max(g[2], g[3]));
+        uint32_t lo = k0 ? g[2] : g[0], hi = k0 ? g[3] : g[1];
+        if constexpr (G == 2) lo = hi = max(lo, hi);
+        if constexpr (G == 4) lo = hi = max(max(g[0], g[1]), max(g[2], g[3]));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint32_t gm = s ? g[2 + h] : g[h];
-            const BlockScale sc = block_scale<F>(gm << 16);
-            const int k = s * 2 + h;
-            s_byte[k][c] = (uint8_t)sc.byte;
+            const BlockScale sc = block_scale<F>((h ? hi : lo) << 16);
+            s_byte[k0 + h][col] = (uint8_t)sc.byte;
+            s_inv[k0 + h][col] = sc.byte == 255u ? __uint_as_float(0x7FC00000u) : sc.inv;
+            poison |= sc.byte == 255u;
         }
     }
-    __syncthreads();
-    if (tid < kTile && c0 + tid < cols) {                    // a column's scale bytes: one store where they are aligned
+    poison = __syncthreads_or(poison);
+    if (tid < kTile && (WHOLE || c0 + tid < cols)) {         // a column's scale bytes: one store where they are aligned
         constexpr int N = 4 / G;
         const size_t per_col = rows_p / BLOCK;
         uint8_t* to = scales_t + (c0 + tid) * per_col + tr * N;
@@ -185,28 +195,50 @@ quantize_matrix_kernel(const uint8_t* __restrict__ src, size_t rows, size_t cols
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k)
-                if (r0 + k * BLOCK < rows_p) st_u8(to + k, s_byte[k * G][tid]);
+                if (WHOLE || r0 + k * BLOCK < rows_p) st_u8(to + k, s_byte[k * G][tid]);
         }
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const uint2 b = *reinterpret_cast<const uint2*>(&s_byte[s * 2 + (rg >> 3)][l * 8]);
+        const float* const from = &s_inv[s * 2 + (rg >> 3)][l * 8];
+        const float4 f0 = *reinterpret_cast<const float4*>(from), f1 = *reinterpret_cast<const float4*>(from + 4);
+        const float inv[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint32_t byte = ((j < 4 ? b.x : b.y) >> (8 * (j & 3))) & 255u;
-            const float inv = __uint_as_float((254u - byte) << 23);          // E4M3: byte <= 246 unless poisoned
-            uint32_t q = quantize_fp_hw_quad<F>(v[s][0].at(j) * inv, v[s][1].at(j) * inv, v[s][2].at(j) * inv, v[s][3].at(j) * inv);
-            if (byte == 255u) q = 0;
+            uint32_t q = quantize_fp_hw_quad<F>(v[s][0].at(j) * inv[j], v[s][1].at(j) * inv[j], v[s][2].at(j) * inv[j], v[s][3].at(j) * inv[j]);
+            if (poison && inv[j] != inv[j]) q = 0;           // (`poison` is the CTA's)
             s_codes[l * 8 + j][(rg + 16 * s) ^ (2 * l)] = q;
         }
     }
     __syncthreads();
-    const size_t row = r0 + (size_t)lane * 4;
-#pragma unroll 4
-    for (int c = warp; c < kTile; c += kMatThreads / 32) {
-        if (c0 + c >= cols || row >= rows_p) continue;
-        st_u32(codes_t + (c0 + c) * rows_p + row, s_codes[c][lane ^ (2 * (c >> 3))]);
+    // a column's 128 rows: 16 lanes of eight bytes each
+    const size_t at = r0 + (size_t)l * 8;
+    const int c1 = warp * 2 + (lane >> 4);
+    uint8_t* to = codes_t + (c0 + c1) * rows_p + at;
+    const size_t step = 16 * rows_p;
+#pragma unroll
+    for (int n = 0; n < kTile / 16; ++n, to += step) {
+        const int cc = c1 + n * 16;
+        const uint2 q = *reinterpret_cast<const uint2*>(&s_codes[cc][(2 * l) ^ (2 * (cc >> 3))]);
+        if (!WHOLE && (c0 + cc >= cols || at >= rows_p)) continue;
+        MXQ_CHECKED(to, 8, continue)
+        *reinterpret_cast<uint2*>(to) = q;
     }
+}
+
+template <class T, class F, int BLOCK, bool VEC>
+__global__ void __launch_bounds__(kMatThreads, T::size == 2 && VEC ? 4 : T::size == 2 ? 3 : 2)
+quantize_matrix_kernel(const uint8_t* __restrict__ src, size_t rows, size_t cols, uint8_t* __restrict__ codes,
+                       uint8_t* __restrict__ scales, uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t, uint32_t row_tiles, uint32_t col_tiles)
+{
+    __shared__ MatrixShared sh;
+    pdl_release();
+    // eight tiles of a column one after another: the transpose's lines then meet in L2 as longer runs
+    const uint32_t band = blockIdx.x / (8 * col_tiles), height = min(8u, row_tiles - band * 8), in_band = blockIdx.x - band * 8 * col_tiles;
+    const size_t tr = band * 8 + in_band % height, tc = in_band / height;
+    pdl_acquire();
+    if ((tr + 1) * kTile <= rows && (tc + 1) * kTile <= cols) matrix_tile<T, F, BLOCK, VEC, true>(src, rows, cols, codes, scales, codes_t, scales_t, tr, tc, sh);
+    else matrix_tile<T, F, BLOCK, VEC, false>(src, rows, cols, codes, scales, codes_t, scales_t, tr, tc, sh);
 }
 
 template <class T, int BLOCK>
