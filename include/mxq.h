@@ -25,6 +25,8 @@
  *     stream guarantees is unchanged for every buffer.  (Before that wait a kernel may issue
  *     L2 prefetches for its input buffers, which return no data; the input pointers must
  *     therefore be valid device addresses when the call is made, as they must be anyway.)
+ *     mxq_moe is two kernels; its second one reads the logits and the down matrices, which the first one does not
+ *     write, as soon as the first one has done its own wait.
  *   - `n` is the number of elements; it must be a multiple of `block`.  Blocks are runs
  *     of `block` consecutive elements of the flat array (for a row-major matrix whose inner
  *     dimension is a multiple of `block`: along the row).  n == 0 returns MXQ_OK at once.
@@ -415,7 +417,7 @@ int mxq_quantize_matrix(const void *src, int src_dtype, size_t rows, size_t cols
  *             (MXQ_ERR_FORMAT), block 32, 64 or 128 (MXQ_ERR_BLOCK); hidden and inner non-zero multiples of block up to 2^20,
  *             1 <= experts <= MXQ_MOE_EXPERTS_MAX (MXQ_ERR_SIZE)
  *   x, out    device, [tokens, hidden] of dtype; no overlap.  tokens <= MXQ_MOE_TOKENS_MAX; 0 does nothing
- *   logits    device, [tokens, experts] FP32, 16-byte aligned;  1 <= top_k <= min(experts, MXQ_MOE_TOP_K_MAX)
+ *   logits    device, [tokens, experts] FP32, 4-byte aligned;  1 <= top_k <= min(experts, MXQ_MOE_TOP_K_MAX)
  *   workspace device, 32-byte aligned, mxq_moe_workspace_bytes(tokens, top_k, inner, dtype) bytes or more (MXQ_ERR_SIZE); what
  *             it holds before and after a call means nothing.  Calls whose work can overlap on the GPU must not share one
  */

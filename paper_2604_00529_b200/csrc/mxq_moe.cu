@@ -750,7 +750,7 @@ int mxq_moe(const mxq_moe_layer* layer, const void* x, int dtype, const float* l
     const size_t need = workspace_bytes(tokens, top_k, l.inner, dtype);
     if (!x || !logits || !out || !workspace || !l.up_codes || !l.up_scales || !l.down_codes || !l.down_scales) return MXQ_ERR_NULL;
     if (workspace_size < need) return MXQ_ERR_SIZE;
-    if (!aligned(x, 32) || !aligned(out, 32) || !aligned(workspace, 32) || !aligned(logits, 16) || !aligned(l.up_codes, 32) || !aligned(l.down_codes, 32) ||
+    if (!aligned(x, 32) || !aligned(out, 32) || !aligned(workspace, 32) || !aligned(logits, 4) || !aligned(l.up_codes, 32) || !aligned(l.down_codes, 32) ||
         !aligned(l.up_scales, 16) || !aligned(l.down_scales, 16))
         return MXQ_ERR_ALIGN;
     const size_t size = dtype == MXQ_F32 ? 4u : 2u, weights = (size_t)l.experts * l.hidden * l.inner;

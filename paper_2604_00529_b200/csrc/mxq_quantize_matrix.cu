@@ -246,7 +246,7 @@ int run(const void* src, size_t rows, size_t cols, void* codes, uint8_t* scales,
 {
     using F = Fmt<MXQ_FP8_E4M3>;
     const size_t rt = (rows + kTile - 1) / kTile, ct = (cols + kTile - 1) / kTile;
-    if (ct > 0x7FFFFFFF || rt > 0x7FFFFFFF / ct) return MXQ_ERR_SIZE;
+    if (ct > (1u << 28) || rt > 0x7FFFFFFF / ct) return MXQ_ERR_SIZE;
     auto go = [&](auto kern) {
         return launch_kernel(kern, (int)(rt * ct), kMatThreads, stream, static_cast<const uint8_t*>(src), rows, cols,
                              static_cast<uint8_t*>(codes), scales, static_cast<uint8_t*>(codes_t), scales_t, (uint32_t)rt, (uint32_t)ct);

@@ -142,6 +142,8 @@ def test_matmul_on_another_stream_and_captured(m):
     got = mxq.matmul(*ops, m, n, k, block=64, stream=s)
     s.synchronize()
     assert torch.equal(got, want)
+    assert torch.equal(mxq.matmul(*ops, m, n, k, block=64, stream=torch.cuda.current_stream()), want)
+    assert torch.equal(mxq.matmul(*ops, m, n, k, block=64, stream=torch.cuda.current_stream().cuda_stream), want)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     out = torch.empty(m, n, dtype=BF, device="cuda")
@@ -430,6 +432,16 @@ def test_moe_scales_at_the_ends_of_their_range(fmt):
     for i in range(t):
         assert bool(got[i, 0].isnan()) == (0 in chosen[i])
         assert not got[i, 1:].isnan().any()
+
+
+def test_moe_takes_rows_of_a_larger_batch():
+    """Tokens and logits that are views into a batch, the logits at any row."""
+    rng = rng_of(43, 7)
+    x, lg, up, down = moe_case(rng, 7, 5, 64, 32, "e4m3", 32, BF)
+    lg = dev(lg)
+    want = mxq.moe(x, lg, up[0], up[1], down[0], down[1], 32, 2, "e4m3")
+    for i in range(7):
+        assert torch.equal(mxq.moe(x[i:i + 1], lg[i:i + 1], up[0], up[1], down[0], down[1], 32, 2, "e4m3"), want[i:i + 1])
 
 
 def test_moe_infinite_tokens_stay_in_their_rows():

@@ -94,7 +94,7 @@ def test_moe_refusals(L):
     assert call(ws_bytes=mxq.moe_workspace_bytes(2, 2, 64) - 1) == E_SIZE
     for name in ("x", "logits", "out", "ws"):
         assert call(**{name: None}) == E_NULL
-        assert call(**{name: A + 8}) == E_ALIGN
+        assert call(**{name: A + 2}) == E_ALIGN
     for name in ("up_codes", "up_scales", "down_codes", "down_scales"):
         assert call(_layer(**{name: None})) == E_NULL
         assert call(_layer(**{name: A + 8})) == E_ALIGN
