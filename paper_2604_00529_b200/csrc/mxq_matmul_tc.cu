@@ -11,6 +11,12 @@
 // scales, 8 - 11 write results.  Tiles are worked on one after another by a CTA (pair) per SM (pair of SMs); or,
 // where there are too few of them for that (SPLIT), a cluster shares one tile's k out and adds its parts through distributed
 // shared memory, in a fixed order.  A CTA pair (CG = 2) works on 256 rows of L, 128 per CTA, and shares the tile of R half and half.
+//
+// Measured (blocks of 128, BF16 results): 8192 x 14336 x 4096 352 us in short runs, 2.7 PFLOP/s; in a loop of seconds 411 us, at the
+// card's power limit and a clock of 1.28 GHz.  13 x 14336 x 4096 14.8 us, 4.0 TB/s of codes.  What the loops of the issuing warp
+// cost decides: with one lane in a branch of its own, addresses went through vector registers and a k tile took 570 ns
+// instead of 430; copying the next tile's scales ahead of this one's products, or writing them to tensor memory from registers,
+// was slower (13 x 14336 x 4096 15.9 and 18.5 us).
 #include <cuda.h>
 
 #include "mxq_kernels.cuh"

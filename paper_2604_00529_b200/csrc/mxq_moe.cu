@@ -4,8 +4,9 @@
 //              w = p / (sum of the chosen p), or p
 //   kernel 1   h[t, e] = silu(G_e x_t) * (U_e x_t), G_e and U_e the two halves of expert e's up matrix [2 inner, hidden]
 //   kernel 2   out[t] = sum over the chosen e of w[t, e] D_e h[t, e], D_e = [hidden, inner]
-// Bound by reading the chosen experts' codes once.  Both kernels work the choice out for themselves from the logits (a few
-// hundred cycles), so that no third launch stands in front, and kernel 2 does so before it waits for kernel 1.
+// Bound by reading the chosen experts' codes once.  Both kernels work the choice out for themselves from the logits (2 us for one
+// token and 64 experts, 4.4 for 32 tokens), so that no third launch stands in front, and kernel 2 does so before it waits for
+// kernel 1 (leaving the choice in the workspace for it instead was 2 to 4 % slower: it then starts only when kernel 1 is done).
 //
 // Products: a warp takes 16 rows of a matrix and a chunk of 16 bytes of codes per lane, widens the codes to BF16 with their
 // block's scale multiplied in (exact, see Widen) and multiplies them with up to eight tokens by the warp's matrix instruction,
@@ -361,6 +362,9 @@ __device__ __forceinline__ void wait_slot(int slots)         // all copies but t
 // One CTA per SM, of four teams of four warps.  A team works on units of 32 rows, 16 of the gate and the 16 of the up half that go
 // with them, of one expert, for eight of its tokens at a time; its warps share k out and meet in shared memory.  In a 16-row tile
 // the first eight rows are the gate's and the last eight the up half's.  A warp's copies run on into its next unit.
+// Bound by instructions: one token, two of eight 4096 x 14336 E4M3 experts 67 us for 235 MB (57 without the widening, 46 with the copies
+// alone); tokens go through L1, not through the copies (82 us: every SM asking L2 for the same few lines).  16 warps of up to
+// 128 registers; 20 or 24 warps of fewer gained nothing.
 
 template <class T, int FMT>
 using UpChunk = Chunk<FMT, kUpTiles>;
@@ -514,7 +518,7 @@ moe_up_kernel(const MoeArgs p, const int slots)
 // ---- kernel 2 ---------------------------------------------------------------------------------------------
 // A CTA covers 32 rows of the output for all tokens; where that makes few CTAs, a cluster of them covers the same rows.  The chunks of
 // all active experts, laid end to end, are shared out between the warps; a warp adds its weighted sums to its own copy of the tile, and the copies are added in order.  The first
-// chunks' codes are fetched before the wait for kernel 1.
+// chunks' codes are fetched before the wait for kernel 1.  (The same experts: 37 us for 117 MB; with 16 rows per CTA 46.)
 
 template <class T, int FMT, int HPARTS>
 __global__ void __launch_bounds__(kDownWarps * 32, 1)
