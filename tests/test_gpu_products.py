@@ -89,6 +89,25 @@ def test_matmul_many_tiles(m, n, k, block, dtype):
     assert torch.equal(got.view(m, n), again)
 
 
+@pytest.mark.parametrize("m", [1, 20, 300])
+def test_matmul_zero_blocks_against_the_largest_scales(m):
+    """A block of zeros (scale byte 0) met by scales of 2^127, and the other way round: zeros, of either sign, not NaN."""
+    n, k = 200, 128
+    zero, low = torch.zeros(m * k, dtype=torch.uint8, device="cuda"), torch.zeros(m, dtype=torch.uint8, device="cuda")
+    big, high = torch.full((n * k,), 0x7E, dtype=torch.uint8, device="cuda"), torch.full((n,), 254, dtype=torch.uint8, device="cuda")
+    got = mxq.matmul(zero, low, big, high, m, n, k, block=128, dtype=FP)
+    assert torch.equal(got, torch.zeros_like(got))
+    got = mxq.matmul(big, high, zero, low, n, m, k, block=128)
+    assert torch.equal(got, torch.zeros_like(got))
+
+
+def test_no_wait_ran_out():
+    a, s = torch.full((300 * 256,), 0x38, dtype=torch.uint8, device="cuda"), torch.full((600,), 127, dtype=torch.uint8, device="cuda")
+    got = mxq.matmul(a, s, a, s, 300, 300, 256, block=128, dtype=FP)
+    assert bool((got == 256).all())
+    assert mxq.load_library().mxq_wait_status(1) == 0
+
+
 def test_matmul_empty():
     c, s = torch.empty(0, dtype=torch.uint8, device="cuda"), torch.empty(0, dtype=torch.uint8, device="cuda")
     assert mxq.matmul(c, s, c, s, 0, 0, 128, block=128).shape == (0, 0)
@@ -258,6 +277,24 @@ def test_linear_ste_shapes_views_and_frozen_leaves():
     (gx,) = torch.autograd.grad(mxq.linear_ste(x2, w2.detach(), 32), x2, torch.ones_like(y2))
     assert torch.equal(gx, x2.grad)
     assert not mxq.linear_ste(x3, w2.detach(), 32).requires_grad
+
+
+def test_linear_ste_parameters_shared_and_broadcast():
+    """A parameter used twice, and one row broadcast over the batch: the gradients add up."""
+    w = torch.nn.Parameter(torch.randn(48, 64, device="cuda") * 0.1)
+    x = torch.randn(6, 64, device="cuda", requires_grad=True)
+    dy = torch.randn(6, 48, device="cuda")
+    (mxq.linear_ste(x, w) * dy).sum().backward()
+    one_w, one_x = w.grad.clone(), x.grad.clone()
+    w.grad = x.grad = None
+    ((mxq.linear_ste(x, w) + mxq.linear_ste(x, w)) * dy).sum().backward()
+    assert torch.equal(w.grad, 2 * one_w) and torch.equal(x.grad, 2 * one_x)
+    row = torch.randn(1, 64, device="cuda", requires_grad=True)
+    y = mxq.linear_ste(row.expand(6, 64), w)
+    (g,) = torch.autograd.grad(y, row, dy)
+    full = row.detach().repeat(6, 1).requires_grad_()
+    (want,) = torch.autograd.grad(mxq.linear_ste(full, w), full, dy)
+    assert torch.equal(g, want.sum(0, keepdim=True))
 
 
 def test_linear_ste_gradients_against_differences():
@@ -432,6 +469,14 @@ def test_moe_scales_at_the_ends_of_their_range(fmt):
     for i in range(t):
         assert bool(got[i, 0].isnan()) == (0 in chosen[i])
         assert not got[i, 1:].isnan().any()
+
+
+def test_moe_without_any_choice():
+    rng = rng_of(47, 7)
+    x, lg, up, down = moe_case(rng, 3, 5, 64, 32, "int8", 32, BF)
+    got = mxq.moe(x, torch.full((3, 5), -float("inf"), device="cuda"), up[0], up[1], down[0], down[1], 32, 2, "int8", out=torch.full_like(x, 9))
+    assert not got.any()
+    assert mxq.moe(x[:0], dev(lg[:0]), up[0], up[1], down[0], down[1], 32, 2, "int8").shape == (0, 64)
 
 
 def test_moe_takes_rows_of_a_larger_batch():
