@@ -24,6 +24,8 @@ namespace {
 constexpr int kMaxTokens = MXQ_MOE_TOKENS_MAX, kMaxExperts = MXQ_MOE_EXPERTS_MAX, kMaxTopK = MXQ_MOE_TOP_K_MAX;
 constexpr int kTeam = 4, kUpTeams = 4;  // kernel 1: warps of a team, teams of a CTA
 constexpr int kUpTiles = 2;             // 16-row tiles of a team's unit: eight rows of the gate and eight of the up half each
+constexpr int kDownWarps = 16;          // kernel 2: warps of a CTA
+constexpr int kDownTiles = 2;           // 16-row tiles of its rows of the output
 
 struct MoeArgs {
     const uint8_t *x, *up, *up_s, *down, *down_s;
@@ -32,8 +34,6 @@ struct MoeArgs {
     size_t hidden, inner;
     int tokens, experts, top_k, renormalize, block_shift;
 };
-
-constexpr int kDownWarps = 16, kDownTiles = 2;     // kernel 2
 
 // ---- the choice -------------------------------------------------------------------------------------------
 
@@ -191,8 +191,8 @@ __device__ __forceinline__ void bf16_parts(float v, uint32_t (&o)[PARTS])
 }
 
 // ---- the pipeline of a warp -------------------------------------------------------------------------------
-// A warp's codes and token pieces of a few chunks are always under way to shared memory (asynchronous copies, each
-// lane's own 16 bytes in a slot of its own: no lane reads what another one copied, so waiting for the own copies is enough).
+// A warp's codes of a few chunks are always under way to shared memory (asynchronous copies, each lane's own 16 bytes in a
+// place of its own: no lane reads what another one copied, so waiting for the own copies is enough).
 // A chunk is 16 bytes of codes per lane and row: four lanes cover 64 (128) elements of k of an 8-bit (4-bit) row.
 
 __device__ __forceinline__ void copy16(uint32_t to, const uint8_t* from, bool in)      // zeros where `in` is false
@@ -211,6 +211,7 @@ __device__ __forceinline__ uint4 lds16(uint32_t at)
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
+
 // 16-row tiles of codes times eight tokens.  What a lane holds of a row lies at byte 16 t of the chunk's 64 bytes.
 template <int FMT, int TILES>
 struct Chunk {
@@ -233,6 +234,7 @@ struct Chunk {
             copy16(to + m * 1024 + 512, hi + (m * next + off), in);
         }
     }
+
     // acc += the tiles times the token pieces.  ORDERED: the tokens' values lie in the order of the widened pairs already.
     template <bool ORDERED, class X>
     static __device__ __forceinline__ void multiply(float (&acc)[TILES][4], uint32_t slot, int lane, const X& x, const uint32_t (&byte)[TILES][2])
@@ -366,14 +368,11 @@ __device__ __forceinline__ void wait_slot(int slots)         // all copies but t
 // alone); tokens go through L1, not through the copies (82 us: every SM asking L2 for the same few lines).  16 warps of up to
 // 128 registers; 20 or 24 warps of fewer gained nothing.
 
-template <class T, int FMT>
-using UpChunk = Chunk<FMT, kUpTiles>;
-
 template <class T, int FMT, int HPARTS>
 __global__ void __launch_bounds__(kUpTeams * kTeam * 32, 1)
 moe_up_kernel(const MoeArgs p, const int slots)
 {
-    using C = UpChunk<T, FMT>;
+    using C = Chunk<FMT, kUpTiles>;
     constexpr int TILES = kUpTiles;
     constexpr int bytes = C::bytes;
     extern __shared__ __align__(16) uint8_t s_ring[];
@@ -392,7 +391,7 @@ moe_up_kernel(const MoeArgs p, const int slots)
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + warp * slots * bytes;
 
     // A warp's sequence of chunks: units, groups of eight of the unit's tokens, turns.  It is followed three times: where the copies
-    // are, one turn ahead where the scale bytes are, and where the products are.
+    // are; one turn ahead, where the loads of scale bytes and BF16 tokens are; and where the products are.
     struct At {
         int unit, group, turn;
     };
@@ -425,7 +424,7 @@ moe_up_kernel(const MoeArgs p, const int slots)
     At soon = ahead;
     const uint8_t *s_lo = nullptr, *s_x = nullptr;
     bool s_live = false;
-    auto enter_scales = [&] {
+    auto enter_operands = [&] {
         if (soon.unit >= units) return;
         s_lo = p.up_s + row_of(soon.unit) * srow + (size_t)g * srow;
         const int pos = soon.unit / per_expert, first = ch.first[pos], cnt = ch.first[pos + 1] - first;
@@ -435,7 +434,7 @@ moe_up_kernel(const MoeArgs p, const int slots)
     uint32_t byte[TILES][2];
     TokenPiece<1, C::N> x_next;                              // (BF16 tokens)
     x_next.zero();
-    auto fetch_scales = [&] {
+    auto fetch_operands = [&] {
         if (soon.unit >= units) return;
         const uint32_t at = ((uint32_t)(soon.turn * kTeam + part) * 64 + t * 16) * (8 / C::W::bits);
         const uint8_t* s = s_lo + (at < H ? at >> p.block_shift : 0);
@@ -445,13 +444,13 @@ moe_up_kernel(const MoeArgs p, const int slots)
             byte[m][1] = ld_u8(s + half_s + m * 8 * srow);
         }
         if constexpr (T::size == 2) x_next.load(s_x + (at < H ? (size_t)at * 2 : 0), s_live, at < H);
-        if (step(soon)) enter_scales();
+        if (step(soon)) enter_operands();
     };
     At now = ahead;
     enter_copies();
-    enter_scales();
+    enter_operands();
     for (int i = 0; i < slots - 1; ++i) fetch(i);
-    fetch_scales();
+    fetch_operands();
     int slot = 0;
     while (now.unit < units) {
         const int pos = now.unit / per_expert, first = ch.first[pos], cnt = ch.first[pos + 1] - first, unit = now.unit, group = now.group;
@@ -470,7 +469,7 @@ moe_up_kernel(const MoeArgs p, const int slots)
                 scale[m][1] = byte[m][1];
             }
             const TokenPiece<1, C::N> x_now = x_next;
-            fetch_scales();
+            fetch_operands();
             if constexpr (T::size == 2) {
                 C::template multiply<false>(sum, at, lane, x_now, scale);
             } else {                                         // sums kept outside the matrix instruction, which truncates
@@ -516,9 +515,10 @@ moe_up_kernel(const MoeArgs p, const int slots)
 }
 
 // ---- kernel 2 ---------------------------------------------------------------------------------------------
-// A CTA covers 32 rows of the output for all tokens; where that makes few CTAs, a cluster of them covers the same rows.  The chunks of
-// all active experts, laid end to end, are shared out between the warps; a warp adds its weighted sums to its own copy of the tile, and the copies are added in order.  The first
-// chunks' codes are fetched before the wait for kernel 1.  (The same experts: 37 us for 117 MB; with 16 rows per CTA 46.)
+// A CTA covers 32 rows of the output for all tokens; where that makes few CTAs, a cluster of them covers the same rows.  The
+// chunks of all active experts, laid end to end, are shared out between the warps; a warp adds its weighted sums to its own
+// copy of the tile, and the copies are added in order, then the cluster's.  The first chunks' codes are fetched before the
+// wait for kernel 1.  (The same experts: 37 us for 117 MB; with 16 rows per CTA 46.)
 
 template <class T, int FMT, int HPARTS>
 __global__ void __launch_bounds__(kDownWarps * 32, 1)
@@ -540,8 +540,8 @@ moe_down_kernel(const MoeArgs p, const int slots, const int share)
     for (int i = lane; i < p.tokens * ROWS; i += 32) mine[i] = 0.f;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + warp * slots * bytes;
 
-    // A warp's sequence of chunks: its part of each expert's, for eight of the expert's tokens at a time; followed three times as in
-    // kernel 1.
+    // A warp's sequence of chunks: its part of each expert's, for eight of the expert's tokens at a time; followed three times as
+    // in kernel 1 (one turn ahead, h in the tokens' place).
     const int per_expert = (int)((irow + 63) / 64), total = ch.active * per_expert;
     const int begin = (int)((long long)total * (rank * WARPS + warp) / (share * WARPS)), end = (int)((long long)total * (rank * WARPS + warp + 1) / (share * WARPS));
     struct At {
@@ -573,7 +573,7 @@ moe_down_kernel(const MoeArgs p, const int slots, const int share)
         }
         copies_done();
     };
-    auto enter_scales = [&] {
+    auto enter_operands = [&] {
         if (soon.pos < 0) return;
         s_lo = p.down_s + ((size_t)ch.expert[soon.pos] * H + j0 + g) * srow;
         const int first = ch.first[soon.pos], cnt = ch.first[soon.pos + 1] - first;
@@ -583,7 +583,7 @@ moe_down_kernel(const MoeArgs p, const int slots, const int share)
     uint32_t byte[TILES][2] = {};
     TokenPiece<HPARTS, C::N> x_next;
     x_next.zero();
-    auto fetch_scales = [&] {
+    auto fetch_operands = [&] {
         if (soon.pos < 0) return;
         const uint32_t at = ((uint32_t)soon.c * 64 + t * 16) * (8 / C::W::bits);
         const uint8_t* s = s_lo + (at < I ? at >> p.block_shift : 0);
@@ -592,14 +592,14 @@ moe_down_kernel(const MoeArgs p, const int slots, const int share)
 #pragma unroll
             for (int h = 0; h < 2; ++h) byte[m][h] = ld_u8(s + (uint32_t)(m * 16 + h * 8) * srow);
         x_next.load(s_h + (at < I ? (size_t)at * 2 : 0), s_live, at < I, plane);
-        if (step(soon)) enter_scales();
+        if (step(soon)) enter_operands();
     };
     // the first slots' codes before the wait for kernel 1
     enter_copies();
     for (int i = 0; i < slots - 1; ++i) fetch(i);
     pdl_acquire();
-    enter_scales();
-    fetch_scales();
+    enter_operands();
+    fetch_operands();
     int slot = 0;
     while (now.pos >= 0) {
         const int first = ch.first[now.pos], cnt = ch.first[now.pos + 1] - first, chunks = now.hi - now.lo, group = now.group;
@@ -615,7 +615,7 @@ moe_down_kernel(const MoeArgs p, const int slots, const int share)
                 scale[m][1] = byte[m][1];
             }
             const TokenPiece<HPARTS, C::N> x = x_next;
-            fetch_scales();
+            fetch_operands();
             if constexpr (T::size == 2) {
                 C::template multiply<true>(sum, at, lane, x, scale);
             } else {
@@ -684,7 +684,7 @@ int run(const MoeArgs& p, cudaStream_t stream)
     auto up = moe_up_kernel<T, FMT, h_parts(T::id)>;
     constexpr int kUpWarps = kUpTeams * kTeam;
     constexpr size_t kUpStatic = sizeof(Choice) + (size_t)kUpWarps * kUpTiles * 512 + 64;
-    constexpr int up_bytes = UpChunk<T, FMT>::bytes;
+    constexpr int up_bytes = Chunk<FMT, kUpTiles>::bytes;
     if (int rc = allow_smem(reinterpret_cast<const void*>(up), kShared - kUpStatic, done)) return rc;
     const size_t most = (size_t)p.tokens * p.top_k < (size_t)p.experts ? (size_t)p.tokens * p.top_k : (size_t)p.experts;
     const size_t units = most * (p.inner / (8 * kUpTiles)), ctas = (units + kUpTeams - 1) / kUpTeams;
