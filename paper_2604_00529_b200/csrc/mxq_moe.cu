@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kMaxTokens = MXQ_MOE_TOKENS_MAX, kMaxExperts = MXQ_MOE_EXPERTS_MAX, kMaxTopK = MXQ_MOE_TOP_K_MAX;
 constexpr int kTeam = 4, kUpTeams = 4;  // kernel 1: warps of a team, teams of a CTA
+constexpr int kUpWarps = kTeam * kUpTeams;
 constexpr int kUpTiles = 2;             // 16-row tiles of a team's unit: eight rows of the gate and eight of the up half each
 constexpr int kDownWarps = 16;          // kernel 2: warps of a CTA
 constexpr int kDownTiles = 2;           // 16-row tiles of its rows of the output
@@ -362,24 +363,30 @@ __device__ __forceinline__ void wait_slot(int slots)         // all copies but t
 
 // ---- kernel 1 ---------------------------------------------------------------------------------------------
 // One CTA per SM, of four teams of four warps.  A team works on units of 32 rows, 16 of the gate and the 16 of the up half that go
-// with them, of one expert, for eight of its tokens at a time; its warps share k out and meet in shared memory.  In a 16-row tile
-// the first eight rows are the gate's and the last eight the up half's.  A warp's copies run on into its next unit.
-// Bound by instructions: one token, two of eight 4096 x 14336 E4M3 experts 67 us for 235 MB (57 without the widening, 46 with the copies
-// alone); tokens go through L1, not through the copies (82 us: every SM asking L2 for the same few lines).  16 warps of up to
-// 128 registers; 20 or 24 warps of fewer gained nothing.
+// with them, of one expert, for eight of its tokens at a time; its warps share k out and meet in shared memory, once per unit (in
+// two sets of sums in turn).  In a 16-row tile the first eight rows are the gate's and the last eight the up half's.  Units go
+// to the CTAs' first teams before their second ones, so that few of them are on many SMs (256 units of 4096: both kernels 25 us;
+// four at a time 31).  A warp's copies run on into its next unit.
+// Bound by instructions: one token, two of eight 4096 x 14336 E4M3 experts 65 us for 235 MB (67 us when tried: 57 without the
+// widening, 46 with the copies alone; about 6 of them for the last 16 of 1792 units, which 592 teams share.  The whole CTA on each
+// of those saved 3 us there and cost other shapes 0.3 to 0.6; teams of 8 or 16 for all units cost 5 and 16 us).  Tokens go through
+// L1, not through the copies (82 us: every SM asking L2 for the same few lines).  Asking for a unit's scales as early as for its
+// codes, 20 or 24 warps of fewer registers: nothing gained.
 
 template <class T, int FMT, int HPARTS>
-__global__ void __launch_bounds__(kUpTeams * kTeam * 32, 1)
+__global__ void __launch_bounds__(kUpWarps * 32, 1)
 moe_up_kernel(const MoeArgs p, const int slots)
 {
     using C = Chunk<FMT, kUpTiles>;
     constexpr int TILES = kUpTiles;
     constexpr int bytes = C::bytes;
-    extern __shared__ __align__(16) uint8_t s_ring[];
+    extern __shared__ __align__(16) uint8_t s_ring[];        // the warps' slots, then two sets of the warps' sums
     __shared__ Choice ch;
-    __shared__ float s_sum[kUpTeams][kTeam][TILES][4][32];
+    using Sums = float[TILES][4][32];
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int team = warp / kTeam, part = warp % kTeam;
+    Sums* sums = reinterpret_cast<Sums*>(s_ring + kUpWarps * slots * bytes) + team * kTeam;      // this unit's, of the team
+    int other = kUpWarps;                                    // the other set lies there
     pdl_acquire();
     pdl_release();                                           // after the wait: kernel 2 may read the logits at once
     choose(p, ch);
@@ -488,7 +495,7 @@ moe_up_kernel(const MoeArgs p, const int slots)
 #pragma unroll
         for (int m = 0; m < TILES; ++m)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s_sum[team][part][m][j][lane] = sum[m][j];
+            for (int j = 0; j < 4; ++j) sums[part][m][j][lane] = sum[m][j];
         asm volatile("bar.sync %0, %1;" :: "r"(1 + team), "n"(kTeam * 32) : "memory");
         // row r of the gate and of the up half, token c: elements (c & 1) and 2 + (c & 1) of lane r * 4 + c / 2
         for (int o = part * 32 + lane; o < TILES * 64; o += kTeam * 32) {
@@ -497,8 +504,8 @@ moe_up_kernel(const MoeArgs p, const int slots)
             float gate = 0.f, lift = 0.f;
 #pragma unroll
             for (int w = 0; w < kTeam; ++w) {
-                gate += s_sum[team][w][m][c & 1][ln];
-                lift += s_sum[team][w][m][2 + (c & 1)][ln];
+                gate += sums[w][m][c & 1][ln];
+                lift += sums[w][m][2 + (c & 1)][ln];
             }
             const float h = gate / (1.f + expf(-gate)) * lift;
             uint32_t hp[HPARTS];
@@ -507,7 +514,8 @@ moe_up_kernel(const MoeArgs p, const int slots)
 #pragma unroll
             for (int q = 0; q < HPARTS; ++q) st_u16(to + q * plane, hp[q]);
         }
-        asm volatile("bar.sync %0, %1;" :: "r"(1 + team), "n"(kTeam * 32) : "memory");
+        sums += other;                                       // (what the team reads now is written again after its next meeting)
+        other = -other;
         now.turn = turns - 1;
         step(now);
     }
@@ -682,14 +690,13 @@ int run(const MoeArgs& p, cudaStream_t stream)
 {
     static std::atomic<uint64_t> done{0};
     auto up = moe_up_kernel<T, FMT, h_parts(T::id)>;
-    constexpr int kUpWarps = kUpTeams * kTeam;
-    constexpr size_t kUpStatic = sizeof(Choice) + (size_t)kUpWarps * kUpTiles * 512 + 64;
+    constexpr size_t kUpStatic = sizeof(Choice) + 64, kUpSums = (size_t)2 * kUpWarps * kUpTiles * 512;
     constexpr int up_bytes = Chunk<FMT, kUpTiles>::bytes;
     if (int rc = allow_smem(reinterpret_cast<const void*>(up), kShared - kUpStatic, done)) return rc;
     const size_t most = (size_t)p.tokens * p.top_k < (size_t)p.experts ? (size_t)p.tokens * p.top_k : (size_t)p.experts;
-    const size_t units = most * (p.inner / (8 * kUpTiles)), ctas = (units + kUpTeams - 1) / kUpTeams;
-    const int up_slots = slots_for(kShared - kUpStatic, kUpWarps, up_bytes);
-    if (int rc = launch_grid(up, dim3((unsigned)(ctas < 148 ? ctas : 148)), kUpWarps * 32, (size_t)kUpWarps * up_slots * up_bytes, 1, stream, p, up_slots))
+    const size_t units = most * (p.inner / (8 * kUpTiles));    // as many CTAs as may have one
+    const int up_slots = slots_for(kShared - kUpStatic - kUpSums, kUpWarps, up_bytes);
+    if (int rc = launch_grid(up, dim3((unsigned)(units < 148 ? units : 148)), kUpWarps * 32, (size_t)kUpWarps * up_slots * up_bytes + kUpSums, 1, stream, p, up_slots))
         return rc;
     static std::atomic<uint64_t> down_done{0};
     auto down = moe_down_kernel<T, FMT, h_parts(T::id)>;
