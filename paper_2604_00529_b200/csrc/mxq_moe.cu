@@ -254,14 +254,22 @@ struct Chunk {
     // WIDE: some scale is beyond what one BF16 factor holds
     template <bool ORDERED, bool WIDE, class X>
     static __device__ __forceinline__ void products(float (&acc)[TILES][4], uint32_t slot, int lane, const X& x, const uint32_t (&byte)[TILES][2],
-                                                    const uint32_t (&f)[TILES][2])
+                                                    uint32_t (&f)[TILES][2])
     {
         constexpr int NP = W::NP;
         uint4 c[TILES][2];
 #pragma unroll
         for (int m = 0; m < TILES; ++m)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) c[m][h] = lds16(slot + (m * 2 + h) * 512 + lane * 16);
+            for (int h = 0; h < 2; ++h) {
+                c[m][h] = lds16(slot + (m * 2 + h) * 512 + lane * 16);
+                uint32_t seen = 0;
+                W::note_nan(c[m][h].x, seen);
+                W::note_nan(c[m][h].y, seen);
+                W::note_nan(c[m][h].z, seen);
+                W::note_nan(c[m][h].w, seen);
+                f[m][h] = W::factor_or_nan(f[m][h], seen);
+            }
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             uint32_t b[X::PARTS][NP];

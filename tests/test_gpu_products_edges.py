@@ -1,0 +1,65 @@
+"""The operators that multiply by stored codes where the values, addresses and derivatives are unusual: against their definitions in
+64 bits (product_util)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_00529_b200 as mxq
+import paper_2604_00529_b200.binding  # noqa: F401
+
+import product_util as pu
+
+pytestmark = pytest.mark.gpu
+BF, FP = torch.bfloat16, torch.float32
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+# ---- E4M3's NaN codes -----------------------------------------------------------------------------------------
+
+
+def e4m3_values(codes, scales, block):
+    """Values in 64 bits, S.1111.111 a NaN."""
+    v = pu.values64(codes.astype(np.int64), scales.astype(np.int64), "e4m3", block)
+    return np.where((codes & 0x7F) == 0x7F, np.nan, v)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_moe_weights_that_are_nan_codes(dtype):
+    """One token per expert, one NaN code in most experts: at each of a lane's 16 places, of either sign, in up or in down matrices.  A NaN
+    in an up matrix makes all of the token NaN, one in a down matrix the element of its row; every other code is a number."""
+    rng = np.random.default_rng(5)
+    t, e, hidden, inner, block = 40, 41, 256, 64, 32
+    up = rng.integers(0, 256, (e, 2 * inner, hidden)).astype(np.uint8)
+    down = rng.integers(0, 256, (e, hidden, inner)).astype(np.uint8)
+    up[(up & 0x7F) == 0x7F] ^= 1                            # all codes, the NaN codes aside
+    down[(down & 0x7F) == 0x7F] ^= 1
+    for i in range(16):
+        up[i, (37 * i) % (2 * inner), 16 * ((5 * i) % 16) + i] = 0x7F | (i & 1) << 7
+        down[16 + i, (53 * i) % hidden, 16 * (i % 4) + i] = 0x7F | (~i & 1) << 7
+    up[40], down[40] = 0x7F, 0xFF                           # the expert that nobody chooses
+    us = rng.integers(110, 118, (e, 2 * inner, hidden // block)).astype(np.uint8)
+    ds = rng.integers(110, 118, (e, hidden, inner // block)).astype(np.uint8)
+    x = torch.from_numpy(rng.standard_normal((t, hidden)).astype(np.float32)).cuda().to(dtype)
+    lg = np.full((t, e), -np.inf, np.float32)
+    lg[np.arange(t), np.arange(t)] = 1.0
+    got = mxq.moe(x, dev(lg), dev(up), dev(us), dev(down), dev(ds), inner, 1, "e4m3", block)
+    want, bound = pu.moe64(pu.to64(x), lg, e4m3_values(up, us, block), e4m3_values(down, ds, block), inner, 1, True, dtype)
+    assert np.isnan(want[:16]).all() and (np.isnan(want[16:32]).sum(1) == 1).all() and not np.isnan(want[32:]).any()
+    pu.check(got, want, bound)
+
+
+@pytest.mark.parametrize("m", [2, 40, 300])
+def test_matmul_operands_that_are_nan_codes(m):
+    rng = np.random.default_rng(m)
+    n, k, block = 130, 256, 64
+    a, b = (rng.integers(0, 256, (r, k)).astype(np.uint8) for r in (m, n))
+    for c in (a, b):
+        c[(c & 0x7F) == 0x7F] ^= 1
+    a[m // 2, 77], b[n // 3, 200] = 0x7F, 0xFF
+    sa, sb = (rng.integers(110, 118, (r, k // block)).astype(np.uint8) for r in (m, n))
+    av, bv = e4m3_values(a, sa, block), e4m3_values(b, sb, block)
+    got = mxq.matmul(dev(a), dev(sa), dev(b), dev(sb), m, n, k, block=block, dtype=FP)
+    pu.check(got, av @ bv.T, pu.sum_bound(k, np.abs(av) @ np.abs(bv).T))
