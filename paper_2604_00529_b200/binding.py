@@ -746,6 +746,12 @@ def _up(v: int, block: int) -> int:
     return -(-v // block) * block
 
 
+def _placed(t: torch.Tensor) -> torch.Tensor:
+    """t, contiguous and at an address that the kernels take, a multiple of 32: itself where it is both already."""
+    t = t.contiguous()
+    return t.clone(memory_format=torch.contiguous_format) if t.data_ptr() % 32 else t
+
+
 class _LinearSTE(torch.autograd.Function):
     """y = Q(x) Q(w)^T; backward dx = Q(dy) Q(w^T)^T and dw = Q(dy^T) Q(x^T)^T, the quantizers passed straight through."""
 
@@ -753,8 +759,8 @@ class _LinearSTE(torch.autograd.Function):
     def forward(ctx, x, w, block):
         m, k, n = x.shape[0], x.shape[1], w.shape[0]
         need_x, need_w = ctx.needs_input_grad[:2]
-        xc, xs, xct, xst = quantize_matrix(x, "e4m3", block, cols=need_w)
-        wc, ws, wct, wst = quantize_matrix(w, "e4m3", block, cols=need_x)
+        xc, xs, xct, xst = quantize_matrix(_placed(x), "e4m3", block, cols=need_w)
+        wc, ws, wct, wst = quantize_matrix(_placed(w), "e4m3", block, cols=need_x)
         ctx.save_for_backward(xct, xst, wct, wst)
         ctx.sizes, ctx.block, ctx.dtypes = (m, n, k), block, (x.dtype, w.dtype)
         return matmul(xc, xs, wc, ws, m, n, _up(k, block), "e4m3", block, x.dtype)
@@ -765,7 +771,7 @@ class _LinearSTE(torch.autograd.Function):
         xct, xst, wct, wst = ctx.saved_tensors
         (m, n, k), block = ctx.sizes, ctx.block
         need_x, need_w = ctx.needs_input_grad[:2]
-        dc, ds, dct, dst = quantize_matrix(dy.contiguous(), "e4m3", block, rows=need_x, cols=need_w)
+        dc, ds, dct, dst = quantize_matrix(_placed(dy), "e4m3", block, rows=need_x, cols=need_w)
         dx = matmul(dc, ds, wct, wst, m, k, _up(n, block), "e4m3", block, ctx.dtypes[0]) if need_x else None
         dw = matmul(dct, dst, xct, xst, n, k, _up(m, block), "e4m3", block, ctx.dtypes[1]) if need_w else None
         return dx, dw, None
@@ -774,8 +780,9 @@ class _LinearSTE(torch.autograd.Function):
 def linear_ste(x: torch.Tensor, w: torch.Tensor, block: int = 32) -> torch.Tensor:
     """A linear layer whose three products run on MXFP8 E4M3 operands, differentiable: y = Q(x) Q(w)^T for x [..., k] and
     w [n, k] (float32 or bfloat16), with dx = Q(dy) Q(w^T)^T and dw = Q(dy^T) Q(x^T)^T, each operand quantized in blocks
-    along the dimension that its product sums over and the quantizers passed straight through.  Any sizes; y and dx have x's type,
-    dw has w's.  The backward pass keeps the transposes' codes (a byte per element), not x and w."""
+    along the dimension that its product sums over and the quantizers passed straight through.  Any sizes, strides and offsets (what
+    is not contiguous at an address that is a multiple of 32 is copied first); y and dx have x's type, dw has w's.  The backward pass
+    keeps the transposes' codes (a byte per element), not x and w."""
     if _lib is None:
         load_library()
     made = _host.linear_ste(x, w, block)
@@ -789,7 +796,7 @@ def linear_ste(x: torch.Tensor, w: torch.Tensor, block: int = 32) -> torch.Tenso
         _dtype_id(t)
         if not t.is_cuda or t.device != x.device:
             raise ValueError("%s must be a CUDA tensor on x's device (libmxq has no CPU path)" % what)
-    y = _LinearSTE.apply(x.reshape(-1, x.shape[-1]).contiguous(), w.contiguous(), block)
+    y = _LinearSTE.apply(x.reshape(-1, x.shape[-1]), w, block)
     return y.view(*x.shape[:-1], w.shape[0])
 
 

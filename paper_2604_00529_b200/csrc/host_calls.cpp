@@ -597,6 +597,13 @@ PyObject* moe(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
+// A contiguous tensor at an address that the kernels take, a multiple of 32: itself, or a copy where it is a view that begins elsewhere (a
+// slice, a parameter in a flat buffer, the gradient of an output that went through cat).
+at::Tensor placed(const at::Tensor& t)
+{
+    return reinterpret_cast<uintptr_t>(t.data_ptr()) % 32 ? t.clone(at::MemoryFormat::Contiguous) : t;
+}
+
 // y = Q(x) Q(w)^T with dx = Q(dy) Q(w^T)^T and dw = Q(dy^T) Q(x^T)^T: what _LinearSTE of binding.py does, for x [..., k] and w [n, k].
 struct LinearSTE : torch::autograd::Function<LinearSTE> {
     static int64_t up(int64_t v, int64_t block) { return (v + block - 1) / block * block; }
@@ -616,8 +623,8 @@ struct LinearSTE : torch::autograd::Function<LinearSTE> {
         dtype_id(x, &xt);
         dtype_id(w, &wt);
         MatrixCodes qx, qw;
-        if (qx.make(x, xt, m, k, MXQ_FP8_E4M3, (int)block, true, need_w) != MXQ_OK) throw NotPlain{};
-        if (qw.make(w, wt, n, k, MXQ_FP8_E4M3, (int)block, true, need_x) != MXQ_OK) throw NotPlain{};
+        if (qx.make(placed(x), xt, m, k, MXQ_FP8_E4M3, (int)block, true, need_w) != MXQ_OK) throw NotPlain{};
+        if (qw.make(placed(w), wt, n, k, MXQ_FP8_E4M3, (int)block, true, need_x) != MXQ_OK) throw NotPlain{};
         std::vector<int64_t> sizes = x.sizes().vec();
         sizes.back() = n;
         at::Tensor y = at::empty(sizes, x.options());
@@ -644,10 +651,10 @@ struct LinearSTE : torch::autograd::Function<LinearSTE> {
         const bool twice = at::GradMode::is_enabled() && grads[0].requires_grad();
         {
             at::NoGradGuard no_grad;
-            const at::Tensor dy = grads[0].contiguous();
             int dt = 0;
-            TORCH_CHECK_TYPE(dtype_id(dy, &dt), "mxq tensors are float32 or bfloat16, got ", dy.scalar_type());
-            TORCH_CHECK_VALUE(dy.is_cuda(), "the gradient must be a CUDA tensor (libmxq has no CPU path)");
+            TORCH_CHECK_TYPE(dtype_id(grads[0], &dt), "mxq tensors are float32 or bfloat16, got ", grads[0].scalar_type());
+            TORCH_CHECK_VALUE(grads[0].is_cuda(), "the gradient must be a CUDA tensor (libmxq has no CPU path)");
+            const at::Tensor dy = placed(grads[0].contiguous());
             MatrixCodes q;
             int rc = q.make(dy, dt, m, n, MXQ_FP8_E4M3, (int)block, need_x, need_w);
             if (rc != MXQ_OK) throw_mxq_error(rc, "mxq_quantize_matrix");

@@ -63,3 +63,57 @@ def test_matmul_operands_that_are_nan_codes(m):
     av, bv = e4m3_values(a, sa, block), e4m3_values(b, sb, block)
     got = mxq.matmul(dev(a), dev(sa), dev(b), dev(sb), m, n, k, block=block, dtype=FP)
     pu.check(got, av @ bv.T, pu.sum_bound(k, np.abs(av) @ np.abs(bv).T))
+
+
+# ---- linear_ste -----------------------------------------------------------------------------------------------
+
+
+@pytest.fixture(params=[True, False], ids=["native", "general"])
+def path(request, monkeypatch):
+    """Both ways a linear_ste call can go: the binding's native code, and the Python code behind it."""
+    if not request.param:
+        mxq.load_library()
+        monkeypatch.setattr(mxq.binding._host, "linear_ste", lambda *a: None)
+
+
+def offset_copy(t, elements):
+    """t's values in a contiguous view that begins `elements` elements into its storage."""
+    flat = torch.empty(t.numel() + elements, device=t.device, dtype=t.dtype)
+    v = flat[elements:].view(t.shape)
+    v.copy_(t)
+    assert v.is_contiguous() and v.data_ptr() % 32
+    return v
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("m,n,k", [(9, 33, 37), (40, 64, 96)])
+def test_linear_ste_at_any_address(path, m, n, k, dtype):
+    """Operands and gradients that are contiguous at addresses of no particular alignment: the bits of the aligned ones."""
+    g = torch.Generator(device="cuda").manual_seed(m)
+    x, w, dy = (torch.randn(*s, generator=g, device="cuda").to(dtype) for s in ((m, k), (n, k), (m, n)))
+    xa, wa = x.clone().requires_grad_(), w.clone().requires_grad_()
+    want = mxq.linear_ste(xa, wa)
+    want = [want.detach(), *torch.autograd.grad(want, (xa, wa), dy)]
+    for off in ((1, 0, 0), (0, 3, 0), (0, 0, 1), (5, 7, 3)):
+        xo, wo, go = (offset_copy(t, o) if o else t.clone() for t, o in zip((x, w, dy), off))
+        xo.requires_grad_(), wo.requires_grad_()
+        y = mxq.linear_ste(xo, wo)
+        for a, b in zip([y.detach(), *torch.autograd.grad(y, (xo, wo), go)], want):
+            assert torch.equal(a, b)
+
+
+def test_linear_ste_of_slices_and_joined_outputs(path):
+    """x[1:] of an odd width, a weight inside a flat parameter buffer, outputs joined by cat: the gradients arrive as views at offsets."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(8, 37, generator=g, device="cuda", dtype=BF)
+    flat = torch.randn(1 + 1000 * 37, generator=g, device="cuda").to(BF).requires_grad_()
+    w = flat[1:].view(1000, 37)
+    dy = torch.randn(7 + 333, 1000, generator=g, device="cuda").to(BF)
+    other = torch.randn(333, 37, generator=g, device="cuda", dtype=BF)
+    joined = torch.cat((mxq.linear_ste(other, w), mxq.linear_ste(x[1:], w)))
+    (got,) = torch.autograd.grad(joined, flat, dy)
+    w2 = flat.detach()[1:].clone().view(1000, 37).requires_grad_()
+    y1, y2 = mxq.linear_ste(other, w2), mxq.linear_ste(x[1:].clone(), w2)
+    assert torch.equal(joined, torch.cat((y1, y2)))
+    (want,) = torch.autograd.grad((y1, y2), w2, (dy[:333].clone(), dy[333:].clone()))
+    assert torch.equal(got[1:].view(1000, 37), want) and got[0] == 0
