@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import importlib.util
+import math
 import os
 import struct
 from typing import Optional, Sequence, Tuple
@@ -796,7 +797,7 @@ def linear_ste(x: torch.Tensor, w: torch.Tensor, block: int = 32) -> torch.Tenso
         _dtype_id(t)
         if not t.is_cuda or t.device != x.device:
             raise ValueError("%s must be a CUDA tensor on x's device (libmxq has no CPU path)" % what)
-    y = _LinearSTE.apply(x.reshape(-1, x.shape[-1]), w, block)
+    y = _LinearSTE.apply(x.reshape(math.prod(x.shape[:-1]), x.shape[-1]), w, block)
     return y.view(*x.shape[:-1], w.shape[0])
 
 

@@ -117,3 +117,14 @@ def test_linear_ste_of_slices_and_joined_outputs(path):
     assert torch.equal(joined, torch.cat((y1, y2)))
     (want,) = torch.autograd.grad((y1, y2), w2, (dy[:333].clone(), dy[333:].clone()))
     assert torch.equal(got[1:].view(1000, 37), want) and got[0] == 0
+
+
+@pytest.mark.parametrize("shape,n", [((5, 0), 3), ((0,), 4), ((2, 3, 0), 5), ((0, 0), 3), ((4, 7), 0), ((2, 0, 7), 0)])
+def test_linear_ste_without_any_products(path, shape, n):
+    """Empty sums are zeros; empty results have their shapes."""
+    x = torch.randn(shape, device="cuda", requires_grad=True)
+    w = torch.randn(n, shape[-1], device="cuda", requires_grad=True)
+    y = mxq.linear_ste(x, w)
+    assert y.shape == (*shape[:-1], n) and not y.any()
+    dx, dw = torch.autograd.grad(y, (x, w), torch.ones_like(y))
+    assert dx.shape == x.shape and dw.shape == w.shape and not dx.any() and not dw.any()
