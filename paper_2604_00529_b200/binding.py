@@ -753,6 +753,18 @@ def _placed(t: torch.Tensor) -> torch.Tensor:
     return t.clone(memory_format=torch.contiguous_format) if t.data_ptr() % 32 else t
 
 
+class _Once(torch.autograd.Function):
+    """The gradients of a layer that has no second derivative: themselves, and an error where they are differentiated."""
+
+    @staticmethod
+    def forward(ctx, *grads):
+        return tuple(None if g is None else g.clone() for g in grads)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("linear_ste can be differentiated once only")
+
+
 class _LinearSTE(torch.autograd.Function):
     """y = Q(x) Q(w)^T; backward dx = Q(dy) Q(w^T)^T and dw = Q(dy^T) Q(x^T)^T, the quantizers passed straight through."""
 
@@ -767,14 +779,16 @@ class _LinearSTE(torch.autograd.Function):
         return matmul(xc, xs, wc, ws, m, n, _up(k, block), "e4m3", block, x.dtype)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         xct, xst, wct, wst = ctx.saved_tensors
         (m, n, k), block = ctx.sizes, ctx.block
         need_x, need_w = ctx.needs_input_grad[:2]
-        dc, ds, dct, dst = quantize_matrix(_placed(dy), "e4m3", block, rows=need_x, cols=need_w)
-        dx = matmul(dc, ds, wct, wst, m, k, _up(n, block), "e4m3", block, ctx.dtypes[0]) if need_x else None
-        dw = matmul(dct, dst, xct, xst, n, k, _up(m, block), "e4m3", block, ctx.dtypes[1]) if need_w else None
+        with torch.no_grad():
+            dc, ds, dct, dst = quantize_matrix(_placed(dy), "e4m3", block, rows=need_x, cols=need_w)
+            dx = matmul(dc, ds, wct, wst, m, k, _up(n, block), "e4m3", block, ctx.dtypes[0]) if need_x else None
+            dw = matmul(dct, dst, xct, xst, n, k, _up(m, block), "e4m3", block, ctx.dtypes[1]) if need_w else None
+        if torch.is_grad_enabled():         # (create_graph: dx depends on w, dw on x, even for a constant dy)
+            dx, dw = _Once.apply(*[None if g is None else g.requires_grad_() for g in (dx, dw)])
         return dx, dw, None
 
 
@@ -783,7 +797,8 @@ def linear_ste(x: torch.Tensor, w: torch.Tensor, block: int = 32) -> torch.Tenso
     w [n, k] (float32 or bfloat16), with dx = Q(dy) Q(w^T)^T and dw = Q(dy^T) Q(x^T)^T, each operand quantized in blocks
     along the dimension that its product sums over and the quantizers passed straight through.  Any sizes, strides and offsets (what
     is not contiguous at an address that is a multiple of 32 is copied first); y and dx have x's type, dw has w's.  The backward pass
-    keeps the transposes' codes (a byte per element), not x and w."""
+    keeps the transposes' codes (a byte per element), not x and w.  There is no second derivative: gradients taken with create_graph raise
+    where they are differentiated."""
     if _lib is None:
         load_library()
     made = _host.linear_ste(x, w, block)

@@ -648,7 +648,6 @@ struct LinearSTE : torch::autograd::Function<LinearSTE> {
         const bool need_x = saved[2].defined() && ctx->needs_input_grad(0), need_w = saved[0].defined() && ctx->needs_input_grad(1);
         torch::autograd::variable_list out(5);
         if (!grads[0].defined() || !(need_x || need_w)) return out;
-        const bool twice = at::GradMode::is_enabled() && grads[0].requires_grad();
         {
             at::NoGradGuard no_grad;
             int dt = 0;
@@ -669,7 +668,11 @@ struct LinearSTE : torch::autograd::Function<LinearSTE> {
                 if (rc != MXQ_OK) throw_mxq_error(rc, "mxq_matmul");
             }
         }
-        if (twice) {                       // the quantizers have no second derivative: say so where one is asked for
+        // The quantizers have no second derivative, and dx depends on w, dw on x, even for a constant dy: what a pass with a graph
+        // of its own (create_graph) returns says so where it is differentiated.
+        if (at::GradMode::is_enabled()) {
+            for (const at::Tensor& t : out)
+                if (t.defined()) t.set_requires_grad(true);
             const auto refuse = std::make_shared<torch::autograd::DelayedError>("linear_ste can be differentiated once only", 5);
             return (*refuse)(std::move(out));
         }

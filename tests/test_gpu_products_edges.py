@@ -128,3 +128,26 @@ def test_linear_ste_without_any_products(path, shape, n):
     assert y.shape == (*shape[:-1], n) and not y.any()
     dx, dw = torch.autograd.grad(y, (x, w), torch.ones_like(y))
     assert dx.shape == x.shape and dw.shape == w.shape and not dx.any() and not dw.any()
+
+
+def test_linear_ste_gradients_refuse_to_be_differentiated(path):
+    """Also where the incoming gradient is a constant: dx depends on w and dw on x all the same."""
+    x = torch.randn(4, 32, device="cuda", requires_grad=True)
+    w = torch.randn(8, 32, device="cuda", requires_grad=True)
+    plain = torch.autograd.grad(mxq.linear_ste(x, w).sum(), (x, w))
+    for loss in (lambda y: y.sum(), lambda y: y.square().sum()):
+        for leaves in ((x,), (w,), (x, w)):
+            y = mxq.linear_ste(x, w)
+            grads = torch.autograd.grad(loss(y), leaves, create_graph=True)
+            penalty = sum(g.square().sum() for g in grads)
+            with pytest.raises(RuntimeError, match="differentiated once"):
+                (loss(y) + penalty).backward()
+    x.grad = w.grad = None
+    mxq.linear_ste(x, w).sum().backward(create_graph=True)     # gradients that nobody differentiates are the usual ones
+    assert torch.equal(x.grad, plain[0]) and torch.equal(w.grad, plain[1])
+    with pytest.raises(RuntimeError, match="differentiated once"):
+        x.grad.square().sum().backward()
+    x.grad, w.grad = x.grad.detach(), w.grad.detach()
+    mxq.linear_ste(x, w).sum().backward()
+    assert torch.equal(x.grad, 2 * plain[0]) and torch.equal(w.grad, 2 * plain[1])
+    assert not any(g.requires_grad for g in torch.autograd.grad(mxq.linear_ste(x, w).sum(), (x, w)))
