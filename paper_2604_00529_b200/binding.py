@@ -681,7 +681,9 @@ class _Place:
 
     def __enter__(self):
         if self.stream is not None:
-            s = self.stream if hasattr(self.stream, "cuda_stream") else torch.cuda.ExternalStream(int(self.stream), device=self.device)
+            s = self.stream
+            if not hasattr(s, "cuda_stream"):   # a handle; torch has no stream of the handle 1 (cudaStreamLegacy), which is the default one
+                s = torch.cuda.ExternalStream(0 if int(s) == 1 else int(s), device=self.device)
             if s.device != self.device:
                 raise ValueError("the stream is on %s, the tensors on %s" % (s.device, self.device))
             self.inner = torch.cuda.stream(s)

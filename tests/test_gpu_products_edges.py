@@ -151,3 +151,19 @@ def test_linear_ste_gradients_refuse_to_be_differentiated(path):
     mxq.linear_ste(x, w).sum().backward()
     assert torch.equal(x.grad, 2 * plain[0]) and torch.equal(w.grad, 2 * plain[1])
     assert not any(g.requires_grad for g in torch.autograd.grad(mxq.linear_ste(x, w).sum(), (x, w)))
+
+
+# ---- streams --------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("handle", [0, 1, 2])
+def test_streams_given_as_the_fixed_handles(handle):
+    """The default stream, cudaStreamLegacy and cudaStreamPerThread."""
+    x = torch.randn(96, 160, device="cuda")
+    want = mxq.quantize_matrix(x)
+    torch.cuda.synchronize()
+    got = mxq.quantize_matrix(x, stream=handle)
+    d = mxq.matmul(got[0], got[1], got[0], got[1], 96, 96, 160, stream=handle)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(d, mxq.matmul(*want[:2], *want[:2], 96, 96, 160))
