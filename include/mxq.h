@@ -102,6 +102,9 @@ const char *mxq_status_string(int status);
  *   mxq_debug_trim_ranges test hook: from now on this thread registers every range `bytes` short, so
  *                         that the checker can be seen to catch the kernels' (legitimate) last accesses
  *                         without any access leaving its real buffer.  Returns 1 in a debug build, 0 otherwise.
+ *   mxq_debug_wait        test hook: one warp waits as the kernels of mxq_matmul do, for at most `milliseconds` (up to 1000, MXQ_ERR_SIZE),
+ *                         its even lanes for something that has happened, its odd ones for something that never does; `lanes` gets a
+ *                         bit for each lane that went on.  Waits for the device.  Returns 1 in a debug build, 0 otherwise.
  */
 typedef struct mxq_debug_info {
     int enabled;                      /* 1: the library was built with -DMXQ_DEBUG */
@@ -113,6 +116,7 @@ typedef struct mxq_debug_info {
 
 int mxq_debug_report(mxq_debug_info *out, int reset);
 int mxq_debug_trim_ranges(size_t bytes);
+int mxq_debug_wait(unsigned int milliseconds, unsigned int *lanes);
 
 /* Bits per element code of `fmt`, or 0 for an unknown format. */
 int mxq_format_bits(int fmt);

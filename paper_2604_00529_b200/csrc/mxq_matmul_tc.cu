@@ -228,8 +228,8 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
             tile_at(t, p.tiles_l, p.tiles_r, tl, tr);
             const int yl = (int)(tl * (kRowsL * CG) + rank * kRowsL), yr = (int)(tr * BN + rank * S::rows_r);
             for (uint32_t kt = k_lo; ok && kt < k_hi; ++kt, advance()) {
-                if (!(ok = wait(s_empty[stage], phase ^ 1))) break;
-                if (elect_one()) {
+                ok = wait(s_empty[stage], phase ^ 1);
+                if (elect_one() && ok) {
                     uint32_t bar = smem_addr(&s_full[stage]);
                     const uint32_t at = base + stage * S::stage;
                     if (rank == 0) mbar_expect(bar, CG * (S::bytes_l + S::bytes_r));
@@ -237,7 +237,7 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
                     tma_tile<CG>(at, &map_l, (int)(kt * kTileK), yl, bar);
                     tma_tile<CG>(at + S::bytes_l, &map_r, (int)(kt * kTileK), yr, bar);
                 }
-                __syncwarp();
+                ok = warp_agrees(ok);
             }
         }
     } else if (warp == 1 && rank == 0) {                     // matrix instructions
@@ -246,18 +246,18 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
         for (uint32_t t = first; ok && t < tiles; t += step, ++n) {
             // The last tile's shared columns have been read; and since whoever read them had done with the tile before, so has
             // the accumulator that this tile goes to.
-            if (n > 0 && !(ok = wait(s_acc_free, (n - 1) & 1))) break;
+            if (n > 0 && !(ok = warp_agrees(wait(s_acc_free, (n - 1) & 1)))) break;
             tc_fence_after();
             const uint32_t buf = n & 1, d = tmem + buf * S::second;
-            for (uint32_t kt = 0; kt < k_hi - k_lo; ++kt, advance()) {
-                if (!(ok = wait(s_full[stage], phase))) break;
-                if (kt % S::ahead == 0 && !(ok = wait(s_sf_full[slot & 1], (slot >> 1) & 1))) break;
+            for (uint32_t kt = 0; ok && kt < k_hi - k_lo; ++kt, advance()) {
+                ok = wait(s_full[stage], phase);
+                if (kt % S::ahead == 0) ok = wait(s_sf_full[slot & 1], (slot >> 1) & 1) && ok;
                 tc_fence_after();
                 const uint32_t at = base + stage * S::stage, sf = slots + (slot & 1) * S::slot + kt % S::ahead * (S::sets * 512);
                 const uint32_t tsf = tmem + S::sf_at + stage * S::sf_cols;
                 const uint64_t a = operand_desc(at), b = operand_desc(at + S::bytes_l);
                 const bool end = kt + 1 == k_hi - k_lo, last = kt % S::ahead == S::ahead - 1 || end;
-                if (elect_one()) {
+                if (elect_one() && ok) {
 #pragma unroll
                     for (int i = 0; i < S::sets; ++i) scales_to_tmem<CG>(tsf + 4 * i, scales_desc(sf + 512 * i));
 #pragma unroll
@@ -267,7 +267,7 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
                     if (last) mma_commit<CG>(smem_addr(&s_sf_empty[slot & 1]), leader);
                     if (end) mma_commit<CG>(smem_addr(&s_acc_full[buf]), leader);
                 }
-                __syncwarp();
+                ok = warp_agrees(ok);
                 slot += last;
             }
         }
@@ -291,7 +291,7 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
         };
         load();
         for (slot = turn; t < tiles; slot += 2) {
-            if (!__all_sync(0xFFFFFFFFu, wait(s_sf_empty[turn], ((slot >> 1) & 1) ^ 1))) break;
+            if (!warp_agrees(wait(s_sf_empty[turn], ((slot >> 1) & 1) ^ 1))) break;
             uint4* to = reinterpret_cast<uint4*>(base_p + S::stages * S::stage + turn * S::slot + set * 512) + lane;
 #pragma unroll
             for (int j = 0; j < S::ahead; ++j)
@@ -310,8 +310,7 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
             uint32_t tl, tr;
             tile_at(t, p.tiles_l, p.tiles_r, tl, tr);
             const uint32_t buf = n & 1;
-            ok = __all_sync(0xFFFFFFFFu, wait(s_acc_full[buf], (n >> 1) & 1));
-            if (!ok) break;
+            if (!(ok = warp_agrees(wait(s_acc_full[buf], (n >> 1) & 1)))) break;
             tc_fence_after();
             const size_t row = (size_t)tl * (kRowsL * CG) + rank * kRowsL + q * 32 + lane;
             auto release = [&] {
@@ -339,13 +338,14 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
         }
     }
     __syncwarp();
-    // A wait that gave up may have left copies under way: let those of this CTA land before its memory goes.
-    if (s_gave_up && threadIdx.x == 0) {
-        const uint64_t began = global_ns();
-        while (global_ns() - began < 1000ull * 1000) {}
-    }
     tc_fence_before();
     __syncthreads();
+    // A wait that gave up, in whichever warp, may have left copies under way: let those of this CTA land before its memory goes.
+    if (s_gave_up) {
+        const uint64_t began = global_ns();
+        while (global_ns() - began < 1000ull * 1000) {}
+        __syncthreads();
+    }
     if constexpr (SPLIT) {                                   // this CTA's share of the columns, the parts in order
         static_assert(S::stages * S::stage >= BN * kRowsL * 4, "a part fits in the stages");
         cluster_sync();
@@ -483,6 +483,25 @@ Plan plan(const MatmulArgs& m)
     return best;
 }
 
+#ifdef MXQ_DEBUG
+__device__ unsigned int g_went_on;
+
+// One warp whose even lanes wait for a phase that is over and whose odd lanes for one that nothing ends: which lanes went on.
+__global__ void wait_kernel(uint64_t limit_ns)
+{
+    __shared__ __align__(8) uint64_t s_bar;
+    __shared__ uint32_t s_gave_up;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_addr(&s_bar), 1);
+        s_gave_up = 0;
+    }
+    __syncwarp();
+    const bool went_on = warp_agrees(mbar_wait(smem_addr(&s_bar), (threadIdx.x & 1) ^ 1, &s_gave_up, &g_status, limit_ns));
+    const unsigned int lanes = __ballot_sync(0xFFFFFFFFu, went_on);
+    if (threadIdx.x == 0) g_went_on = lanes;
+}
+#endif
+
 template <class OUT>
 int choose(const MatmulArgs& m, cudaStream_t stream)
 {
@@ -522,3 +541,21 @@ int tc_status(int reset)
 }
 
 }  // namespace mxq
+
+#pragma GCC visibility push(default)
+extern "C" int mxq_debug_wait(unsigned int milliseconds, unsigned int* lanes)
+{
+#ifdef MXQ_DEBUG
+    if (!lanes) return MXQ_ERR_NULL;
+    if (milliseconds > 1000) return MXQ_ERR_SIZE;
+    mxq::wait_kernel<<<1, 32>>>((uint64_t)milliseconds * 1000000ull);
+    if (cudaDeviceSynchronize() == cudaSuccess && cudaMemcpyFromSymbol(lanes, mxq::g_went_on, sizeof *lanes) == cudaSuccess) return 1;
+    (void)cudaGetLastError();
+    return MXQ_ERR_CUDA;
+#else
+    (void)milliseconds;
+    (void)lanes;
+    return 0;
+#endif
+}
+#pragma GCC visibility pop

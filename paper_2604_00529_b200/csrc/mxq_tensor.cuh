@@ -74,7 +74,8 @@ __device__ __forceinline__ uint64_t global_ns()
 // wait of the CTA already had (`gave_up`, shared).  Whoever gives up says so to the host through `status`.
 constexpr uint64_t kWaitLimitNs = 10ull * 1000 * 1000 * 1000;
 
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, unsigned int* status)
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, unsigned int* status,
+                                          uint64_t limit_ns = kWaitLimitNs)
 {
     uint64_t began = 0;                                      // (the timer is slow to read: not before many tries)
     for (uint32_t i = 1;; ++i) {
@@ -83,7 +84,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
             if (*gave_up) return false;
             const uint64_t now = global_ns();
             if (began == 0) began = now;
-            if (now - began > kWaitLimitNs) {
+            if (now - began > limit_ns) {
                 *gave_up = 1;
                 atomicOr(status, 1u);
                 return false;
@@ -91,6 +92,11 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
         }
     }
 }
+
+// At the limit the lanes of a warp may see different things (the last try, the timer), and lanes that went on alone would wait in the
+// next instruction of the whole warp (elect.sync, a store's meeting) for those that left: what a wait answers is agreed on before
+// anyone leaves a loop.
+__device__ __forceinline__ bool warp_agrees(bool ok) { return __all_sync(0xFFFFFFFFu, ok); }
 
 // ---- TMA --------------------------------------------------------------------------------------------------
 
