@@ -1,5 +1,6 @@
 // D = L^ R^T on the fifth-generation tensor cores (block-scaled E4M3 matrix instructions): the product of mxq_matmul for more
-// rows than a few.  L's rows go to the accumulator's lanes, R's rows to its columns; which operand is which is the launcher's choice.
+// rows than a few.  L's rows go to the accumulator's lanes, R's rows to its columns: A and B, or, where parts are added (SPLIT), B and A,
+// so that a lane's neighbours are consecutive elements of a row of D.
 //
 // The instruction takes one scale byte per row and 32 values of k, multiplied in by the hardware; a block of 64 or 128
 // repeats its byte.  Scales therefore come in as plain bytes and are spread by the warps that bring them to shared memory
@@ -128,15 +129,11 @@ __device__ __forceinline__ void put(uint8_t* dst, size_t i, float v)
     }
 }
 
-// 32 columns of one row per lane to memory.  T: D's rows are the accumulator's columns.
-template <class OUT, bool T>
+// 32 columns of one row per lane to memory.
+template <class OUT>
 __device__ __forceinline__ void store_block(const TcArgs& p, const uint32_t (&v)[32], size_t row, size_t col, float* stage, int lane)
 {
-    if constexpr (T) {                                       // a warp's 32 lanes are consecutive elements of a row of D
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (row < p.rows_l && col + j < p.rows_r) put<OUT>(p.dst, (col + j) * p.ld + row, __uint_as_float(v[j]));
-    } else if (p.ld % (32 / OUT::size) == 0) {               // whole 32-byte sectors
+    if (p.ld % (32 / OUT::size) == 0) {               // whole 32-byte sectors
         constexpr int PER = 32 / OUT::size;
         if (row >= p.rows_l) return;
 #pragma unroll
@@ -160,7 +157,7 @@ __device__ __forceinline__ void store_block(const TcArgs& p, const uint32_t (&v)
     }
 }
 
-template <class OUT, int CG, int BN, bool T, int BLOCK, bool SPLIT>
+template <class OUT, int CG, int BN, int BLOCK, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
 matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_r, const TcArgs p)
 {
@@ -168,8 +165,7 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
     extern __shared__ uint8_t s_raw[];
     __shared__ __align__(8) uint64_t s_full[S::stages], s_empty[S::stages], s_sf_full[2], s_sf_empty[2], s_acc_full[2], s_acc_free;
     __shared__ uint32_t s_tmem, s_gave_up;
-    static_assert(!SPLIT || T, "parts are added along D's rows");
-    __shared__ float s_out[T ? 1 : 4 * 32 * 33];
+    __shared__ float s_out[SPLIT ? 1 : 4 * 32 * 33];
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t in_cluster = CG == 2 || SPLIT ? cluster_rank() : 0u, rank = in_cluster % CG, leader = in_cluster - rank;
     const uint32_t base = (smem_addr(s_raw) + 1023u) & ~1023u;
@@ -331,9 +327,9 @@ matmul_tc_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constan
                     float* part = reinterpret_cast<float*>(base_p) + q * 32 + lane;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) part[(c + j) * kRowsL] = __uint_as_float(v[j]);
-                    continue;
+                } else {
+                    store_block<OUT>(p, v, row, (size_t)tr * BN + c, s_out + q * 32 * 33, lane);
                 }
-                store_block<OUT, T>(p, v, row, (size_t)tr * BN + c, s_out + (T ? 0 : q * 32 * 33), lane);
             }
         }
     }
@@ -414,18 +410,18 @@ bool make_map(CUtensorMap* map, const uint8_t* p, size_t rows, size_t k, int box
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class OUT, int CG, int BN, bool T, int BLOCK, bool SPLIT>
+template <class OUT, int CG, int BN, int BLOCK, bool SPLIT>
 int run_block(const MatmulArgs& m, uint32_t split, cudaStream_t stream)
 {
     using S = Shape<CG, BN>;
     static std::atomic<uint64_t> done{0};
-    auto kern = matmul_tc_kernel<OUT, CG, BN, T, BLOCK, SPLIT>;
+    auto kern = matmul_tc_kernel<OUT, CG, BN, BLOCK, SPLIT>;
     if (int rc = allow_smem(reinterpret_cast<const void*>(kern), S::smem, done)) return rc;
     TcArgs p;
-    p.ls = T ? m.bs : m.as;
-    p.rs = T ? m.as : m.bs;
-    p.rows_l = T ? m.n : m.m;
-    p.rows_r = T ? m.m : m.n;
+    p.ls = SPLIT ? m.bs : m.as;
+    p.rs = SPLIT ? m.as : m.bs;
+    p.rows_l = SPLIT ? m.n : m.m;
+    p.rows_r = SPLIT ? m.m : m.n;
     p.dst = m.dst;
     p.ld = m.n;
     p.split = split;
@@ -435,18 +431,18 @@ int run_block(const MatmulArgs& m, uint32_t split, cudaStream_t stream)
     p.tiles_r = (uint32_t)((p.rows_r + BN - 1) / BN);
     if ((uint64_t)p.tiles_l * p.tiles_r > 0x7FFFFFFFull / (CG * split)) return MXQ_ERR_SIZE;
     CUtensorMap ml, mr;
-    if (!make_map(&ml, T ? m.b : m.a, p.rows_l, m.k, kRowsL) || !make_map(&mr, T ? m.a : m.b, p.rows_r, m.k, S::rows_r)) return MXQ_ERR_CUDA;
+    if (!make_map(&ml, SPLIT ? m.b : m.a, p.rows_l, m.k, kRowsL) || !make_map(&mr, SPLIT ? m.a : m.b, p.rows_r, m.k, S::rows_r)) return MXQ_ERR_CUDA;
     const uint32_t tiles = p.tiles_l * p.tiles_r, most = 148 / CG;
     const unsigned grid = SPLIT ? tiles * split * CG : (tiles < most ? tiles : most) * CG;
     return launch_grid(kern, dim3(grid), kThreads, S::smem, (int)(CG * split), stream, ml, mr, p);
 }
 
-template <class OUT, int CG, int BN, bool T, bool SPLIT>
+template <class OUT, int CG, int BN, bool SPLIT>
 int run(const MatmulArgs& m, uint32_t split, cudaStream_t stream)
 {
-    if (m.block == 32) return run_block<OUT, CG, BN, T, 32, SPLIT>(m, split, stream);
-    if (m.block == 64) return run_block<OUT, CG, BN, T, 64, SPLIT>(m, split, stream);
-    return run_block<OUT, CG, BN, T, 128, SPLIT>(m, split, stream);
+    if (m.block == 32) return run_block<OUT, CG, BN, 32, SPLIT>(m, split, stream);
+    if (m.block == 64) return run_block<OUT, CG, BN, 64, SPLIT>(m, split, stream);
+    return run_block<OUT, CG, BN, 128, SPLIT>(m, split, stream);
 }
 
 // What a launch is expected to take, in microseconds: a fixed part per wave of CTAs (start, first loads, sums and stores of the
@@ -506,11 +502,11 @@ template <class OUT>
 int choose(const MatmulArgs& m, cudaStream_t stream)
 {
     const Plan p = plan(m);
-    if (p.split && p.bn == 32) return run<OUT, 1, 32, true, true>(m, (uint32_t)p.split, stream);
-    if (p.split && p.bn == 64) return run<OUT, 1, 64, true, true>(m, (uint32_t)p.split, stream);
-    if (p.split) return run<OUT, 2, 128, true, true>(m, (uint32_t)p.split, stream);
-    if (p.bn == 128) return run<OUT, 2, 128, false, false>(m, 1, stream);
-    return run<OUT, 2, 256, false, false>(m, 1, stream);
+    if (p.split && p.bn == 32) return run<OUT, 1, 32, true>(m, (uint32_t)p.split, stream);
+    if (p.split && p.bn == 64) return run<OUT, 1, 64, true>(m, (uint32_t)p.split, stream);
+    if (p.split) return run<OUT, 2, 128, true>(m, (uint32_t)p.split, stream);
+    if (p.bn == 128) return run<OUT, 2, 128, false>(m, 1, stream);
+    return run<OUT, 2, 256, false>(m, 1, stream);
 }
 
 }  // namespace
