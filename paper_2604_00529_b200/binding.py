@@ -800,7 +800,8 @@ def linear_ste(x: torch.Tensor, w: torch.Tensor, block: int = 32) -> torch.Tenso
     along the dimension that its product sums over and the quantizers passed straight through.  Any sizes, strides and offsets (what
     is not contiguous at an address that is a multiple of 32 is copied first); y and dx have x's type, dw has w's.  The backward pass
     keeps the transposes' codes (a byte per element), not x and w.  There is no second derivative: gradients taken with create_graph raise
-    where they are differentiated."""
+    where they are differentiated.  Under vmap, torch.func's derivatives and forward-mode derivatives it raises; jit.trace
+    records it as one call."""
     if _lib is None:
         load_library()
     made = _host.linear_ste(x, w, block)
@@ -832,7 +833,8 @@ def moe(x: torch.Tensor, logits: torch.Tensor, up_codes: torch.Tensor, up_scales
     """mxq_moe: a mixture-of-experts layer for up to MOE_TOKENS_MAX tokens x [tokens, hidden] with the router's float32 logits
     [tokens, experts] over experts held as codes: up matrices [experts, 2 * inner, hidden] (gate rows first) and
     down matrices [experts, hidden, inner], as ``quantize`` writes them.  ``workspace`` (uint8, ``moe_workspace_bytes``) saves
-    the allocation of one per call; calls that can overlap on the GPU must not share it."""
+    the allocation of one per call; calls that can overlap on the GPU must not share it.  For serving: the result has no gradient,
+    whatever x and the logits require."""
     L = _lib or load_library()
     made = _host.moe(x, logits, up_codes, up_scales, down_codes, down_scales, inner, top_k, fmt, block, renormalize, out, workspace, stream)
     if made is not None:

@@ -6,6 +6,7 @@ import torch
 
 import paper_2604_00529_b200 as mxq
 import paper_2604_00529_b200.binding  # noqa: F401
+import torch.utils.checkpoint  # noqa: F401
 
 import product_util as pu
 
@@ -167,3 +168,50 @@ def test_streams_given_as_the_fixed_handles(handle):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert torch.equal(d, mxq.matmul(*want[:2], *want[:2], 96, 96, 160))
+
+
+# ---- linear_ste inside the rest of torch ----------------------------------------------------------------------
+
+
+def test_linear_ste_refuses_transforms(path):
+    """vmap, the functional derivatives and forward-mode derivatives raise; nothing is answered silently."""
+    x, w = torch.randn(4, 32, device="cuda"), torch.randn(8, 32, device="cuda")
+    for call in (lambda: torch.func.vmap(lambda t: mxq.linear_ste(t, w))(x[None]),
+                 lambda: torch.func.vmap(lambda t: t * mxq.linear_ste(x, w).sum())(x),
+                 lambda: torch.func.grad(lambda t: mxq.linear_ste(t, w).sum())(x),
+                 lambda: torch.func.jvp(lambda t: mxq.linear_ste(t, w), (x,), (x,))):
+        with pytest.raises(RuntimeError):
+            call()
+    with torch.autograd.forward_ad.dual_level(), pytest.raises(RuntimeError):
+        mxq.linear_ste(torch.autograd.forward_ad.make_dual(x, x), w)
+
+
+def test_linear_ste_traced_hooked_and_recomputed(path):
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x, w = torch.randn(4, 32, generator=g, device="cuda"), torch.randn(8, 32, generator=g, device="cuda")
+    traced = torch.jit.trace(lambda t: mxq.linear_ste(t, w), (x,), check_trace=False)
+    other = torch.randn(6, 32, generator=g, device="cuda")
+    assert torch.equal(traced(other), mxq.linear_ste(other, w))
+    xr, wr = x.clone().requires_grad_(), w.clone().requires_grad_()
+    want = torch.autograd.grad(mxq.linear_ste(xr, wr), (xr, wr), torch.full((4, 8), 2.0, device="cuda"))
+    seen = []
+    y = mxq.linear_ste(xr, wr)
+    y.register_hook(lambda t: 2 * t)
+    handle = xr.register_hook(lambda t: seen.append(t.shape))
+    y.sum().backward()
+    handle.remove()
+    assert seen == [xr.shape] and torch.equal(xr.grad, want[0]) and torch.equal(wr.grad, want[1])
+    y = torch.utils.checkpoint.checkpoint(mxq.linear_ste, xr, wr, use_reentrant=False)
+    for a, b in zip(torch.autograd.grad(2 * y.sum(), (xr, wr)), want):
+        assert torch.equal(a, b)
+    y = mxq.linear_ste(xr, wr)                              # twice through one graph, where it was kept
+    first = torch.autograd.grad(2 * y.sum(), (xr, wr), retain_graph=True)
+    for a, b, c in zip(first, torch.autograd.grad(2 * y.sum(), (xr, wr)), want):
+        assert torch.equal(a, c) and torch.equal(b, c)
+
+
+def test_moe_has_no_gradient():
+    x = torch.randn(2, 64, device="cuda", requires_grad=True)
+    up, down = mxq.quantize(torch.randn(4 * 64 * 64, device="cuda"), "int8"), mxq.quantize(torch.randn(4 * 64 * 32, device="cuda"), "int8")
+    got = mxq.moe(x, torch.randn(2, 4, device="cuda"), *up, *down, 32, 2, "int8")
+    assert not got.requires_grad and got.isfinite().all()
