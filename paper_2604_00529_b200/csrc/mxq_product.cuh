@@ -43,7 +43,7 @@ __device__ __forceinline__ uint4 ld_once(const uint8_t* p)
 // subnormal's rounding).  MXFP: the code's fields put in the places of BF16's stand for 2^-120 (E4M3) or 2^-126 (E2M1) times
 // the element, subnormal elements being BF16 subnormals, and the scale's multiplier puts that back.  MXINT: the code under the
 // exponent of 128 is 128 + its low bits.  E4M3's NaN codes (S.1111.111) would come out as 480 and are looked for by themselves
-// (note_nan): a lane that holds one among its codes of a row takes NaN as that row's multiplier, and the row's sums are NaN.
+// (note_nan).
 // Word w of a lane's 16 bytes gives NP = 2 (8 bits) or 4 (4 bits) pairs; pair p holds elements x_order(p) of the word.
 
 template <int FMT>
@@ -69,19 +69,17 @@ struct Widen {
         const uint32_t h = byte == 255u ? 0x7FC0u : byte <= limit ? 0x3F80u : (byte - limit + 127u) << 7;
         return h * 0x10001u;
     }
+    static constexpr bool has_nan = FMT == MXQ_FP8_E4M3;
     // Adding one to a byte flips its top bit exactly if the seven bits below are ones.  (The carry out of 0xFF may flip more; 0xFF is a
-    // NaN code itself.)  Two instructions per four codes: one token, two of eight 4096 x 14336 experts 110.6 us instead of 104.2.
-    // (Kept in registers over a whole unit and applied to its sums 110.0; one vote per chunk for the four rows 111.4; an 8-bit matrix
-    // instruction of the codes by zeros 116.6.)
-    static __device__ __forceinline__ void note_nan(uint32_t w, uint32_t& seen)
+    // NaN code itself.)  Two instructions per four codes.
+    static __device__ __forceinline__ void note_nan(const uint4& c, uint32_t& seen)
     {
-        if constexpr (FMT == MXQ_FP8_E4M3) seen |= (w + 0x01010101u) ^ w;
+        seen |= (c.x + 0x01010101u) ^ c.x;
+        seen |= (c.y + 0x01010101u) ^ c.y;
+        seen |= (c.z + 0x01010101u) ^ c.z;
+        seen |= (c.w + 0x01010101u) ^ c.w;
     }
-    static __device__ __forceinline__ uint32_t factor_or_nan(uint32_t f, uint32_t seen)
-    {
-        if constexpr (FMT == MXQ_FP8_E4M3) return seen & 0x80808080u ? 0x7FC07FC0u : f;
-        else return f;
-    }
+    static __device__ __forceinline__ bool saw_nan(uint32_t seen) { return (seen & 0x80808080u) != 0; }
     static __device__ __forceinline__ uint32_t mul(uint32_t a, uint32_t b)
     {
         uint32_t d;
