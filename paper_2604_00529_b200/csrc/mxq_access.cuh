@@ -25,7 +25,9 @@ namespace mxq {
 // launching; pdl_acquire() blocks until the previous kernel has completed and its writes are
 // visible.  Each kernel calls pdl_release() first and pdl_acquire() before its first global
 // load or store (and before it returns, so that completion stays transitive along the stream),
-// which keeps plain stream-order semantics for every buffer.
+// which keeps plain stream-order semantics for every buffer.  One pair of kernels parts from that order: mxq_moe's first kernel
+// releases behind its own acquire, so that its second one may read at once what the first one does not write (the logits,
+// the down matrices); it still acquires before it reads the first one's results and before it writes.
 
 __device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void pdl_acquire() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

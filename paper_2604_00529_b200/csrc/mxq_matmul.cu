@@ -1,5 +1,5 @@
-// D = A^ B^T of two MXFP8 E4M3 operands with one E8M0 scale per block along k (the product that the converted weights are for,
-// Sec. 3.5): D[i, j] = sum over blocks b of Xa[i, b] Xb[j, b] sum over k in b of Pa[i, k] Pb[j, k].
+// D = A^ B^T of two operands in the MXFP anchor's format, E4M3, with one E8M0 scale per block along k (Sec. 3.5; the lower formats have no
+// product but mxq_moe's): D[i, j] = sum over blocks b of Xa[i, b] Xb[j, b] sum over k in b of Pa[i, k] Pb[j, k].
 #include "mxq_kernels.cuh"
 #include "mxq_launch.h"
 #include "mxq_product.cuh"
@@ -15,7 +15,7 @@ inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintp
 // meet in shared memory at the end, in a fixed order.  Codes go from global memory straight into the fragments of the warp's
 // matrix instruction: widened to FP16, exactly, by the conversion instruction, and the block's two scales multiply the
 // FP32 sum of the block.  (One row of A, B 4096 x 4096: 6.2 us; eight warps 9.7, 16 rows of B 8.6, one chunk under way per warp
-// instead of two 6.8.)
+// instead of two 6.8.  The variant for blocks of 32 spills 52 bytes per thread.)
 //   BLK32: blocks of 32.  Two of the four lanes of a row then hold one block and two the other: a step is taken twice, with the other
 //   lanes' elements of A zero (the matrix instructions are the least of this kernel's time).
 

@@ -17,7 +17,11 @@
 // card's power limit and a clock of 1.28 GHz.  13 x 14336 x 4096 14.8 us, 4.0 TB/s of codes.  What the loops of the issuing warp
 // cost decides: with one lane in a branch of its own, addresses went through vector registers and a k tile took 570 ns
 // instead of 430; copying the next tile's scales ahead of this one's products, or writing them to tensor memory from registers,
-// was slower (13 x 14336 x 4096 15.9 and 18.5 us).
+// was slower (13 x 14336 x 4096 15.9 and 18.5 us).  The two issuing warps agree on what a wait answered (warp_agrees) behind what they
+// issue: 200 x 4096 x 14336 takes 24.4 us, 24.5 with that in front, 24.1 where each lane goes by itself.
+//
+// The accumulator is FP32 and the instruction cuts: it loses less than 2^-23 of the sum at each step of 32 values, always toward zero
+// (k = 14336 in one run 8.4e-6 of D in norm; in four parts, whose sum rounds, 2.1e-6).
 #include <cuda.h>
 
 #include "mxq_kernels.cuh"

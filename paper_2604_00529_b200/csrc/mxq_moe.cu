@@ -1,17 +1,23 @@
-// A mixture-of-experts layer for a few tokens over experts held as MX codes (the products that the converted weights are for,
-// Sec. 3.5), in two kernels:
+// A mixture-of-experts layer for a few tokens over experts held as MX codes, anchors or converted to 4 bits (Sec. 3.5), in two
+// kernels:
 //   choice     p = softmax(logits[t]); the top_k largest logits (ties: the lowest expert; -inf is never chosen);
 //              w = p / (sum of the chosen p), or p
 //   kernel 1   h[t, e] = silu(G_e x_t) * (U_e x_t), G_e and U_e the two halves of expert e's up matrix [2 inner, hidden]
 //   kernel 2   out[t] = sum over the chosen e of w[t, e] D_e h[t, e], D_e = [hidden, inner]
 // Bound by reading the chosen experts' codes once.  Both kernels work the choice out for themselves from the logits (2 us for one
 // token and 64 experts, 4.4 for 32 tokens), so that no third launch stands in front, and kernel 2 does so before it waits for
-// kernel 1 (leaving the choice in the workspace for it instead was 2 to 4 % slower: it then starts only when kernel 1 is done).
+// kernel 1 (leaving the choice in the workspace for it instead was 2 to 4 % slower: it then starts only when kernel 1 is done).  A CTA of
+// either kernel fills an SM, so that kernel 2's begin where CTAs of kernel 1 have left.
 //
 // Products: a warp takes 16 rows of a matrix and a chunk of 16 bytes of codes per lane, widens the codes to BF16 with their
 // block's scale multiplied in (exact, see Widen) and multiplies them with up to eight tokens by the warp's matrix instruction,
 // sums in FP32.  FP32 operands go in as BF16 parts that add up to them: FP32 tokens as three (all 24 bits), h as two for
-// BF16 tokens (16 bits: its error, 2^-17 of a value, is far below the output's rounding) and as three for FP32 ones.
+// BF16 tokens (16 bits: its error, 2^-17 of a value, is far below the output's rounding) and as three for FP32 ones.  The instruction cuts
+// its sums, by less than 2^-23 of them per step of 16 values: with BF16 tokens a warp's share of k stays in it (64 steps for
+// hidden = 4096, 2^-17.6 in norm at worst), with FP32 ones its sums leave it chunk by chunk.  With BF16 tokens these two move outputs
+// next to a halfway point, 1e-4 of them in norm, and leave their distance to 64 bits at 1.7e-3; three parts of h cost 3 to 9 %
+// (one token, two of eight 4096 x 14336 E4M3 experts 115 us where two parts took 111; eight small experts 24.9 and 22.9), with sums
+// outside as well 5 to 11 % (117 and 25.4).
 // Warps meet in shared memory in a fixed order: results do not depend on timing.
 #include "mxq_kernels.cuh"
 #include "mxq_launch.h"
@@ -391,11 +397,11 @@ __device__ __forceinline__ void wait_slot(int slots)         // all copies but t
 // two sets of sums in turn).  In a 16-row tile the first eight rows are the gate's and the last eight the up half's.  Units go
 // to the CTAs' first teams before their second ones, so that few of them are on many SMs (256 units of 4096: both kernels 25 us;
 // four at a time 31).  A warp's copies run on into its next unit.
-// Bound by instructions: one token, two of eight 4096 x 14336 E4M3 experts 65 us for 235 MB (67 us when tried: 57 without the
-// widening, 46 with the copies alone; about 6 of them for the last 16 of 1792 units, which 592 teams share.  The whole CTA on each
-// of those saved 3 us there and cost other shapes 0.3 to 0.6; teams of 8 or 16 for all units cost 5 and 16 us).  Tokens go through
-// L1, not through the copies (82 us: every SM asking L2 for the same few lines).  Asking for a unit's scales as early as for its
-// codes, 20 or 24 warps of fewer registers: nothing gained.
+// Bound by instructions: one token, two of eight 4096 x 14336 E4M3 experts 65 us for 235 MB, about 5 more since NaN codes are looked
+// for (67 us when tried: 57 without the widening, 46 with the copies alone; about 6 of them for the last 16 of 1792 units, which 592
+// teams share.  The whole CTA on each of those saved 3 us there and cost other shapes 0.3 to 0.6; teams of 8 or 16 for all units
+// cost 5 and 16 us).  Tokens go through L1, not through the copies (82 us: every SM asking L2 for the same few lines).  Asking for a
+// unit's scales as early as for its codes, 20 or 24 warps of fewer registers: nothing gained.
 
 template <class T, int FMT, int HPARTS>
 __global__ void __launch_bounds__(kUpWarps * 32, 1)
@@ -550,7 +556,8 @@ moe_up_kernel(const MoeArgs p, const int slots)
 // A CTA covers 32 rows of the output for all tokens; where that makes few CTAs, a cluster of them covers the same rows.  The
 // chunks of all active experts, laid end to end, are shared out between the warps; a warp adds its weighted sums to its own
 // copy of the tile, and the copies are added in order, then the cluster's.  The first chunks' codes are fetched before the
-// wait for kernel 1.  (The same experts: 37 us for 117 MB; with 16 rows per CTA 46.)
+// wait for kernel 1.  (The same experts: 37 us for 117 MB; with 16 rows per CTA 46.)  Spills, FP32 tokens: 192 bytes per thread over
+// MXINT4 experts, 240 over E2M1 ones (kernel 1: 4 and 20).
 
 template <class T, int FMT, int HPARTS>
 __global__ void __launch_bounds__(kDownWarps * 32, 1)

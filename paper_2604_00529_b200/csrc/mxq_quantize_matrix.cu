@@ -78,7 +78,8 @@ struct MatrixShared {
 // FP32 bit patterns are ordered like the values, and only the exponent field of a maximum is used (0xFF: the block is
 // poisoned): the patterns' upper halves are enough, two to a word.
 //   WHOLE: the tile lies inside the matrix; nothing is compared with its edges.  (The kernel is bound by instructions: 14336 x 4096 BF16
-//   took 25 per element and 55 us with every access compared and addressed for itself, 45 us like this: 5.2 TB/s.)
+//   took 25 per element and 55 us with every access compared and addressed for itself, 45 us like this: 5.2 TB/s.  The variants
+//   without vector loads, for cols % 8 != 0, spill 8 to 68 bytes per thread.)
 template <class T, class F, int BLOCK, bool VEC, bool WHOLE>
 __device__ __forceinline__ void matrix_tile(const uint8_t* __restrict__ src, size_t rows, size_t cols, uint8_t* __restrict__ codes,
                                             uint8_t* __restrict__ scales, uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t, size_t tr, size_t tc, MatrixShared& sh)

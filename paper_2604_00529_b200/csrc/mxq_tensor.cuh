@@ -70,7 +70,7 @@ __device__ __forceinline__ uint64_t global_ns()
     return t;
 }
 
-// Waits for the phase of `parity`, at most kWaitLimitNs (far beyond any kernel's run); false when it gave up, or when another
+// Waits for the phase of `parity`, at most `limit_ns` (by default far beyond any kernel's run); false when it gave up, or when another
 // wait of the CTA already had (`gave_up`, shared).  Whoever gives up says so to the host through `status`.
 constexpr uint64_t kWaitLimitNs = 10ull * 1000 * 1000 * 1000;
 
