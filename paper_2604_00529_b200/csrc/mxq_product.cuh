@@ -44,7 +44,7 @@ __device__ __forceinline__ uint4 ld_once(const uint8_t* p)
 // the element, subnormal elements being BF16 subnormals, and the scale's multiplier puts that back.  MXINT: the code under the
 // exponent of 128 is 128 + its low bits.  E4M3's NaN codes (S.1111.111) would come out as 480 and are looked for by themselves
 // (note_nan).
-// Word w of a lane's 16 bytes gives NP = 2 (8 bits) or 4 (4 bits) pairs; pair p holds elements x_order(p) of the word.
+// Word w of a lane's 16 bytes gives NP = 2 (8 bits) or 4 (4 bits) pairs; pairs hold the word's elements in the order of order_pairs.
 
 template <int FMT>
 struct Widen {
