@@ -444,6 +444,81 @@ size_t mxq_moe_workspace_bytes(size_t tokens, int top_k, size_t inner, int dtype
 int mxq_moe(const mxq_moe_layer *layer, const void *x, int dtype, const float *logits, size_t tokens, int top_k,
             int renormalize, void *out, void *workspace, size_t workspace_bytes, mxq_stream stream);
 
+/*
+ * A paged cache of keys and values held as codes.  A page holds `page` tokens of every head; a token's row of head_dim elements
+ * is quantized along itself (blocks of `block`), so that a token is written without its neighbours:
+ *   k_codes, v_codes    [pages, heads, page, head_dim] packed codes of fmt, 32-byte aligned
+ *   k_scales, v_scales  [pages, heads, page, head_dim / block] E8M0 bytes, 16-byte aligned
+ * fmt one of MXQ_FP8_E4M3, MXQ_FP4_E2M1, MXQ_INT8, MXQ_INT4 (MXQ_ERR_FORMAT); block 32, 64 or 128 (MXQ_ERR_BLOCK); head_dim 64, 128 or
+ * 256 and a multiple of block; page 16, 32, 64, 128 or 256; 1 <= heads <= MXQ_CACHE_HEADS_MAX; pages below 2^31 (MXQ_ERR_SIZE).
+ *
+ * A batch says where sequences lie and which of their tokens are new.  Its arrays are on the device and 4-byte aligned:
+ *   table    [batch, width]  the pages of sequence b in order.  An entry outside [0, pages) is never accessed: what would be written
+ *                            there is dropped, its tokens are read as zeros and left out of the attention
+ *   lengths  [batch]         tokens of each sequence, the new ones among them; at most width * page count
+ *   starts   [batch + 1]     rows starts[b] ... starts[b + 1] - 1 of the tokens' tensors are sequence b's last (newest) tokens, in
+ *                            order; rows in front of starts[0] and behind starts[batch] belong to none.  Null: row b is sequence b's one
+ *                            newest token, and tokens must equal batch (MXQ_ERR_SIZE)
+ * A row that would lie in front of its sequence's first token (a padded slot of length 0) is not written, and attends nothing.
+ * Structs are HOST structs, free to reuse when a call returns.  batch, width and tokens are below 2^31 (MXQ_ERR_SIZE).
+ */
+#define MXQ_CACHE_HEADS_MAX 1024
+typedef struct mxq_cache {
+    void *k_codes;
+    uint8_t *k_scales;
+    void *v_codes;
+    uint8_t *v_scales;
+    size_t pages;
+    int page, heads, head_dim, fmt, block;
+} mxq_cache;
+
+typedef struct mxq_batch {
+    const int32_t *table, *lengths, *starts;
+    size_t batch, width;
+} mxq_batch;
+
+/* Rows [tokens, heads, head_dim], the last dimension contiguous, strides in elements; address and strides multiples of 32 bytes. */
+typedef struct mxq_rows {
+    const void *data;
+    size_t token_stride, head_stride;
+} mxq_rows;
+
+/*
+ * Quantizes the new tokens' keys and values, `heads` rows per token, into their pages: the bytes are those of mxq_quantize on each row.  Rows that
+ * belong to no sequence, and tokens without a page, are skipped; nothing else of the cache changes.  Two tokens of one call must
+ * not share a place in the cache (sequences that share a page may not write to it): what it then holds is undefined.
+ */
+int mxq_cache_write(const mxq_cache *cache, const mxq_batch *batch, const mxq_rows *k, const mxq_rows *v, int dtype, size_t tokens,
+                    mxq_stream stream);
+
+/*
+ * Reconstructs the FIRST starts[b + 1] - starts[b] tokens of each sequence (starts is required, lengths is not read) to rows
+ * starts[b] ... of k and v, [total, heads, head_dim] of dtype, contiguous and 32-byte aligned; values are those of mxq_dequantize.
+ * Rows behind the last sequence are left as they were.
+ */
+int mxq_cache_read(const mxq_cache *cache, const mxq_batch *batch, size_t total, void *k, void *v, int dtype, mxq_stream stream);
+
+/*
+ * Attention of the new tokens' queries over their sequences' cached keys and values: for query head j (which uses the cache's head
+ * j / (q_heads / heads)) of the token at position p
+ *   out = sum over visible t of softmax_t(scale q . K^[t]) V^[t]
+ * with K^ and V^ the reconstructions (NaN codes and poisoned blocks as NaN).  causal != 0: tokens up to p are visible, and with
+ * window > 0 only the last `window` of them, p included; causal == 0: all tokens (window must be 0, MXQ_ERR_SIZE).  What is not visible
+ * has no influence, whatever it holds.  A query that sees nothing gives zeros, and -inf in lse.
+ * Sums and the softmax are held in FP32.  Queries enter exactly for BF16 (elements below 2^-31 of a row's largest excepted) and
+ * with 22 bits for FP32; the softmax's weights enter the second product with 11 bits for BF16 and 22 for FP32.  A NaN or an infinity in a
+ * query gives NaN.  Results do not depend on timing.
+ *   q          [tokens, q_heads, head_dim] of dtype; q_heads a multiple of heads, at most 2^16 (MXQ_ERR_SIZE)
+ *   out        [tokens, q_heads, head_dim] of dtype, contiguous, 32-byte aligned; overlaps nothing else
+ *   lse        null, or [tokens, q_heads] FP32, 4-byte aligned: the natural logarithm of sum over visible t of exp(scale q . K^[t])
+ *   workspace  32-byte aligned, mxq_cache_attention_workspace_bytes(...) bytes or more (MXQ_ERR_SIZE); what it holds before and after
+ *              a call means nothing.  Calls whose work can overlap on the GPU must not share one
+ * Rows that belong to no sequence are left as they were.
+ */
+size_t mxq_cache_attention_workspace_bytes(const mxq_cache *cache, const mxq_batch *batch, int q_heads, int dtype, size_t tokens);  /* 0: refused */
+int mxq_cache_attention(const mxq_cache *cache, const mxq_batch *batch, const mxq_rows *q, int q_heads, int dtype, size_t tokens, float scale,
+                        int causal, size_t window, void *out, float *lse, void *workspace, size_t workspace_bytes, mxq_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

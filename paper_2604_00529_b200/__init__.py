@@ -13,5 +13,6 @@ from .binding import (  # noqa: F401
     slice_scale_pair_batched, make_pair_items,
     quantize_batched, make_q_items, dequantize_batched, make_dq_items,
     matmul, quantize_matrix, linear_ste, moe, moe_workspace_bytes, MOE_TOKENS_MAX, MOE_EXPERTS_MAX, MOE_TOP_K_MAX,
+    make_cache, cache_write, cache_read, cache_attention, cache_attention_workspace_bytes, CACHE_HEADS_MAX,
     PreparedCall, prepare_quantize, prepare_slice_scale, prepare_dequantize, prepare_fake_quant, prepare_fake_quant_bwd,
 )

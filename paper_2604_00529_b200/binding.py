@@ -67,6 +67,21 @@ class _MoeLayer(ctypes.Structure):
                 ("experts", ctypes.c_int), ("fmt", ctypes.c_int), ("block", ctypes.c_int)]
 
 
+class _Cache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("pages", ctypes.c_size_t), ("page", ctypes.c_int), ("heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("fmt", ctypes.c_int), ("block", ctypes.c_int)]
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("batch", ctypes.c_size_t),
+                ("width", ctypes.c_size_t)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_size_t), ("head_stride", ctypes.c_size_t)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 _host = None            # the native module _mxq_host (csrc/host_calls.cpp): the plain case of the per-tensor calls
 
@@ -151,6 +166,15 @@ def load_library() -> ctypes.CDLL:
     L.mxq_moe_workspace_bytes.restype = sz
     L.mxq_moe.argtypes = [ctypes.POINTER(_MoeLayer), vp, i, vp, sz, i, i, vp, vp, sz, vp]
     L.mxq_moe.restype = i
+    cache, batch, rows = ctypes.POINTER(_Cache), ctypes.POINTER(_Batch), ctypes.POINTER(_Rows)
+    L.mxq_cache_write.argtypes = [cache, batch, rows, rows, i, sz, vp]
+    L.mxq_cache_write.restype = i
+    L.mxq_cache_read.argtypes = [cache, batch, sz, vp, vp, i, vp]
+    L.mxq_cache_read.restype = i
+    L.mxq_cache_attention_workspace_bytes.argtypes = [cache, batch, i, i, sz]
+    L.mxq_cache_attention_workspace_bytes.restype = sz
+    L.mxq_cache_attention.argtypes = [cache, batch, rows, i, i, sz, ctypes.c_float, i, sz, vp, vp, vp, sz, vp]
+    L.mxq_cache_attention.restype = i
     for name in ("mxq_quantize", "mxq_slice_scale", "mxq_dequantize", "mxq_fake_quant", "mxq_fake_quant_bwd",
                  "mxq_slice_scale_batched"):
         getattr(L, name).restype = i
@@ -861,4 +885,162 @@ def moe(x: torch.Tensor, logits: torch.Tensor, up_codes: torch.Tensor, up_scales
             workspace = torch.empty(L.mxq_moe_workspace_bytes(tokens, top_k, inner, dt), dtype=torch.uint8, device=dev)
         _check(L.mxq_moe(ctypes.byref(layer), _dev(x, "x"), dt, _on(logits, "logits", dev), tokens, top_k, int(bool(renormalize)),
                          _on(out, "out", dev), _operand(workspace, "workspace", 0, dev), workspace.numel(), _stream(None)), "mxq_moe")
+    return out
+
+
+# ---- a paged cache of keys and values held as codes -----------------------------------------------------------------
+
+
+def make_cache(pages: int, heads: int, head_dim: int, fmt: str, block: int = 32, page: int = 64, device="cuda"):
+    """Buffers of an empty cache: (k_codes, k_scales, v_codes, v_scales), codes [pages, heads, page, head_dim * bits / 8] and
+    scales [pages, heads, page, head_dim / block], uint8, zeros (every token of it reads as zeros)."""
+    if fmt not in ("e4m3", "e2m1", "int8", "int4"):
+        raise MxqError(-2, "make_cache")
+    if block not in (32, 64, 128):
+        raise MxqError(-3, "make_cache")
+    if head_dim not in (64, 128, 256) or head_dim % block or page not in (16, 32, 64, 128, 256) or pages < 0 or not 1 <= heads <= CACHE_HEADS_MAX:
+        raise MxqError(-4, "make_cache")
+    codes, scales = (pages, heads, page, head_dim * (8 if fmt in ("e4m3", "int8") else 4) // 8), (pages, heads, page, head_dim // block)
+    return tuple(torch.zeros(shape, dtype=torch.uint8, device=device) for shape in (codes, scales, codes, scales))
+
+
+#: limit of a cache's heads (MXQ_CACHE_HEADS_MAX in include/mxq.h)
+CACHE_HEADS_MAX = 1024
+
+
+def _cache(k_codes, k_scales, v_codes, v_scales, fmt: str, block: int) -> _Cache:
+    """The marshalled description of a cache's four buffers, whose shapes must agree."""
+    f = FORMATS[fmt]
+    for t, what in ((k_codes, "k_codes"), (k_scales, "k_scales"), (v_codes, "v_codes"), (v_scales, "v_scales")):
+        if t.dtype != torch.uint8:
+            raise TypeError("%s must be uint8, got %s" % (what, t.dtype))
+        if t.dim() != 4:
+            raise ValueError("%s has the shape [pages, heads, page, bytes of a row], got %s" % (what, tuple(t.shape)))
+    pages, heads, page, row = k_codes.shape
+    bits = load_library().mxq_format_bits(f)
+    dim = row * 8 // bits
+    srow = (pages, heads, page, dim // block if block > 0 else 0)
+    if v_codes.shape != k_codes.shape or k_scales.shape != srow or v_scales.shape != srow:
+        raise ValueError("the cache's buffers do not belong together: codes %s and %s, scales %s and %s, block %d" % (
+            tuple(k_codes.shape), tuple(v_codes.shape), tuple(k_scales.shape), tuple(v_scales.shape), block))
+    dev = k_codes.device
+    return _Cache(_on(k_codes, "k_codes", dev), _on(k_scales, "k_scales", dev), _on(v_codes, "v_codes", dev), _on(v_scales, "v_scales", dev),
+                  pages, page, heads, dim, f, block)
+
+
+def _ints(t: torch.Tensor, what: str, shape, device) -> int:
+    if t.dtype != torch.int32:
+        raise TypeError("%s must be int32, got %s" % (what, t.dtype))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have the shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+    return _on(t, what, device)
+
+
+def _batch(table, lengths, starts, device) -> _Batch:
+    if table.dim() != 2:
+        raise ValueError("table has the shape [batch, pages of the longest sequence], got %s" % (tuple(table.shape),))
+    n, width = table.shape
+    return _Batch(_ints(table, "table", (n, width), device), None if lengths is None else _ints(lengths, "lengths", (n,), device),
+                  None if starts is None else _ints(starts, "starts", (n + 1,), device), n, width)
+
+
+def _rows(t: torch.Tensor, what: str, shape, device) -> Tuple[_Rows, torch.Tensor]:
+    """A [tokens, heads, head_dim] tensor as the kernels take it: itself, or a contiguous copy where its last dimension is not
+    contiguous or its address or strides are no multiples of 32 bytes."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have the shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+    if not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor (libmxq has no CPU path)" % what)
+    if t.device != device:
+        raise ValueError("%s is on %s, the other tensors on %s" % (what, t.device, device))
+    size = t.element_size()
+    if t.stride(2) != 1 or t.stride(0) * size % 32 or t.stride(1) * size % 32 or t.stride(0) < 0 or t.stride(1) < 0 or t.data_ptr() % 32:
+        t = t.clone(memory_format=torch.contiguous_format)
+    return _Rows(t.data_ptr(), t.stride(0), t.stride(1)), t
+
+
+def cache_write(k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor, v_scales: torch.Tensor,
+                table: torch.Tensor, lengths: torch.Tensor, fmt: str, block: int = 32, starts: Optional[torch.Tensor] = None,
+                stream=None) -> None:
+    """mxq_cache_write: quantizes the new tokens' keys and values [tokens, heads, head_dim] into their pages of a cache (``make_cache``'s
+    buffers).  ``table`` [batch, width], ``lengths`` [batch] (the new tokens counted) and ``starts`` [batch + 1] are int32 tensors on the
+    device; without ``starts`` row b is sequence b's one new token.  Any strides (rows that are no multiples of 32 bytes apart are copied
+    first).  Two sequences of a call must not write to the same place."""
+    L = load_library()
+    dev = k_codes.device
+    with _Place(dev, stream):
+        c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, lengths, starts, dev)
+        if k.dim() != 3 or k.dtype != v.dtype:
+            raise ValueError("cache_write takes k and v [tokens, heads, head_dim] of one type")
+        shape = (k.shape[0], c.heads, c.head_dim)
+        kr, k = _rows(k, "k", shape, dev)
+        vr, v = _rows(v, "v", shape, dev)
+        _check(L.mxq_cache_write(ctypes.byref(c), ctypes.byref(b), ctypes.byref(kr), ctypes.byref(vr), _dtype_id(k), shape[0], _stream(None)),
+               "mxq_cache_write")
+
+
+def cache_read(k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor, v_scales: torch.Tensor, table: torch.Tensor,
+               starts: torch.Tensor, total: int, fmt: str, block: int = 32, dtype: torch.dtype = torch.bfloat16,
+               out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """mxq_cache_read: keys and values, [total, heads, head_dim] each, of the first starts[b + 1] - starts[b] tokens of every sequence, in
+    rows starts[b] ...  ``out`` (a pair): rows behind starts[batch] are left as they were."""
+    L = load_library()
+    dev = k_codes.device
+    if total < 0:
+        raise ValueError("negative size")
+    with _Place(dev, stream):
+        c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, None, starts, dev)
+        shape = (total, c.heads, c.head_dim)
+        if out is None:
+            out = (torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev))
+        k, v = out
+        if tuple(k.shape) != shape or tuple(v.shape) != shape or k.dtype != v.dtype:
+            raise ValueError("out holds two tensors of the shape %s and one type" % (shape,))
+        _check(L.mxq_cache_read(ctypes.byref(c), ctypes.byref(b), total, _on(k, "out[0]", dev), _on(v, "out[1]", dev), _dtype_id(k), _stream(None)),
+               "mxq_cache_read")
+    return k, v
+
+
+def cache_attention_workspace_bytes(tokens: int, q_heads: int, batch: int, width: int, page: int, heads: int, head_dim: int,
+                                    dtype: torch.dtype = torch.bfloat16) -> int:
+    """Bytes of ``cache_attention``'s workspace for `tokens` queries of `batch` sequences with tables of `width` pages (0: refused)."""
+    c = _Cache(None, None, None, None, 0, page, heads, head_dim, FORMATS["e4m3"], 32)
+    b = _Batch(None, None, 1, batch, width)
+    return load_library().mxq_cache_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(b), q_heads, F32 if dtype == torch.float32 else BF16, tokens)
+
+
+def cache_attention(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor, v_scales: torch.Tensor,
+                    table: torch.Tensor, lengths: torch.Tensor, fmt: str, block: int = 32, starts: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None, causal: bool = True, window: int = 0, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """mxq_cache_attention: softmax(scale q K^T) V of the new tokens' queries q [tokens, q_heads, head_dim] over their sequences' cached
+    tokens, K and V as the cache's codes stand for them; q_heads is a multiple of the cache's heads, query head j uses head
+    j // (q_heads // heads).  ``table``, ``lengths`` and ``starts`` as in ``cache_write``; scale: 1 / sqrt(head_dim) by default; causal: a
+    query sees the tokens up to its own, with ``window`` only the last so many of them; lse: a float32 tensor [tokens, q_heads] for the
+    logarithms of the softmax's sums.  ``workspace`` (uint8, ``cache_attention_workspace_bytes``) saves the allocation of one per call; calls that
+    can overlap on the GPU must not share it.  A query that sees nothing gives zeros.  For serving: the result has no gradient."""
+    L = load_library()
+    dev = k_codes.device
+    with _Place(dev, stream):
+        c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, lengths, starts, dev)
+        if q.dim() != 3 or q.shape[2] != c.head_dim:
+            raise ValueError("q has the shape [tokens, q_heads, %d], got %s" % (c.head_dim, tuple(q.shape)))
+        if window < 0:
+            raise ValueError("negative size")
+        tokens, q_heads = q.shape[:2]
+        dt = _dtype_id(q)
+        qr, q = _rows(q.detach(), "q", q.shape, dev)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        elif out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out must have q's shape and type")
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2]):
+            raise ValueError("lse is float32 of the shape [tokens, q_heads]")
+        if workspace is None:
+            workspace = torch.empty(L.mxq_cache_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(b), q_heads, dt, tokens), dtype=torch.uint8,
+                                    device=dev)
+        _check(L.mxq_cache_attention(ctypes.byref(c), ctypes.byref(b), ctypes.byref(qr), q_heads, dt, tokens,
+                                     1 / math.sqrt(c.head_dim) if scale is None else scale, int(bool(causal)), window, _on(out, "out", dev),
+                                     None if lse is None else _on(lse, "lse", dev), _operand(workspace, "workspace", 0, dev), workspace.numel(),
+                                     _stream(None)), "mxq_cache_attention")
     return out

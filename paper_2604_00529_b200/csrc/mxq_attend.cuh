@@ -1,0 +1,904 @@
+// Attention over a paged cache of MX codes: out = sum over t of softmax_t(scale q . K^[t]) V^[t], the codes read once.
+//
+// A row is a query head of a token; the rows that use one cache head read the same keys and values and are worked on together, up
+// to 8 NT of them at a time.  An item is one such group of rows, one cache head and the range of keys that its rows see, cut into tiles of
+// 64 keys.  All items' tiles, laid end to end, are shared out evenly among the CTAs, whatever the lengths are: a CTA works on a run of
+// tiles that may begin and end inside an item, and the parts of such an item are added up, in order, by a second kernel.
+//
+// A warp takes 16 keys at a time, with the maximum and the sum of a softmax carried along:
+//   S^T = K Q^T     keys are the 16 rows of the matrix step, the group's rows its 8 columns; codes become FP16, exactly, and
+//                   the sum over a block of 32 is multiplied by its scale in FP32
+//   P = 2^(S - m)   m is moved only when a score exceeds it by 2^12; FP16 holds what lies below
+//   O^T += V^T P^T  V^T by the transposing load of shared memory; the scales, which belong to (key, block) here, are multiplied
+//                   into P, relative to the largest seen so far of the block of dimensions
+// FP32 rows enter as two FP16 parts, neighbouring columns of the same step, and so do their P.
+#pragma once
+#include "mxq_attend_items.cuh"
+#include "mxq_kernels.cuh"
+#include "mxq_launch.h"
+#include "mxq_product.cuh"
+#include "mxq_tensor.cuh"
+
+namespace mxq {
+namespace {
+
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kStep = 16;                                   // keys that a warp takes at a time
+constexpr int kStagesMax = 6;
+constexpr float kBias = 8.f;                                // P is held as 2^kBias times itself: more of FP16's range below 1
+constexpr float kSlack = 12.f;                              // m moves when 2^kSlack would be exceeded
+constexpr int kScaleSlack = 3;                              // and a block's reference scale when 2^kScaleSlack would be
+
+// ---- codes to FP16 pairs --------------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t add_f16(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t mul_f16(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ float f16_lo(uint32_t v)
+{
+    float f;
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %1; cvt.f32.f16 %0, l; }" : "=f"(f) : "r"(v));
+    return f;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
+{
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+__device__ __forceinline__ void e2m1_word(uint32_t w, uint32_t& b0, uint32_t& b1, uint32_t& b2, uint32_t& b3)
+{
+    asm("{ .reg .b8 a, b, c, d; mov.b32 {a, b, c, d}, %4;\n"
+        "cvt.rn.f16x2.e2m1x2 %0, a; cvt.rn.f16x2.e2m1x2 %1, b; cvt.rn.f16x2.e2m1x2 %2, c; cvt.rn.f16x2.e2m1x2 %3, d; }"
+        : "=r"(b0), "=r"(b1), "=r"(b2), "=r"(b3) : "r"(w));
+}
+__device__ __forceinline__ void e4m3_word(uint32_t w, uint32_t& lo, uint32_t& hi)
+{
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+// Nibbles i and i + 4 of a word (MXINT4): under the exponent of 1024 a nibble, its sign bit flipped, is 1024 + 8 + its value.
+__device__ __forceinline__ void int4_word(uint32_t w, uint32_t (&o)[4])
+{
+    const uint32_t h = w >> 8;
+    o[0] = add_f16((w & 0x000F000Fu) ^ 0x64086408u, 0xE408E408u);                       // - 1032
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(o[1]) : "r"((w & 0x00F000F0u) ^ 0x64806480u), "r"(0x2C002C00u), "r"(0xD480D480u));   // / 16 - 72
+    o[2] = add_f16((h & 0x000F000Fu) ^ 0x64086408u, 0xE408E408u);
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(o[3]) : "r"((h & 0x00F000F0u) ^ 0x64806480u), "r"(0x2C002C00u), "r"(0xD480D480u));
+}
+// Two bytes of a word (MXINT8), the word's sign bits flipped: under the exponent of 1024 a byte is 1024 + 128 + its value.
+template <uint32_t SEL>
+__device__ __forceinline__ uint32_t int8_pair(uint32_t flipped) { return add_f16(__byte_perm(flipped, 0x64646464u, SEL), 0xE480E480u); }
+
+// K: the word that a lane holds of a row, as pairs of neighbouring elements (MXINT4: elements i and i + 4).
+template <int FMT, int NP>
+__device__ __forceinline__ void key_pairs(uint32_t w, uint32_t (&o)[NP])
+{
+    if constexpr (FMT == MXQ_FP4_E2M1) e2m1_word(w, o[0], o[1], o[2], o[3]);
+    else if constexpr (FMT == MXQ_INT4) int4_word(w, o);
+    else if constexpr (FMT == MXQ_FP8_E4M3) e4m3_word(w, o[0], o[1]);
+    else {
+        const uint32_t x = w ^ 0x80808080u;
+        o[0] = int8_pair<0x4140>(x);
+        o[1] = int8_pair<0x4342>(x);
+    }
+}
+
+// V: x holds 16 bits of key 2t in its lower half and of key 2t + 1 in its upper one, y of keys 2t + 8 and 2t + 9: pairs of two keys'
+// codes of the same dimension, X of x and Y of y, dimensions in order.
+template <int FMT, int NP>
+__device__ __forceinline__ void value_pairs(uint32_t x, uint32_t y, uint32_t (&X)[NP], uint32_t (&Y)[NP])
+{
+    if constexpr (FMT == MXQ_FP4_E2M1) {
+        const uint32_t u = __byte_perm(x, y, 0x5410), w = __byte_perm(x, y, 0x7632);
+        e2m1_word((u & 0x0F0F0F0Fu) | ((w << 4) & 0xF0F0F0F0u), X[0], X[2], Y[0], Y[2]);
+        e2m1_word(((u >> 4) & 0x0F0F0F0Fu) | (w & 0xF0F0F0F0u), X[1], X[3], Y[1], Y[3]);
+    } else if constexpr (FMT == MXQ_INT4) {
+        int4_word(x, X);
+        int4_word(y, Y);
+    } else if constexpr (FMT == MXQ_FP8_E4M3) {
+        e4m3_word(__byte_perm(x, x, 0x3120), X[0], X[1]);
+        e4m3_word(__byte_perm(y, y, 0x3120), Y[0], Y[1]);
+    } else {
+        const uint32_t a = x ^ 0x80808080u, b = y ^ 0x80808080u;
+        X[0] = int8_pair<0x4240>(a);
+        X[1] = int8_pair<0x4341>(a);
+        Y[0] = int8_pair<0x4240>(b);
+        Y[1] = int8_pair<0x4341>(b);
+    }
+}
+
+// The top bit of each byte that is an E4M3 NaN code.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+
+__device__ __forceinline__ void ldmatrix4(uint32_t at, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t at, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(at) : "memory");
+}
+
+// 16 bytes to shared memory, asynchronously; zeros where `in` is false.
+__device__ __forceinline__ void copy16(uint32_t to, const uint8_t* from, bool in)
+{
+    uint32_t size = in ? 16u : 0u;
+    MXQ_CHECKED(from, size, size = 0)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(from), "r"(size) : "memory");
+}
+
+__device__ __forceinline__ float lds_f32(uint32_t at)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds_u8(uint32_t at)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+template <int N>
+__device__ __forceinline__ void lds_words(uint32_t at, uint32_t (&v)[N])      // N = 2, 4, 8
+{
+    if constexpr (N == 2) {
+        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(at) : "memory");
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]) : "r"(at + i * 4) : "memory");
+    }
+}
+
+// ---- layout of shared memory ----------------------------------------------------------------------------------
+
+template <int FMT, int D, int NT>
+struct Shape {
+    static constexpr int bits = fmt_info(FMT).bits;
+    static constexpr int RB = D * bits / 8;                 // bytes of a row of codes
+    static constexpr int CPR = RB / 16;                     // its 16-byte chunks
+    static constexpr int NB = D / 32;                       // blocks of 32 elements
+    static constexpr int MT = D / 16;                       // 16-row tiles of V^T
+    static constexpr int NP = bits == 8 ? 2 : 4;            // pairs in a word of codes
+    // a warp's slot: a step's keys, values and scale bytes
+    static constexpr int k_at = 0, v_at = kStep * RB, ks_at = 2 * kStep * RB, vs_at = ks_at + kStep * NB, slot = vs_at + kStep * NB;
+    // tables of a warp's step: the keys' scales (FP32), the values' multipliers (FP16, pairs of keys)
+    static constexpr int kf_at = 0, vm_at = kStep * NB * 4, tables = vm_at + kStep * NB * 2;
+    static constexpr int q_row = D * 2 + (bits == 4 ? 16 : 32);       // padded: lanes of a read lie in different banks
+    static constexpr int q_bytes = 8 * NT * q_row;
+    static constexpr int ctas = NT == 4 ? 2 : NT * D <= 128 ? 4 : NT * D <= 256 ? 3 : 2;     // per SM, by registers
+    // steps of a warp under way to shared memory, and the one worked on: as many as the CTA's share of an SM holds
+    static constexpr int fixed = kWarps * tables + q_bytes + 8 * NT * 4;
+    static constexpr int fit = (227 * 1024 / ctas - 1536 - fixed) / (kWarps * slot);
+    static constexpr int stages = fit < kStagesMax ? fit : kStagesMax;
+    static constexpr int ring = stages * slot;
+    static constexpr int merge = kWarps * 8 * NT * (D + 2) * 4;       // the warps' results, in the ring's place
+    static constexpr int work = (kWarps * ring > merge ? kWarps * ring : merge);
+    static constexpr int total = work + fixed;
+    static constexpr bool q_in_registers = NT * MT * 2 <= 32;
+    static_assert(stages >= 2 && (total + 1536) * ctas <= 227 * 1024, "shared memory");
+
+    // Chunk c of row r lies at r * RB + (c ^ twist(r)) * 16: the eight rows that a matrix load reads at once are in different banks.
+    static __host__ __device__ constexpr int twist(int r) { return CPR >= 8 ? r & 7 : CPR == 4 ? (r >> 1) & 3 : (r >> 2) & 1; }
+};
+
+template <int FMT, int D, int NT, int PIECES>
+struct Attend {
+    using S = Shape<FMT, D, NT>;
+    static constexpr int NB = S::NB, MT = S::MT, NP = S::NP;
+    static constexpr bool has_nan = FMT == MXQ_FP8_E4M3;
+
+    const AttendArgs& p;
+    const int warp, lane, g, t;
+    uint32_t ring, tables, qs;                              // shared addresses: the warp's ring and tables, the CTA's rows
+    uint32_t twisted;                                       // a lane's part of its matrix loads' addresses
+    float acc[MT][NT][4], l[NT][2], m[NT][2], f[NT][2];
+    int vref;                                               // reference scale byte of block (lane >> 1) % NB
+    uint32_t q[S::q_in_registers ? NT * MT : 1][2];
+    // the item
+    int b, head, row0, rows;                                // rows: how many of the item are there
+    Sequence s;
+    int some_lo, some_hi, all_lo, all_hi;                   // keys that some row sees, that all rows see
+
+    __device__ __forceinline__ int column_row(int c) const { return min(row0 + c / PIECES, row0 + rows - 1); }
+
+    // -- a step's codes and scales on their way to shared memory
+
+    __device__ __forceinline__ void fetch(uint32_t slot, int key, bool wanted) const
+    {
+        if (wanted) {
+            const int page = ld_int(p.batch.table + (size_t)b * p.batch.width + (key >> p.cache.page_shift));
+            const bool ok = (unsigned)page < (unsigned)p.cache.pages;
+            const size_t row = ok ? ((((size_t)page * p.cache.heads + head) << p.cache.page_shift) | (key & ((1 << p.cache.page_shift) - 1))) : 0;
+            const int left = ok ? some_hi - key : 0;         // rows from here on that exist
+            constexpr int per = S::CPR / 2;                  // chunks of 16 rows per lane: 16 CPR / 32
+            constexpr int rows_apart = 32 / S::CPR;
+            const int r0 = lane / S::CPR, c = lane % S::CPR;
+#pragma unroll
+            for (int j = 0; j < per; ++j) {
+                const int r = r0 + j * rows_apart;
+                const uint32_t to = slot + r * S::RB + ((c ^ S::twist(r)) << 4);
+                const size_t from = (row + r) * S::RB + c * 16;
+                const bool in = r < left;
+                copy16(to + S::k_at, p.cache.kc + (in ? from : 0), in);
+                copy16(to + S::v_at, p.cache.vc + (in ? from : 0), in);
+            }
+            const int nb = D >> p.cache.block_shift;         // scale bytes of a row: 16 rows are nb chunks
+            if (lane < 2 * nb) {
+                const bool v = lane >= nb;
+                const int at = (v ? lane - nb : lane) * 16;
+                const uint8_t* base = v ? p.cache.vs : p.cache.ks;
+                copy16(slot + (v ? S::vs_at : S::ks_at) + at, base + (ok ? row * nb + at : 0), ok);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+
+    // -- one step
+
+    template <bool CAREFUL>
+    __device__ __forceinline__ void step(uint32_t slot, int key)
+    {
+        const int bs = p.cache.block_shift - 5, nb = D >> p.cache.block_shift;
+        // the scales of the step, shared out among the lanes
+        constexpr int per = kStep * NB / 32;
+        uint32_t vb[per];
+        bool raise = false, poison = false;
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            const int e = lane + 32 * i, kk = e / NB, kd = e % NB;
+            const uint32_t kb = lds_u8(slot + S::ks_at + kk * nb + (kd >> bs));
+            const float kv = kb == 255u ? __uint_as_float(0x7FC00000u) : scale_value(kb);
+            asm volatile("st.shared.f32 [%0], %1;" :: "r"(tables + S::kf_at + e * 4), "f"(kv) : "memory");
+            const int vk = (e >> 1) / NB * 2 + (e & 1), vd = (e >> 1) % NB;
+            vb[i] = lds_u8(slot + S::vs_at + vk * nb + (vd >> bs));
+            if (CAREFUL && (key + vk < some_lo || key + vk >= some_hi)) vb[i] = 256u;         // seen by no row
+            raise |= (int)vb[i] > vref + kScaleSlack && vb[i] < 255u;
+            poison |= vb[i] == 255u;
+        }
+        if (__any_sync(0xFFFFFFFFu, raise)) raise_reference(vb);
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            const int e = lane + 32 * i;
+            const float mult = vb[i] == 256u ? 0.f : __uint_as_float((uint32_t)max((int)vb[i] - vref + 127, 0) << 23);
+            uint32_t h = pack_f16(mult, 0.f);
+            if (vb[i] == 255u) h = 0x7E00u;
+            asm volatile("st.shared.u16 [%0], %1;" :: "r"(tables + S::vm_at + e * 2), "h"((unsigned short)h) : "memory");
+        }
+        if (CAREFUL) poison = __any_sync(0xFFFFFFFFu, poison);
+        __syncwarp();
+
+        // scores: 16 keys x 8 NT columns
+        float sc[NT][4] = {};
+        {
+            uint32_t kf_lo[NB], kf_hi[NB];
+            lds_words<NB>(tables + S::kf_at + g * NB * 4, kf_lo);
+            lds_words<NB>(tables + S::kf_at + (g + 8) * NB * 4, kf_hi);
+            constexpr int per_load = S::bits == 4 ? 2 : 1;   // blocks of 32 in two chunks
+#pragma unroll
+            for (int c = 0; c < S::CPR; c += 2) {
+                uint32_t w[2][2];                            // [chunk][row g, row g + 8]
+                ldmatrix4(slot + S::k_at + (twisted ^ (c << 4)), w[0][0], w[0][1], w[1][0], w[1][1]);
+#pragma unroll
+                for (int h = 0; h < per_load; ++h) {
+                    const int blk = S::bits == 4 ? c + h : c / 2;
+                    uint32_t a[2][4];                        // [row g, row g + 8][pairs of the block]
+                    if constexpr (S::bits == 4) {
+                        key_pairs<FMT>(w[h][0], a[0]);
+                        key_pairs<FMT>(w[h][1], a[1]);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            uint32_t x[2], y[2];
+                            key_pairs<FMT>(w[0][r], x);
+                            key_pairs<FMT>(w[1][r], y);
+                            a[r][0] = x[0];
+                            a[r][1] = x[1];
+                            a[r][2] = y[0];
+                            a[r][3] = y[1];
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t qb[4];
+                        q_block(n, blk, qb);
+                        float d[4] = {};
+                        F16Mma::mma(d, a[0][0], a[1][0], a[0][1], a[1][1], qb[0], qb[1]);
+                        F16Mma::mma(d, a[0][2], a[1][2], a[0][3], a[1][3], qb[2], qb[3]);
+                        const float lo = __uint_as_float(kf_lo[blk]), hi = __uint_as_float(kf_hi[blk]);
+                        sc[n][0] = fmaf(d[0], lo, sc[n][0]);
+                        sc[n][1] = fmaf(d[1], lo, sc[n][1]);
+                        sc[n][2] = fmaf(d[2], hi, sc[n][2]);
+                        sc[n][3] = fmaf(d[3], hi, sc[n][3]);
+                    }
+                }
+            }
+        }
+        // weights
+        uint32_t pb[NT][2], seen[CAREFUL ? NT : 1][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if constexpr (PIECES == 2) {                     // the two parts' columns are one row's
+                sc[n][0] = sc[n][1] = sc[n][0] + sc[n][1];
+                sc[n][2] = sc[n][3] = sc[n][2] + sc[n][3];
+            }
+            if constexpr (CAREFUL) {
+                uint32_t vis[2] = {0, 0};
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int row = column_row(8 * n + 2 * t + j), lo = row_lo(p, s, row), hi = row_hi(p, s, row);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int at = key + g + 8 * h;
+                        const bool on = at >= lo && at < hi;
+                        if (!on) sc[n][2 * h + j] = __uint_as_float(0xFF800000u);
+                        vis[h] |= (on ? 0x3C00u : 0u) << (16 * j);
+                    }
+                }
+                seen[n][0] = vis[0];
+                seen[n][1] = vis[1];
+                // (a factor of 0 or NaN must not make NaN of what is hidden)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sc[n][j] = sc[n][j] == __uint_as_float(0xFF800000u) ? sc[n][j] : sc[n][j] * f[n][j & 1];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sc[n][j] *= f[n][j & 1];
+            }
+        }
+        bool over = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) over |= sc[n][j] > m[n][j & 1] + kSlack;
+        if (__any_sync(0xFFFFFFFFu, over)) raise_maximum(sc);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = exp2_approx(sc[n][j] - m[n][j & 1]);
+            l[n][0] += e[0] + e[2];
+            if constexpr (PIECES == 1) {
+                l[n][1] += e[1] + e[3];
+                pb[n][0] = transpose8x8(pack_f16(e[0], e[1]));
+                pb[n][1] = transpose8x8(pack_f16(e[2], e[3]));
+            } else {
+                const uint32_t a = pack_f16(e[0], 0.f), c = pack_f16(e[2], 0.f);
+                pb[n][0] = transpose8x8(a | pack_f16(0.f, e[0] - f16_lo(a)));
+                pb[n][1] = transpose8x8(c | pack_f16(0.f, e[2] - f16_lo(c)));
+            }
+        }
+        // O^T += V^T P^T
+        {
+            uint32_t vm_lo[NB], vm_hi[NB];                   // keys 2t, 2t + 1 and 2t + 8, 2t + 9
+            lds_words<NB>(tables + S::vm_at + t * NB * 4, vm_lo);
+            lds_words<NB>(tables + S::vm_at + (t + 4) * NB * 4, vm_hi);
+            uint32_t nan_lo[CAREFUL ? NB : 1], nan_hi[CAREFUL ? NB : 1], any_nan = 0;
+            if constexpr (CAREFUL) {                         // poisoned blocks: flags in the place of NaN
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    nan_lo[i] = take_nan(vm_lo[i]);
+                    nan_hi[i] = take_nan(vm_hi[i]);
+                    any_nan |= nan_lo[i] | nan_hi[i];
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < S::CPR; c += 2) {
+                uint32_t w[2][2];                            // [chunk][keys 0 - 7, keys 8 - 15]
+                ldmatrix4_trans(slot + S::v_at + (twisted ^ (c << 4)), w[0][0], w[0][1], w[1][0], w[1][1]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int blk = S::bits == 4 ? c + h : c / 2;
+                    if constexpr (CAREFUL && has_nan) {
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const uint32_t bad = nan_bytes(w[h][k]);
+                            any_nan |= bad;
+                            w[h][k] &= ~((bad >> 7) * 255u);
+                        }
+                    }
+                    uint32_t X[NP], Y[NP];
+                    value_pairs<FMT>(w[h][0], w[h][1], X, Y);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint32_t b0 = mul_f16(pb[n][0], vm_lo[blk]), b1 = mul_f16(pb[n][1], vm_hi[blk]);
+#pragma unroll
+                        for (int j = 0; j < NP / 2; ++j)
+                            F16Mma::mma(acc[(c + h) * (NP / 2) + j][n], X[2 * j], X[2 * j + 1], Y[2 * j], Y[2 * j + 1], b0, b1);
+                    }
+                }
+            }
+            if constexpr (CAREFUL) {
+                if (__any_sync(0xFFFFFFFFu, any_nan != 0)) spread_nan(slot, seen, nan_lo, nan_hi);
+            }
+        }
+        (void)poison;
+    }
+
+    // FP16 NaN halves of v become zeros and are flagged as ones (0x3C00) in the result.
+    static __device__ __forceinline__ uint32_t take_nan(uint32_t& v)
+    {
+        const uint32_t bit = (v >> 13) & (v >> 14) & 0x00010001u;      // multipliers stay below 2^9: bits 13 and 14 are NaN's
+        v &= ~(bit * 0xFFFFu);
+        return bit * 0x3C00u;
+    }
+
+    // Accumulators of dimensions in which a key that their row sees holds a NaN become NaN: counts such keys by matrix steps.
+    __device__ __forceinline__ void spread_nan(uint32_t slot, const uint32_t (&seen)[NT][2], const uint32_t (&nan_lo)[NB], const uint32_t (&nan_hi)[NB])
+    {
+        uint32_t vis[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            vis[n][0] = transpose8x8(seen[n][0]);
+            vis[n][1] = transpose8x8(seen[n][1]);
+        }
+#pragma unroll
+        for (int c = 0; c < S::CPR; c += 2) {
+            uint32_t w[2][2];
+            ldmatrix4_trans(slot + S::v_at + (twisted ^ (c << 4)), w[0][0], w[0][1], w[1][0], w[1][1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int blk = S::bits == 4 ? c + h : c / 2;
+#pragma unroll
+                for (int j = 0; j < NP / 2; ++j) {
+                    uint32_t a[4] = {nan_lo[blk], nan_lo[blk], nan_hi[blk], nan_hi[blk]};
+                    if constexpr (has_nan) {
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const uint32_t bad = nan_bytes(w[h][k]);
+                            a[2 * k] |= ((bad >> 7) & 0x00010001u) * 0x3C00u;
+                            a[2 * k + 1] |= ((bad >> 15) & 0x00010001u) * 0x3C00u;
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float d[4] = {};
+                        F16Mma::mma(d, a[0], a[1], a[2], a[3], vis[n][0], vis[n][1]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (d[i] > 0.f) acc[(c + h) * (NP / 2) + j][n][i] = __uint_as_float(0x7FC00000u);
+                    }
+                }
+            }
+        }
+    }
+
+    // The columns' maxima moved up to the step's scores.
+    __device__ __forceinline__ void raise_maximum(const float (&sc)[NT][4])
+    {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float top = fmaxf(sc[n][j], sc[n][2 + j]);
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                const float to = fmaxf(m[n][j], top - kBias), by = exp2_approx(m[n][j] - to);
+                m[n][j] = to;
+                l[n][j] *= by;
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    acc[i][n][j] *= by;
+                    acc[i][n][2 + j] *= by;
+                }
+            }
+    }
+
+    // Reference scales moved up to the step's largest ones (vb: the bytes of the lane's block).
+    template <int PER>
+    __device__ __forceinline__ void raise_reference(const uint32_t (&vb)[PER])
+    {
+        int top = -1000;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) top = max(top, vb[i] < 255u ? (int)vb[i] : -1000);
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+#pragma unroll
+        for (int o = 2 * NB; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        const int to = top > vref + kScaleSlack ? top : vref;
+        const float by = __uint_as_float((uint32_t)max(vref - to + 127, 0) << 23);      // (2^-127 and less: nothing)
+        vref = to;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const float of = __shfl_sync(0xFFFFFFFFu, by, 2 * i);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[2 * i + k][n][j] *= of;
+        }
+    }
+
+    // -- rows
+
+    // The step operands of block blk and column group n: four pairs of column g.
+    __device__ __forceinline__ void q_block(int n, int blk, uint32_t (&o)[4]) const
+    {
+        if constexpr (S::q_in_registers) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                o[2 * i] = q[n * MT + 2 * blk + i][0];
+                o[2 * i + 1] = q[n * MT + 2 * blk + i][1];
+            }
+        } else {
+            load_q_block(n, blk, o);
+        }
+    }
+    __device__ __forceinline__ void load_q_block(int n, int blk, uint32_t (&o)[4]) const
+    {
+        const uint32_t at = qs + (8 * n + g) * S::q_row + blk * 64;
+        if constexpr (S::bits == 4) {
+            lds_words<4>(at + t * 16, o);
+        } else {
+            uint32_t x[2], y[2];
+            lds_words<2>(at + t * 8, x);
+            lds_words<2>(at + 32 + t * 8, y);
+            o[0] = x[0];
+            o[1] = x[1];
+            o[2] = y[0];
+            o[3] = y[1];
+        }
+    }
+
+    // The item's rows to shared memory as FP16 parts, each row times the power of two that brings its largest element to
+    // [2^14, 2^15): BF16's eight bits fit FP16's eleven, down to 2^-31 of the largest.  `factors` get what takes that back.
+    __device__ __forceinline__ void load_rows(uint32_t factors) const
+    {
+        constexpr int per = D / 32;
+        for (int c = warp; c < 8 * NT; c += kWarps) {
+            const int r = c / PIECES, row = row0 + r;
+            float v[per];
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < per; ++i) v[i] = 0.f;
+            if (r < rows) {
+                const uint8_t* at = p.q + (size_t)(s.first + row / p.group) * p.q_token + (size_t)(head * p.group + row % p.group) * p.q_head;
+                if constexpr (PIECES == 2) {
+#pragma unroll
+                    for (int i = 0; i < per; ++i) v[i] = __uint_as_float(ld_u32(at + (lane * per + i) * 4));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < per; i += 2) {
+                        const uint32_t x = ld_u32(at + (lane * per + i) * 2);
+                        v[i] = __uint_as_float(x << 16);
+                        v[i + 1] = __uint_as_float(x & 0xFFFF0000u);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < per; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+            top = __reduce_max_sync(0xFFFFFFFFu, top) >> 23;
+            const int up = 127 + 14 - (int)max(top, 1u), half = up / 2;
+            const float by0 = __uint_as_float((uint32_t)(127 + half) << 23), by1 = __uint_as_float((uint32_t)(127 + up - half) << 23);
+            const float back0 = __uint_as_float((uint32_t)(127 - half) << 23), back1 = __uint_as_float((uint32_t)(127 - up + half) << 23);
+#pragma unroll
+            for (int i = 0; i < per; ++i) {
+                const float x = v[i] * by0 * by1;
+                uint32_t h = pack_f16(x, 0.f);
+                if (PIECES == 2 && c % 2 == 1) h = pack_f16(x - f16_lo(h), 0.f);
+                int e = lane * per + i;                      // MXINT4's pairs are elements i and i + 4 of eight
+                if constexpr (FMT == MXQ_INT4) e = (e & ~7) | (e & 3) << 1 | ((e >> 2) & 1);
+                asm volatile("st.shared.u16 [%0], %1;" :: "r"(qs + c * S::q_row + e * 2), "h"((unsigned short)h) : "memory");
+            }
+            if (lane == 0) {
+                float back = p.scale * back0 * back1;
+                if (top == 255u) back = __uint_as_float(0x7FC00000u);
+                asm volatile("st.shared.f32 [%0], %1;" :: "r"(factors + c * 4), "f"(back) : "memory");
+            }
+        }
+    }
+
+    // -- a run of keys [from, to) of the item, from a multiple of kTile on
+
+    __device__ __forceinline__ void run(int from, int to, uint32_t factors)
+    {
+        load_rows(factors);
+        int key = from + warp * kStep;
+        constexpr int stride = kWarps * kStep;
+#pragma unroll
+        for (int i = 0; i < S::stages - 1; ++i) fetch(ring + i * S::slot, key + i * stride, key + i * stride < to);
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                f[n][j] = lds_f32(factors + (8 * n + 2 * t + j) * 4);
+                m[n][j] = kNone;
+                l[n][j] = 0.f;
+            }
+        if constexpr (S::q_in_registers) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int blk = 0; blk < NB; ++blk) {
+                    uint32_t o[4];
+                    load_q_block(n, blk, o);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        q[n * MT + 2 * blk + i][0] = o[2 * i];
+                        q[n * MT + 2 * blk + i][1] = o[2 * i + 1];
+                    }
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][n][j] = 0.f;
+        vref = -1000;
+        int slot = 0, next = S::stages - 1;
+        for (; key < to; key += stride) {
+            const int ahead = key + (S::stages - 1) * stride;
+            fetch(ring + next * S::slot, ahead, ahead < to);
+            asm volatile("cp.async.wait_group %0;" :: "n"(S::stages - 1) : "memory");
+            __syncwarp();
+            if (key + kStep > some_lo && key < some_hi && there(key)) {
+                if (key >= all_lo && key + kStep <= all_hi) step<false>(ring + slot * S::slot, key);
+                else step<true>(ring + slot * S::slot, key);
+            }
+            __syncwarp();
+            slot = slot + 1 == S::stages ? 0 : slot + 1;
+            next = next + 1 == S::stages ? 0 : next + 1;
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();
+    }
+
+    __device__ __forceinline__ bool there(int key) const
+    {
+        const int page = ld_int(p.batch.table + (size_t)b * p.batch.width + (key >> p.cache.page_shift));
+        return (unsigned)page < (unsigned)p.cache.pages;
+    }
+
+    // -- the warps' results together: normalized sums and their weights in shared memory, then to the output or to a part
+
+    __device__ __forceinline__ void finish(float* area, bool whole, uint8_t* part)
+    {
+        constexpr int R = 8 * NT / PIECES;                   // rows of the tile
+        float* const o_at = area + warp * R * D;
+        float* const ml = area + kWarps * R * D;             // [warp][row][m, l]
+        float scales[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int byte = __shfl_sync(0xFFFFFFFFu, vref, 2 * i);
+            scales[i] = scale_value((uint32_t)max(byte, 0));
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 3 - PIECES; ++j) {
+                float sum = l[n][j];
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                const int r = PIECES == 1 ? 8 * n + 2 * t + j : 4 * n + t;
+                if (g == 0) {
+                    ml[(warp * R + r) * 2] = m[n][j];
+                    ml[(warp * R + r) * 2 + 1] = sum;
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    float x = acc[i][n][j], y = acc[i][n][2 + j];
+                    if constexpr (PIECES == 2) {
+                        x += acc[i][n][1];
+                        y += acc[i][n][3];
+                    }
+                    const int d = S::bits == 4 ? (i >> 1) * 32 + 4 * g + (i & 1) * 2 : i * 16 + 2 * g;
+                    *reinterpret_cast<float2*>(o_at + r * D + d) = make_float2(x * inv * scales[i >> 1], y * inv * scales[i >> 1]);
+                }
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+            const int r = i / (D / 4), d = i % (D / 4) * 4;
+            float top = kNone;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[(w * R + r) * 2]);
+            float sum = 0.f, v[4] = {};
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float wt = ml[(w * R + r) * 2 + 1] * exp2_approx(ml[(w * R + r) * 2] - top);
+                const float4 x = *reinterpret_cast<const float4*>(area + (w * R + r) * D + d);
+                sum += wt;
+                v[0] += wt * x.x;
+                v[1] += wt * x.y;
+                v[2] += wt * x.z;
+                v[3] += wt * x.w;
+            }
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] *= inv;
+            if (whole) {
+                const int row = row0 + r;
+                write_row<PIECES>(p, (size_t)(s.first + row / p.group) * (p.cache.heads * p.group) + head * p.group + row % p.group, D, d, v, top, sum);
+            } else {
+                float* const to = reinterpret_cast<float*>(part);
+                MXQ_CHECKED(to + r * D + d, 16, continue)
+                *reinterpret_cast<float4*>(to + r * D + d) = make_float4(v[0], v[1], v[2], v[3]);
+                if (d == 0) {
+                    to[p.rows * D + 2 * r] = top;
+                    to[p.rows * D + 2 * r + 1] = sum;
+                }
+            }
+        }
+        __syncthreads();
+    }
+};
+
+// The run of a CTA: its first and one past its last tile, and the sequence that the first lies in.
+struct Plan {
+    long long total, from, to, base;                         // base: tiles in front of sequence b
+    int b, ctas;
+};
+
+__device__ __forceinline__ void make_plan(const AttendArgs& p, Plan& plan, long long (&warp_sum)[kWarps])
+{
+    const int per = (p.batch.batch + kThreads - 1) / kThreads, first = min((int)threadIdx.x * per, p.batch.batch), last = min(first + per, p.batch.batch);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long mine = 0;
+    for (int b = first; b < last; ++b) mine += sequence_tiles(p, sequence(p.batch, b, p.cache.page_shift)) * p.cache.heads;
+    long long before = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long up = __shfl_up_sync(0xFFFFFFFFu, before, o);
+        if (lane >= o) before += up;
+    }
+    if (lane == 31) warp_sum[warp] = before;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) before += warp_sum[w];
+        total += warp_sum[w];
+    }
+    before -= mine;
+    const int ctas = (int)min((long long)gridDim.x, max(total, 1ll));
+    const long long from = (int)blockIdx.x < ctas ? run_start(total, ctas, blockIdx.x) : total;
+    if (threadIdx.x == 0) {
+        plan.total = total;
+        plan.ctas = ctas;
+        plan.from = from;
+        plan.to = (int)blockIdx.x < ctas ? run_start(total, ctas, blockIdx.x + 1) : total;
+        plan.b = p.batch.batch;
+    }
+    __syncthreads();
+    if (from >= before && from < before + mine) {            // one thread's
+        int b = first;
+        for (; b < last; ++b) {
+            const long long n = sequence_tiles(p, sequence(p.batch, b, p.cache.page_shift)) * p.cache.heads;
+            if (from < before + n) break;
+            before += n;
+        }
+        plan.b = b;
+        plan.base = before;
+    }
+    __syncthreads();
+}
+
+template <int FMT, int D, int NT, int PIECES>
+__global__ void __launch_bounds__(kThreads, Shape<FMT, D, NT>::ctas)
+attend_kernel(const __grid_constant__ AttendArgs p)
+{
+    using S = Shape<FMT, D, NT>;
+    extern __shared__ __align__(1024) uint8_t shared[];
+    __shared__ Plan plan;
+    __shared__ long long warp_sum[kWarps];
+    pdl_acquire();
+    pdl_release();                                           // (the second kernel reads nothing before its own wait)
+    make_plan(p, plan, warp_sum);
+    const uint32_t base = smem_addr(shared);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Attend<FMT, D, NT, PIECES> a{p, warp, lane, lane >> 2, lane & 3};
+    a.ring = base + warp * S::ring;
+    a.tables = base + S::work + warp * S::tables;
+    a.qs = base + S::work + kWarps * S::tables;
+    const uint32_t factors = a.qs + S::q_bytes;
+    // matrix i of a load: keys 8 (i & 1) ..., chunk i >> 1; the lane gives the address of row lane % 8 of matrix lane / 8
+    a.twisted = (((lane >> 3) & 1) * 8 + (lane & 7)) * S::RB + (((lane >> 4) ^ S::twist(lane & 7)) << 4);
+    uint8_t* const parts = p.ws + (size_t)p.ctas * sizeof(PartMeta);
+    const size_t part = part_bytes(p.rows, D);
+
+    long long at = plan.from, seq_at = plan.base;
+    const long long to = plan.to;
+    int b = plan.b;
+    bool first = true;
+    if (at >= to && threadIdx.x == 0 && (int)blockIdx.x < plan.ctas) {
+        PartMeta* meta = reinterpret_cast<PartMeta*>(p.ws) + blockIdx.x;
+        *meta = PartMeta{at, at, at, plan.total, 0, 0, 0, 0};
+    }
+    while (at < to) {
+        const Sequence s = sequence(p.batch, b, p.cache.page_shift);
+        const long long per_head = sequence_tiles(p, s);
+        if (at - seq_at >= per_head * p.cache.heads) {
+            seq_at += per_head * p.cache.heads;
+            ++b;
+            continue;
+        }
+        const int head = (int)((at - seq_at) / per_head);
+        long long item = seq_at + per_head * head;           // the item's first tile
+        int r0 = 0, tiles;
+        for (;; r0 += p.rows, item += tiles) {
+            tiles = item_tiles(p, s, r0);
+            if (at < item + tiles) break;
+        }
+        const int rows = (int)min((long long)p.rows, (long long)s.n * p.group - r0);
+        const long long end = min(item + tiles, to);
+        a.b = b;
+        a.head = head;
+        a.row0 = r0;
+        a.rows = rows;
+        a.s = s;
+        a.some_lo = row_lo(p, s, r0);
+        a.some_hi = row_hi(p, s, r0 + rows - 1);
+        a.all_lo = row_lo(p, s, r0 + rows - 1);
+        a.all_hi = row_hi(p, s, r0);
+        const int key0 = a.some_lo / kTile * kTile;
+        const int from_key = key0 + (int)(at - item) * kTile, to_key = (int)min((long long)key0 + (end - item) * kTile, (long long)a.some_hi);
+        a.run(from_key, to_key, factors);
+        const bool whole = at == item && end == item + tiles;
+        if (first && threadIdx.x == 0) {
+            PartMeta* meta = reinterpret_cast<PartMeta*>(p.ws) + blockIdx.x;
+            bool ok = true;
+            MXQ_CHECKED(meta, sizeof(PartMeta), ok = false)
+            if (ok) *meta = PartMeta{at, item, item + tiles, plan.total, b, head, r0, rows};
+        }
+        a.finish(reinterpret_cast<float*>(shared), whole, parts + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * part);
+        first = false;
+        at = end;
+    }
+}
+
+// ---- launches -------------------------------------------------------------------------------------------------
+
+template <int FMT, int D, int NT, int PIECES>
+int run(const AttendArgs& p, cudaStream_t stream)
+{
+    using S = Shape<FMT, D, NT>;
+    static std::atomic<uint64_t> done{0};
+    auto kern = attend_kernel<FMT, D, NT, PIECES>;
+    if (int rc = allow_smem(reinterpret_cast<const void*>(kern), S::total, done)) return rc;
+    return launch_grid(kern, dim3((unsigned)p.ctas), kThreads, S::total, 1, stream, p);
+}
+
+template <int FMT, int D, int PIECES>
+int by_columns(int nt, const AttendArgs& p, cudaStream_t stream)
+{
+    if (nt == 1) return run<FMT, D, 1, PIECES>(p, stream);
+    if (nt == 2) return run<FMT, D, 2, PIECES>(p, stream);
+    if constexpr (D < 256) return run<FMT, D, 4, PIECES>(p, stream);
+    else return MXQ_ERR_SIZE;
+}
+
+template <int FMT, int PIECES>
+int by_dim(int dim, int nt, const AttendArgs& p, cudaStream_t stream)
+{
+    if (dim == 64) return by_columns<FMT, 64, PIECES>(nt, p, stream);
+    if (dim == 128) return by_columns<FMT, 128, PIECES>(nt, p, stream);
+    return by_columns<FMT, 256, PIECES>(nt, p, stream);
+}
+
+}  // namespace
+
+// The first kernel for a cache of format FMT: its `nt` column groups, 16- or 32-bit rows.
+template <int FMT>
+int launch_attend(int dim, int nt, int dtype, const AttendArgs& p, cudaStream_t stream)
+{
+    return dtype == MXQ_F32 ? by_dim<FMT, 2>(dim, nt, p, stream) : by_dim<FMT, 1>(dim, nt, p, stream);
+}
+
+}  // namespace mxq

@@ -1,0 +1,6 @@
+// The attention kernels over a cache of E4M3 codes (a unit of their own: formats compile side by side).
+#include "mxq_attend.cuh"
+
+namespace mxq {
+template int launch_attend<MXQ_FP8_E4M3>(int dim, int nt, int dtype, const AttendArgs& p, cudaStream_t stream);
+}

@@ -1,0 +1,87 @@
+// What the two kernels of mxq_cache_attention share: how rows and keys are cut into items and tiles, how runs of tiles are
+// shared out among CTAs, and how a row of the output is written.
+#pragma once
+#include "mxq_cache.cuh"
+#include "mxq_kernels.cuh"
+
+namespace mxq {
+namespace {
+
+constexpr int kTile = 64;                                   // keys: what is shared out among CTAs
+constexpr float kNone = -1e30f;                             // m of a row that has seen nothing (finite: -inf - kNone is no NaN)
+
+// ---- items ----------------------------------------------------------------------------------------------------
+
+// Keys that rows r0 ... r1 - 1 of a sequence see between them.
+struct Span {
+    int lo, hi;
+};
+
+__device__ __forceinline__ int row_hi(const AttendArgs& p, const Sequence& s, int row)
+{
+    if (!p.causal) return s.length;
+    return max(s.length - s.n + row / p.group + 1, 0);
+}
+__device__ __forceinline__ int row_lo(const AttendArgs& p, const Sequence& s, int row)
+{
+    return p.window ? max(s.length - s.n + row / p.group + 1 - p.window, 0) : 0;
+}
+
+__device__ __forceinline__ int item_tiles(const AttendArgs& p, const Sequence& s, int r0)
+{
+    const int last = (int)min((long long)r0 + p.rows, (long long)s.n * p.group) - 1;
+    const int lo = row_lo(p, s, r0) / kTile, hi = (row_hi(p, s, last) + kTile - 1) / kTile;
+    return max(hi - lo, 1);                                 // (an item that sees nothing still writes its zeros)
+}
+
+// Tiles of one head of a sequence.
+__device__ __forceinline__ long long sequence_tiles(const AttendArgs& p, const Sequence& s)
+{
+    const long long rows = (long long)s.n * p.group;
+    long long sum = 0;
+    for (long long r = 0; r < rows; r += p.rows) sum += item_tiles(p, s, (int)r);
+    return sum;
+}
+
+// What the second kernel needs of a CTA of the first: the tiles of the item that its run begins in.
+struct PartMeta {
+    long long from, item_from, item_to, total;              // this run's first tile, the item's first and one past its last, all tiles
+    int b, head, r0, rows;
+};
+
+__host__ __device__ inline size_t part_bytes(int rows, int dim) { return ((size_t)rows * (dim + 2) * 4 + 31) / 32 * 32; }
+
+__device__ __forceinline__ long long run_start(long long total, int ctas, int c)
+{
+    return total / ctas * c + total % ctas * c / ctas;
+}
+
+__device__ __forceinline__ float exp2_approx(float v)
+{
+    float d;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(v));
+    return d;
+}
+
+// Four elements of an output row, and the row's logarithm with the first of them.
+template <int PIECES>
+__device__ __forceinline__ void write_row(const AttendArgs& p, size_t row, int dim, int d, const float (&v)[4], float m, float l)
+{
+    if constexpr (PIECES == 2) {
+        float* to = reinterpret_cast<float*>(p.out) + row * dim + d;
+        MXQ_CHECKED(to, 16, return)
+        *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+        uint8_t* to = p.out + (row * dim + d) * 2;
+        MXQ_CHECKED(to, 8, return)
+        *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    }
+    if (d == 0 && p.lse) {
+        float* to = p.lse + row;
+        MXQ_CHECKED(to, 4, return)
+        *to = l == 0.f ? __uint_as_float(0xFF800000u) : (m + log2f(l)) * 0.6931471805599453f;
+    }
+}
+
+}  // namespace
+}  // namespace mxq

@@ -1811,6 +1811,38 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
 }
 
 
+// The codes of a lane unit of T::epl elements, scale byte sb, as 32 bytes of output.
+template <class F, class T, int NWI>
+__device__ __forceinline__ void widen_unit(const uint32_t (&w)[NWI], uint32_t sb, uint32_t (&out)[8])
+{
+    const float X = scale_value(min(sb, 254u));
+    static_for<T::epl / 2>([&](auto i) {
+        constexpr int I = 2 * decltype(i)::value;
+        const uint32_t c0 = get_code<F::bits, I>(w), c1 = get_code<F::bits, I + 1>(w);
+        float y0 = decode<F>(c0) * X;
+        float y1 = decode<F>(c1) * X;
+        // an E4M3 NaN code reconstructs to the canonical quiet NaN
+        bool n0 = false, n1 = false;
+        if constexpr (F::has_nan) {
+            n0 = (c0 & 0x7Fu) == 0x7Fu;
+            n1 = (c1 & 0x7Fu) == 0x7Fu;
+        }
+        if constexpr (T::size == 4) {
+            out[I] = n0 ? 0x7FC00000u : __float_as_uint(y0);
+            out[I + 1] = n1 ? 0x7FC00000u : __float_as_uint(y1);
+        } else {
+            uint32_t p = pack_bf16x2(y0, y1);
+            if (n0) p = (p & 0xFFFF0000u) | 0x7FC0u;
+            if (n1) p = (p & 0x0000FFFFu) | 0x7FC00000u;
+            out[I / 2] = p;
+        }
+    });
+    if (sb == 0xFFu) {                                        // poisoned block
+#pragma unroll
+        for (int j = 0; j < 8; ++j) out[j] = T::size == 4 ? 0x7FC00000u : 0x7FC07FC0u;
+    }
+}
+
 // A lane unit is 32 bytes of OUTPUT (16 BF16 or 8 FP32 elements), so that every store instruction
 // of a warp covers 1 KB of consecutive addresses; the codes of a unit are 2 x bits or bits bytes,
 // read with the widest access their alignment allows.  A unit never straddles a block (blocks are
@@ -1847,32 +1879,7 @@ __device__ __forceinline__ void dequantize_wide_tile(const uint8_t* __restrict__
     for (int u = 0; u < U; ++u) {
         const size_t unit = u0 + u * 32;
         uint32_t out[8];
-        const float X = scale_value(min(sb[u], 254u));
-        static_for<EPL / 2>([&](auto i) {
-            constexpr int I = 2 * decltype(i)::value;
-            const uint32_t c0 = get_code<F::bits, I>(w[u]), c1 = get_code<F::bits, I + 1>(w[u]);
-            float y0 = decode<F>(c0) * X;
-            float y1 = decode<F>(c1) * X;
-            // an E4M3 NaN code reconstructs to the canonical quiet NaN
-            bool n0 = false, n1 = false;
-            if constexpr (F::has_nan) {
-                n0 = (c0 & 0x7Fu) == 0x7Fu;
-                n1 = (c1 & 0x7Fu) == 0x7Fu;
-            }
-            if constexpr (T::size == 4) {
-                out[I] = n0 ? 0x7FC00000u : __float_as_uint(y0);
-                out[I + 1] = n1 ? 0x7FC00000u : __float_as_uint(y1);
-            } else {
-                uint32_t p = pack_bf16x2(y0, y1);
-                if (n0) p = (p & 0xFFFF0000u) | 0x7FC0u;
-                if (n1) p = (p & 0x0000FFFFu) | 0x7FC00000u;
-                out[I / 2] = p;
-            }
-        });
-        if (sb[u] == 0xFFu) {                                 // poisoned block
-#pragma unroll
-            for (int j = 0; j < 8; ++j) out[j] = T::size == 4 ? 0x7FC00000u : 0x7FC07FC0u;
-        }
+        widen_unit<F, T>(w[u], sb[u], out);
         if (unit < nunits) st256(dst + unit * 32, out);
     }
 }
