@@ -23,7 +23,7 @@ namespace mxq {
 namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
-constexpr int kStep = 16;                                   // keys that a warp takes at a time
+constexpr int kGroup = 16;                                  // keys of a matrix step
 constexpr int kStagesMax = 6;
 constexpr float kBias = 8.f;                                // P is held as 2^kBias times itself: more of FP16's range below 1
 constexpr float kSlack = 12.f;                              // m moves when 2^kSlack would be exceeded
@@ -125,27 +125,37 @@ __device__ __forceinline__ void value_pairs(uint32_t x, uint32_t y, uint32_t (&X
 // The top bit of each byte that is an E4M3 NaN code.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
+template <int AT>
 __device__ __forceinline__ void ldmatrix4(uint32_t at, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d)
 {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(at) : "memory");
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4 + %5];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(at), "n"(AT) : "memory");
 }
+template <int AT>
 __device__ __forceinline__ void ldmatrix4_trans(uint32_t at, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d)
 {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(at) : "memory");
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4 + %5];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(at), "n"(AT) : "memory");
 }
 
-// 16 bytes to shared memory, asynchronously; zeros where `in` is false.
-__device__ __forceinline__ void copy16(uint32_t to, const uint8_t* from, bool in)
+// 16 bytes to shared memory, asynchronously; copy16_some: only the first `size` of them, zeros behind.  (Offsets that are known here go
+// into the instructions.)
+template <int TO, int FROM>
+__device__ __forceinline__ void copy16(uint32_t to, const uint8_t* from)
 {
-    uint32_t size = in ? 16u : 0u;
-    MXQ_CHECKED(from, size, size = 0)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(from), "r"(size) : "memory");
+    MXQ_CHECKED(from + FROM, 16, return)
+    asm volatile("cp.async.cg.shared.global [%0 + %2], [%1 + %3], 16;" :: "r"(to), "l"(from), "n"(TO), "n"(FROM) : "memory");
+}
+template <int TO, int FROM>
+__device__ __forceinline__ void copy16_some(uint32_t to, const uint8_t* from, uint32_t size)
+{
+    MXQ_CHECKED(from + FROM, size, size = 0)
+    asm volatile("cp.async.cg.shared.global [%0 + %2], [%1 + %3], 16, %4;" :: "r"(to), "l"(from), "n"(TO), "n"(FROM), "r"(size) : "memory");
 }
 
+template <int AT = 0>
 __device__ __forceinline__ float lds_f32(uint32_t at)
 {
     float v;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared.f32 %0, [%1 + %2];" : "=f"(v) : "r"(at), "n"(AT) : "memory");
     return v;
 }
 __device__ __forceinline__ uint32_t lds_u8(uint32_t at)
@@ -154,16 +164,31 @@ __device__ __forceinline__ uint32_t lds_u8(uint32_t at)
     asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     return v;
 }
-template <int N>
-__device__ __forceinline__ void lds_words(uint32_t at, uint32_t (&v)[N])      // N = 2, 4, 8
+template <int N, int AT = 0>
+__device__ __forceinline__ void lds_words(uint32_t at, uint32_t (&v)[N])      // N = 1, 2, 4, 8
 {
-    if constexpr (N == 2) {
-        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(at) : "memory");
+    if constexpr (N == 1) {
+        asm volatile("ld.shared.u32 %0, [%1 + %2];" : "=r"(v[0]) : "r"(at), "n"(AT) : "memory");
+    } else if constexpr (N == 2) {
+        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2 + %3];" : "=r"(v[0]), "=r"(v[1]) : "r"(at), "n"(AT) : "memory");
     } else {
-#pragma unroll
-        for (int i = 0; i < N; i += 4)
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]) : "r"(at + i * 4) : "memory");
+        static_for<N / 4>([&](auto k) {
+            constexpr int I = 4 * decltype(k)::value;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4 + %5];" : "=r"(v[I]), "=r"(v[I + 1]), "=r"(v[I + 2]), "=r"(v[I + 3]) : "r"(at), "n"(AT + I * 4) : "memory");
+        });
     }
+}
+template <int AT>
+__device__ __forceinline__ void sts_u16(uint32_t at, uint32_t v)
+{
+    asm volatile("st.shared.u16 [%0 + %2], %1;" :: "r"(at), "h"((unsigned short)v), "n"(AT) : "memory");
+}
+
+// The first of a chain of matrix steps: sums from zero.
+__device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // ---- layout of shared memory ----------------------------------------------------------------------------------
@@ -176,10 +201,12 @@ struct Shape {
     static constexpr int NB = D / 32;                       // blocks of 32 elements
     static constexpr int MT = D / 16;                       // 16-row tiles of V^T
     static constexpr int NP = bits == 8 ? 2 : 4;            // pairs in a word of codes
+    // Keys that a warp takes at a time: two matrix steps where their codes are few, for one round of waiting, page lookup and votes.
+    static constexpr int groups = RB <= 64 && NT == 1 ? 2 : 1, step = groups * kGroup;
     // a warp's slot: a step's keys, values and scale bytes
-    static constexpr int k_at = 0, v_at = kStep * RB, ks_at = 2 * kStep * RB, vs_at = ks_at + kStep * NB, slot = vs_at + kStep * NB;
+    static constexpr int k_at = 0, v_at = step * RB, ks_at = 2 * step * RB, vs_at = ks_at + step * NB, slot = vs_at + step * NB;
     // tables of a warp's step: the keys' scales (FP32), the values' multipliers (FP16, pairs of keys)
-    static constexpr int kf_at = 0, vm_at = kStep * NB * 4, tables = vm_at + kStep * NB * 2;
+    static constexpr int kf_at = 0, vm_at = step * NB * 4, tables = vm_at + step * NB * 2;
     static constexpr int q_row = D * 2 + (bits == 4 ? 16 : 32);       // padded: lanes of a read lie in different banks
     static constexpr int q_bytes = 8 * NT * q_row;
     static constexpr int ctas = NT == 4 ? 2 : NT * D <= 128 ? 4 : NT * D <= 256 ? 3 : 2;     // per SM, by registers
@@ -201,7 +228,7 @@ struct Shape {
 template <int FMT, int D, int NT, int PIECES>
 struct Attend {
     using S = Shape<FMT, D, NT>;
-    static constexpr int NB = S::NB, MT = S::MT, NP = S::NP;
+    static constexpr int NB = S::NB, MT = S::MT, NP = S::NP, GROUPS = S::groups;
     static constexpr bool has_nan = FMT == MXQ_FP8_E4M3;
 
     const AttendArgs& p;
@@ -209,7 +236,7 @@ struct Attend {
     uint32_t ring, tables, qs;                              // shared addresses: the warp's ring and tables, the CTA's rows
     uint32_t twisted;                                       // a lane's part of its matrix loads' addresses
     float acc[MT][NT][4], l[NT][2], m[NT][2], f[NT][2];
-    int vref;                                               // reference scale byte of block (lane >> 1) % NB
+    int vref[NB * S::step / 32], vlim[NB * S::step / 32];   // reference scale bytes of the lane's blocks (make_tables), and what raises them
     uint32_t q[S::q_in_registers ? NT * MT : 1][2];
     // the item
     int b, head, row0, rows;                                // rows: how many of the item are there
@@ -220,214 +247,350 @@ struct Attend {
 
     // -- a step's codes and scales on their way to shared memory
 
-    __device__ __forceinline__ void fetch(uint32_t slot, int key, bool wanted) const
+    // Where the lane's chunks of keys and values and its chunk of scales would lie in page 0, and the bytes from page to page.
+    const uint8_t *k_lane, *v_lane, *s_lane;
+    uint32_t page_bytes, page_scales;
+    uint32_t to_codes, to_scales;                           // the same in a slot (chunks of j > 0: see fetch)
+    const int* pages_of;                                    // the sequence's page table
+    int page_next[GROUPS];                                  // the entries for the next fetch, on their way
+    uint32_t there;                                         // bit GROUPS i + h: group h of the step fetched i fetches ago has a page
+
+    __device__ __forceinline__ void place(int h)
     {
-        if (wanted) {
-            const int page = ld_int(p.batch.table + (size_t)b * p.batch.width + (key >> p.cache.page_shift));
-            const bool ok = (unsigned)page < (unsigned)p.cache.pages;
-            const size_t row = ok ? ((((size_t)page * p.cache.heads + head) << p.cache.page_shift) | (key & ((1 << p.cache.page_shift) - 1))) : 0;
-            const int left = ok ? some_hi - key : 0;         // rows from here on that exist
-            constexpr int per = S::CPR / 2;                  // chunks of 16 rows per lane: 16 CPR / 32
-            constexpr int rows_apart = 32 / S::CPR;
-            const int r0 = lane / S::CPR, c = lane % S::CPR;
+        const uint32_t nb = (uint32_t)D >> p.cache.block_shift;
+        const size_t rows_before = (size_t)h << p.cache.page_shift;
+        page_bytes = ((uint32_t)p.cache.heads << p.cache.page_shift) * S::RB;
+        page_scales = ((uint32_t)p.cache.heads << p.cache.page_shift) * nb;
+        k_lane = p.cache.kc + rows_before * S::RB + lane * 16;
+        v_lane = p.cache.vc + rows_before * S::RB + lane * 16;
+        const bool v = lane >= (int)nb;                     // 16 rows' scales are nb chunks
+        s_lane = (v ? p.cache.vs : p.cache.ks) + rows_before * nb + (v ? lane - nb : lane) * 16;
+        to_scales = (v ? S::vs_at + (lane - nb) * 16 : S::ks_at + lane * 16);
+    }
+    __device__ __forceinline__ void ask_page(int key, int to)
+    {
+        page_next[0] = ld_int(pages_of + (key >> p.cache.page_shift));
+        if constexpr (GROUPS == 2) {
+            page_next[1] = page_next[0];
+            if (p.cache.page_shift == 4 && key + kGroup < to) page_next[1] = ld_int(pages_of + (key >> 4) + 1);
+        }
+    }
+
+    // The step of `key`; the next one to be fetched is that of `after`.
+    __device__ __forceinline__ void fetch(uint32_t slot, int key, int after, int to)
+    {
+        there <<= GROUPS;
+        if (key < to) {
+            uint32_t page[GROUPS];
 #pragma unroll
-            for (int j = 0; j < per; ++j) {
-                const int r = r0 + j * rows_apart;
-                const uint32_t to = slot + r * S::RB + ((c ^ S::twist(r)) << 4);
-                const size_t from = (row + r) * S::RB + c * 16;
-                const bool in = r < left;
-                copy16(to + S::k_at, p.cache.kc + (in ? from : 0), in);
-                copy16(to + S::v_at, p.cache.vc + (in ? from : 0), in);
-            }
-            const int nb = D >> p.cache.block_shift;         // scale bytes of a row: 16 rows are nb chunks
-            if (lane < 2 * nb) {
-                const bool v = lane >= nb;
-                const int at = (v ? lane - nb : lane) * 16;
-                const uint8_t* base = v ? p.cache.vs : p.cache.ks;
-                copy16(slot + (v ? S::vs_at : S::ks_at) + at, base + (ok ? row * nb + at : 0), ok);
-            }
+            for (int h = 0; h < GROUPS; ++h) page[h] = (uint32_t)page_next[h];
+            if (after < to) ask_page(after, to);
+            static_for<GROUPS>([&](auto hc) {
+                constexpr int H = decltype(hc)::value;
+                const int left = some_hi - key - H * kGroup; // rows from here on that exist
+                if (page[H] >= (uint32_t)p.cache.pages || (H > 0 && left <= 0)) return;
+                there |= 1u << H;
+                const uint32_t in_page = (uint32_t)(key + H * kGroup) & ((1u << p.cache.page_shift) - 1u);
+                const uint32_t nb = (uint32_t)D >> p.cache.block_shift;
+                const size_t off = (size_t)page[H] * page_bytes + in_page * S::RB;
+                const uint8_t *k = k_lane + off, *v = v_lane + off;
+                constexpr int per = S::CPR / 2;              // chunks of 16 rows per lane: 16 CPR / 32
+                constexpr int rows_apart = 32 / S::CPR;
+                if (left >= kGroup) {
+                    static_for<per>([&](auto jc) {
+                        constexpr int J = decltype(jc)::value;
+                        const uint32_t at = slot + (to_codes ^ (S::twist(J * rows_apart) << 4));
+                        copy16<S::k_at + H * kGroup * S::RB + J * 512, J * 512>(at, k);
+                        copy16<S::v_at + H * kGroup * S::RB + J * 512, J * 512>(at, v);
+                    });
+                } else {
+                    static_for<per>([&](auto jc) {
+                        constexpr int J = decltype(jc)::value;
+                        const uint32_t at = slot + (to_codes ^ (S::twist(J * rows_apart) << 4)), size = lane / S::CPR + J * rows_apart < left ? 16u : 0u;
+                        copy16_some<S::k_at + H * kGroup * S::RB + J * 512, J * 512>(at, k, size);
+                        copy16_some<S::v_at + H * kGroup * S::RB + J * 512, J * 512>(at, v, size);
+                    });
+                }
+                if (lane < 2 * (int)nb) copy16<0, 0>(slot + to_scales + H * kGroup * nb, s_lane + ((size_t)page[H] * page_scales + in_page * nb));
+            });
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
 
-    // -- one step
+    // -- the scales of a step, shared out among the lanes: with two groups a lane has a key, with one half of a key's blocks
+
+    static constexpr int LPK = 32 / S::step, HB = NB / LPK; // lanes per key, blocks of a lane
+
+    // Bytes of the lane's blocks (up to eight), from the scale bytes at `at`.
+    __device__ __forceinline__ void scale_bytes(uint32_t at, uint32_t (&w)[(HB + 3) / 4]) const
+    {
+        const int bs = p.cache.block_shift - 5;
+        if (bs == 0) {
+            const uint32_t from = at + lane * HB;
+            if constexpr (HB == 1) w[0] = lds_u8(from);
+            else if constexpr (HB == 2) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(w[0]) : "r"(from) : "memory");
+            else lds_words(from, w);
+            return;
+        }
+        const uint32_t from = at + (lane / LPK) * (NB >> bs);
+#pragma unroll
+        for (int j = 0; j < HB; ++j) {
+            const uint32_t byte = lds_u8(from + (((lane % LPK) * HB + j) >> bs));
+            w[j / 4] = j % 4 ? w[j / 4] | byte << (8 * (j % 4)) : byte;
+        }
+    }
 
     template <bool CAREFUL>
-    __device__ __forceinline__ void step(uint32_t slot, int key)
+    __device__ __forceinline__ void make_tables(uint32_t slot, int key, uint32_t has)
     {
-        const int bs = p.cache.block_shift - 5, nb = D >> p.cache.block_shift;
-        // the scales of the step, shared out among the lanes
-        constexpr int per = kStep * NB / 32;
-        uint32_t vb[per];
-        bool raise = false, poison = false;
+        uint32_t kw[(HB + 3) / 4], vw[(HB + 3) / 4];
+        scale_bytes(slot + S::ks_at, kw);
+        scale_bytes(slot + S::vs_at, vw);
+        const int mine = key + lane / LPK;
+        // seen by no row, or not there
+        const bool hidden = CAREFUL && (mine < some_lo || mine >= some_hi || !((has >> (lane / LPK / kGroup)) & 1u));
+        uint32_t kb[HB], vb[HB];
+        bool rare = false;
 #pragma unroll
-        for (int i = 0; i < per; ++i) {
-            const int e = lane + 32 * i, kk = e / NB, kd = e % NB;
-            const uint32_t kb = lds_u8(slot + S::ks_at + kk * nb + (kd >> bs));
-            const float kv = kb == 255u ? __uint_as_float(0x7FC00000u) : scale_value(kb);
-            asm volatile("st.shared.f32 [%0], %1;" :: "r"(tables + S::kf_at + e * 4), "f"(kv) : "memory");
-            const int vk = (e >> 1) / NB * 2 + (e & 1), vd = (e >> 1) % NB;
-            vb[i] = lds_u8(slot + S::vs_at + vk * nb + (vd >> bs));
-            if (CAREFUL && (key + vk < some_lo || key + vk >= some_hi)) vb[i] = 256u;         // seen by no row
-            raise |= (int)vb[i] > vref + kScaleSlack && vb[i] < 255u;
-            poison |= vb[i] == 255u;
+        for (int j = 0; j < HB; ++j) {
+            kb[j] = __byte_perm(kw[j / 4], 0, 0x4440 + j % 4);
+            vb[j] = __byte_perm(vw[j / 4], 0, 0x4440 + j % 4);
+            rare |= kb[j] == 255u || ((int)vb[j] > vlim[j] && !hidden);
         }
-        if (__any_sync(0xFFFFFFFFu, raise)) raise_reference(vb);
+        const bool any_rare = __any_sync(0xFFFFFFFFu, rare);
+        if (any_rare) raise_reference(vb, hidden);
+        float kf[HB], mult[HB];
 #pragma unroll
-        for (int i = 0; i < per; ++i) {
-            const int e = lane + 32 * i;
-            const float mult = vb[i] == 256u ? 0.f : __uint_as_float((uint32_t)max((int)vb[i] - vref + 127, 0) << 23);
-            uint32_t h = pack_f16(mult, 0.f);
-            if (vb[i] == 255u) h = 0x7E00u;
-            asm volatile("st.shared.u16 [%0], %1;" :: "r"(tables + S::vm_at + e * 2), "h"((unsigned short)h) : "memory");
+        for (int j = 0; j < HB; ++j) {
+            kf[j] = __uint_as_float(max(kb[j] << 23, 0x00400000u));
+            // (2^-127 and less: nothing; no more than 2^kScaleSlack)
+            mult[j] = __uint_as_float((uint32_t)max((int)vb[j] + 127 - vref[j], 0) << 23);
+            if (hidden) mult[j] = 0.f;
         }
-        if (CAREFUL) poison = __any_sync(0xFFFFFFFFu, poison);
-        __syncwarp();
+        uint32_t h[(HB + 1) / 2];
+#pragma unroll
+        for (int j = 0; j < HB; j += 2) h[j / 2] = pack_f16(mult[j], j + 1 < HB ? mult[j + 1] : 0.f);
+        if (any_rare) {                                      // poisoned blocks (or just a reference raised)
+#pragma unroll
+            for (int j = 0; j < HB; ++j) {
+                if (kb[j] == 255u) kf[j] = __uint_as_float(0x7FC00000u);
+                if (vb[j] == 255u && !hidden) h[j / 2] = j & 1 ? (h[j / 2] & 0xFFFFu) | 0x7E000000u : (h[j / 2] & 0xFFFF0000u) | 0x7E00u;
+            }
+        }
+        const uint32_t kt = tables + lane * HB * 4;
+        if constexpr (HB == 1) {
+            asm volatile("st.shared.f32 [%0], %1;" :: "r"(kt), "f"(kf[0]) : "memory");
+        } else if constexpr (HB == 2) {
+            asm volatile("st.shared.v2.f32 [%0], {%1, %2};" :: "r"(kt), "f"(kf[0]), "f"(kf[1]) : "memory");
+        } else {
+            static_for<HB / 4>([&](auto jc) {
+                constexpr int J = 4 * decltype(jc)::value;
+                asm volatile("st.shared.v4.f32 [%0 + %5], {%1, %2, %3, %4};" :: "r"(kt), "f"(kf[J]), "f"(kf[J + 1]), "f"(kf[J + 2]), "f"(kf[J + 3]), "n"(J * 4) : "memory");
+            });
+        }
+        // the values' multipliers as pairs of keys: [pair][block]
+        const int kk = lane / LPK;
+        const uint32_t vt = tables + ((kk >> 1) * NB + (lane % LPK) * HB) * 4 + (kk & 1) * 2;
+        static_for<HB>([&](auto jc) {
+            constexpr int J = decltype(jc)::value;
+            sts_u16<S::vm_at + J * 4>(vt, J & 1 ? h[J / 2] >> 16 : h[J / 2]);
+        });
+    }
 
-        // scores: 16 keys x 8 NT columns
-        float sc[NT][4] = {};
-        {
-            uint32_t kf_lo[NB], kf_hi[NB];
-            lds_words<NB>(tables + S::kf_at + g * NB * 4, kf_lo);
-            lds_words<NB>(tables + S::kf_at + (g + 8) * NB * 4, kf_hi);
-            constexpr int per_load = S::bits == 4 ? 2 : 1;   // blocks of 32 in two chunks
-#pragma unroll
-            for (int c = 0; c < S::CPR; c += 2) {
-                uint32_t w[2][2];                            // [chunk][row g, row g + 8]
-                ldmatrix4(slot + S::k_at + (twisted ^ (c << 4)), w[0][0], w[0][1], w[1][0], w[1][1]);
-#pragma unroll
-                for (int h = 0; h < per_load; ++h) {
-                    const int blk = S::bits == 4 ? c + h : c / 2;
-                    uint32_t a[2][4];                        // [row g, row g + 8][pairs of the block]
-                    if constexpr (S::bits == 4) {
-                        key_pairs<FMT>(w[h][0], a[0]);
-                        key_pairs<FMT>(w[h][1], a[1]);
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            uint32_t x[2], y[2];
-                            key_pairs<FMT>(w[0][r], x);
-                            key_pairs<FMT>(w[1][r], y);
-                            a[r][0] = x[0];
-                            a[r][1] = x[1];
-                            a[r][2] = y[0];
-                            a[r][3] = y[1];
-                        }
-                    }
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        uint32_t qb[4];
-                        q_block(n, blk, qb);
-                        float d[4] = {};
-                        F16Mma::mma(d, a[0][0], a[1][0], a[0][1], a[1][1], qb[0], qb[1]);
-                        F16Mma::mma(d, a[0][2], a[1][2], a[0][3], a[1][3], qb[2], qb[3]);
-                        const float lo = __uint_as_float(kf_lo[blk]), hi = __uint_as_float(kf_hi[blk]);
-                        sc[n][0] = fmaf(d[0], lo, sc[n][0]);
-                        sc[n][1] = fmaf(d[1], lo, sc[n][1]);
-                        sc[n][2] = fmaf(d[2], hi, sc[n][2]);
-                        sc[n][3] = fmaf(d[3], hi, sc[n][3]);
-                    }
-                }
-            }
-        }
-        // weights
-        uint32_t pb[NT][2], seen[CAREFUL ? NT : 1][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if constexpr (PIECES == 2) {                     // the two parts' columns are one row's
-                sc[n][0] = sc[n][1] = sc[n][0] + sc[n][1];
-                sc[n][2] = sc[n][3] = sc[n][2] + sc[n][3];
-            }
-            if constexpr (CAREFUL) {
-                uint32_t vis[2] = {0, 0};
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int row = column_row(8 * n + 2 * t + j), lo = row_lo(p, s, row), hi = row_hi(p, s, row);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int at = key + g + 8 * h;
-                        const bool on = at >= lo && at < hi;
-                        if (!on) sc[n][2 * h + j] = __uint_as_float(0xFF800000u);
-                        vis[h] |= (on ? 0x3C00u : 0u) << (16 * j);
-                    }
-                }
-                seen[n][0] = vis[0];
-                seen[n][1] = vis[1];
-                // (a factor of 0 or NaN must not make NaN of what is hidden)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sc[n][j] = sc[n][j] == __uint_as_float(0xFF800000u) ? sc[n][j] : sc[n][j] * f[n][j & 1];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sc[n][j] *= f[n][j & 1];
-            }
-        }
-        bool over = false;
+    // -- one step
+
+    // Scores of group H, 16 keys x 8 NT columns, without their rows' factors.
+    template <int H>
+    __device__ __forceinline__ void scores(uint32_t slot, float (&sc)[NT][4]) const
+    {
+        uint32_t kf_lo[NB], kf_hi[NB];
+        lds_words<NB, S::kf_at + H * kGroup * NB * 4>(tables + g * NB * 4, kf_lo);
+        lds_words<NB, S::kf_at + H * kGroup * NB * 4 + 32 * NB>(tables + g * NB * 4, kf_hi);
+        constexpr int per_load = S::bits == 4 ? 2 : 1;       // blocks of 32 in two chunks
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) over |= sc[n][j] > m[n][j & 1] + kSlack;
-        if (__any_sync(0xFFFFFFFFu, over)) raise_maximum(sc);
+            for (int j = 0; j < 4; ++j) sc[n][j] = 0.f;
+#pragma unroll
+        for (int c = 0; c < S::CPR; c += 2) {
+            uint32_t w[2][2];                                // [chunk][row g, row g + 8]
+            ldmatrix4<S::k_at + H * kGroup * S::RB>(slot + (twisted ^ (c << 4)), w[0][0], w[0][1], w[1][0], w[1][1]);
+#pragma unroll
+            for (int h = 0; h < per_load; ++h) {
+                const int blk = S::bits == 4 ? c + h : c / 2;
+                uint32_t a[2][4];                            // [row g, row g + 8][pairs of the block]
+                if constexpr (S::bits == 4) {
+                    key_pairs<FMT>(w[h][0], a[0]);
+                    key_pairs<FMT>(w[h][1], a[1]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        uint32_t x[2], y[2];
+                        key_pairs<FMT>(w[0][r], x);
+                        key_pairs<FMT>(w[1][r], y);
+                        a[r][0] = x[0];
+                        a[r][1] = x[1];
+                        a[r][2] = y[0];
+                        a[r][3] = y[1];
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    uint32_t qb[4];
+                    q_block(n, blk, qb);
+                    float d[4];
+                    mma_first(d, a[0][0], a[1][0], a[0][1], a[1][1], qb[0], qb[1]);
+                    F16Mma::mma(d, a[0][2], a[1][2], a[0][3], a[1][3], qb[2], qb[3]);
+                    const float lo = __uint_as_float(kf_lo[blk]), hi = __uint_as_float(kf_hi[blk]);
+                    sc[n][0] = fmaf(d[0], lo, sc[n][0]);
+                    sc[n][1] = fmaf(d[1], lo, sc[n][1]);
+                    sc[n][2] = fmaf(d[2], hi, sc[n][2]);
+                    sc[n][3] = fmaf(d[3], hi, sc[n][3]);
+                }
+            }
+        }
+        if constexpr (PIECES == 2) {                         // the two parts' columns are one row's
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                sc[n][0] = sc[n][1] = sc[n][0] + sc[n][1];
+                sc[n][2] = sc[n][3] = sc[n][2] + sc[n][3];
+            }
+        }
+    }
+
+    // Hidden scores of a group become -inf; `seen` gets a one (FP16) for each of the others.
+    __device__ __forceinline__ void hide(int key, float (&sc)[NT][4], uint32_t (&seen)[NT][2]) const
+    {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float e[4];
+            seen[n][0] = seen[n][1] = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = exp2_approx(sc[n][j] - m[n][j & 1]);
-            l[n][0] += e[0] + e[2];
-            if constexpr (PIECES == 1) {
-                l[n][1] += e[1] + e[3];
-                pb[n][0] = transpose8x8(pack_f16(e[0], e[1]));
-                pb[n][1] = transpose8x8(pack_f16(e[2], e[3]));
-            } else {
-                const uint32_t a = pack_f16(e[0], 0.f), c = pack_f16(e[2], 0.f);
-                pb[n][0] = transpose8x8(a | pack_f16(0.f, e[0] - f16_lo(a)));
-                pb[n][1] = transpose8x8(c | pack_f16(0.f, e[2] - f16_lo(c)));
-            }
-        }
-        // O^T += V^T P^T
-        {
-            uint32_t vm_lo[NB], vm_hi[NB];                   // keys 2t, 2t + 1 and 2t + 8, 2t + 9
-            lds_words<NB>(tables + S::vm_at + t * NB * 4, vm_lo);
-            lds_words<NB>(tables + S::vm_at + (t + 4) * NB * 4, vm_hi);
-            uint32_t nan_lo[CAREFUL ? NB : 1], nan_hi[CAREFUL ? NB : 1], any_nan = 0;
-            if constexpr (CAREFUL) {                         // poisoned blocks: flags in the place of NaN
-#pragma unroll
-                for (int i = 0; i < NB; ++i) {
-                    nan_lo[i] = take_nan(vm_lo[i]);
-                    nan_hi[i] = take_nan(vm_hi[i]);
-                    any_nan |= nan_lo[i] | nan_hi[i];
-                }
-            }
-#pragma unroll
-            for (int c = 0; c < S::CPR; c += 2) {
-                uint32_t w[2][2];                            // [chunk][keys 0 - 7, keys 8 - 15]
-                ldmatrix4_trans(slot + S::v_at + (twisted ^ (c << 4)), w[0][0], w[0][1], w[1][0], w[1][1]);
+            for (int j = 0; j < 2; ++j) {
+                const int row = column_row(8 * n + 2 * t + j), lo = row_lo(p, s, row), hi = row_hi(p, s, row);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int blk = S::bits == 4 ? c + h : c / 2;
-                    if constexpr (CAREFUL && has_nan) {
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const uint32_t bad = nan_bytes(w[h][k]);
-                            any_nan |= bad;
-                            w[h][k] &= ~((bad >> 7) * 255u);
-                        }
-                    }
-                    uint32_t X[NP], Y[NP];
-                    value_pairs<FMT>(w[h][0], w[h][1], X, Y);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const uint32_t b0 = mul_f16(pb[n][0], vm_lo[blk]), b1 = mul_f16(pb[n][1], vm_hi[blk]);
-#pragma unroll
-                        for (int j = 0; j < NP / 2; ++j)
-                            F16Mma::mma(acc[(c + h) * (NP / 2) + j][n], X[2 * j], X[2 * j + 1], Y[2 * j], Y[2 * j + 1], b0, b1);
-                    }
+                    const int at = key + g + 8 * h;
+                    const bool on = at >= lo && at < hi;
+                    if (!on) sc[n][2 * h + j] = __uint_as_float(0xFF800000u);
+                    seen[n][h] |= (on ? 0x3C00u : 0u) << (16 * j);
                 }
             }
-            if constexpr (CAREFUL) {
-                if (__any_sync(0xFFFFFFFFu, any_nan != 0)) spread_nan(slot, seen, nan_lo, nan_hi);
+        }
+    }
+
+    // O^T += V^T P^T of group H, P as matrix operands.
+    template <int H, bool CAREFUL>
+    __device__ __forceinline__ void add_values(uint32_t slot, const uint32_t (&pb)[NT][2], const uint32_t (&seen)[NT][2])
+    {
+        uint32_t vm_lo[NB], vm_hi[NB];                       // keys 2t, 2t + 1 and 2t + 8, 2t + 9
+        lds_words<NB, S::vm_at + H * 8 * NB * 4>(tables + t * NB * 4, vm_lo);
+        lds_words<NB, S::vm_at + H * 8 * NB * 4 + 16 * NB>(tables + t * NB * 4, vm_hi);
+        uint32_t nan_lo[CAREFUL ? NB : 1], nan_hi[CAREFUL ? NB : 1], any_nan = 0;
+        if constexpr (CAREFUL) {                             // poisoned blocks: flags in the place of NaN
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                nan_lo[i] = take_nan(vm_lo[i]);
+                nan_hi[i] = take_nan(vm_hi[i]);
+                any_nan |= nan_lo[i] | nan_hi[i];
             }
         }
-        (void)poison;
+#pragma unroll
+        for (int c = 0; c < S::CPR; c += 2) {
+            uint32_t w[2][2];                                // [chunk][keys 0 - 7, keys 8 - 15]
+            ldmatrix4_trans<S::v_at + H * kGroup * S::RB>(slot + (twisted ^ (c << 4)), w[0][0], w[0][1], w[1][0], w[1][1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int blk = S::bits == 4 ? c + h : c / 2;
+                if constexpr (CAREFUL && has_nan) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t bad = nan_bytes(w[h][k]);
+                        any_nan |= bad;
+                        w[h][k] &= ~((bad >> 7) * 255u);
+                    }
+                }
+                uint32_t X[NP], Y[NP];
+                value_pairs<FMT>(w[h][0], w[h][1], X, Y);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint32_t b0 = mul_f16(pb[n][0], vm_lo[blk]), b1 = mul_f16(pb[n][1], vm_hi[blk]);
+#pragma unroll
+                    for (int j = 0; j < NP / 2; ++j)
+                        F16Mma::mma(acc[(c + h) * (NP / 2) + j][n], X[2 * j], X[2 * j + 1], Y[2 * j], Y[2 * j + 1], b0, b1);
+                }
+            }
+        }
+        if constexpr (CAREFUL) {
+            if (__any_sync(0xFFFFFFFFu, any_nan != 0)) spread_nan<H>(slot, seen, nan_lo, nan_hi);
+        }
+    }
+
+    // Groups FIRST ... FIRST + N - 1 of a step.
+    template <int FIRST, int N, bool CAREFUL>
+    __device__ __forceinline__ void step(uint32_t slot, int key)
+    {
+        float sc[N][NT][4], x[N][NT][4];                     // scores; times their rows' factors, less m
+        uint32_t seen[N][NT][2];
+        static_for<N>([&](auto hc) {
+            constexpr int H = decltype(hc)::value;
+            scores<FIRST + H>(slot, sc[H]);
+            if constexpr (CAREFUL) hide(key + (FIRST + H) * kGroup, sc[H], seen[H]);
+        });
+        float over = 0.f;
+#pragma unroll
+        for (int h = 0; h < N; ++h)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[h][n][j] = CAREFUL ? less(sc[h][n][j], f[n][j & 1], m[n][j & 1]) : fmaf(sc[h][n][j], f[n][j & 1], -m[n][j & 1]);
+                    over = fmaxf(over, x[h][n][j]);
+                }
+        if (__any_sync(0xFFFFFFFFu, over > kSlack)) raise_maximum<N>(sc, x);
+        uint32_t pb[N][NT][2];
+#pragma unroll
+        for (int h = 0; h < N; ++h)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float e[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) e[j] = exp2_approx(x[h][n][j]);
+                l[n][0] += e[0] + e[2];
+                if constexpr (PIECES == 1) {
+                    l[n][1] += e[1] + e[3];
+                    pb[h][n][0] = transpose8x8(pack_f16(e[0], e[1]));
+                    pb[h][n][1] = transpose8x8(pack_f16(e[2], e[3]));
+                } else {
+                    const uint32_t a = pack_f16(e[0], 0.f), c = pack_f16(e[2], 0.f);
+                    pb[h][n][0] = transpose8x8(a | pack_f16(0.f, e[0] - f16_lo(a)));
+                    pb[h][n][1] = transpose8x8(c | pack_f16(0.f, e[2] - f16_lo(c)));
+                }
+            }
+        static_for<N>([&](auto hc) {
+            constexpr int H = decltype(hc)::value;
+            add_values<FIRST + H, CAREFUL>(slot, pb[H], seen[H]);
+        });
+    }
+
+    // A fetched step: all of it at once where every row sees all of it, else group by group.
+    __device__ __forceinline__ void take(uint32_t slot, int key)
+    {
+        constexpr uint32_t every = (1u << GROUPS) - 1u;
+        const uint32_t has = (there >> (GROUPS * (S::stages - 1))) & every;
+        if (!has || key + S::step <= some_lo || key >= some_hi) return;
+        if (has == every && key >= all_lo && key + S::step <= all_hi) {
+            make_tables<false>(slot, key, has);
+            __syncwarp();
+            step<0, GROUPS, false>(slot, key);
+            return;
+        }
+        make_tables<true>(slot, key, has);
+        __syncwarp();
+        static_for<GROUPS>([&](auto hc) {
+            constexpr int H = decltype(hc)::value;
+            const int at = key + H * kGroup;
+            if (((has >> H) & 1u) && at + kGroup > some_lo && at < some_hi) step<H, 1, true>(slot, key);
+        });
     }
 
     // FP16 NaN halves of v become zeros and are flagged as ones (0x3C00) in the result.
@@ -439,6 +602,7 @@ struct Attend {
     }
 
     // Accumulators of dimensions in which a key that their row sees holds a NaN become NaN: counts such keys by matrix steps.
+    template <int H>
     __device__ __forceinline__ void spread_nan(uint32_t slot, const uint32_t (&seen)[NT][2], const uint32_t (&nan_lo)[NB], const uint32_t (&nan_hi)[NB])
     {
         uint32_t vis[NT][2];
@@ -450,7 +614,7 @@ struct Attend {
 #pragma unroll
         for (int c = 0; c < S::CPR; c += 2) {
             uint32_t w[2][2];
-            ldmatrix4_trans(slot + S::v_at + (twisted ^ (c << 4)), w[0][0], w[0][1], w[1][0], w[1][1]);
+            ldmatrix4_trans<S::v_at + H * kGroup * S::RB>(slot + (twisted ^ (c << 4)), w[0][0], w[0][1], w[1][0], w[1][1]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int blk = S::bits == 4 ? c + h : c / 2;
@@ -478,14 +642,20 @@ struct Attend {
         }
     }
 
+    // A score less m; hidden ones are -inf, which a factor that is NaN must not make NaN of.
+    __device__ __forceinline__ float less(float sc, float f, float m) const { return sc == __uint_as_float(0xFF800000u) ? sc : fmaf(sc, f, -m); }
+
     // The columns' maxima moved up to the step's scores.
-    __device__ __forceinline__ void raise_maximum(const float (&sc)[NT][4])
+    template <int N>
+    __device__ __forceinline__ void raise_maximum(const float (&sc)[N][NT][4], float (&x)[N][NT][4])
     {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                float top = fmaxf(sc[n][j], sc[n][2 + j]);
+                float top = kNone;
+#pragma unroll
+                for (int h = 0; h < N; ++h) top = fmaxf(top, fmaxf(less(sc[h][n][j], f[n][j], 0.f), less(sc[h][n][2 + j], f[n][j], 0.f)));
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
                 const float to = fmaxf(m[n][j], top - kBias), by = exp2_approx(m[n][j] - to);
@@ -496,31 +666,36 @@ struct Attend {
                     acc[i][n][j] *= by;
                     acc[i][n][2 + j] *= by;
                 }
+#pragma unroll
+                for (int h = 0; h < N; ++h) {
+                    x[h][n][j] = less(sc[h][n][j], f[n][j], to);
+                    x[h][n][2 + j] = less(sc[h][n][2 + j], f[n][j], to);
+                }
             }
     }
 
-    // Reference scales moved up to the step's largest ones (vb: the bytes of the lane's block).
-    template <int PER>
-    __device__ __forceinline__ void raise_reference(const uint32_t (&vb)[PER])
+    // Reference scales moved up to the step's largest ones (vb: the bytes of the lane's key and blocks).
+    __device__ __forceinline__ void raise_reference(const uint32_t (&vb)[HB], bool hidden)
     {
-        int top = -1000;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) top = max(top, vb[i] < 255u ? (int)vb[i] : -1000);
-        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        for (int j = 0; j < HB; ++j) {
+            int top = hidden || vb[j] == 255u ? -1000 : (int)vb[j];
 #pragma unroll
-        for (int o = 2 * NB; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        const int to = top > vref + kScaleSlack ? top : vref;
-        const float by = __uint_as_float((uint32_t)max(vref - to + 127, 0) << 23);      // (2^-127 and less: nothing)
-        vref = to;
+            for (int o = LPK; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            const int to = top > vlim[j] ? top : vref[j];
+            const float by = __uint_as_float((uint32_t)max(vref[j] - to + 127, 0) << 23);      // (2^-127 and less: nothing)
+            vref[j] = to;
+            vlim[j] = to < 0 ? to : min(to + kScaleSlack, 254);      // (255 is always looked at)
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            const float of = __shfl_sync(0xFFFFFFFFu, by, 2 * i);
+            for (int part = 0; part < LPK; ++part) {
+                const float of = LPK == 1 ? by : __shfl_sync(0xFFFFFFFFu, by, part);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[2 * i + k][n][j] *= of;
+                        for (int i = 0; i < 4; ++i) acc[2 * (part * HB + j) + k][n][i] *= of;
+            }
         }
     }
 
@@ -607,11 +782,15 @@ struct Attend {
 
     __device__ __forceinline__ void run(int from, int to, uint32_t factors)
     {
-        load_rows(factors);
-        int key = from + warp * kStep;
-        constexpr int stride = kWarps * kStep;
+        place(head);
+        pages_of = p.batch.table + (size_t)b * p.batch.width;
+        there = 0;
+        int key = from + warp * S::step;
+        constexpr int stride = kWarps * S::step;
+        if (key < to) ask_page(key, to);
 #pragma unroll
-        for (int i = 0; i < S::stages - 1; ++i) fetch(ring + i * S::slot, key + i * stride, key + i * stride < to);
+        for (int i = 0; i < S::stages - 1; ++i) fetch(ring + i * S::slot, key + i * stride, key + (i + 1) * stride, to);
+        load_rows(factors);
         __syncthreads();
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -641,29 +820,21 @@ struct Attend {
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[i][n][j] = 0.f;
-        vref = -1000;
+#pragma unroll
+        for (int j = 0; j < HB; ++j) vref[j] = vlim[j] = -1000;
         int slot = 0, next = S::stages - 1;
         for (; key < to; key += stride) {
             const int ahead = key + (S::stages - 1) * stride;
-            fetch(ring + next * S::slot, ahead, ahead < to);
+            fetch(ring + next * S::slot, ahead, ahead + stride, to);
             asm volatile("cp.async.wait_group %0;" :: "n"(S::stages - 1) : "memory");
             __syncwarp();
-            if (key + kStep > some_lo && key < some_hi && there(key)) {
-                if (key >= all_lo && key + kStep <= all_hi) step<false>(ring + slot * S::slot, key);
-                else step<true>(ring + slot * S::slot, key);
-            }
+            take(ring + slot * S::slot, key);
             __syncwarp();
             slot = slot + 1 == S::stages ? 0 : slot + 1;
             next = next + 1 == S::stages ? 0 : next + 1;
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncthreads();
-    }
-
-    __device__ __forceinline__ bool there(int key) const
-    {
-        const int page = ld_int(p.batch.table + (size_t)b * p.batch.width + (key >> p.cache.page_shift));
-        return (unsigned)page < (unsigned)p.cache.pages;
     }
 
     // -- the warps' results together: normalized sums and their weights in shared memory, then to the output or to a part
@@ -676,7 +847,7 @@ struct Attend {
         float scales[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-            const int byte = __shfl_sync(0xFFFFFFFFu, vref, 2 * i);
+            const int byte = __shfl_sync(0xFFFFFFFFu, vref[i % HB], i / HB);
             scales[i] = scale_value((uint32_t)max(byte, 0));
         }
 #pragma unroll
@@ -809,6 +980,7 @@ attend_kernel(const __grid_constant__ AttendArgs p)
     a.qs = base + S::work + kWarps * S::tables;
     const uint32_t factors = a.qs + S::q_bytes;
     // matrix i of a load: keys 8 (i & 1) ..., chunk i >> 1; the lane gives the address of row lane % 8 of matrix lane / 8
+    a.to_codes = (lane / S::CPR) * S::RB + ((lane % S::CPR ^ S::twist(lane / S::CPR)) << 4);
     a.twisted = (((lane >> 3) & 1) * 8 + (lane & 7)) * S::RB + (((lane >> 4) ^ S::twist(lane & 7)) << 4);
     uint8_t* const parts = p.ws + (size_t)p.ctas * sizeof(PartMeta);
     const size_t part = part_bytes(p.rows, D);
