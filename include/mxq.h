@@ -463,6 +463,7 @@ int mxq_moe(const mxq_moe_layer *layer, const void *x, int dtype, const float *l
  * Structs are HOST structs, free to reuse when a call returns.  batch, width and tokens are below 2^31 (MXQ_ERR_SIZE).
  */
 #define MXQ_CACHE_HEADS_MAX 1024
+#define MXQ_CACHE_ROWS_MAX ((size_t)1 << 26)
 typedef struct mxq_cache {
     void *k_codes;
     uint8_t *k_scales;
@@ -508,7 +509,8 @@ int mxq_cache_read(const mxq_cache *cache, const mxq_batch *batch, size_t total,
  * Sums and the softmax are held in FP32.  Queries enter exactly for BF16 (elements below 2^-31 of a row's largest excepted) and
  * with 22 bits for FP32; the softmax's weights enter the second product with 11 bits for BF16 and 22 for FP32.  A NaN or an infinity in a
  * query gives NaN.  Results do not depend on timing.
- *   q          [tokens, q_heads, head_dim] of dtype; q_heads a multiple of heads, at most 2^16 (MXQ_ERR_SIZE)
+ *   q          [tokens, q_heads, head_dim] of dtype; q_heads a multiple of heads, at most 2^16, tokens * q_heads + batch * heads at most
+ *              MXQ_CACHE_ROWS_MAX (MXQ_ERR_SIZE)
  *   out        [tokens, q_heads, head_dim] of dtype, contiguous, 32-byte aligned; overlaps nothing else
  *   lse        null, or [tokens, q_heads] FP32, 4-byte aligned: the natural logarithm of sum over visible t of exp(scale q . K^[t])
  *   workspace  32-byte aligned, mxq_cache_attention_workspace_bytes(...) bytes or more (MXQ_ERR_SIZE); what it holds before and after

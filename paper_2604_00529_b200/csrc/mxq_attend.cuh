@@ -22,7 +22,7 @@
 namespace mxq {
 namespace {
 
-constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kWarps = 4;                                   // of a CTA, where that is not the launch's choice
 constexpr int kGroup = 16;                                  // keys of a matrix step
 constexpr int kStagesMax = 6;
 constexpr float kBias = 8.f;                                // P is held as 2^kBias times itself: more of FP16's range below 1
@@ -158,6 +158,13 @@ __device__ __forceinline__ float lds_f32(uint32_t at)
     asm volatile("ld.shared.f32 %0, [%1 + %2];" : "=f"(v) : "r"(at), "n"(AT) : "memory");
     return v;
 }
+template <int AT = 0>
+__device__ __forceinline__ uint32_t lds_u32(uint32_t at)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1 + %2];" : "=r"(v) : "r"(at), "n"(AT) : "memory");
+    return v;
+}
 __device__ __forceinline__ uint32_t lds_u8(uint32_t at)
 {
     uint32_t v;
@@ -209,17 +216,20 @@ struct Shape {
     static constexpr int kf_at = 0, vm_at = step * NB * 4, tables = vm_at + step * NB * 2;
     static constexpr int q_row = D * 2 + (bits == 4 ? 16 : 32);       // padded: lanes of a read lie in different banks
     static constexpr int q_bytes = 8 * NT * q_row;
-    static constexpr int ctas = NT == 4 ? 2 : NT * D <= 128 ? 4 : NT * D <= 256 ? 3 : 2;     // per SM, by registers
+    static constexpr int columns_at = q_bytes;                        // of each column: its factor, the keys that its row sees
+    static constexpr int rows_bytes = q_bytes + 8 * NT * 12;
+    static constexpr int ctas = NT == 4 ? 2 : NT * D <= 128 ? 4 : NT * D <= 256 ? 3 : 2;     // of kWarps warps per SM, by registers
+    // Warps of a CTA: kWarps, or with one column group as many as an SM holds.
+    static constexpr int most = NT > 1 ? kWarps : kWarps * ctas;
     // steps of a warp under way to shared memory, and the one worked on: as many as the CTA's share of an SM holds
-    static constexpr int fixed = kWarps * tables + q_bytes + 8 * NT * 4;
-    static constexpr int fit = (227 * 1024 / ctas - 1536 - fixed) / (kWarps * slot);
+    static constexpr int fit = (227 * 1024 / ctas - 1536 - rows_bytes - kWarps * tables) / (kWarps * slot);
     static constexpr int stages = fit < kStagesMax ? fit : kStagesMax;
     static constexpr int ring = stages * slot;
-    static constexpr int merge = kWarps * 8 * NT * (D + 2) * 4;       // the warps' results, in the ring's place
-    static constexpr int work = (kWarps * ring > merge ? kWarps * ring : merge);
-    static constexpr int total = work + fixed;
+    static constexpr int merge = 8 * NT * (D + 2) * 4;                // a warp's results, in the rings' place
+    static constexpr int work = ring > merge ? ring : merge;
+    static constexpr size_t total(int warps) { return (size_t)warps * (work + tables) + rows_bytes; }
     static constexpr bool q_in_registers = NT * MT * 2 <= 32;
-    static_assert(stages >= 2 && (total + 1536) * ctas <= 227 * 1024, "shared memory");
+    static_assert(stages >= 2 && (total(kWarps) + 1536) * ctas <= 227 * 1024, "shared memory");
 
     // Chunk c of row r lies at r * RB + (c ^ twist(r)) * 16: the eight rows that a matrix load reads at once are in different banks.
     static __host__ __device__ constexpr int twist(int r) { return CPR >= 8 ? r & 7 : CPR == 4 ? (r >> 1) & 3 : (r >> 2) & 1; }
@@ -232,7 +242,7 @@ struct Attend {
     static constexpr bool has_nan = FMT == MXQ_FP8_E4M3;
 
     const AttendArgs& p;
-    const int warp, lane, g, t;
+    const int warps, warp, lane, g, t;
     uint32_t ring, tables, qs;                              // shared addresses: the warp's ring and tables, the CTA's rows
     uint32_t twisted;                                       // a lane's part of its matrix loads' addresses
     float acc[MT][NT][4], l[NT][2], m[NT][2], f[NT][2];
@@ -242,8 +252,6 @@ struct Attend {
     int b, head, row0, rows;                                // rows: how many of the item are there
     Sequence s;
     int some_lo, some_hi, all_lo, all_hi;                   // keys that some row sees, that all rows see
-
-    __device__ __forceinline__ int column_row(int c) const { return min(row0 + c / PIECES, row0 + rows - 1); }
 
     // -- a step's codes and scales on their way to shared memory
 
@@ -466,7 +474,8 @@ struct Attend {
             seen[n][0] = seen[n][1] = 0;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int row = column_row(8 * n + 2 * t + j), lo = row_lo(p, s, row), hi = row_hi(p, s, row);
+                const uint32_t at_column = qs + S::columns_at + (8 * n + 2 * t + j) * 12;
+                const int lo = (int)lds_u32<4>(at_column), hi = (int)lds_u32<8>(at_column);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int at = key + g + 8 * h;
@@ -731,12 +740,13 @@ struct Attend {
     }
 
     // The item's rows to shared memory as FP16 parts, each row times the power of two that brings its largest element to
-    // [2^14, 2^15): BF16's eight bits fit FP16's eleven, down to 2^-31 of the largest.  `factors` get what takes that back.
-    __device__ __forceinline__ void load_rows(uint32_t factors) const
+    // [2^14, 2^15): BF16's eight bits fit FP16's eleven, down to 2^-31 of the largest.  The columns get the factor that
+    // takes that back and the keys that their rows see.
+    __device__ __forceinline__ void load_rows() const
     {
         constexpr int per = D / 32;
-        for (int c = warp; c < 8 * NT; c += kWarps) {
-            const int r = c / PIECES, row = row0 + r;
+        for (int c = warp; c < 8 * NT; c += warps) {
+            const int r = c / PIECES, row = row0 + min(r, rows - 1);
             float v[per];
             uint32_t top = 0;
 #pragma unroll
@@ -773,30 +783,33 @@ struct Attend {
             if (lane == 0) {
                 float back = p.scale * back0 * back1;
                 if (top == 255u) back = __uint_as_float(0x7FC00000u);
-                asm volatile("st.shared.f32 [%0], %1;" :: "r"(factors + c * 4), "f"(back) : "memory");
+                const uint32_t at = qs + S::columns_at + c * 12;
+                asm volatile("st.shared.f32 [%0], %1;" :: "r"(at), "f"(back) : "memory");
+                asm volatile("st.shared.u32 [%0 + 4], %1;" :: "r"(at), "r"(row_lo(p, s, row)) : "memory");
+                asm volatile("st.shared.u32 [%0 + 8], %1;" :: "r"(at), "r"(row_hi(p, s, row)) : "memory");
             }
         }
     }
 
-    // -- a run of keys [from, to) of the item, from a multiple of kTile on
+    // -- a run of keys [from, to) of the item, from a multiple of a tile on
 
-    __device__ __forceinline__ void run(int from, int to, uint32_t factors)
+    __device__ __forceinline__ void run(int from, int to)
     {
         place(head);
         pages_of = p.batch.table + (size_t)b * p.batch.width;
         there = 0;
         int key = from + warp * S::step;
-        constexpr int stride = kWarps * S::step;
+        const int stride = warps * S::step;
         if (key < to) ask_page(key, to);
 #pragma unroll
         for (int i = 0; i < S::stages - 1; ++i) fetch(ring + i * S::slot, key + i * stride, key + (i + 1) * stride, to);
-        load_rows(factors);
+        load_rows();
         __syncthreads();
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                f[n][j] = lds_f32(factors + (8 * n + 2 * t + j) * 4);
+                f[n][j] = lds_f32(qs + S::columns_at + (8 * n + 2 * t + j) * 12);
                 m[n][j] = kNone;
                 l[n][j] = 0.f;
             }
@@ -843,7 +856,7 @@ struct Attend {
     {
         constexpr int R = 8 * NT / PIECES;                   // rows of the tile
         float* const o_at = area + warp * R * D;
-        float* const ml = area + kWarps * R * D;             // [warp][row][m, l]
+        float* const ml = area + warps * R * D;             // [warp][row][m, l]
         float scales[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
@@ -875,14 +888,14 @@ struct Attend {
                 }
             }
         __syncthreads();
-        for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+        for (int i = threadIdx.x; i < rows * (D / 4); i += warps * 32) {
             const int r = i / (D / 4), d = i % (D / 4) * 4;
             float top = kNone;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[(w * R + r) * 2]);
+#pragma unroll 4
+            for (int w = 0; w < warps; ++w) top = fmaxf(top, ml[(w * R + r) * 2]);
             float sum = 0.f, v[4] = {};
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
+#pragma unroll 4
+            for (int w = 0; w < warps; ++w) {
                 const float wt = ml[(w * R + r) * 2 + 1] * exp2_approx(ml[(w * R + r) * 2] - top);
                 const float4 x = *reinterpret_cast<const float4*>(area + (w * R + r) * D + d);
                 sum += wt;
@@ -911,107 +924,96 @@ struct Attend {
     }
 };
 
-// The run of a CTA: its first and one past its last tile, and the sequence that the first lies in.
+// The run of a CTA: its first and one past its last tile, the sequence that the first lies in and the tiles in front of that.
 struct Plan {
-    long long total, from, to, base;                         // base: tiles in front of sequence b
-    int b, ctas;
+    uint32_t total, from, to, base;
+    int b;
 };
 
-__device__ __forceinline__ void make_plan(const AttendArgs& p, Plan& plan, long long (&warp_sum)[kWarps])
+__device__ __forceinline__ void make_plan(const AttendArgs& p, int warps, Plan& plan, uint32_t (&warp_sum)[16])
 {
-    const int per = (p.batch.batch + kThreads - 1) / kThreads, first = min((int)threadIdx.x * per, p.batch.batch), last = min(first + per, p.batch.batch);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long mine = 0;
+    const int threads = warps * 32, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int per = (p.batch.batch + threads - 1) / threads, first = min((int)threadIdx.x * per, p.batch.batch), last = min(first + per, p.batch.batch);
+    uint32_t mine = 0;
     for (int b = first; b < last; ++b) mine += sequence_tiles(p, sequence(p.batch, b, p.cache.page_shift)) * p.cache.heads;
-    long long before = mine;
+    uint32_t before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const long long up = __shfl_up_sync(0xFFFFFFFFu, before, o);
+        const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, before, o);
         if (lane >= o) before += up;
     }
     if (lane == 31) warp_sum[warp] = before;
     __syncthreads();
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
+    uint32_t total = 0;
+    for (int w = 0; w < warps; ++w) {
         if (w < warp) before += warp_sum[w];
         total += warp_sum[w];
     }
     before -= mine;
-    const int ctas = (int)min((long long)gridDim.x, max(total, 1ll));
-    const long long from = (int)blockIdx.x < ctas ? run_start(total, ctas, blockIdx.x) : total;
-    if (threadIdx.x == 0) {
-        plan.total = total;
-        plan.ctas = ctas;
-        plan.from = from;
-        plan.to = (int)blockIdx.x < ctas ? run_start(total, ctas, blockIdx.x + 1) : total;
-        plan.b = p.batch.batch;
-    }
-    __syncthreads();
-    if (from >= before && from < before + mine) {            // one thread's
+    const uint32_t ctas = working_ctas(total, gridDim.x);
+    const Runs runs(total, ctas);
+    const uint32_t from = blockIdx.x < ctas ? runs.start(blockIdx.x) : total, to = blockIdx.x < ctas ? runs.start(blockIdx.x + 1) : total;
+    if (from < to ? from >= before && from < before + mine : threadIdx.x == 0) {            // one thread's
         int b = first;
-        for (; b < last; ++b) {
-            const long long n = sequence_tiles(p, sequence(p.batch, b, p.cache.page_shift)) * p.cache.heads;
+        for (; from < to && b < last; ++b) {
+            const uint32_t n = sequence_tiles(p, sequence(p.batch, b, p.cache.page_shift)) * p.cache.heads;
             if (from < before + n) break;
             before += n;
         }
-        plan.b = b;
-        plan.base = before;
+        plan = Plan{total, from, to, before, b};
     }
     __syncthreads();
 }
 
 template <int FMT, int D, int NT, int PIECES>
-__global__ void __launch_bounds__(kThreads, Shape<FMT, D, NT>::ctas)
+__global__ void __launch_bounds__(Shape<FMT, D, NT>::most * 32, NT == 1 ? 1 : Shape<FMT, D, NT>::ctas)
 attend_kernel(const __grid_constant__ AttendArgs p)
 {
     using S = Shape<FMT, D, NT>;
     extern __shared__ __align__(1024) uint8_t shared[];
     __shared__ Plan plan;
-    __shared__ long long warp_sum[kWarps];
+    __shared__ uint32_t warp_sum[16];
     pdl_acquire();
     pdl_release();                                           // (the second kernel reads nothing before its own wait)
-    make_plan(p, plan, warp_sum);
+    const int warps = NT == 1 ? p.warps : kWarps;
+    make_plan(p, warps, plan, warp_sum);
     const uint32_t base = smem_addr(shared);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    Attend<FMT, D, NT, PIECES> a{p, warp, lane, lane >> 2, lane & 3};
+    Attend<FMT, D, NT, PIECES> a{p, warps, warp, lane, lane >> 2, lane & 3};
     a.ring = base + warp * S::ring;
-    a.tables = base + S::work + warp * S::tables;
-    a.qs = base + S::work + kWarps * S::tables;
-    const uint32_t factors = a.qs + S::q_bytes;
-    // matrix i of a load: keys 8 (i & 1) ..., chunk i >> 1; the lane gives the address of row lane % 8 of matrix lane / 8
+    a.tables = base + warps * S::work + warp * S::tables;
+    a.qs = base + warps * (S::work + S::tables);
     a.to_codes = (lane / S::CPR) * S::RB + ((lane % S::CPR ^ S::twist(lane / S::CPR)) << 4);
+    // matrix i of a load: keys 8 (i & 1) ..., chunk i >> 1; the lane gives the address of row lane % 8 of matrix lane / 8
     a.twisted = (((lane >> 3) & 1) * 8 + (lane & 7)) * S::RB + (((lane >> 4) ^ S::twist(lane & 7)) << 4);
     uint8_t* const parts = p.ws + (size_t)p.ctas * sizeof(PartMeta);
+    PartMeta* const meta = reinterpret_cast<PartMeta*>(p.ws) + blockIdx.x;
     const size_t part = part_bytes(p.rows, D);
 
-    long long at = plan.from, seq_at = plan.base;
-    const long long to = plan.to;
+    uint32_t at = plan.from, seq_at = plan.base;
+    const uint32_t to = plan.to, total = plan.total;
     int b = plan.b;
     bool first = true;
-    if (at >= to && threadIdx.x == 0 && (int)blockIdx.x < plan.ctas) {
-        PartMeta* meta = reinterpret_cast<PartMeta*>(p.ws) + blockIdx.x;
-        *meta = PartMeta{at, at, at, plan.total, 0, 0, 0, 0};
-    }
+    if (blockIdx.x == 0 && total == 0 && threadIdx.x == 0) *meta = PartMeta{};
     while (at < to) {
         const Sequence s = sequence(p.batch, b, p.cache.page_shift);
-        const long long per_head = sequence_tiles(p, s);
+        const uint32_t per_head = sequence_tiles(p, s);
         if (at - seq_at >= per_head * p.cache.heads) {
             seq_at += per_head * p.cache.heads;
             ++b;
             continue;
         }
-        const int head = (int)((at - seq_at) / per_head);
-        long long item = seq_at + per_head * head;           // the item's first tile
-        int r0 = 0, tiles;
+        const uint32_t head = (at - seq_at) / per_head;
+        uint32_t item = seq_at + per_head * head, tiles;     // the item's first tile
+        int r0 = 0;
         for (;; r0 += p.rows, item += tiles) {
             tiles = item_tiles(p, s, r0);
             if (at < item + tiles) break;
         }
-        const int rows = (int)min((long long)p.rows, (long long)s.n * p.group - r0);
-        const long long end = min(item + tiles, to);
+        const int rows = min(p.rows, s.n * p.group - r0);
+        const uint32_t end = min(item + tiles, to);
         a.b = b;
-        a.head = head;
+        a.head = (int)head;
         a.row0 = r0;
         a.rows = rows;
         a.s = s;
@@ -1019,15 +1021,14 @@ attend_kernel(const __grid_constant__ AttendArgs p)
         a.some_hi = row_hi(p, s, r0 + rows - 1);
         a.all_lo = row_lo(p, s, r0 + rows - 1);
         a.all_hi = row_hi(p, s, r0);
-        const int key0 = a.some_lo / kTile * kTile;
-        const int from_key = key0 + (int)(at - item) * kTile, to_key = (int)min((long long)key0 + (end - item) * kTile, (long long)a.some_hi);
-        a.run(from_key, to_key, factors);
+        const int key0 = a.some_lo >> p.tile_shift << p.tile_shift;
+        const long long past = (long long)key0 + ((long long)(end - item) << p.tile_shift);
+        a.run((int)min(key0 + ((long long)(at - item) << p.tile_shift), (long long)a.some_hi), (int)min(past, (long long)a.some_hi));
         const bool whole = at == item && end == item + tiles;
         if (first && threadIdx.x == 0) {
-            PartMeta* meta = reinterpret_cast<PartMeta*>(p.ws) + blockIdx.x;
             bool ok = true;
             MXQ_CHECKED(meta, sizeof(PartMeta), ok = false)
-            if (ok) *meta = PartMeta{at, item, item + tiles, plan.total, b, head, r0, rows};
+            if (ok) *meta = PartMeta{at, item, item + tiles, total, b, (int)head, r0, rows};
         }
         a.finish(reinterpret_cast<float*>(shared), whole, parts + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * part);
         first = false;
@@ -1043,8 +1044,8 @@ int run(const AttendArgs& p, cudaStream_t stream)
     using S = Shape<FMT, D, NT>;
     static std::atomic<uint64_t> done{0};
     auto kern = attend_kernel<FMT, D, NT, PIECES>;
-    if (int rc = allow_smem(reinterpret_cast<const void*>(kern), S::total, done)) return rc;
-    return launch_grid(kern, dim3((unsigned)p.ctas), kThreads, S::total, 1, stream, p);
+    if (int rc = allow_smem(reinterpret_cast<const void*>(kern), S::total(S::most), done)) return rc;
+    return launch_grid(kern, dim3((unsigned)p.ctas), p.warps * 32, S::total(p.warps), 1, stream, p);
 }
 
 template <int FMT, int D, int PIECES>

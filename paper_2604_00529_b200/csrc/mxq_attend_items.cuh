@@ -7,7 +7,6 @@
 namespace mxq {
 namespace {
 
-constexpr int kTile = 64;                                   // keys: what is shared out among CTAs
 constexpr float kNone = -1e30f;                             // m of a row that has seen nothing (finite: -inf - kNone is no NaN)
 
 // ---- items ----------------------------------------------------------------------------------------------------
@@ -27,34 +26,44 @@ __device__ __forceinline__ int row_lo(const AttendArgs& p, const Sequence& s, in
     return p.window ? max(s.length - s.n + row / p.group + 1 - p.window, 0) : 0;
 }
 
-__device__ __forceinline__ int item_tiles(const AttendArgs& p, const Sequence& s, int r0)
+// Tiles of the item that begins with row r0; those of one head of a sequence.
+__device__ __forceinline__ uint32_t item_tiles(const AttendArgs& p, const Sequence& s, int r0)
 {
     const int last = (int)min((long long)r0 + p.rows, (long long)s.n * p.group) - 1;
-    const int lo = row_lo(p, s, r0) / kTile, hi = (row_hi(p, s, last) + kTile - 1) / kTile;
-    return max(hi - lo, 1);                                 // (an item that sees nothing still writes its zeros)
+    const int lo = row_lo(p, s, r0) >> p.tile_shift, hi = (int)(((long long)row_hi(p, s, last) + (1 << p.tile_shift) - 1) >> p.tile_shift);
+    return (uint32_t)max(hi - lo, 1);                       // (an item that sees nothing still writes its zeros)
 }
-
-// Tiles of one head of a sequence.
-__device__ __forceinline__ long long sequence_tiles(const AttendArgs& p, const Sequence& s)
+__device__ __forceinline__ uint32_t sequence_tiles(const AttendArgs& p, const Sequence& s)
 {
-    const long long rows = (long long)s.n * p.group;
-    long long sum = 0;
-    for (long long r = 0; r < rows; r += p.rows) sum += item_tiles(p, s, (int)r);
+    const int rows = s.n * p.group;                         // below 2^31: the host has seen to that, and to the sum of all tiles
+    uint32_t sum = 0;
+    for (int r = 0; r < rows; r += p.rows) sum += item_tiles(p, s, r);
     return sum;
 }
 
-// What the second kernel needs of a CTA of the first: the tiles of the item that its run begins in.
+// Run c of `ctas` nearly equal runs of tiles 0 ... total - 1: each has `each` of them, the first `more` one besides.
+struct Runs {
+    uint32_t each, more;
+    __device__ __forceinline__ Runs(uint32_t total, uint32_t ctas) : each(total / ctas), more(total % ctas) {}
+    __device__ __forceinline__ uint32_t start(uint32_t c) const { return each * c + min(c, more); }
+    __device__ __forceinline__ uint32_t of(uint32_t tile) const         // the run that a tile lies in
+    {
+        const uint32_t big = (each + 1) * more;
+        return tile < big ? tile / (each + 1) : more + (tile - big) / each;
+    }
+};
+
+// What the second kernel needs of a CTA of the first: its run's first tile, the tiles of the item that it lies in, all tiles; and that
+// item's rows.
 struct PartMeta {
-    long long from, item_from, item_to, total;              // this run's first tile, the item's first and one past its last, all tiles
+    uint32_t from, item_from, item_to, total;
     int b, head, r0, rows;
 };
 
-__host__ __device__ inline size_t part_bytes(int rows, int dim) { return ((size_t)rows * (dim + 2) * 4 + 31) / 32 * 32; }
+// CTAs that work, of `ctas`: none without a round of keys for its warps, where that leaves enough of them.
+__device__ __forceinline__ uint32_t working_ctas(uint32_t total, uint32_t ctas) { return min(ctas, max(total, 1u)); }
 
-__device__ __forceinline__ long long run_start(long long total, int ctas, int c)
-{
-    return total / ctas * c + total % ctas * c / ctas;
-}
+__host__ __device__ inline size_t part_bytes(int rows, int dim) { return ((size_t)rows * (dim + 2) * 4 + 31) / 32 * 32; }
 
 __device__ __forceinline__ float exp2_approx(float v)
 {

@@ -81,7 +81,7 @@ struct AttendArgs {
     int group, rows;                                        // rows of a cache head per token; rows of an item
     int causal, window;
     float scale;                                            // times log2 e
-    int ctas;                                               // of the first kernel
+    int ctas, warps, tile_shift;                            // of the first kernel; keys of a tile: what is shared out among CTAs
 };
 
 template <int FMT>

@@ -5,124 +5,108 @@
 namespace mxq {
 namespace {
 
-// Items that the first kernel worked on in several parts: CTA c (and a row of its grid's second dimension) takes the item that run c begins
-// inside, if no earlier run begins inside it too.
+// Items that the first kernel worked on in several parts: CTA c takes the item that run c + 1 begins inside, if no earlier run begins
+// inside it too.  Its threads are shared out among the item's elements, four to a thread, and what is left of them among its parts.
+constexpr int kJoinThreads = 256;
+
 template <int PIECES>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const __grid_constant__ AttendArgs p, int dim)
 {
     pdl_release();
     pdl_acquire();
-    __shared__ float sums[256 * 4];
-    __shared__ float weight[256];
+    __shared__ float4 sums[kJoinThreads];
+    __shared__ float weights[kJoinThreads];
     const PartMeta* metas = reinterpret_cast<const PartMeta*>(p.ws);
-    const PartMeta meta0 = metas[0];
-    const int ctas = (int)min((long long)p.ctas, max(meta0.total, 1ll)), c = blockIdx.x + 1, r = blockIdx.y;
-    if (c >= ctas) return;
-    const PartMeta meta = metas[c];
-    if (meta.from <= meta.item_from || r >= meta.rows) return;
-    if (run_start(meta.total, ctas, c - 1) > meta.item_from) return;
-    int last = c;                                            // the runs c - 1 ... last have parts of it
-    {
-        long long lo = c, hi = ctas;                         // the last run that begins in front of the item's end
-        while (hi - lo > 1) {
-            const long long mid = (lo + hi) >> 1;
-            if (run_start(meta.total, ctas, (int)mid) < meta.item_to) lo = mid;
-            else hi = mid;
-        }
-        last = (int)lo;
-    }
-    const uint8_t* const parts = p.ws + (size_t)p.ctas * sizeof(PartMeta);
-    const size_t part = part_bytes(p.rows, dim);
-    const bool own = run_start(meta.total, ctas, c - 1) == meta.item_from;      // the item is the first of run c - 1
-    const int n = last - c + 2;
-    auto at = [&](int i) { return reinterpret_cast<const float*>(parts + ((size_t)(c - 1 + i) * 2 + (i == 0 && !own ? 1 : 0)) * part); };
-    // the largest maximum, then every part's weight
-    float top = kNone;
-    for (int i = threadIdx.x; i < n; i += 256) top = fmaxf(top, at(i)[p.rows * dim + 2 * r]);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    if ((threadIdx.x & 31) == 0) weight[threadIdx.x >> 5] = top;
-    __syncthreads();
-    top = weight[0];
-#pragma unroll
-    for (int w = 1; w < 8; ++w) top = fmaxf(top, weight[w]);
-    __syncthreads();
-    const int quads = dim / 4, lanes = 256 / quads;          // parts in turn among `lanes` threads of the same elements
-    const int d = threadIdx.x % quads * 4, mine = threadIdx.x / quads;
-    float v[4] = {}, sum = 0.f;
-    for (int i0 = 0; i0 < n; i0 += 256) {
-        if (i0 + (int)threadIdx.x < n) {
-            const float* x = at(i0 + threadIdx.x) + p.rows * dim + 2 * r;
-            weight[threadIdx.x] = x[1] * exp2_approx(x[0] - top);
-        }
-        __syncthreads();
-        const int some = min(256, n - i0);
+    const uint32_t c = blockIdx.x + 1, total = metas[0].total;
+    if (c >= working_ctas(total, p.ctas)) return;
+    const PartMeta meta = metas[c];                         // (every CTA that works has written its own)
+    const Runs runs(total, working_ctas(total, p.ctas));
+    const uint32_t before = runs.start(c - 1);
+    if (meta.from <= meta.item_from || before > meta.item_from) return;
+    const int n = (int)(runs.of(meta.item_to - 1) - (c - 1) + 1);      // runs c - 1 ... have parts of it
+    const size_t part = part_bytes(p.rows, dim) / 4;        // in floats
+    const float* const parts = reinterpret_cast<const float*>(p.ws + (size_t)p.ctas * sizeof(PartMeta));
+    // the first part is its run's last piece (slot 1), unless the item is that run's first; the others are their runs' first pieces (slot 0)
+    const float* const part0 = parts + ((size_t)(c - 1) * 2 + (before == meta.item_from ? 0 : 1)) * part;
+    const float* const part1 = parts + (size_t)c * 2 * part;
+    const int quads = dim / 4, slots = meta.rows * quads, lanes = slots < kJoinThreads ? kJoinThreads / slots : 1;
+    for (int slot0 = 0; slot0 < slots; slot0 += kJoinThreads) {
+        const int slot = lanes > 1 ? (int)threadIdx.x % slots : slot0 + (int)threadIdx.x, mine = lanes > 1 ? (int)threadIdx.x / slots : 0;
+        const bool on = mine < lanes && slot < slots;
+        const int r = on ? slot / quads : 0, d = on ? slot % quads * 4 : 0;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        float top = kNone, sum = 0.f;
+        if (on) {
+            const float* ml = part0 + p.rows * dim + 2 * r;
+            top = ml[0];
+#pragma unroll 8
+            for (int i = 1; i < n; ++i) top = fmaxf(top, (part1 + (size_t)(i - 1) * 2 * part + p.rows * dim + 2 * r)[0]);
 #pragma unroll 4
-        for (int i = mine; i < some; i += lanes) {
-            const float4 x = *reinterpret_cast<const float4*>(at(i0 + i) + r * dim + d);
-            const float w = weight[i];
-            sum += w;
-            v[0] += w * x.x;
-            v[1] += w * x.y;
-            v[2] += w * x.z;
-            v[3] += w * x.w;
+            for (int i = mine; i < n; i += lanes) {
+                const float* x = i ? part1 + (size_t)(i - 1) * 2 * part : part0;
+                const float2 w = *reinterpret_cast<const float2*>(x + p.rows * dim + 2 * r);
+                const float4 e = *reinterpret_cast<const float4*>(x + r * dim + d);
+                const float by = w.y * exp2_approx(w.x - top);
+                sum += by;
+                v.x += by * e.x;
+                v.y += by * e.y;
+                v.z += by * e.z;
+                v.w += by * e.w;
+            }
         }
-        __syncthreads();
+        if (lanes > 1) {
+            sums[threadIdx.x] = v;
+            weights[threadIdx.x] = sum;
+            __syncthreads();
+            if (mine != 0) return;
+            for (int k = 1; k < lanes; ++k) {
+                const float4 e = sums[threadIdx.x + k * slots];
+                sum += weights[threadIdx.x + k * slots];
+                v.x += e.x;
+                v.y += e.y;
+                v.z += e.z;
+                v.w += e.w;
+            }
+        }
+        if (!on) continue;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float out[4] = {v.x * inv, v.y * inv, v.z * inv, v.w * inv};
+        const int first = p.batch.starts ? max(ld_int(p.batch.starts + meta.b), 0) : meta.b, row = meta.r0 + r;
+        write_row<PIECES>(p, (size_t)(first + row / p.group) * (p.cache.heads * p.group) + meta.head * p.group + row % p.group, dim, d, out, top, sum);
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sums[threadIdx.x * 4 + j] = v[j];
-    weight[threadIdx.x] = sum;
-    __syncthreads();
-    if (mine != 0) return;
-    for (int k = 1; k < lanes; ++k) {
-        sum += weight[threadIdx.x + k * quads];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] += sums[(threadIdx.x + k * quads) * 4 + j];
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] *= inv;
-    const Sequence s = sequence(p.batch, meta.b, p.cache.page_shift);
-    const int row = meta.r0 + r;
-    write_row<PIECES>(p, (size_t)(s.first + row / p.group) * (p.cache.heads * p.group) + meta.head * p.group + row % p.group, dim, d, v, top, sum);
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------
 
-// Column groups of a kernel for `tokens` new tokens of `batch` sequences: as many as their rows fill, as registers allow.
-inline int column_groups(size_t tokens, size_t batch, int group, int pieces, int dim)
-{
-    const size_t per = (tokens + batch - 1) / (batch ? batch : 1), columns = per * (size_t)group * (size_t)pieces;
-    const int most = dim == 256 ? 2 : 4;
-    int nt = 1;
-    while (nt < most && columns > (size_t)8 * nt) nt *= 2;
-    return nt;
-}
-
-inline int ctas_per_sm(int nt, int dim) { return nt == 4 ? 2 : nt * dim <= 128 ? 4 : nt * dim <= 256 ? 3 : 2; }
-
-// CTAs of the first kernel: as many as the GPU holds, or tiles there can be.
-inline size_t grid_size(size_t batch, size_t tokens, int heads, int group, int rows, size_t width, int page, int nt, int dim)
-{
-    const size_t room = (size_t)148 * ctas_per_sm(nt, dim);
-    const size_t items = (tokens * group / rows + batch) * heads, tiles = (width * page + kTile - 1) / kTile + 1;
-    return items >= room || tiles >= room ? room : (items * tiles < room ? items * tiles : room);
-}
-
+// How a call is cut up: column groups of its kernel, rows of an item, CTAs and their warps, a tile's keys, bytes of workspace.
 struct Sizes {
-    int nt, rows;
+    int nt, rows, warps, tile_shift;
     size_t ctas, bytes;
 };
 
 Sizes sizes(const mxq_cache* c, const mxq_batch* b, int q_heads, int dtype, size_t tokens)
 {
+    constexpr size_t kSms = 148;
     Sizes z;
-    const int pieces = dtype == MXQ_F32 ? 2 : 1, group = q_heads / c->heads;
-    z.nt = column_groups(tokens, b->batch, group, pieces, c->head_dim);
+    const int pieces = dtype == MXQ_F32 ? 2 : 1, group = q_heads / c->heads, dim = c->head_dim;
+    // as many column groups as the rows of a mean sequence fill, as registers allow
+    const size_t columns = (tokens + b->batch - 1) / b->batch * (size_t)group * (size_t)pieces;
+    z.nt = 1;
+    while (z.nt < (dim == 256 ? 2 : 4) && columns > (size_t)8 * z.nt) z.nt *= 2;
     z.rows = 8 * z.nt / pieces;
-    z.ctas = grid_size(b->batch, tokens, c->heads, group, z.rows, b->width, c->page, z.nt, c->head_dim);
-    z.bytes = z.ctas * (sizeof(PartMeta) + 2 * part_bytes(z.rows, c->head_dim));
+    const size_t items = (tokens * group / z.rows + b->batch) * c->heads, keys = b->width * (size_t)c->page < (size_t)1 << 31 ? b->width * (size_t)c->page : (size_t)1 << 31;     // at most
+    const int ctas = z.nt == 4 ? 2 : z.nt * dim <= 128 ? 4 : z.nt * dim <= 256 ? 3 : 2;      // per SM, of four warps
+    // Few items: one CTA per SM with all the warps that it holds, so that an item has a quarter of the parts.
+    const bool wide = z.nt == 1 && items <= kSms;
+    z.warps = wide ? 4 * ctas : 4;
+    const size_t room = wide ? kSms : kSms * ctas;
+    // tiles of 64 keys, longer ones where there could be more of them than 32 bits count
+    z.tile_shift = 6;
+    while ((keys >> z.tile_shift) + 1 > (((size_t)1 << 31) - 1) / items) ++z.tile_shift;
+    const size_t tiles = items * ((keys >> z.tile_shift) + 1);
+    z.ctas = tiles < room ? tiles : room;
+    z.bytes = z.ctas * (sizeof(PartMeta) + 2 * part_bytes(z.rows, dim));
     return z;
 }
 
@@ -132,7 +116,7 @@ int check(const mxq_cache* c, const mxq_batch* b, int q_heads, int dtype, size_t
     if (int rc = check_batch(b, tokens)) return rc;
     if (dtype != MXQ_F32 && dtype != MXQ_BF16) return MXQ_ERR_FORMAT;
     if (q_heads < 1 || q_heads > (1 << 16) || q_heads % c->heads) return MXQ_ERR_SIZE;
-    if (tokens * (size_t)(q_heads / c->heads) >= ((size_t)1 << 31)) return MXQ_ERR_SIZE;
+    if (tokens * (size_t)q_heads + b->batch * (size_t)c->heads > MXQ_CACHE_ROWS_MAX) return MXQ_ERR_SIZE;
     return MXQ_OK;
 }
 
@@ -186,6 +170,8 @@ int mxq_cache_attention(const mxq_cache* cache, const mxq_batch* batch, const mx
     a.window = window > (size_t)0x7FFFFFFF ? 0 : (int)window;
     a.scale = scale * 1.4426950408889634f;
     a.ctas = (int)z.ctas;
+    a.warps = z.warps;
+    a.tile_shift = z.tile_shift;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     int rc = MXQ_ERR_FORMAT;
     switch (cache->fmt) {
@@ -197,7 +183,7 @@ int mxq_cache_attention(const mxq_cache* cache, const mxq_batch* batch, const mx
     }
     if (rc != MXQ_OK || a.ctas == 1) return rc;
     auto join = dtype == MXQ_F32 ? join_kernel<2> : join_kernel<1>;
-    return launch_grid(join, dim3((unsigned)a.ctas - 1, (unsigned)a.rows), 256, 0, 1, s, a, cache->head_dim);
+    return launch_grid(join, dim3((unsigned)a.ctas - 1), kJoinThreads, 0, 1, s, a, cache->head_dim);
 }
 
 }  // extern "C"
