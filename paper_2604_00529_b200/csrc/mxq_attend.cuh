@@ -752,7 +752,8 @@ struct Attend {
 #pragma unroll
             for (int i = 0; i < per; ++i) v[i] = 0.f;
             if (r < rows) {
-                const uint8_t* at = p.q + (size_t)(s.first + row / p.group) * p.q_token + (size_t)(head * p.group + row % p.group) * p.q_head;
+                const int i = row_token(p, s, row);
+                const uint8_t* at = p.q + (size_t)(s.first + i) * p.q_token + (size_t)(head * p.group + row - i * p.group) * p.q_head;
                 if constexpr (PIECES == 2) {
 #pragma unroll
                     for (int i = 0; i < per; ++i) v[i] = __uint_as_float(ld_u32(at + (lane * per + i) * 4));
@@ -785,8 +786,8 @@ struct Attend {
                 if (top == 255u) back = __uint_as_float(0x7FC00000u);
                 const uint32_t at = qs + S::columns_at + c * 12;
                 asm volatile("st.shared.f32 [%0], %1;" :: "r"(at), "f"(back) : "memory");
-                asm volatile("st.shared.u32 [%0 + 4], %1;" :: "r"(at), "r"(row_lo(p, s, row)) : "memory");
-                asm volatile("st.shared.u32 [%0 + 8], %1;" :: "r"(at), "r"(row_hi(p, s, row)) : "memory");
+                asm volatile("st.shared.u32 [%0 + 4], %1;" :: "r"(at), "r"(token_lo(p, s, row_token(p, s, row))) : "memory");
+                asm volatile("st.shared.u32 [%0 + 8], %1;" :: "r"(at), "r"(token_hi(p, s, row_token(p, s, row))) : "memory");
             }
         }
     }
@@ -852,50 +853,52 @@ struct Attend {
 
     // -- the warps' results together: normalized sums and their weights in shared memory, then to the output or to a part
 
-    __device__ __forceinline__ void finish(float* area, bool whole, uint8_t* part)
+    __device__ __forceinline__ void finish(float* area, bool whole, uint8_t* part, int some)      // some: warps that had keys, one at least
     {
         constexpr int R = 8 * NT / PIECES;                   // rows of the tile
         float* const o_at = area + warp * R * D;
         float* const ml = area + warps * R * D;             // [warp][row][m, l]
-        float scales[NB];
+        if (warp < some) {
+            float scales[NB];
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            const int byte = __shfl_sync(0xFFFFFFFFu, vref[i % HB], i / HB);
-            scales[i] = scale_value((uint32_t)max(byte, 0));
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int j = 0; j < 3 - PIECES; ++j) {
-                float sum = l[n][j];
-#pragma unroll
-                for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                const int r = PIECES == 1 ? 8 * n + 2 * t + j : 4 * n + t;
-                if (g == 0) {
-                    ml[(warp * R + r) * 2] = m[n][j];
-                    ml[(warp * R + r) * 2 + 1] = sum;
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    float x = acc[i][n][j], y = acc[i][n][2 + j];
-                    if constexpr (PIECES == 2) {
-                        x += acc[i][n][1];
-                        y += acc[i][n][3];
-                    }
-                    const int d = S::bits == 4 ? (i >> 1) * 32 + 4 * g + (i & 1) * 2 : i * 16 + 2 * g;
-                    *reinterpret_cast<float2*>(o_at + r * D + d) = make_float2(x * inv * scales[i >> 1], y * inv * scales[i >> 1]);
-                }
+            for (int i = 0; i < NB; ++i) {
+                const int byte = __shfl_sync(0xFFFFFFFFu, vref[i % HB], i / HB);
+                scales[i] = scale_value((uint32_t)max(byte, 0));
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 3 - PIECES; ++j) {
+                    float sum = l[n][j];
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    const int r = PIECES == 1 ? 8 * n + 2 * t + j : 4 * n + t;
+                    if (g == 0) {
+                        ml[(warp * R + r) * 2] = m[n][j];
+                        ml[(warp * R + r) * 2 + 1] = sum;
+                    }
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        float x = acc[i][n][j], y = acc[i][n][2 + j];
+                        if constexpr (PIECES == 2) {
+                            x += acc[i][n][1];
+                            y += acc[i][n][3];
+                        }
+                        const int d = S::bits == 4 ? (i >> 1) * 32 + 4 * g + (i & 1) * 2 : i * 16 + 2 * g;
+                        *reinterpret_cast<float2*>(o_at + r * D + d) = make_float2(x * inv * scales[i >> 1], y * inv * scales[i >> 1]);
+                    }
+                }
+        }
         __syncthreads();
-        for (int i = threadIdx.x; i < rows * (D / 4); i += warps * 32) {
-            const int r = i / (D / 4), d = i % (D / 4) * 4;
+        for (int at = threadIdx.x; at < rows * (D / 4); at += warps * 32) {
+            const int r = at / (D / 4), d = at % (D / 4) * 4;
             float top = kNone;
 #pragma unroll 4
-            for (int w = 0; w < warps; ++w) top = fmaxf(top, ml[(w * R + r) * 2]);
+            for (int w = 0; w < some; ++w) top = fmaxf(top, ml[(w * R + r) * 2]);
             float sum = 0.f, v[4] = {};
 #pragma unroll 4
-            for (int w = 0; w < warps; ++w) {
+            for (int w = 0; w < some; ++w) {
                 const float wt = ml[(w * R + r) * 2 + 1] * exp2_approx(ml[(w * R + r) * 2] - top);
                 const float4 x = *reinterpret_cast<const float4*>(area + (w * R + r) * D + d);
                 sum += wt;
@@ -908,8 +911,8 @@ struct Attend {
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] *= inv;
             if (whole) {
-                const int row = row0 + r;
-                write_row<PIECES>(p, (size_t)(s.first + row / p.group) * (p.cache.heads * p.group) + head * p.group + row % p.group, D, d, v, top, sum);
+                const int row = row0 + r, i = row_token(p, s, row);
+                write_row<PIECES>(p, (size_t)(s.first + i) * (p.cache.heads * p.group) + head * p.group + row - i * p.group, D, d, v, top, sum);
             } else {
                 float* const to = reinterpret_cast<float*>(part);
                 MXQ_CHECKED(to + r * D + d, 16, continue)
@@ -926,16 +929,24 @@ struct Attend {
 
 // The run of a CTA: its first and one past its last tile, the sequence that the first lies in and the tiles in front of that.
 struct Plan {
-    uint32_t total, from, to, base;
+    uint32_t total, from, to, base, per_head;
     int b;
+    Sequence s;
 };
 
 __device__ __forceinline__ void make_plan(const AttendArgs& p, int warps, Plan& plan, uint32_t (&warp_sum)[16])
 {
     const int threads = warps * 32, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int per = (p.batch.batch + threads - 1) / threads, first = min((int)threadIdx.x * per, p.batch.batch), last = min(first + per, p.batch.batch);
-    uint32_t mine = 0;
-    for (int b = first; b < last; ++b) mine += sequence_tiles(p, sequence(p.batch, b, p.cache.page_shift)) * p.cache.heads;
+    // a sequence per thread, or a few in a row
+    const int per = p.batch.batch <= threads ? 1 : (p.batch.batch + threads - 1) / threads;
+    const int first = min((int)threadIdx.x * per, p.batch.batch), last = min(first + per, p.batch.batch);
+    Sequence s = {0, 0, 0};
+    uint32_t mine = 0, per_head = 0;
+    for (int b = first; b < last; ++b) {
+        s = sequence(p.batch, b, p.cache.page_shift);
+        per_head = sequence_tiles(p, s);
+        mine += per_head * p.cache.heads;
+    }
     uint32_t before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -944,23 +955,24 @@ __device__ __forceinline__ void make_plan(const AttendArgs& p, int warps, Plan& 
     }
     if (lane == 31) warp_sum[warp] = before;
     __syncthreads();
-    uint32_t total = 0;
-    for (int w = 0; w < warps; ++w) {
-        if (w < warp) before += warp_sum[w];
-        total += warp_sum[w];
-    }
-    before -= mine;
+    uint32_t sum = lane < warps ? warp_sum[lane] : 0u;
+    const uint32_t total = __reduce_add_sync(0xFFFFFFFFu, sum);
+    if (lane >= warp) sum = 0;
+    before += __reduce_add_sync(0xFFFFFFFFu, sum) - mine;
     const uint32_t ctas = working_ctas(total, gridDim.x);
     const Runs runs(total, ctas);
     const uint32_t from = blockIdx.x < ctas ? runs.start(blockIdx.x) : total, to = blockIdx.x < ctas ? runs.start(blockIdx.x + 1) : total;
     if (from < to ? from >= before && from < before + mine : threadIdx.x == 0) {            // one thread's
         int b = first;
-        for (; from < to && b < last; ++b) {
-            const uint32_t n = sequence_tiles(p, sequence(p.batch, b, p.cache.page_shift)) * p.cache.heads;
-            if (from < before + n) break;
-            before += n;
+        if (per > 1) {
+            for (; from < to && b < last; ++b) {
+                s = sequence(p.batch, b, p.cache.page_shift);
+                per_head = sequence_tiles(p, s);
+                if (from < before + per_head * p.cache.heads) break;
+                before += per_head * p.cache.heads;
+            }
         }
-        plan = Plan{total, from, to, before, b};
+        plan = Plan{total, from, to, before, per_head, b, s};
     }
     __syncthreads();
 }
@@ -995,42 +1007,49 @@ attend_kernel(const __grid_constant__ AttendArgs p)
     int b = plan.b;
     bool first = true;
     if (blockIdx.x == 0 && total == 0 && threadIdx.x == 0) *meta = PartMeta{};
+    Sequence s = plan.s;
+    uint32_t per_head = plan.per_head;
     while (at < to) {
-        const Sequence s = sequence(p.batch, b, p.cache.page_shift);
-        const uint32_t per_head = sequence_tiles(p, s);
         if (at - seq_at >= per_head * p.cache.heads) {
             seq_at += per_head * p.cache.heads;
             ++b;
+            s = sequence(p.batch, b, p.cache.page_shift);
+            per_head = sequence_tiles(p, s);
             continue;
         }
         const uint32_t head = (at - seq_at) / per_head;
-        uint32_t item = seq_at + per_head * head, tiles;     // the item's first tile
+        uint32_t item = seq_at + per_head * head, tiles = per_head;      // the item's first tile
         int r0 = 0;
-        for (;; r0 += p.rows, item += tiles) {
-            tiles = item_tiles(p, s, r0);
-            if (at < item + tiles) break;
+        if (s.n * p.group > p.rows) {
+            for (;; r0 += p.rows, item += tiles) {
+                tiles = item_tiles(p, s, r0);
+                if (at < item + tiles) break;
+            }
         }
-        const int rows = min(p.rows, s.n * p.group - r0);
+        const int rows = min(p.rows, s.n * p.group - r0), first_token = row_token(p, s, r0), last_token = row_token(p, s, r0 + rows - 1);
         const uint32_t end = min(item + tiles, to);
         a.b = b;
         a.head = (int)head;
         a.row0 = r0;
         a.rows = rows;
         a.s = s;
-        a.some_lo = row_lo(p, s, r0);
-        a.some_hi = row_hi(p, s, r0 + rows - 1);
-        a.all_lo = row_lo(p, s, r0 + rows - 1);
-        a.all_hi = row_hi(p, s, r0);
-        const int key0 = a.some_lo >> p.tile_shift << p.tile_shift;
-        const long long past = (long long)key0 + ((long long)(end - item) << p.tile_shift);
-        a.run((int)min(key0 + ((long long)(at - item) << p.tile_shift), (long long)a.some_hi), (int)min(past, (long long)a.some_hi));
+        a.some_lo = token_lo(p, s, first_token);
+        a.some_hi = token_hi(p, s, last_token);
+        a.all_lo = token_lo(p, s, last_token);
+        a.all_hi = token_hi(p, s, first_token);
+        // (keys are below 2^31, tiles behind the last one reach no further than one tile beyond it)
+        const uint32_t key0 = (uint32_t)(a.some_lo >> p.tile_shift << p.tile_shift);
+        const int from_key = (int)min(key0 + ((at - item) << p.tile_shift), (uint32_t)a.some_hi);
+        const int to_key = (int)min(key0 + ((end - item) << p.tile_shift), (uint32_t)a.some_hi);
+        a.run(from_key, to_key);
         const bool whole = at == item && end == item + tiles;
         if (first && threadIdx.x == 0) {
             bool ok = true;
             MXQ_CHECKED(meta, sizeof(PartMeta), ok = false)
-            if (ok) *meta = PartMeta{at, item, item + tiles, total, b, (int)head, r0, rows};
+            if (ok) *meta = PartMeta{at, item, item + tiles, total, s.first, (int)head, r0, rows};
         }
-        a.finish(reinterpret_cast<float*>(shared), whole, parts + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * part);
+        a.finish(reinterpret_cast<float*>(shared), whole, parts + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * part,
+                 min(warps, max((to_key - from_key + S::step - 1) / S::step, 1)));
         first = false;
         at = end;
     }

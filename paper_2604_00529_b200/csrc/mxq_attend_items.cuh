@@ -11,31 +11,30 @@ constexpr float kNone = -1e30f;                             // m of a row that h
 
 // ---- items ----------------------------------------------------------------------------------------------------
 
-// Keys that rows r0 ... r1 - 1 of a sequence see between them.
-struct Span {
-    int lo, hi;
-};
+// The new token that a row belongs to.  (A division costs some thirty instructions that depend on one another; one token is the common case.)
+__device__ __forceinline__ int row_token(const AttendArgs& p, const Sequence& s, int row) { return s.n == 1 ? 0 : row / p.group; }
 
-__device__ __forceinline__ int row_hi(const AttendArgs& p, const Sequence& s, int row)
+// The keys [lo, hi) that a new token of a sequence sees.
+__device__ __forceinline__ int token_hi(const AttendArgs& p, const Sequence& s, int i) { return p.causal ? max(s.length - s.n + i + 1, 0) : s.length; }
+__device__ __forceinline__ int token_lo(const AttendArgs& p, const Sequence& s, int i) { return p.window ? max(s.length - s.n + i + 1 - p.window, 0) : 0; }
+
+__device__ __forceinline__ uint32_t span_tiles(const AttendArgs& p, int lo, int hi)
 {
-    if (!p.causal) return s.length;
-    return max(s.length - s.n + row / p.group + 1, 0);
-}
-__device__ __forceinline__ int row_lo(const AttendArgs& p, const Sequence& s, int row)
-{
-    return p.window ? max(s.length - s.n + row / p.group + 1 - p.window, 0) : 0;
+    const int tiles = (int)(((uint32_t)hi + ((1u << p.tile_shift) - 1u)) >> p.tile_shift) - (lo >> p.tile_shift);
+    return (uint32_t)max(tiles, 1);                         // (an item that sees nothing still writes its zeros)
 }
 
-// Tiles of the item that begins with row r0; those of one head of a sequence.
+// Tiles of the item that begins with row r0, and of one head of a sequence.
 __device__ __forceinline__ uint32_t item_tiles(const AttendArgs& p, const Sequence& s, int r0)
 {
-    const int last = (int)min((long long)r0 + p.rows, (long long)s.n * p.group) - 1;
-    const int lo = row_lo(p, s, r0) >> p.tile_shift, hi = (int)(((long long)row_hi(p, s, last) + (1 << p.tile_shift) - 1) >> p.tile_shift);
-    return (uint32_t)max(hi - lo, 1);                       // (an item that sees nothing still writes its zeros)
+    const int last = min(r0 + p.rows, s.n * p.group) - 1;
+    return span_tiles(p, token_lo(p, s, row_token(p, s, r0)), token_hi(p, s, row_token(p, s, last)));
 }
 __device__ __forceinline__ uint32_t sequence_tiles(const AttendArgs& p, const Sequence& s)
 {
-    const int rows = s.n * p.group;                         // below 2^31: the host has seen to that, and to the sum of all tiles
+    const int rows = s.n * p.group;                         // far below 2^31: the host has seen to that, and to the sum of all tiles
+    if (rows == 0) return 0;
+    if (rows <= p.rows) return span_tiles(p, token_lo(p, s, 0), token_hi(p, s, s.n - 1));
     uint32_t sum = 0;
     for (int r = 0; r < rows; r += p.rows) sum += item_tiles(p, s, r);
     return sum;
@@ -57,7 +56,7 @@ struct Runs {
 // item's rows.
 struct PartMeta {
     uint32_t from, item_from, item_to, total;
-    int b, head, r0, rows;
+    int first, head, r0, rows;                              // first: the row of the tokens' tensors that its sequence begins with
 };
 
 // CTAs that work, of `ctas`: none without a round of keys for its warps, where that leaves enough of them.

@@ -72,8 +72,8 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
         if (!on) continue;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const float out[4] = {v.x * inv, v.y * inv, v.z * inv, v.w * inv};
-        const int first = p.batch.starts ? max(ld_int(p.batch.starts + meta.b), 0) : meta.b, row = meta.r0 + r;
-        write_row<PIECES>(p, (size_t)(first + row / p.group) * (p.cache.heads * p.group) + meta.head * p.group + row % p.group, dim, d, out, top, sum);
+        const int i = meta.r0 + r < p.group ? 0 : (meta.r0 + r) / p.group;      // the row's token
+        write_row<PIECES>(p, (size_t)(meta.first + i) * (p.cache.heads * p.group) + meta.head * p.group + meta.r0 + r - i * p.group, dim, d, out, top, sum);
     }
 }
 
