@@ -89,7 +89,7 @@ _host = None            # the native module _mxq_host (csrc/host_calls.cpp): the
 _HOST_CALLS = ("mxq_quantize", "mxq_slice_scale", "mxq_slice_scale_multi", "mxq_dequantize", "mxq_tiled_scales_bytes",
                "mxq_quantize_tiled", "mxq_slice_scale_tiled", "mxq_fake_quant", "mxq_fake_quant_bwd", "mxq_codes_bytes",
                "mxq_matmul", "mxq_quantize_matrix", "mxq_matrix_codes_bytes", "mxq_matrix_scales_bytes", "mxq_moe",
-               "mxq_moe_workspace_bytes")
+               "mxq_moe_workspace_bytes", "mxq_cache_write", "mxq_cache_read", "mxq_cache_attention", "mxq_cache_attention_workspace_bytes")
 
 
 def library_path() -> str:
@@ -966,7 +966,9 @@ def cache_write(k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor, k_scale
     buffers).  ``table`` [batch, width], ``lengths`` [batch] (the new tokens counted) and ``starts`` [batch + 1] are int32 tensors on the
     device; without ``starts`` row b is sequence b's one new token.  Any strides (rows that are no multiples of 32 bytes apart are copied
     first).  Two sequences of a call must not write to the same place."""
-    L = load_library()
+    L = _lib or load_library()
+    if _host.cache_write(k, v, k_codes, k_scales, v_codes, v_scales, table, lengths, fmt, block, starts, stream):
+        return
     dev = k_codes.device
     with _Place(dev, stream):
         c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, lengths, starts, dev)
@@ -984,7 +986,10 @@ def cache_read(k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Ten
                out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """mxq_cache_read: keys and values, [total, heads, head_dim] each, of the first starts[b + 1] - starts[b] tokens of every sequence, in
     rows starts[b] ...  ``out`` (a pair): rows behind starts[batch] are left as they were."""
-    L = load_library()
+    L = _lib or load_library()
+    made = _host.cache_read(k_codes, k_scales, v_codes, v_scales, table, starts, total, fmt, block, dtype, out, stream)
+    if made is not None:
+        return made
     dev = k_codes.device
     if total < 0:
         raise ValueError("negative size")
@@ -1019,7 +1024,11 @@ def cache_attention(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tens
     query sees the tokens up to its own, with ``window`` only the last so many of them; lse: a float32 tensor [tokens, q_heads] for the
     logarithms of the softmax's sums.  ``workspace`` (uint8, ``cache_attention_workspace_bytes``) saves the allocation of one per call; calls that
     can overlap on the GPU must not share it.  A query that sees nothing gives zeros.  For serving: the result has no gradient."""
-    L = load_library()
+    L = _lib or load_library()
+    made = _host.cache_attention(q, k_codes, k_scales, v_codes, v_scales, table, lengths, fmt, block, starts, scale, causal, window, out, lse, workspace,
+                                 stream)
+    if made is not None:
+        return made
     dev = k_codes.device
     with _Place(dev, stream):
         c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, lengths, starts, dev)

@@ -9,6 +9,8 @@
 // always raised.
 #include <Python.h>
 
+#include <cmath>
+
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
@@ -44,6 +46,10 @@ struct Api {
     decltype(&mxq_matrix_scales_bytes) matrix_scales_bytes;
     decltype(&mxq_moe) moe;
     decltype(&mxq_moe_workspace_bytes) moe_workspace_bytes;
+    decltype(&mxq_cache_write) cache_write;
+    decltype(&mxq_cache_read) cache_read;
+    decltype(&mxq_cache_attention) cache_attention;
+    decltype(&mxq_cache_attention_workspace_bytes) cache_attention_workspace_bytes;
 } api;
 
 PyObject* formats = nullptr;          // the binding's name -> id dict
@@ -704,6 +710,143 @@ PyObject* linear_ste(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- a paged cache of keys and values held as codes ---------------------------------------------------------
+
+// The four buffers of a cache, whose shapes agree, on the current device.
+bool cache_of(PyObject* const* a, int fmt, int block, mxq_cache* c, c10::Device* dev)
+{
+    const at::Tensor* t[4];
+    for (int i = 0; i < 4; ++i)
+        if (!(t[i] = plain(a[i])) || t[i]->scalar_type() != at::kByte || t[i]->dim() != 4) return false;
+    *dev = t[0]->device();
+    const int64_t bits = fmt == MXQ_FP8_E4M3 || fmt == MXQ_INT8 ? 8 : fmt == MXQ_FP4_E2M1 || fmt == MXQ_INT4 ? 4 : 0;
+    if (!bits || block <= 0) return false;
+    const int64_t pages = t[0]->size(0), heads = t[0]->size(1), page = t[0]->size(2), dim = t[0]->size(3) * 8 / bits;
+    if (heads > MXQ_CACHE_HEADS_MAX || page > 4096 || dim > 4096) return false;
+    for (int i = 0; i < 4; ++i)
+        if (!here(*t[i], *dev) || t[i]->size(0) != pages || t[i]->size(1) != heads || t[i]->size(2) != page ||
+            t[i]->size(3) != (i % 2 ? dim / block : t[0]->size(3)))
+            return false;
+    *c = mxq_cache{t[0]->data_ptr(), bytes(*t[1]), t[2]->data_ptr(), bytes(*t[3]), (size_t)pages, (int)page, (int)heads, (int)dim, fmt, block};
+    return true;
+}
+
+bool ints(PyObject* o, int64_t n, c10::Device dev, const int32_t** to)
+{
+    const at::Tensor* t = plain(o);
+    if (!t || t->scalar_type() != at::kInt || t->dim() != 1 || t->size(0) != n || !here(*t, dev)) return false;
+    *to = static_cast<const int32_t*>(t->data_ptr());
+    return true;
+}
+
+bool batch_of(PyObject* table, PyObject* lengths, PyObject* starts, c10::Device dev, mxq_batch* b)
+{
+    const at::Tensor* t = plain(table);
+    if (!t || t->scalar_type() != at::kInt || t->dim() != 2 || !here(*t, dev)) return false;
+    *b = mxq_batch{static_cast<const int32_t*>(t->data_ptr()), nullptr, nullptr, (size_t)t->size(0), (size_t)t->size(1)};
+    return (!lengths || ints(lengths, t->size(0), dev, &b->lengths)) && (starts == Py_None || ints(starts, t->size(0) + 1, dev, &b->starts));
+}
+
+// A [tokens, heads, head_dim] tensor that the kernels take as it lies.
+const at::Tensor* rows_of(PyObject* o, c10::Device dev, mxq_rows* r)
+{
+    if (!THPVariable_CheckExact(o) && Py_TYPE(o) != parameter) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    int dt;
+    if (!t.defined() || !t.is_cuda() || t.unsafeGetTensorImpl()->is_python_dispatch() || !t.has_storage() || t.layout() != at::kStrided || t.dim() != 3 ||
+        !dtype_id(t, &dt) || !here(t, dev))
+        return nullptr;
+    const int64_t size = t.element_size();
+    if (t.stride(2) != 1 || t.stride(0) < 0 || t.stride(1) < 0 || t.stride(0) * size % 32 || t.stride(1) * size % 32) return nullptr;
+    *r = mxq_rows{t.data_ptr(), (size_t)t.stride(0), (size_t)t.stride(1)};
+    return &t;
+}
+
+// cache_write(k, v, k_codes, k_scales, v_codes, v_scales, table, lengths, fmt, block, starts, stream)
+PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int fmt, block, dt;
+    mxq_cache c;
+    mxq_batch b;
+    mxq_rows kr, vr;
+    c10::Device dev(c10::kCUDA, 0);
+    GENERAL_UNLESS(nargs == 12 && a[11] == Py_None && format_id(a[8], &fmt) && as_int(a[9], &block) && !modes_active());
+    GENERAL_UNLESS(cache_of(a + 2, fmt, block, &c, &dev) && batch_of(a[6], a[7], a[10], dev, &b));
+    const at::Tensor *k = rows_of(a[0], dev, &kr), *v = rows_of(a[1], dev, &vr);
+    GENERAL_UNLESS(k && v && dtype_id(*k, &dt) && v->scalar_type() == k->scalar_type() && k->sizes() == v->sizes() && k->size(1) == c.heads &&
+                   k->size(2) == c.head_dim);
+    const int rc = unlocked([&] { return api.cache_write(&c, &b, &kr, &vr, dt, (size_t)k->size(0), current_stream()); });
+    GENERAL_UNLESS(rc == MXQ_OK);
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// cache_read(k_codes, k_scales, v_codes, v_scales, table, starts, total, fmt, block, dtype, out, stream), out None
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int fmt, block, dt;
+    int64_t total;
+    mxq_cache c;
+    mxq_batch b;
+    c10::Device dev(c10::kCUDA, 0);
+    GENERAL_UNLESS(nargs == 12 && a[10] == Py_None && a[11] == Py_None && as_count(a[6], &total) && format_id(a[7], &fmt) && as_int(a[8], &block) &&
+                   THPDtype_Check(a[9]) && !modes_active());
+    const at::ScalarType type = reinterpret_cast<THPDtype*>(a[9])->scalar_type;
+    GENERAL_UNLESS(dtype_id(type, &dt) && cache_of(a, fmt, block, &c, &dev) && a[5] != Py_None && batch_of(a[4], nullptr, a[5], dev, &b));
+    at::Tensor k, v;
+    const int rc = unlocked([&] {
+        const auto options = at::TensorOptions().dtype(type).device(dev);
+        k = at::empty({total, c.heads, c.head_dim}, options);
+        v = at::empty({total, c.heads, c.head_dim}, options);
+        return api.cache_read(&c, &b, (size_t)total, k.data_ptr(), v.data_ptr(), dt, current_stream());
+    });
+    GENERAL_UNLESS(rc == MXQ_OK);
+    return pair(THPVariable_Wrap(k), THPVariable_Wrap(v));
+    END_HANDLE_TH_ERRORS
+}
+
+// cache_attention(q, k_codes, k_scales, v_codes, v_scales, table, lengths, fmt, block, starts, scale, causal, window, out, lse, workspace, stream)
+PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    int fmt, block, dt;
+    int64_t window;
+    mxq_cache c;
+    mxq_batch b;
+    mxq_rows qr;
+    c10::Device dev(c10::kCUDA, 0);
+    GENERAL_UNLESS(nargs == 17 && a[16] == Py_None && format_id(a[7], &fmt) && as_int(a[8], &block) && (a[10] == Py_None || PyFloat_CheckExact(a[10])) &&
+                   PyBool_Check(a[11]) && as_count(a[12], &window) && !modes_active());
+    GENERAL_UNLESS(cache_of(a + 1, fmt, block, &c, &dev) && batch_of(a[5], a[6], a[9], dev, &b));
+    const at::Tensor* q = rows_of(a[0], dev, &qr);
+    Output out, ws;
+    GENERAL_UNLESS(q && dtype_id(*q, &dt) && q->size(2) == c.head_dim && q->size(1) <= (1 << 16) && out.take(a[13]) && ws.take(a[15]));
+    GENERAL_UNLESS(!out.tensor || (out.tensor->sizes() == q->sizes() && out.tensor->scalar_type() == q->scalar_type() && here(*out.tensor, dev)));
+    GENERAL_UNLESS(!ws.tensor || operand(ws.tensor, 0, dev));
+    float* lse = nullptr;
+    if (a[14] != Py_None) {
+        const at::Tensor* t = plain(a[14]);
+        GENERAL_UNLESS(t && t->scalar_type() == at::kFloat && t->dim() == 2 && t->size(0) == q->size(0) && t->size(1) == q->size(1) && here(*t, dev));
+        lse = static_cast<float*>(t->data_ptr());
+    }
+    const int q_heads = (int)q->size(1);
+    const size_t tokens = (size_t)q->size(0);
+    const double scale = a[10] == Py_None ? 1 / std::sqrt((double)c.head_dim) : PyFloat_AS_DOUBLE(a[10]);
+    const int rc = unlocked([&] {
+        out.make(q->sizes(), q->scalar_type(), *q);
+        ws.make({(int64_t)api.cache_attention_workspace_bytes(&c, &b, q_heads, dt, tokens)}, at::kByte, *q);
+        return api.cache_attention(&c, &b, &qr, q_heads, dt, tokens, (float)scale, a[11] == Py_True, (size_t)window, out.data(), lse, ws.data(),
+                                   (size_t)ws.tensor->numel(), current_stream());
+    });
+    // (the first of the call's two launches may precede the one that failed)
+    if (rc == MXQ_ERR_CUDA) return raise_mxq_error(rc, "mxq_cache_attention");
+    GENERAL_UNLESS(rc == MXQ_OK);
+    return out.result(a[13]);
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(addresses by name, formats, torch.nn.Parameter, MxqError)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs)
 {
@@ -735,6 +878,10 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     take("mxq_matrix_scales_bytes", n.matrix_scales_bytes);
     take("mxq_moe", n.moe);
     take("mxq_moe_workspace_bytes", n.moe_workspace_bytes);
+    take("mxq_cache_write", n.cache_write);
+    take("mxq_cache_read", n.cache_read);
+    take("mxq_cache_attention", n.cache_attention);
+    take("mxq_cache_attention_workspace_bytes", n.cache_attention_workspace_bytes);
     if (!ok) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "an entry point has no address");
         return nullptr;
@@ -753,7 +900,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs)
 PyMethodDef methods[] = {FAST(bind),           FAST(quantize),          FAST(slice_scale), FAST(slice_scale_multi),
                          FAST(dequantize),     FAST(quantize_tiled),    FAST(slice_scale_tiled), FAST(fake_quant),
                          FAST(fake_quant_bwd), FAST(run_prepared),      FAST(fake_quant_ste),
-                         FAST(matmul),         FAST(quantize_matrix),   FAST(moe),         FAST(linear_ste), {nullptr, nullptr, 0, nullptr}};
+                         FAST(matmul),         FAST(quantize_matrix),   FAST(moe),         FAST(linear_ste),
+                         FAST(cache_write),    FAST(cache_read),        FAST(cache_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mxq_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

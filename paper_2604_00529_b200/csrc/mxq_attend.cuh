@@ -253,6 +253,20 @@ struct Attend {
     Sequence s;
     int some_lo, some_hi, all_lo, all_hi;                   // keys that some row sees, that all rows see
 
+    __device__ __forceinline__ void item(int sequence, int h, int r0, const Sequence& of)
+    {
+        b = sequence;
+        head = h;
+        row0 = r0;
+        s = of;
+        rows = min(p.rows, s.n * p.group - r0);
+        const int first = row_token(p, s, r0), last = row_token(p, s, r0 + rows - 1);
+        some_lo = token_lo(p, s, first);
+        some_hi = token_hi(p, s, last);
+        all_lo = token_lo(p, s, last);
+        all_hi = token_hi(p, s, first);
+    }
+
     // -- a step's codes and scales on their way to shared memory
 
     // Where the lane's chunks of keys and values and its chunk of scales would lie in page 0, and the bytes from page to page.
@@ -853,11 +867,13 @@ struct Attend {
 
     // -- the warps' results together: normalized sums and their weights in shared memory, then to the output or to a part
 
-    __device__ __forceinline__ void finish(float* area, bool whole, uint8_t* part, int some)      // some: warps that had keys, one at least
+    // (some: warps that had keys, one at least; share: CTAs of the cluster that has the item, 0 without one)
+    __device__ __forceinline__ void finish(float* area, bool whole, uint8_t* part, int some, int share)
     {
         constexpr int R = 8 * NT / PIECES;                   // rows of the tile
         float* const o_at = area + warp * R * D;
         float* const ml = area + warps * R * D;             // [warp][row][m, l]
+        float* const shared_ml = area + (size_t)warps * S::work / 4;          // [row][m, l] for the cluster, where the first warp's tables were
         if (warp < some) {
             float scales[NB];
 #pragma unroll
@@ -910,9 +926,11 @@ struct Attend {
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] *= inv;
-            if (whole) {
-                const int row = row0 + r, i = row_token(p, s, row);
-                write_row<PIECES>(p, (size_t)(s.first + i) * (p.cache.heads * p.group) + head * p.group + row - i * p.group, D, d, v, top, sum);
+            if (share > 1) {                                 // (this thread alone has read what lies here)
+                *reinterpret_cast<float4*>(area + r * D + d) = make_float4(v[0], v[1], v[2], v[3]);
+                if (d == 0) reinterpret_cast<float2*>(shared_ml)[r] = make_float2(top, sum);
+            } else if (whole) {
+                put(r, d, v, top, sum);
             } else {
                 float* const to = reinterpret_cast<float*>(part);
                 MXQ_CHECKED(to + r * D + d, 16, continue)
@@ -923,7 +941,38 @@ struct Attend {
                 }
             }
         }
-        __syncthreads();
+        if (share > 1) {
+            cluster_sync();
+            const uint32_t at = smem_addr(area), at_ml = smem_addr(shared_ml);
+            for (int slot = threadIdx.x * share + cluster_rank(); slot < rows * (D / 4); slot += warps * 32 * share) {
+                const int r = slot / (D / 4), d = slot % (D / 4) * 4;
+                float top = kNone, sum = 0.f, v[4] = {};
+#pragma unroll 8
+                for (int c = 0; c < share; ++c) top = fmaxf(top, ld_peer(peer_addr(at_ml + r * 8, c)));
+#pragma unroll 8
+                for (int c = 0; c < share; ++c) {
+                    const float wt = ld_peer(peer_addr(at_ml + r * 8 + 4, c)) * exp2_approx(ld_peer(peer_addr(at_ml + r * 8, c)) - top);
+                    const float4 x = ld_peer4(peer_addr(at + (r * D + d) * 4, c));
+                    sum += wt;
+                    v[0] += wt * x.x;
+                    v[1] += wt * x.y;
+                    v[2] += wt * x.z;
+                    v[3] += wt * x.w;
+                }
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] *= inv;
+                put(r, d, v, top, sum);
+            }
+            cluster_sync();                                  // no CTA leaves while another one reads its sums
+        } else {
+            __syncthreads();
+        }
+    }
+    __device__ __forceinline__ void put(int r, int d, const float (&v)[4], float top, float sum) const
+    {
+        const int row = row0 + r, i = row_token(p, s, row);
+        write_row<PIECES>(p, (size_t)(s.first + i) * (p.cache.heads * p.group) + head * p.group + row - i * p.group, D, d, v, top, sum);
     }
 };
 
@@ -988,7 +1037,6 @@ attend_kernel(const __grid_constant__ AttendArgs p)
     pdl_acquire();
     pdl_release();                                           // (the second kernel reads nothing before its own wait)
     const int warps = NT == 1 ? p.warps : kWarps;
-    make_plan(p, warps, plan, warp_sum);
     const uint32_t base = smem_addr(shared);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Attend<FMT, D, NT, PIECES> a{p, warps, warp, lane, lane >> 2, lane & 3};
@@ -998,6 +1046,18 @@ attend_kernel(const __grid_constant__ AttendArgs p)
     a.to_codes = (lane / S::CPR) * S::RB + ((lane % S::CPR ^ S::twist(lane / S::CPR)) << 4);
     // matrix i of a load: keys 8 (i & 1) ..., chunk i >> 1; the lane gives the address of row lane % 8 of matrix lane / 8
     a.twisted = (((lane >> 3) & 1) * 8 + (lane & 7)) * S::RB + (((lane >> 4) ^ S::twist(lane & 7)) << 4);
+    if (NT == 1 && p.share) {                                // a cluster's item: tiles by rank, one token per sequence
+        const int item = blockIdx.x / p.share, rank = p.share > 1 ? (int)cluster_rank() : 0, b = item / p.cache.heads;
+        const Sequence s = sequence(p.batch, b, p.cache.page_shift);
+        a.item(b, item - b * p.cache.heads, 0, s);
+        const uint32_t tiles = sequence_tiles(p, s), key0 = (uint32_t)(a.some_lo >> p.tile_shift << p.tile_shift);
+        const int from = (int)min(key0 + (tiles * rank / p.share << p.tile_shift), (uint32_t)a.some_hi);
+        const int to = (int)min(key0 + (tiles * (rank + 1) / p.share << p.tile_shift), (uint32_t)a.some_hi);
+        a.run(from, to);
+        a.finish(reinterpret_cast<float*>(shared), true, nullptr, min(warps, max((to - from + S::step - 1) / S::step, 1)), p.share);
+        return;
+    }
+    make_plan(p, warps, plan, warp_sum);
     uint8_t* const parts = p.ws + (size_t)p.ctas * sizeof(PartMeta);
     PartMeta* const meta = reinterpret_cast<PartMeta*>(p.ws) + blockIdx.x;
     const size_t part = part_bytes(p.rows, D);
@@ -1026,17 +1086,8 @@ attend_kernel(const __grid_constant__ AttendArgs p)
                 if (at < item + tiles) break;
             }
         }
-        const int rows = min(p.rows, s.n * p.group - r0), first_token = row_token(p, s, r0), last_token = row_token(p, s, r0 + rows - 1);
+        a.item(b, (int)head, r0, s);
         const uint32_t end = min(item + tiles, to);
-        a.b = b;
-        a.head = (int)head;
-        a.row0 = r0;
-        a.rows = rows;
-        a.s = s;
-        a.some_lo = token_lo(p, s, first_token);
-        a.some_hi = token_hi(p, s, last_token);
-        a.all_lo = token_lo(p, s, last_token);
-        a.all_hi = token_hi(p, s, first_token);
         // (keys are below 2^31, tiles behind the last one reach no further than one tile beyond it)
         const uint32_t key0 = (uint32_t)(a.some_lo >> p.tile_shift << p.tile_shift);
         const int from_key = (int)min(key0 + ((at - item) << p.tile_shift), (uint32_t)a.some_hi);
@@ -1046,10 +1097,10 @@ attend_kernel(const __grid_constant__ AttendArgs p)
         if (first && threadIdx.x == 0) {
             bool ok = true;
             MXQ_CHECKED(meta, sizeof(PartMeta), ok = false)
-            if (ok) *meta = PartMeta{at, item, item + tiles, total, s.first, (int)head, r0, rows};
+            if (ok) *meta = PartMeta{at, item, item + tiles, total, s.first, (int)head, r0, a.rows};
         }
         a.finish(reinterpret_cast<float*>(shared), whole, parts + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * part,
-                 min(warps, max((to_key - from_key + S::step - 1) / S::step, 1)));
+                 min(warps, max((to_key - from_key + S::step - 1) / S::step, 1)), 0);
         first = false;
         at = end;
     }
@@ -1064,7 +1115,7 @@ int run(const AttendArgs& p, cudaStream_t stream)
     static std::atomic<uint64_t> done{0};
     auto kern = attend_kernel<FMT, D, NT, PIECES>;
     if (int rc = allow_smem(reinterpret_cast<const void*>(kern), S::total(S::most), done)) return rc;
-    return launch_grid(kern, dim3((unsigned)p.ctas), p.warps * 32, S::total(p.warps), 1, stream, p);
+    return launch_grid(kern, dim3((unsigned)p.ctas), p.warps * 32, S::total(p.warps), p.share > 1 ? p.share : 1, stream, p);
 }
 
 template <int FMT, int D, int PIECES>

@@ -82,6 +82,7 @@ struct AttendArgs {
     int causal, window;
     float scale;                                            // times log2 e
     int ctas, warps, tile_shift;                            // of the first kernel; keys of a tile: what is shared out among CTAs
+    int share;                                              // CTAs of a cluster, which has one item; 0: all tiles in runs
 };
 
 template <int FMT>

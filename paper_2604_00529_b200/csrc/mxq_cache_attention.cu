@@ -80,12 +80,15 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
 // ---- launches -------------------------------------------------------------------------------------------------
 
 // How a call is cut up: column groups of its kernel, rows of an item, CTAs and their warps, a tile's keys, bytes of workspace.
+constexpr size_t kClusterKeys = 2048;                       // at most, per CTA of a cluster
+
 struct Sizes {
-    int nt, rows, warps, tile_shift;
+    int nt, rows, warps, tile_shift, share;
     size_t ctas, bytes;
 };
 
-Sizes sizes(const mxq_cache* c, const mxq_batch* b, int q_heads, int dtype, size_t tokens)
+// `window`: 0 for none, or what the call says; the workspace does not depend on it.
+Sizes sizes(const mxq_cache* c, const mxq_batch* b, int q_heads, int dtype, size_t tokens, size_t window)
 {
     constexpr size_t kSms = 148;
     Sizes z;
@@ -107,6 +110,17 @@ Sizes sizes(const mxq_cache* c, const mxq_batch* b, int q_heads, int dtype, size
     const size_t tiles = items * ((keys >> z.tile_shift) + 1);
     z.ctas = tiles < room ? tiles : room;
     z.bytes = z.ctas * (sizeof(PartMeta) + 2 * part_bytes(z.rows, dim));
+    // Few items that cannot be long: a cluster of CTAs each, which joins its sums itself, without a plan and a second kernel.
+    z.share = 0;
+    if (wide && !b->starts && group <= z.rows) {
+        const size_t most = window && window < keys ? window + 64 : keys, own = (size_t)b->batch * c->heads;
+        size_t share = 1;
+        while (share < 8 && own * share * 2 <= kSms) share *= 2;
+        if (most <= share * kClusterKeys) {
+            z.share = (int)share;
+            z.ctas = own * share;
+        }
+    }
     return z;
 }
 
@@ -133,7 +147,7 @@ extern "C" {
 size_t mxq_cache_attention_workspace_bytes(const mxq_cache* cache, const mxq_batch* batch, int q_heads, int dtype, size_t tokens)
 {
     if (check(cache, batch, q_heads, dtype, tokens) != MXQ_OK || tokens == 0 || batch->batch == 0) return 0;
-    return sizes(cache, batch, q_heads, dtype, tokens).bytes;
+    return sizes(cache, batch, q_heads, dtype, tokens, 0).bytes;
 }
 
 int mxq_cache_attention(const mxq_cache* cache, const mxq_batch* batch, const mxq_rows* q, int q_heads, int dtype, size_t tokens, float scale,
@@ -153,7 +167,7 @@ int mxq_cache_attention(const mxq_cache* cache, const mxq_batch* batch, const mx
     a.q_token = q->token_stride * size;
     a.q_head = q->head_stride * size;
     if (!aligned(a.q, 32) || a.q_token % 32 || a.q_head % 32 || !aligned(out, 32) || !aligned(workspace, 32) || !aligned(lse, 4)) return MXQ_ERR_ALIGN;
-    const Sizes z = sizes(cache, batch, q_heads, dtype, tokens);
+    const Sizes z = sizes(cache, batch, q_heads, dtype, tokens, window);
     if (workspace_bytes < z.bytes) return MXQ_ERR_SIZE;
     MXQ_DEBUG_SCOPE();
     debug_expect_cache(cache, batch);
@@ -172,6 +186,7 @@ int mxq_cache_attention(const mxq_cache* cache, const mxq_batch* batch, const mx
     a.ctas = (int)z.ctas;
     a.warps = z.warps;
     a.tile_shift = z.tile_shift;
+    a.share = z.share;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     int rc = MXQ_ERR_FORMAT;
     switch (cache->fmt) {
@@ -181,7 +196,7 @@ int mxq_cache_attention(const mxq_cache* cache, const mxq_batch* batch, const mx
     case MXQ_INT4: rc = launch_attend<MXQ_INT4>(cache->head_dim, z.nt, dtype, a, s); break;
     default: break;
     }
-    if (rc != MXQ_OK || a.ctas == 1) return rc;
+    if (rc != MXQ_OK || a.share || a.ctas == 1) return rc;
     auto join = dtype == MXQ_F32 ? join_kernel<2> : join_kernel<1>;
     return launch_grid(join, dim3((unsigned)a.ctas - 1), kJoinThreads, 0, 1, s, a, cache->head_dim);
 }
