@@ -24,7 +24,7 @@ LIB = os.path.join(HERE, "libmxq.so")
 TIMING_EXE = os.path.join(HERE, "mxq_abi_timing")      # C-level caller of the ABI (csrc/abi_timing.cu)
 UNITS = ["mxq_api", "mxq_quantize", "mxq_slice_scale", "mxq_dequantize", "mxq_fake_quant", "mxq_static_batch", "mxq_slice_scale_multi", "mxq_slice_scale_multi_fp", "mxq_layout", "mxq_fake_quant_batched",
          "mxq_matmul", "mxq_matmul_tc", "mxq_quantize_matrix", "mxq_moe", "mxq_cache", "mxq_cache_attention", "mxq_attend_e4m3", "mxq_attend_e2m1", "mxq_attend_int8",
-         "mxq_attend_int4"]
+         "mxq_attend_int4", "mxq_attend_many"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-std=c++20", "-O3", "-lineinfo",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
 

@@ -14,6 +14,7 @@
 // FP32 rows enter as two FP16 parts, neighbouring columns of the same step, and so do their P.
 #pragma once
 #include "mxq_attend_items.cuh"
+#include "mxq_attend_plan.cuh"
 #include "mxq_kernels.cuh"
 #include "mxq_launch.h"
 #include "mxq_product.cuh"
@@ -976,56 +977,6 @@ struct Attend {
     }
 };
 
-// The run of a CTA: its first and one past its last tile, the sequence that the first lies in and the tiles in front of that.
-struct Plan {
-    uint32_t total, from, to, base, per_head;
-    int b;
-    Sequence s;
-};
-
-__device__ __forceinline__ void make_plan(const AttendArgs& p, int warps, Plan& plan, uint32_t (&warp_sum)[16])
-{
-    const int threads = warps * 32, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    // a sequence per thread, or a few in a row
-    const int per = p.batch.batch <= threads ? 1 : (p.batch.batch + threads - 1) / threads;
-    const int first = min((int)threadIdx.x * per, p.batch.batch), last = min(first + per, p.batch.batch);
-    Sequence s = {0, 0, 0};
-    uint32_t mine = 0, per_head = 0;
-    for (int b = first; b < last; ++b) {
-        s = sequence(p.batch, b, p.cache.page_shift);
-        per_head = sequence_tiles(p, s);
-        mine += per_head * p.cache.heads;
-    }
-    uint32_t before = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, before, o);
-        if (lane >= o) before += up;
-    }
-    if (lane == 31) warp_sum[warp] = before;
-    __syncthreads();
-    uint32_t sum = lane < warps ? warp_sum[lane] : 0u;
-    const uint32_t total = __reduce_add_sync(0xFFFFFFFFu, sum);
-    if (lane >= warp) sum = 0;
-    before += __reduce_add_sync(0xFFFFFFFFu, sum) - mine;
-    const uint32_t ctas = working_ctas(total, gridDim.x);
-    const Runs runs(total, ctas);
-    const uint32_t from = blockIdx.x < ctas ? runs.start(blockIdx.x) : total, to = blockIdx.x < ctas ? runs.start(blockIdx.x + 1) : total;
-    if (from < to ? from >= before && from < before + mine : threadIdx.x == 0) {            // one thread's
-        int b = first;
-        if (per > 1) {
-            for (; from < to && b < last; ++b) {
-                s = sequence(p.batch, b, p.cache.page_shift);
-                per_head = sequence_tiles(p, s);
-                if (from < before + per_head * p.cache.heads) break;
-                before += per_head * p.cache.heads;
-            }
-        }
-        plan = Plan{total, from, to, before, per_head, b, s};
-    }
-    __syncthreads();
-}
-
 template <int FMT, int D, int NT, int PIECES>
 __global__ void __launch_bounds__(Shape<FMT, D, NT>::most * 32, NT == 1 ? 1 : Shape<FMT, D, NT>::ctas)
 attend_kernel(const __grid_constant__ AttendArgs p)
@@ -1033,7 +984,7 @@ attend_kernel(const __grid_constant__ AttendArgs p)
     using S = Shape<FMT, D, NT>;
     extern __shared__ __align__(1024) uint8_t shared[];
     __shared__ Plan plan;
-    __shared__ uint32_t warp_sum[16];
+    __shared__ uint32_t warp_sum[32];
     pdl_acquire();
     pdl_release();                                           // (the second kernel reads nothing before its own wait)
     const int warps = NT == 1 ? p.warps : kWarps;
@@ -1046,61 +997,73 @@ attend_kernel(const __grid_constant__ AttendArgs p)
     a.to_codes = (lane / S::CPR) * S::RB + ((lane % S::CPR ^ S::twist(lane / S::CPR)) << 4);
     // matrix i of a load: keys 8 (i & 1) ..., chunk i >> 1; the lane gives the address of row lane % 8 of matrix lane / 8
     a.twisted = (((lane >> 3) & 1) * 8 + (lane & 7)) * S::RB + (((lane >> 4) ^ S::twist(lane & 7)) << 4);
-    if (NT == 1 && p.share) {                                // a cluster's item: tiles by rank, one token per sequence
-        const int item = blockIdx.x / p.share, rank = p.share > 1 ? (int)cluster_rank() : 0, b = item / p.cache.heads;
-        const Sequence s = sequence(p.batch, b, p.cache.page_shift);
-        a.item(b, item - b * p.cache.heads, 0, s);
-        const uint32_t tiles = sequence_tiles(p, s), key0 = (uint32_t)(a.some_lo >> p.tile_shift << p.tile_shift);
-        const int from = (int)min(key0 + (tiles * rank / p.share << p.tile_shift), (uint32_t)a.some_hi);
-        const int to = (int)min(key0 + (tiles * (rank + 1) / p.share << p.tile_shift), (uint32_t)a.some_hi);
-        a.run(from, to);
-        a.finish(reinterpret_cast<float*>(shared), true, nullptr, min(warps, max((to - from + S::step - 1) / S::step, 1)), p.share);
-        return;
-    }
-    make_plan(p, warps, plan, warp_sum);
     uint8_t* const parts = p.ws + (size_t)p.ctas * sizeof(PartMeta);
     PartMeta* const meta = reinterpret_cast<PartMeta*>(p.ws) + blockIdx.x;
     const size_t part = part_bytes(p.rows, D);
-
-    uint32_t at = plan.from, seq_at = plan.base;
-    const uint32_t to = plan.to, total = plan.total;
-    int b = plan.b;
+    // A run of tiles; or a cluster's item, its tiles by rank, one token per sequence.
+    const int share = NT == 1 ? p.share : 0;
+    uint32_t at, to, seq_at, per_head;
+    int b;
+    Sequence s;
     bool first = true;
-    if (blockIdx.x == 0 && total == 0 && threadIdx.x == 0) *meta = PartMeta{};
-    Sequence s = plan.s;
-    uint32_t per_head = plan.per_head;
-    while (at < to) {
-        if (at - seq_at >= per_head * p.cache.heads) {
-            seq_at += per_head * p.cache.heads;
-            ++b;
-            s = sequence(p.batch, b, p.cache.page_shift);
-            per_head = sequence_tiles(p, s);
-            continue;
-        }
-        const uint32_t head = (at - seq_at) / per_head;
-        uint32_t item = seq_at + per_head * head, tiles = per_head;      // the item's first tile
-        int r0 = 0;
-        if (s.n * p.group > p.rows) {
-            for (;; r0 += p.rows, item += tiles) {
-                tiles = item_tiles(p, s, r0);
-                if (at < item + tiles) break;
+    if (share) {
+        const int item = blockIdx.x / share, rank = share > 1 ? (int)cluster_rank() : 0;
+        b = item / p.cache.heads;
+        s = sequence(p.batch, b, p.cache.page_shift);
+        per_head = sequence_tiles(p, s);
+        seq_at = 0;
+        const uint32_t before = per_head * (item - b * p.cache.heads);
+        at = before + per_head * rank / share;
+        to = before + per_head * (rank + 1) / share;
+        a.item(b, item - b * p.cache.heads, 0, s);
+    } else {
+        make_plan(p, warps, plan, warp_sum);
+        at = plan.from;
+        to = plan.to;
+        seq_at = plan.base;
+        per_head = plan.per_head;
+        b = plan.b;
+        s = plan.s;
+        if (blockIdx.x == 0 && plan.total == 0 && threadIdx.x == 0) *meta = PartMeta{};
+    }
+    while (at < to || share) {
+        uint32_t item, tiles = per_head;                     // the item's first tile, and how many
+        if (share) {
+            item = per_head * a.head;
+        } else {
+            if (at - seq_at >= per_head * p.cache.heads) {
+                seq_at += per_head * p.cache.heads;
+                ++b;
+                s = sequence(p.batch, b, p.cache.page_shift);
+                per_head = sequence_tiles(p, s);
+                continue;
             }
+            const uint32_t head = (at - seq_at) / per_head;
+            item = seq_at + per_head * head;
+            int r0 = 0;
+            if (s.n * p.group > p.rows) {
+                for (;; r0 += p.rows, item += tiles) {
+                    tiles = item_tiles(p, s, r0);
+                    if (at < item + tiles) break;
+                }
+            }
+            a.item(b, (int)head, r0, s);
         }
-        a.item(b, (int)head, r0, s);
         const uint32_t end = min(item + tiles, to);
         // (keys are below 2^31, tiles behind the last one reach no further than one tile beyond it)
         const uint32_t key0 = (uint32_t)(a.some_lo >> p.tile_shift << p.tile_shift);
         const int from_key = (int)min(key0 + ((at - item) << p.tile_shift), (uint32_t)a.some_hi);
         const int to_key = (int)min(key0 + ((end - item) << p.tile_shift), (uint32_t)a.some_hi);
         a.run(from_key, to_key);
-        const bool whole = at == item && end == item + tiles;
-        if (first && threadIdx.x == 0) {
+        const bool whole = share || (at == item && end == item + tiles);
+        if (first && !share && threadIdx.x == 0) {
             bool ok = true;
             MXQ_CHECKED(meta, sizeof(PartMeta), ok = false)
-            if (ok) *meta = PartMeta{at, item, item + tiles, total, s.first, (int)head, r0, a.rows};
+            if (ok) *meta = PartMeta{at, item, item + tiles, plan.total, s.first, a.head, a.row0, a.rows};
         }
         a.finish(reinterpret_cast<float*>(shared), whole, parts + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * part,
-                 min(warps, max((to_key - from_key + S::step - 1) / S::step, 1)), 0);
+                 min(warps, max((to_key - from_key + S::step - 1) / S::step, 1)), share);
+        if (share) break;
         first = false;
         at = end;
     }

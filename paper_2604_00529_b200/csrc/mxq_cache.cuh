@@ -87,6 +87,8 @@ struct AttendArgs {
 
 template <int FMT>
 int launch_attend(int dim, int nt, int dtype, const AttendArgs& p, cudaStream_t stream);
+int launch_attend_many(int fmt, int dim, const AttendArgs& p, cudaStream_t stream);      // BF16, dim 64 or 128, 256 rows to an item
+int many_status(int reset);                                  // as tc_status, of that kernel's waits
 
 // Checks of a cache's and a batch's description, and of their addresses, as the entry points make them (an mxq_status).
 int check_cache(const mxq_cache* c);

@@ -31,7 +31,7 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
     const float* const part0 = parts + ((size_t)(c - 1) * 2 + (before == meta.item_from ? 0 : 1)) * part;
     const float* const part1 = parts + (size_t)c * 2 * part;
     const int quads = dim / 4, slots = meta.rows * quads, lanes = slots < kJoinThreads ? kJoinThreads / slots : 1;
-    for (int slot0 = 0; slot0 < slots; slot0 += kJoinThreads) {
+    for (int slot0 = (int)blockIdx.y * kJoinThreads; slot0 < slots; slot0 += (int)gridDim.y * kJoinThreads) {
         const int slot = lanes > 1 ? (int)threadIdx.x % slots : slot0 + (int)threadIdx.x, mine = lanes > 1 ? (int)threadIdx.x / slots : 0;
         const bool on = mine < lanes && slot < slots;
         const int r = on ? slot / quads : 0, d = on ? slot % quads * 4 : 0;
@@ -80,9 +80,11 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
 // ---- launches -------------------------------------------------------------------------------------------------
 
 // How a call is cut up: column groups of its kernel, rows of an item, CTAs and their warps, a tile's keys, bytes of workspace.
+constexpr size_t kManyColumns = 64;                         // columns of a mean sequence, above which its rows are many
 constexpr size_t kClusterKeys = 2048;                       // at most, per CTA of a cluster
 
 struct Sizes {
+    bool many;
     int nt, rows, warps, tile_shift, share;
     size_t ctas, bytes;
 };
@@ -97,22 +99,24 @@ Sizes sizes(const mxq_cache* c, const mxq_batch* b, int q_heads, int dtype, size
     const size_t columns = (tokens + b->batch - 1) / b->batch * (size_t)group * (size_t)pieces;
     z.nt = 1;
     while (z.nt < (dim == 256 ? 2 : 4) && columns > (size_t)8 * z.nt) z.nt *= 2;
-    z.rows = 8 * z.nt / pieces;
-    const size_t items = (tokens * group / z.rows + b->batch) * c->heads, keys = b->width * (size_t)c->page < (size_t)1 << 31 ? b->width * (size_t)c->page : (size_t)1 << 31;     // at most
+    // Many rows: tiles of 256 of them on the tensor cores that take whole tiles.
+    z.many = dtype == MXQ_BF16 && dim <= 128 && columns > kManyColumns;
+    z.rows = z.many ? 256 : 8 * z.nt / pieces;
+    const size_t items = (b->starts ? tokens * group / z.rows + b->batch : b->batch * ((size_t)(group + z.rows - 1) / z.rows)) * c->heads, keys = b->width * (size_t)c->page < (size_t)1 << 31 ? b->width * (size_t)c->page : (size_t)1 << 31;     // at most
     const int ctas = z.nt == 4 ? 2 : z.nt * dim <= 128 ? 4 : z.nt * dim <= 256 ? 3 : 2;      // per SM, of four warps
     // Few items: one CTA per SM with all the warps that it holds, so that an item has a quarter of the parts.
-    const bool wide = z.nt == 1 && items <= kSms;
+    const bool wide = z.many || (z.nt == 1 && items <= kSms);
     z.warps = wide ? 4 * ctas : 4;
     const size_t room = wide ? kSms : kSms * ctas;
-    // tiles of 64 keys, longer ones where there could be more of them than 32 bits count
-    z.tile_shift = 6;
+    // tiles of 64 (128) keys, longer ones where there could be more of them than 32 bits count
+    z.tile_shift = z.many ? 7 : 6;
     while ((keys >> z.tile_shift) + 1 > (((size_t)1 << 31) - 1) / items) ++z.tile_shift;
     const size_t tiles = items * ((keys >> z.tile_shift) + 1);
     z.ctas = tiles < room ? tiles : room;
     z.bytes = z.ctas * (sizeof(PartMeta) + 2 * part_bytes(z.rows, dim));
     // Few items that cannot be long: a cluster of CTAs each, which joins its sums itself, without a plan and a second kernel.
     z.share = 0;
-    if (wide && !b->starts && group <= z.rows) {
+    if (wide && !z.many && !b->starts && group <= z.rows) {
         const size_t most = window && window < keys ? window + 64 : keys, own = (size_t)b->batch * c->heads;
         size_t share = 1;
         while (share < 8 && own * share * 2 <= kSms) share *= 2;
@@ -189,7 +193,8 @@ int mxq_cache_attention(const mxq_cache* cache, const mxq_batch* batch, const mx
     a.share = z.share;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     int rc = MXQ_ERR_FORMAT;
-    switch (cache->fmt) {
+    if (z.many) rc = launch_attend_many(cache->fmt, cache->head_dim, a, s);
+    else switch (cache->fmt) {
     case MXQ_FP8_E4M3: rc = launch_attend<MXQ_FP8_E4M3>(cache->head_dim, z.nt, dtype, a, s); break;
     case MXQ_FP4_E2M1: rc = launch_attend<MXQ_FP4_E2M1>(cache->head_dim, z.nt, dtype, a, s); break;
     case MXQ_INT8: rc = launch_attend<MXQ_INT8>(cache->head_dim, z.nt, dtype, a, s); break;
@@ -198,7 +203,7 @@ int mxq_cache_attention(const mxq_cache* cache, const mxq_batch* batch, const mx
     }
     if (rc != MXQ_OK || a.share || a.ctas == 1) return rc;
     auto join = dtype == MXQ_F32 ? join_kernel<2> : join_kernel<1>;
-    return launch_grid(join, dim3((unsigned)a.ctas - 1), kJoinThreads, 0, 1, s, a, cache->head_dim);
+    return launch_grid(join, dim3((unsigned)a.ctas - 1, z.many ? 8 : 1), kJoinThreads, 0, 1, s, a, cache->head_dim);
 }
 
 }  // extern "C"

@@ -1,6 +1,7 @@
 // D = A^ B^T of two operands in the MXFP anchor's format, E4M3, with one E8M0 scale per block along k (Sec. 3.5; the lower formats have no
 // product but mxq_moe's): D[i, j] = sum over blocks b of Xa[i, b] Xb[j, b] sum over k in b of Pa[i, k] Pb[j, k].
 #include "mxq_kernels.cuh"
+#include "mxq_cache.cuh"
 #include "mxq_launch.h"
 #include "mxq_product.cuh"
 
@@ -243,7 +244,11 @@ int mxq_matmul(const void* a_codes, const uint8_t* a_scales, const void* b_codes
     return m <= (size_t)kFewRows && few_us(p) <= matmul_tc_us(p) ? launch_matmul_few(p, dst_dtype, s) : launch_matmul_tc(p, dst_dtype, s);
 }
 
-int mxq_wait_status(int reset) { return tc_status(reset); }
+int mxq_wait_status(int reset)
+{
+    const int matmul = tc_status(reset), attention = many_status(reset);
+    return matmul != MXQ_OK ? matmul : attention;
+}
 
 }  // extern "C"
 #pragma GCC visibility pop

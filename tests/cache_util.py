@@ -63,7 +63,12 @@ def rows_of(values, table, n, page):
     return values[np.where(there, pages, 0), :, t % page], there
 
 
-def attention64(q, cache, table, lengths, starts, scale, causal=True, window=0, dtype=torch.bfloat16, tokens=None):
+def many(dtype, dim, tokens, batch, group):
+    """Whether a call is one of many queries: BF16, heads of up to 128, more than 64 rows of a cache head per sequence in the mean."""
+    return dtype == torch.bfloat16 and dim <= 128 and -(-tokens // batch) * group > 64
+
+
+def attention64(q, cache, table, lengths, starts, scale, causal=True, window=0, dtype=torch.bfloat16):
     """(out, lse, bound, touched) in 64 bits for q [tokens, q_heads, dim]."""
     k64, v64 = cache.values()
     tokens, q_heads, dim = q.shape
@@ -71,6 +76,8 @@ def attention64(q, cache, table, lengths, starts, scale, causal=True, window=0, 
     out, bound, lse = np.zeros(q.shape), np.zeros(q.shape), np.full(q.shape[:2], -np.inf)
     touched = np.zeros(tokens, bool)
     held = 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -21
+    if many(dtype, dim, tokens, len(lengths), q_heads // heads):
+        held = 2.0 ** -8
     entry = 0.0 if dtype == torch.bfloat16 else 2.0 ** -21
     for b, length in enumerate(lengths):
         first, n = (b, 1) if starts is None else (starts[b], starts[b + 1] - starts[b])

@@ -71,6 +71,17 @@ def test_several_queries(fmt, dtype, dim, counts, lengths):
         attend(rng, cache, lengths, counts, 3, dtype, causal=causal, window=window)
 
 
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dim,block,page,group,counts,lengths", [
+    (128, 32, 64, 1, [130], [130]), (128, 64, 16, 2, [70, 200, 0, 129], [500, 200, 9, 140]), (64, 32, 32, 4, [300, 33], [301, 640]),
+    (128, 128, 128, 8, [33, 1], [1000, 3]), (64, 64, 256, 3, [90, 90], [60, 777])])
+def test_many_queries(fmt, dim, block, page, group, counts, lengths):
+    rng = np.random.default_rng(sum(counts))
+    cache = cu.Cache(rng, sum(-(-n // page) for n in lengths) + 1, 2, dim, fmt, block, page)
+    for causal, window in ((True, 0), (True, 100), (False, 0)):
+        attend(rng, cache, lengths, counts, group, BF16, causal=causal, window=window)
+
+
 @pytest.mark.parametrize("fmt,dtype", [("e2m1", BF16), ("int4", F32), ("e4m3", BF16), ("int8", F32)])
 def test_long_contexts_in_parts(fmt, dtype):
     rng = np.random.default_rng(5)
