@@ -71,6 +71,14 @@ __device__ __forceinline__ float exp2_approx(float v)
     return d;
 }
 
+__device__ __forceinline__ void write_lse(const AttendArgs& p, size_t row, float m, float l)
+{
+    if (!p.lse) return;
+    float* to = p.lse + row;
+    MXQ_CHECKED(to, 4, return)
+    *to = l == 0.f ? __uint_as_float(0xFF800000u) : (m + log2f(l)) * 0.6931471805599453f;
+}
+
 // Four elements of an output row, and the row's logarithm with the first of them.
 template <int PIECES>
 __device__ __forceinline__ void write_row(const AttendArgs& p, size_t row, int dim, int d, const float (&v)[4], float m, float l)
@@ -84,11 +92,7 @@ __device__ __forceinline__ void write_row(const AttendArgs& p, size_t row, int d
         MXQ_CHECKED(to, 8, return)
         *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
-    if (d == 0 && p.lse) {
-        float* to = p.lse + row;
-        MXQ_CHECKED(to, 4, return)
-        *to = l == 0.f ? __uint_as_float(0xFF800000u) : (m + log2f(l)) * 0.6931471805599453f;
-    }
+    if (d == 0) write_lse(p, row, m, l);
 }
 
 }  // namespace

@@ -82,6 +82,49 @@ __device__ __forceinline__ void st_shared16(uint32_t at, uint32_t a, uint32_t b,
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
+// Two FP32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{ .reg .b64 x, y, z, w; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 w, x, y, z; mov.b64 {%0, %1}, w; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{ .reg .b64 x, y, w; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 w, x, y; mov.b64 {%0, %1}, w; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// A row's sums in tensor memory times `by`.
+template <int D>
+__device__ __forceinline__ void rescale_sums(uint32_t oc, float by)
+{
+#pragma unroll 1
+    for (int c = 0; c < D; c += 32) {
+        uint32_t v[32];
+        tmem_ld32(v, oc + c);
+        tmem_ld_wait();
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * by);
+        tmem_st32(oc + c, v);
+    }
+    tmem_st_wait();
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
+}
+
 // The top bit of each byte that is an E4M3 NaN code.
 __device__ __forceinline__ uint32_t nan_codes(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
@@ -193,36 +236,45 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
         // rows to shared memory, in the order that the keys' elements are widened in; O from zero
         for (int i = threadIdx.x; i < 2 * kRowTile; i += kManyThreads) s_bad[i] = 0;
         __syncthreads();
-        if (ok && warp < kRowWarps) {
-            for (int c = threadIdx.x; c < (two ? 2 : 1) * kRowTile * (D / 8); c += kRowWarps * 32) {
-                const int r = c / (D / 8), e = c % (D / 8);              // eight elements
-                uint32_t x[4] = {0, 0, 0, 0}, o[4];
-                if (r < it.rows) {
-                    const int row = it.row0 + r, i = row_token(p, s, row);
-                    const uint4 v = ld_once(p.q + (size_t)(s.first + i) * p.q_token + (size_t)(it.head * p.group + row - i * p.group) * p.q_head + e * 16);
-                    x[0] = v.x;
-                    x[1] = v.y;
-                    x[2] = v.z;
-                    x[3] = v.w;
+        if (ok) {
+            constexpr int batch = 4;                         // loads under way per thread
+            const int pieces16 = (two ? 2 : 1) * kRowTile * (D / 8);
+            for (int c0 = threadIdx.x; c0 < pieces16; c0 += kManyThreads * batch) {
+                uint4 v[batch];
+#pragma unroll
+                for (int k = 0; k < batch; ++k) {
+                    const int c = c0 + k * kManyThreads, r = c / (D / 8), e = c % (D / 8);       // eight elements
+                    v[k] = make_uint4(0, 0, 0, 0);
+                    if (r < it.rows) {
+                        const int row = it.row0 + r, i = row_token(p, s, row);
+                        v[k] = ld_once(p.q + (size_t)(s.first + i) * p.q_token + (size_t)(it.head * p.group + row - i * p.group) * p.q_head + e * 16);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < batch; ++k) {
+                    const int c = c0 + k * kManyThreads, r = c / (D / 8), e = c % (D / 8);
+                    if (c >= pieces16) continue;
+                    const uint32_t x[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+                    uint32_t o[4];
                     bool bad = false;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) bad |= (x[j] & 0x7F80u) == 0x7F80u || (x[j] & 0x7F800000u) == 0x7F800000u;
                     if (bad) s_bad[r] = 1;
+                    if constexpr (NP == 4) {
+                        order_pairs<4>(x, o);
+                    } else {
+                        const uint32_t lo[2] = {x[0], x[1]}, hi[2] = {x[2], x[3]};
+                        uint32_t l[2], h[2];
+                        order_pairs<2>(lo, l);
+                        order_pairs<2>(hi, h);
+                        o[0] = l[0];
+                        o[1] = l[1];
+                        o[2] = h[0];
+                        o[3] = h[1];
+                    }
+                    const uint32_t tile = base + ((r >> 7) * M::panels + (e >> 3)) * (kRowTile * 128);
+                    st_shared16(tile + (r & 127) * 128 + (((e & 7) ^ (r & 7)) << 4), o[0], o[1], o[2], o[3]);
                 }
-                if constexpr (NP == 4) {
-                    order_pairs<4>(x, o);
-                } else {
-                    const uint32_t lo[2] = {x[0], x[1]}, hi[2] = {x[2], x[3]};
-                    uint32_t l[2], h[2];
-                    order_pairs<2>(lo, l);
-                    order_pairs<2>(hi, h);
-                    o[0] = l[0];
-                    o[1] = l[1];
-                    o[2] = h[0];
-                    o[3] = h[1];
-                }
-                const uint32_t tile = base + ((r >> 7) * M::panels + (e >> 3)) * (kRowTile * 128);
-                st_shared16(tile + (r & 127) * 128 + (((e & 7) ^ (r & 7)) << 4), o[0], o[1], o[2], o[3]);
             }
             fence_async();
         }
@@ -442,40 +494,6 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                 const int k0 = it.from + j * kKeys, from = lo - k0, to_key = hi - k0;
                 const bool edge = k0 < it.all_lo || k0 + kKeys > it.all_hi || (info & 1u);
                 const uint8_t* const absent = base_p + M::absent_at + st * kKeys;
-                float top = kNone;
-                // a score times f; hidden ones -inf
-                auto score = [&](uint32_t v, int k) {
-                    const bool on = k >= from && k < to_key && !((info & 1u) && absent[k]);
-                    return on ? __uint_as_float(v) * f : __uint_as_float(0xFF800000u);
-                };
-#pragma unroll 1
-                for (int c = 0; c < kKeys; c += 32) {
-                    uint32_t v[32];
-                    tmem_ld32(v, sc + c);
-                    tmem_ld_wait();
-                    if (edge) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) top = fmaxf(top, score(v[k], c + k));
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) top = fmaxf(top, __uint_as_float(v[k]) * f);
-                    }
-                }
-                if (__any_sync(0xFFFFFFFFu, top > m + kManySlack)) {      // rare: m moved, the sums so far with it
-                    const float up = fmaxf(m, top), by = exp2_approx(m - up);
-                    m = up;
-                    l *= by;
-#pragma unroll 1
-                    for (int c = 0; c < D; c += 32) {
-                        uint32_t v[32];
-                        tmem_ld32(v, oc + c);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * by);
-                        tmem_st32(oc + c, v);
-                    }
-                    tmem_st_wait();
-                }
                 if (info & 2u) {                             // NaN values that not every row sees: into the sums of those that do
                     uint32_t bad[NB] = {};
                     for (int k = 0; k < kKeys; ++k) {
@@ -497,30 +515,64 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                         tmem_st_wait();
                     }
                 }
+                // 32 keys at a time: scores less m, P over scores that are read already
+                auto weigh = [&](auto edge_t) {
+                    constexpr bool EDGE = decltype(edge_t)::value;
 #pragma unroll 1
-                for (int c = 0; c < kKeys; c += 32) {
-                    uint32_t v[32], o[16];
-                    tmem_ld32(v, sc + c);
-                    tmem_ld_wait();
-                    float sum0 = 0.f, sum1 = 0.f;
+                    for (int c = 0; c < kKeys; c += 32) {
+                        float2 x[16];
+                        auto scores = [&] {                  // less m (or 0, before any key was seen); hidden ones -inf
+                            uint32_t v[32];
+                            tmem_ld32(v, sc + c);
+                            tmem_ld_wait();
+                            const float less = m == kNone ? 0.f : -m;
 #pragma unroll
-                    for (int k = 0; k < 32; k += 2) {
-                        float e0, e1;
-                        if (edge) {
-                            const float s0 = score(v[k], c + k), s1 = score(v[k + 1], c + k + 1);
-                            e0 = exp2_approx(s0 - m);
-                            e1 = exp2_approx(s1 - m);
-                        } else {
-                            e0 = exp2_approx(fmaf(__uint_as_float(v[k]), f, -m));
-                            e1 = exp2_approx(fmaf(__uint_as_float(v[k + 1]), f, -m));
+                            for (int k = 0; k < 16; ++k) {
+                                x[k] = fma2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(f, f), make_float2(less, less));
+                                if constexpr (EDGE) {
+                                    const int at = c + 2 * k;
+                                    if (at < from || at >= to_key || ((info & 1u) && absent[at])) x[k].x = __uint_as_float(0xFF800000u);
+                                    if (at + 1 < from || at + 1 >= to_key || ((info & 1u) && absent[at + 1])) x[k].y = __uint_as_float(0xFF800000u);
+                                }
+                            }
+                        };
+                        scores();
+                        float top = x[0].x;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) top = max3(top, x[k].x, x[k].y);
+                        if (__any_sync(0xFFFFFFFFu, top > (m == kNone ? -3e38f : kManySlack))) {
+                            // m moved, by a whole number, so that nothing is rounded again: the sums so far and P so far in this tile
+                            const float up = fmaxf(m, ceilf(top + (m == kNone ? 0.f : m))), by = exp2_approx(m - up);
+                            m = up;
+                            l *= by;
+                            rescale_sums<D>(oc, by);
+                            const uint32_t by2 = pack_bf16x2(by, by);
+#pragma unroll 1
+                            for (int done = 0; done < c / 2; done += 16) {
+                                uint32_t w[16];
+                                tmem_ld16(w, sc + done);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) w[k] = W::mul(w[k], by2);
+                                tmem_st16(sc + done, w);
+                            }
+                            tmem_st_wait();
+                            scores();
                         }
-                        sum0 += e0;
-                        sum1 += e1;
-                        o[k / 2] = pack_bf16x2(e0, e1);
+                        uint32_t o[16];
+                        float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const float2 e = make_float2(exp2_approx(x[k].x), exp2_approx(x[k].y));
+                            sum = add2(sum, e);
+                            o[k] = pack_bf16x2(e.x, e.y);
+                        }
+                        l += sum.x + sum.y;
+                        tmem_st16(sc + c / 2, o);
                     }
-                    l += sum0 + sum1;
-                    tmem_st16(sc + c / 2, o);                // (over scores that are read already)
-                }
+                };
+                if (edge) weigh(std::true_type{});
+                else weigh(std::false_type{});
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -541,21 +593,28 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                     float o[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[widened_place<NP>(e)]) * inv;
+                    if (whole) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const float x[4] = {o[e], o[e + 1], o[e + 2], o[e + 3]};
-                        if (whole) {
-                            write_row<1>(p, out_row, D, c + e, x, m, l);
-                        } else {
-                            float* const to4 = to_part + row * D + c + e;
-                            MXQ_CHECKED(to4, 16, continue)
-                            *reinterpret_cast<float4*>(to4) = make_float4(x[0], x[1], x[2], x[3]);
-                            if (c + e == 0) {
-                                to_part[p.rows * D + 2 * row] = m;
-                                to_part[p.rows * D + 2 * row + 1] = l;
-                            }
+                        for (int e = 0; e < 32; e += 16) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) w[k] = pack_bf16x2(o[e + 2 * k], o[e + 2 * k + 1]);
+                            st256(p.out + (out_row * D + c + e) * 2, w);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(o[e + k]);
+                            st256(to_part + row * D + c + e, w);
                         }
                     }
+                }
+                if (mine && whole) write_lse(p, out_row, m, l);
+                if (mine && !whole) {
+                    to_part[p.rows * D + 2 * row] = m;
+                    to_part[p.rows * D + 2 * row + 1] = l;
                 }
                 tc_fence_before();
             }
