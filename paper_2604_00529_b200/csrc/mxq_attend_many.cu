@@ -351,21 +351,31 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
             const int* const pages_of = p.batch.table + (size_t)b * p.batch.width;
             uint4 code[2][M::chunks];                        // keys and values of the tile to come
             uint32_t byte[2][M::chunks];
-            uint32_t absent = 0;                             // bit per chunk: its key has no page
-            auto load = [&](int kind, int k0) {
+            uint32_t absent = 0, outside = 0;                // bit per chunk: its key has no page, is seen by no row
+            uint32_t row_at[M::chunks], row_page[M::chunks]; // where the tile to come lies
+            auto locate = [&](int k0) {
+                absent = outside = 0;
 #pragma unroll
                 for (int i = 0; i < M::chunks; ++i) {
-                    const int id = me + i * kWideners * 32, key = k0 + id / M::CPR, c = id % M::CPR;
+                    const int key = k0 + (me + i * kWideners * 32) / M::CPR;
+                    const bool in = key >= it.some_lo && key < it.some_hi;
+                    if (!in) outside |= 1u << i;
+                    row_page[i] = (uint32_t)ld_int(pages_of + ((in ? key : it.some_lo) >> p.cache.page_shift));
+                    row_at[i] = (uint32_t)key & ((1u << p.cache.page_shift) - 1u);
+                }
+#pragma unroll
+                for (int i = 0; i < M::chunks; ++i)
+                    if (row_page[i] >= (uint32_t)p.cache.pages) absent |= 1u << i;
+                absent &= ~outside;
+            };
+            auto load = [&](int kind) {
+#pragma unroll
+                for (int i = 0; i < M::chunks; ++i) {
+                    const int c = (me + i * kWideners * 32) % M::CPR;
                     code[kind][i] = make_uint4(0, 0, 0, 0);
                     byte[kind][i] = 127;
-                    absent &= ~(1u << i);
-                    if (key < it.some_lo || key >= it.some_hi) continue;
-                    const uint32_t page = (uint32_t)ld_int(pages_of + (key >> p.cache.page_shift));
-                    if (page >= (uint32_t)p.cache.pages) {
-                        absent |= 1u << i;
-                        continue;
-                    }
-                    const size_t row = (((size_t)page * p.cache.heads + it.head) << p.cache.page_shift) | (key & ((1 << p.cache.page_shift) - 1));
+                    if (((absent | outside) >> i) & 1u) continue;
+                    const size_t row = (((size_t)row_page[i] * p.cache.heads + it.head) << p.cache.page_shift) | row_at[i];
                     code[kind][i] = ld_once((kind ? p.cache.vc : p.cache.kc) + row * M::RB + c * 16);
                     byte[kind][i] = ld_u8((kind ? p.cache.vs : p.cache.ks) + row * (D >> p.cache.block_shift) + (c * (128 / M::bits) >> p.cache.block_shift));
                 }
@@ -419,8 +429,9 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
             };
             bool fine = true;
             if (count > 0) {
-                load(0, it.from);
-                load(1, it.from);
+                locate(it.from);
+                load(0);
+                load(1);
             }
             for (int j = 0; fine && j < count; ++j) {
                 const uint32_t n = n0 + j, st = n & 1, again = ((n >> 1) & 1) ^ 1;
@@ -435,7 +446,10 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&bars.k_full[st]));
                 const uint32_t gone = absent;
-                if (j + 1 < count) load(0, k0 + kKeys);
+                if (j + 1 < count) {
+                    locate(k0 + kKeys);
+                    load(0);
+                }
                 if (!(fine = warp_agrees(wait(bars.v_empty[st], again)))) break;
                 const bool edge = k0 < it.all_lo || k0 + kKeys > it.all_hi;
                 uint32_t info = gone ? 1u : 0u;
@@ -471,7 +485,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                     mbar_arrive(smem_addr(&bars.v_full[st]));
                 }
                 __syncwarp();
-                if (j + 1 < count) load(1, k0 + kKeys);
+                if (j + 1 < count) load(1);
             }
             ok = fine;
         } else if (ok && (two || warp < 4)) {

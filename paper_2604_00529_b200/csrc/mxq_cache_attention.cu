@@ -80,7 +80,7 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
 // ---- launches -------------------------------------------------------------------------------------------------
 
 // How a call is cut up: column groups of its kernel, rows of an item, CTAs and their warps, a tile's keys, bytes of workspace.
-constexpr size_t kManyColumns = 64;                         // columns of a mean sequence, above which its rows are many
+constexpr size_t kManyColumns = 16;                         // columns of a mean sequence, above which its rows are many
 constexpr size_t kClusterKeys = 2048;                       // at most, per CTA of a cluster
 
 struct Sizes {

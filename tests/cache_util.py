@@ -64,8 +64,8 @@ def rows_of(values, table, n, page):
 
 
 def many(dtype, dim, tokens, batch, group):
-    """Whether a call is one of many queries: BF16, heads of up to 128, more than 64 rows of a cache head per sequence in the mean."""
-    return dtype == torch.bfloat16 and dim <= 128 and -(-tokens // batch) * group > 64
+    """Whether a call is one of many queries: BF16, heads of up to 128, more than 16 rows of a cache head per sequence in the mean."""
+    return dtype == torch.bfloat16 and dim <= 128 and -(-tokens // batch) * group > 16
 
 
 def attention64(q, cache, table, lengths, starts, scale, causal=True, window=0, dtype=torch.bfloat16):
