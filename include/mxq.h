@@ -388,8 +388,8 @@ int mxq_matmul(const void *a_codes, const uint8_t *a_scales, const void *b_codes
                size_t m, size_t n, size_t k, int fmt, int block, void *dst, int dst_dtype, mxq_stream stream);
 
 /*
- * The kernels of mxq_matmul wait inside the device for their own copies and matrix instructions, ten seconds at most.  A wait
- * that runs out (it cannot, unless the GPU is failing) ends the kernel with an unfinished D and is remembered per device:
+ * The kernels of mxq_matmul, and one of mxq_cache_attention, wait inside the device for their own copies and matrix instructions, ten seconds at most.  A wait
+ * that runs out (it cannot, unless the GPU is failing) ends the kernel with an unfinished result and is remembered per device:
  * mxq_wait_status waits for the current device and returns MXQ_ERR_TIMEOUT if that happened since the last reset.
  */
 int mxq_wait_status(int reset);
@@ -507,8 +507,11 @@ int mxq_cache_read(const mxq_cache *cache, const mxq_batch *batch, size_t total,
  * window > 0 only the last `window` of them, p included; causal == 0: all tokens (window must be 0, MXQ_ERR_SIZE).  What is not visible
  * has no influence, whatever it holds.  A query that sees nothing gives zeros, and -inf in lse.
  * Sums and the softmax are held in FP32.  Queries enter exactly for BF16 (elements below 2^-31 of a row's largest excepted) and
- * with 22 bits for FP32; the softmax's weights enter the second product with 11 bits for BF16 and 22 for FP32.  A NaN or an infinity in a
- * query gives NaN.  Results do not depend on timing.
+ * with 22 bits for FP32; the softmax's weights enter the second product with 11 bits for BF16 and 22 for FP32, values of a block of 32
+ * dimensions below 2^-24 of the largest there may count as zeros.  BF16 calls of head_dim 64 or 128 with more than 16 rows of a cache head per
+ * sequence in the mean (tokens / batch * q_heads / heads) run on other tensor cores: weights enter with 8 bits, every value counts.
+ * A NaN or an infinity in a query gives NaN.  Results do not depend on timing.  That kernel waits as those of mxq_matmul do
+ * (mxq_wait_status); a wait that runs out leaves an unfinished out.
  *   q          [tokens, q_heads, head_dim] of dtype; q_heads a multiple of heads, at most 2^16, tokens * q_heads + batch * heads at most
  *              MXQ_CACHE_ROWS_MAX (MXQ_ERR_SIZE)
  *   out        [tokens, q_heads, head_dim] of dtype, contiguous, 32-byte aligned; overlaps nothing else

@@ -970,8 +970,8 @@ def cache_write(k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor, k_scale
     if _host.cache_write(k, v, k_codes, k_scales, v_codes, v_scales, table, lengths, fmt, block, starts, stream):
         return
     dev = k_codes.device
+    c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, lengths, starts, dev)
     with _Place(dev, stream):
-        c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, lengths, starts, dev)
         if k.dim() != 3 or k.dtype != v.dtype:
             raise ValueError("cache_write takes k and v [tokens, heads, head_dim] of one type")
         shape = (k.shape[0], c.heads, c.head_dim)
@@ -993,8 +993,8 @@ def cache_read(k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Ten
     dev = k_codes.device
     if total < 0:
         raise ValueError("negative size")
+    c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, None, starts, dev)
     with _Place(dev, stream):
-        c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, None, starts, dev)
         shape = (total, c.heads, c.head_dim)
         if out is None:
             out = (torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev))
@@ -1030,8 +1030,8 @@ def cache_attention(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tens
     if made is not None:
         return made
     dev = k_codes.device
+    c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, lengths, starts, dev)
     with _Place(dev, stream):
-        c, b = _cache(k_codes, k_scales, v_codes, v_scales, fmt, block), _batch(table, lengths, starts, dev)
         if q.dim() != 3 or q.shape[2] != c.head_dim:
             raise ValueError("q has the shape [tokens, q_heads, %d], got %s" % (c.head_dim, tuple(q.shape)))
         if window < 0:

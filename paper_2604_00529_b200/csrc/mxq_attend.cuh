@@ -759,28 +759,35 @@ struct Attend {
     // takes that back and the keys that their rows see.
     __device__ __forceinline__ void load_rows() const
     {
-        constexpr int per = D / 32;
-        for (int c = warp; c < 8 * NT; c += warps) {
-            const int r = c / PIECES, row = row0 + min(r, rows - 1);
-            float v[per];
-            uint32_t top = 0;
+        constexpr int per = D / 32, columns = 8 * NT / kWarps;         // of a lane; of a warp, at most
+        float all[columns][per];
 #pragma unroll
-            for (int i = 0; i < per; ++i) v[i] = 0.f;
-            if (r < rows) {
+        for (int k = 0; k < columns; ++k) {                  // (all of them under way before the first is looked at)
+            const int c = warp + k * warps, r = c / PIECES, row = row0 + min(r, rows - 1);
+#pragma unroll
+            for (int i = 0; i < per; ++i) all[k][i] = 0.f;
+            if (c < 8 * NT && r < rows) {
                 const int i = row_token(p, s, row);
                 const uint8_t* at = p.q + (size_t)(s.first + i) * p.q_token + (size_t)(head * p.group + row - i * p.group) * p.q_head;
                 if constexpr (PIECES == 2) {
 #pragma unroll
-                    for (int i = 0; i < per; ++i) v[i] = __uint_as_float(ld_u32(at + (lane * per + i) * 4));
+                    for (int j = 0; j < per; ++j) all[k][j] = __uint_as_float(ld_u32(at + (lane * per + j) * 4));
                 } else {
 #pragma unroll
-                    for (int i = 0; i < per; i += 2) {
-                        const uint32_t x = ld_u32(at + (lane * per + i) * 2);
-                        v[i] = __uint_as_float(x << 16);
-                        v[i + 1] = __uint_as_float(x & 0xFFFF0000u);
+                    for (int j = 0; j < per; j += 2) {
+                        const uint32_t x = ld_u32(at + (lane * per + j) * 2);
+                        all[k][j] = __uint_as_float(x << 16);
+                        all[k][j + 1] = __uint_as_float(x & 0xFFFF0000u);
                     }
                 }
             }
+        }
+#pragma unroll
+        for (int k = 0; k < columns; ++k) {
+            const int c = warp + k * warps, row = row0 + min(c / PIECES, rows - 1);
+            if (c >= 8 * NT) break;
+            const float(&v)[per] = all[k];
+            uint32_t top = 0;
 #pragma unroll
             for (int i = 0; i < per; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
             top = __reduce_max_sync(0xFFFFFFFFu, top) >> 23;

@@ -7,7 +7,7 @@ namespace {
 
 // Items that the first kernel worked on in several parts: CTA c takes the item that run c + 1 begins inside, if no earlier run begins
 // inside it too.  Its threads are shared out among the item's elements, four to a thread, and what is left of them among its parts.
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 512;
 
 template <int PIECES>
 __global__ void __launch_bounds__(kJoinThreads)
@@ -16,11 +16,12 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
     pdl_release();
     pdl_acquire();
     __shared__ float4 sums[kJoinThreads];
-    __shared__ float weights[kJoinThreads];
+    __shared__ float2 weights[kJoinThreads];
     const PartMeta* metas = reinterpret_cast<const PartMeta*>(p.ws);
-    const uint32_t c = blockIdx.x + 1, total = metas[0].total;
+    const uint32_t c = blockIdx.x + 1;
+    const PartMeta meta = metas[c];                         // (every CTA that works has written its own; read before that is known)
+    const uint32_t total = metas[0].total;
     if (c >= working_ctas(total, p.ctas)) return;
-    const PartMeta meta = metas[c];                         // (every CTA that works has written its own)
     const Runs runs(total, working_ctas(total, p.ctas));
     const uint32_t before = runs.start(c - 1);
     if (meta.from <= meta.item_from || before > meta.item_from) return;
@@ -36,37 +37,39 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
         const bool on = mine < lanes && slot < slots;
         const int r = on ? slot / quads : 0, d = on ? slot % quads * 4 : 0;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        float top = kNone, sum = 0.f;
+        float top = kNone, sum = 0.f;                       // carried along, like the softmax that they are parts of
+        auto add = [&](float2 w, float4 e) {                // w: a part's maximum and its weight there
+            const float up = fmaxf(top, w.x), keep = exp2_approx(top - up), by = w.y * exp2_approx(w.x - up);
+            top = up;
+            sum = sum * keep + by;
+            v.x = v.x * keep + by * e.x;
+            v.y = v.y * keep + by * e.y;
+            v.z = v.z * keep + by * e.z;
+            v.w = v.w * keep + by * e.w;
+        };
         if (on) {
-            const float* ml = part0 + p.rows * dim + 2 * r;
-            top = ml[0];
-#pragma unroll 8
-            for (int i = 1; i < n; ++i) top = fmaxf(top, (part1 + (size_t)(i - 1) * 2 * part + p.rows * dim + 2 * r)[0]);
 #pragma unroll 4
             for (int i = mine; i < n; i += lanes) {
                 const float* x = i ? part1 + (size_t)(i - 1) * 2 * part : part0;
-                const float2 w = *reinterpret_cast<const float2*>(x + p.rows * dim + 2 * r);
-                const float4 e = *reinterpret_cast<const float4*>(x + r * dim + d);
-                const float by = w.y * exp2_approx(w.x - top);
-                sum += by;
-                v.x += by * e.x;
-                v.y += by * e.y;
-                v.z += by * e.z;
-                v.w += by * e.w;
+                add(*reinterpret_cast<const float2*>(x + p.rows * dim + 2 * r), *reinterpret_cast<const float4*>(x + r * dim + d));
             }
         }
         if (lanes > 1) {
             sums[threadIdx.x] = v;
-            weights[threadIdx.x] = sum;
+            weights[threadIdx.x] = make_float2(top, sum);
             __syncthreads();
             if (mine != 0) return;
+            // (v is not divided yet: a weight of 1 at its maximum)
             for (int k = 1; k < lanes; ++k) {
                 const float4 e = sums[threadIdx.x + k * slots];
-                sum += weights[threadIdx.x + k * slots];
-                v.x += e.x;
-                v.y += e.y;
-                v.z += e.z;
-                v.w += e.w;
+                const float2 w = weights[threadIdx.x + k * slots];
+                const float up = fmaxf(top, w.x), keep = exp2_approx(top - up), by = exp2_approx(w.x - up);
+                top = up;
+                sum = sum * keep + by * w.y;
+                v.x = v.x * keep + by * e.x;
+                v.y = v.y * keep + by * e.y;
+                v.z = v.z * keep + by * e.z;
+                v.w = v.w * keep + by * e.w;
             }
         }
         if (!on) continue;

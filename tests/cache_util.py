@@ -4,7 +4,8 @@ Bounds.  A score is a sum of D exact products (FP32 queries: 22 bits, off by at 
 steps, scaled and added block by block: off by less than (D / 16 + 16) 2^-19 of the sum of the products' magnitudes (product_util).  A weight's
 relative error is twice the largest score's error (the score's own and the sum's), 2^-20 for the exponential and the additions round
 it, and the half step of what the weight is held in: 2^-11 (FP16) or 2^-21 (two FP16 parts).  Weights that FP16 cannot hold are off by 2^-25, where
-the largest is 2^8 or more: 2^-33 of the row's largest value each.  The second sum cuts like the first, n / 16 steps of it, and parts of
+the largest is 2^8 or more: 2^-33 each of the largest value in the 32 dimensions that have a reference scale in common; values that are
+2^-24 of that one or less may be lost altogether.  The second sum cuts like the first, n / 16 steps of it, and parts of
 it are joined a few times.  The result is rounded by half a step of its type."""
 import numpy as np
 import torch
@@ -33,7 +34,14 @@ class Cache:
 
     def values(self):
         kc, ks, vc, vs = self.parts
-        return [pu.values64(unpack(c, self.fmt).astype(np.int64), s, self.fmt, self.block) for c, s in ((kc, ks), (vc, vs))]
+        got = []
+        for c, s in ((kc, ks), (vc, vs)):
+            c = unpack(c, self.fmt).astype(np.int64)
+            v = pu.values64(c, s, self.fmt, self.block)
+            if self.fmt == "e4m3":
+                v[c & 127 == 127] = np.nan                   # S.1111.111
+            got.append(v)
+        return got
 
     def cuda(self):
         return [torch.from_numpy(p.copy()).cuda() for p in self.parts]
@@ -102,6 +110,7 @@ def attention64(q, cache, table, lengths, starts, scale, causal=True, window=0, 
                     p /= p.sum()
                     out[first + i, j] = p @ V
                     a = np.abs(V)
+                    top = np.repeat(np.where(np.isnan(a), 0, a).max(0).reshape(-1, 32).max(1), 32)
                     bound[first + i, j] = (p * (off + off.max() + 2.0 ** -20 + held)) @ a + (length / 16 + 64) * 2.0 ** -19 * (p @ a) \
-                        + length * 2.0 ** -33 * a.max(0)
+                        + (length * 2.0 ** -33 + 2.0 ** -24) * top
     return out, lse, bound, touched
