@@ -10,14 +10,53 @@
 namespace mxq {
 namespace {
 
-constexpr int kThreads = 128, kUnits = 2;                   // lane units per thread
+constexpr int kThreads = 128;
 
-// The token of row r of [tokens, heads].  (A division of 64 bits costs more than the rest of a unit: 390 MB of BF16 out of a 4-bit
-// cache READ_FIGURE.)
-__device__ __forceinline__ int token_of(size_t r, uint32_t heads)
+// A thread has one lane unit of a token, the same one of kTokens tokens in a row: what places it (a division, the search for the sequence,
+// mostly the page) is worked out once for all of them.  (For every unit by itself it was two thirds of the instructions: 98504 tokens of
+// 8 heads of 128 from E2M1 to BF16 took 113 us, and take 87 this way.)
+struct Place {
+    int token, head;                                        // the first token
+    uint32_t unit;                                          // of the row
+};
+
+template <int kTokens>
+__device__ __forceinline__ bool place_of(const BatchArgs& p, uint32_t heads, uint32_t row_shift, Place& at)
 {
-    return r >> 32 ? (int)(r / heads) : (int)((uint32_t)r / heads);
+    const uint32_t per = heads << row_shift;
+    const size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x, group = i >> 32 ? i / per : (uint32_t)i / per;
+    const uint32_t u = (uint32_t)(i - group * per);
+    at.head = (int)(u >> row_shift);
+    at.unit = u & ((1u << row_shift) - 1u);
+    at.token = (int)min(group * kTokens, (size_t)0x7FFFFFFF);
+    return at.token < p.tokens;
 }
+
+// The sequence of a token and its rows [first, next), followed from token to token.
+struct Cursor {
+    int b, first, next;
+    __device__ __forceinline__ void start(const BatchArgs& p, int token)
+    {
+        if (!p.starts) {
+            b = first = token;
+            next = token + 1;
+            return;
+        }
+        b = find_sequence(p.starts, p.batch, token);
+        first = ld_int(p.starts + b);
+        next = ld_int(p.starts + b + 1);
+    }
+    // Whether the token is some sequence's.
+    __device__ __forceinline__ bool at(const BatchArgs& p, int token)
+    {
+        while (token >= next && b + 1 < p.batch) {
+            ++b;
+            first = next;
+            next = p.starts ? ld_int(p.starts + b + 1) : next + 1;
+        }
+        return token >= first && token < next && first >= 0;
+    }
+};
 
 struct WriteArgs {
     CacheArgs cache;
@@ -27,8 +66,8 @@ struct WriteArgs {
     uint32_t row_shift;                                     // lane units of a row, as a power of two
 };
 
-// Lane unit u of [tokens, heads, row units]; a unit never straddles a block, the lanes of a block are neighbours.
-template <class T, class F>
+// A unit never straddles a block, the lanes of a block are neighbours.
+template <class T, class F, int kTokens>
 __global__ void __launch_bounds__(kThreads)
 cache_write_kernel(const __grid_constant__ WriteArgs p)
 {
@@ -36,37 +75,40 @@ cache_write_kernel(const __grid_constant__ WriteArgs p)
     pdl_acquire();
     constexpr int OB = T::epl * F::bits / 8, NW = code_words(T::epl, F::bits);
     const int kind = blockIdx.y;
-    const uint8_t* src = kind ? p.src[1] : p.src[0];
     const size_t ts = kind ? p.token_stride[1] : p.token_stride[0], hs = kind ? p.head_stride[1] : p.head_stride[0];
     uint8_t* codes = const_cast<uint8_t*>(kind ? p.cache.vc : p.cache.kc);
     uint8_t* scales = const_cast<uint8_t*>(kind ? p.cache.vs : p.cache.ks);
-    const uint32_t heads = (uint32_t)p.cache.heads, lpb = (1u << p.cache.block_shift) / T::epl;
-    const size_t total = ((size_t)p.batch.tokens * heads) << p.row_shift;
-    uint32_t w[kUnits][8];
-    long long row[kUnits];
-    const size_t u0 = (size_t)blockIdx.x * (kThreads * kUnits) + threadIdx.x;
+    const uint32_t lpb = (1u << p.cache.block_shift) / T::epl;
+    Place at = {0, 0, 0};
+    const bool in = place_of<kTokens>(p.batch, (uint32_t)p.cache.heads, p.row_shift, at);
+    const uint8_t* src = (kind ? p.src[1] : p.src[0]) + at.head * hs + at.unit * 32;
+    uint32_t w[kTokens][8];
+    long long row[kTokens];
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j) {
-        const size_t u = u0 + j * kThreads;
+    for (int j = 0; j < kTokens; ++j) {
         row[j] = -1;
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[j][i] = 0;
-        if (u >= total) continue;
-        const size_t r = u >> p.row_shift;
-        const int token = token_of(r, heads), head = (int)(r - (size_t)token * heads);
-        ld256(w[j], src + token * ts + head * hs + (u & ((1u << p.row_shift) - 1u)) * 32);
-        int b = token, pos;
-        if (p.batch.starts) {
-            if (token < ld_int(p.batch.starts)) continue;   // (rows in front of the first and behind the last sequence)
-            b = find_sequence(p.batch.starts, p.batch.batch, token);
+        if (in && at.token + j < p.batch.tokens) ld256(w[j], src + (size_t)(at.token + j) * ts);
+    }
+    if (in) {
+        Cursor c;
+        c.start(p.batch, at.token);
+        int b = -1, length = 0;
+#pragma unroll
+        for (int j = 0; j < kTokens; ++j) {
+            const int token = at.token + j;
+            if (token >= p.batch.tokens || !c.at(p.batch, token)) continue;
+            if (c.b != b) {
+                b = c.b;
+                length = sequence(p.batch, b, p.cache.page_shift).length;
+            }
+            const int pos = length - (min(c.next, p.batch.tokens) - token);
+            if (pos >= 0) row[j] = cache_row(p.cache, p.batch, b, pos, at.head);
         }
-        const Sequence s = sequence(p.batch, b, p.cache.page_shift);
-        pos = s.length - s.n + (token - s.first);
-        if (pos < 0 || token - s.first >= s.n) continue;
-        row[j] = cache_row(p.cache, p.batch, b, pos, head);
     }
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j) {
+    for (int j = 0; j < kTokens; ++j) {
         uint32_t amax = unit_amax_bits<T>(w[j]);
         for (uint32_t o = 1; o < lpb; o <<= 1) amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
         const BlockScale s = block_scale<F>(amax);
@@ -78,9 +120,8 @@ cache_write_kernel(const __grid_constant__ WriteArgs p)
             for (int i = 0; i < NW; ++i) out[i] = 0;
         }
         if (row[j] < 0) continue;
-        const uint32_t at = (uint32_t)(u0 + j * kThreads) & ((1u << p.row_shift) - 1u);
-        store_bytes<OB>(codes + ((size_t)row[j] << p.row_shift) * OB + at * OB, out);
-        if ((at & (lpb - 1)) == 0) st_u8(scales + (((size_t)row[j] << p.row_shift) + at) / lpb, s.byte);
+        store_bytes<OB>(codes + ((size_t)row[j] << p.row_shift) * OB + at.unit * OB, out);
+        if ((at.unit & (lpb - 1)) == 0) st_u8(scales + (((size_t)row[j] << p.row_shift) + at.unit) / lpb, s.byte);
     }
 }
 
@@ -91,7 +132,7 @@ struct ReadArgs {
     uint32_t row_shift;
 };
 
-template <class F, class T>
+template <class F, class T, int kTokens>
 __global__ void __launch_bounds__(kThreads)
 cache_read_kernel(const __grid_constant__ ReadArgs p)
 {
@@ -100,39 +141,35 @@ cache_read_kernel(const __grid_constant__ ReadArgs p)
     constexpr int IB = T::epl * F::bits / 8, NWI = (IB + 3) / 4;
     const int kind = blockIdx.y;
     const uint8_t *codes = kind ? p.cache.vc : p.cache.kc, *scales = kind ? p.cache.vs : p.cache.ks;
-    uint8_t* dst = kind ? p.dst[1] : p.dst[0];
-    const uint32_t heads = (uint32_t)p.cache.heads, spb = (1u << p.cache.block_shift) / T::epl;
-    const size_t total = ((size_t)p.batch.tokens * heads) << p.row_shift;
-    const size_t u0 = (size_t)blockIdx.x * (kThreads * kUnits) + threadIdx.x;
-    uint32_t w[kUnits][NWI], sb[kUnits];
-    bool in[kUnits];
+    const uint32_t block_units_shift = p.cache.block_shift - (T::size == 4 ? 3 : 4);
+    Place at;
+    if (!place_of<kTokens>(p.batch, (uint32_t)p.cache.heads, p.row_shift, at)) return;
+    uint32_t w[kTokens][NWI], sb[kTokens];
+    bool in[kTokens];
+    Cursor c;
+    c.start(p.batch, at.token);
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j) {
-        const size_t u = u0 + j * kThreads;
-        in[j] = false;
+    for (int j = 0; j < kTokens; ++j) {
+        const int token = at.token + j;
         sb[j] = 0;
 #pragma unroll
         for (int i = 0; i < NWI; ++i) w[j][i] = 0;
-        if (u >= total) continue;
-        const size_t r = u >> p.row_shift;
-        const int token = token_of(r, heads), head = (int)(r - (size_t)token * heads);
-        if (token < ld_int(p.batch.starts)) continue;
-        const int b = find_sequence(p.batch.starts, p.batch.batch, token);
-        const int first = max(ld_int(p.batch.starts + b), 0), pos = token - first;
-        if (token >= ld_int(p.batch.starts + b + 1)) continue;      // behind the last sequence: left as it is
-        in[j] = true;
-        if ((pos >> p.cache.page_shift) >= p.batch.width) continue;
-        const long long row = cache_row(p.cache, p.batch, b, pos, head);
+        in[j] = token < p.batch.tokens && c.at(p.batch, token);       // (rows of no sequence: left as they are)
+        const int pos = token - c.first;
+        if (!in[j] || (pos >> p.cache.page_shift) >= p.batch.width) continue;
+        const long long row = cache_row(p.cache, p.batch, c.b, pos, at.head);
         if (row < 0) continue;                              // no page: zeros
-        const uint32_t at = (uint32_t)u & ((1u << p.row_shift) - 1u);
-        load_bytes<IB>(w[j], codes + ((size_t)row << p.row_shift) * IB + at * IB);
-        sb[j] = ld_u8(scales + (((size_t)row << p.row_shift) + at) / spb);
+        const size_t unit = ((size_t)row << p.row_shift) + at.unit;
+        load_bytes<IB>(w[j], codes + unit * IB);
+        sb[j] = ld_u8(scales + (unit >> block_units_shift));
     }
+    uint8_t* dst = (kind ? p.dst[1] : p.dst[0]) + ((((size_t)at.token * p.cache.heads + at.head) << p.row_shift) + at.unit) * 32;
+    const size_t next = ((size_t)p.cache.heads << p.row_shift) * 32;
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j) {
+    for (int j = 0; j < kTokens; ++j) {
         uint32_t out[8];
         widen_unit<F, T>(w[j], sb[j], out);
-        if (in[j]) st256(dst + (u0 + j * kThreads) * 32, out);
+        if (in[j]) st256(dst + j * next, out);
     }
 }
 
@@ -155,20 +192,26 @@ int by_cache_format(int fmt, FN&& fn)
     }
 }
 
+// Tokens per thread: one where the call leaves SMs idle, and time is what one thread takes; four, placed together, else.
+template <class FN>
+int by_tokens(size_t tokens, size_t units_per_token, FN&& fn)
+{
+    const bool few = tokens * units_per_token < (size_t)148 * 20 * kThreads;
+    const size_t groups = few ? tokens : (tokens + 3) / 4, ctas = (groups * units_per_token + kThreads - 1) / kThreads;
+    if (ctas > 0x7FFFFFFFu) return MXQ_ERR_SIZE;
+    return few ? fn(std::integral_constant<int, 1>{}, (unsigned)ctas) : fn(std::integral_constant<int, 4>{}, (unsigned)ctas);
+}
+
 template <class T, class F>
 int run_write(const WriteArgs& a, size_t units, cudaStream_t stream)
 {
-    const size_t ctas = (units + kThreads * kUnits - 1) / (kThreads * kUnits);
-    if (ctas > 0x7FFFFFFFu) return MXQ_ERR_SIZE;
-    return launch_grid(cache_write_kernel<T, F>, dim3((unsigned)ctas, 2), kThreads, 0, 1, stream, a);
+    return by_tokens((size_t)a.batch.tokens, units, [&](auto u, unsigned ctas) { return launch_grid(cache_write_kernel<T, F, decltype(u)::value>, dim3(ctas, 2), kThreads, 0, 1, stream, a); });
 }
 
 template <class F, class T>
 int run_read(const ReadArgs& a, size_t units, cudaStream_t stream)
 {
-    const size_t ctas = (units + kThreads * kUnits - 1) / (kThreads * kUnits);
-    if (ctas > 0x7FFFFFFFu) return MXQ_ERR_SIZE;
-    return launch_grid(cache_read_kernel<F, T>, dim3((unsigned)ctas, 2), kThreads, 0, 1, stream, a);
+    return by_tokens((size_t)a.batch.tokens, units, [&](auto u, unsigned ctas) { return launch_grid(cache_read_kernel<F, T, decltype(u)::value>, dim3(ctas, 2), kThreads, 0, 1, stream, a); });
 }
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -271,7 +314,7 @@ int mxq_cache_write(const mxq_cache* cache, const mxq_batch* batch, const mxq_ro
     debug_expect_cache(cache, batch);
     const size_t per_row = cache->head_dim * size / 32;
     a.row_shift = (uint32_t)shift_of((int)per_row);
-    const size_t units = tokens * cache->heads * per_row;
+    const size_t units = cache->heads * per_row;            // of a token
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return by_cache_format(cache->fmt, [&](auto f) {
         using F = decltype(f);
@@ -290,11 +333,11 @@ int mxq_cache_read(const mxq_cache* cache, const mxq_batch* batch, size_t total,
     if (!k || !v) return MXQ_ERR_NULL;
     if (int rc = check_places(cache, batch, false)) return rc;
     if (!aligned(k, 32) || !aligned(v, 32)) return MXQ_ERR_ALIGN;
-    const size_t size = dtype == MXQ_F32 ? 4 : 2, per_row = cache->head_dim * size / 32, units = total * cache->heads * per_row;
+    const size_t size = dtype == MXQ_F32 ? 4 : 2, per_row = cache->head_dim * size / 32, units = cache->heads * per_row;
     MXQ_DEBUG_SCOPE();
     debug_expect_cache(cache, batch);
-    MXQ_DEBUG_EXPECT(k, units * 32);
-    MXQ_DEBUG_EXPECT(v, units * 32);
+    MXQ_DEBUG_EXPECT(k, total * units * 32);
+    MXQ_DEBUG_EXPECT(v, total * units * 32);
     ReadArgs a;
     a.cache = cache_args(cache);
     a.batch = batch_args(batch, total);
