@@ -308,6 +308,29 @@ struct Attend {
 #pragma unroll
             for (int h = 0; h < GROUPS; ++h) page[h] = (uint32_t)page_next[h];
             if (after < to) ask_page(after, to);
+            if constexpr (GROUPS == 2) {
+                // Mostly the step lies in one page and every row of it exists: one place, the rest is in the instructions.
+                if (p.cache.page_shift > 4 && key + S::step <= some_hi && page[0] < (uint32_t)p.cache.pages) {
+                    there |= 3u;
+                    const uint32_t in_page = (uint32_t)key & ((1u << p.cache.page_shift) - 1u);
+                    const uint32_t nb = (uint32_t)D >> p.cache.block_shift;
+                    const size_t off = (size_t)page[0] * page_bytes + in_page * S::RB;
+                    const uint8_t *k = k_lane + off, *v = v_lane + off;
+                    static_for<S::CPR>([&](auto jc) {
+                        constexpr int J = decltype(jc)::value;
+                        const uint32_t at = slot + (to_codes ^ (S::twist(J * (32 / S::CPR)) << 4));
+                        copy16<S::k_at + J * 512, J * 512>(at, k);
+                        copy16<S::v_at + J * 512, J * 512>(at, v);
+                    });
+                    if (lane < 2 * (int)nb) {
+                        const uint8_t* from = s_lane + ((size_t)page[0] * page_scales + in_page * nb);
+                        copy16<0, 0>(slot + to_scales, from);
+                        copy16<0, 0>(slot + to_scales + kGroup * nb, from + kGroup * nb);
+                    }
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    return;
+                }
+            }
             static_for<GROUPS>([&](auto hc) {
                 constexpr int H = decltype(hc)::value;
                 const int left = some_hi - key - H * kGroup; // rows from here on that exist
