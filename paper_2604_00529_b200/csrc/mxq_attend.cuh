@@ -12,6 +12,12 @@
 //   O^T += V^T P^T  V^T by the transposing load of shared memory; the scales, which belong to (key, block) here, are multiplied
 //                   into P, relative to the largest seen so far of the block of dimensions
 // FP32 rows enter as two FP16 parts, neighbouring columns of the same step, and so do their P.
+//
+// Bound by HBM for 8-bit codes (64 sequences of 16384 to 32768 tokens, 32 heads over 8 of 128: 6.0 TB/s E4M3, 6.3 INT8), by instructions for 4-bit ones
+// (E2M1 4.5 TB/s, issue slots 63 %, ALU pipe 57 %): widening takes 4 instructions per 8 codes of K and 7 of V, which is transposed on the way, of
+// some 320 per 16 keys of a warp.  Sequences of up to 8192 tokens, E2M1: 147 us as first written (16 keys at a time, every row of a copy asked for by
+// itself, scales worked out by every lane), 126 with two groups of keys per round and offsets in the instructions, 115 with the parts joined by
+// one block per item, 110 with one question per fetched step.
 #pragma once
 #include "mxq_attend_items.cuh"
 #include "mxq_attend_plan.cuh"
@@ -1111,13 +1117,15 @@ int run(const AttendArgs& p, cudaStream_t stream)
     return launch_grid(kern, dim3((unsigned)p.ctas), p.warps * 32, S::total(p.warps), p.share > 1 ? p.share : 1, stream, p);
 }
 
+// (Four column groups: FP32 rows alone, since BF16 ones are many before that, and heads of 256 leave no registers.)
 template <int FMT, int D, int PIECES>
 int by_columns(int nt, const AttendArgs& p, cudaStream_t stream)
 {
     if (nt == 1) return run<FMT, D, 1, PIECES>(p, stream);
-    if (nt == 2) return run<FMT, D, 2, PIECES>(p, stream);
-    if constexpr (D < 256) return run<FMT, D, 4, PIECES>(p, stream);
-    else return MXQ_ERR_SIZE;
+    if constexpr (PIECES == 2 && D < 256) {
+        if (nt == 4) return run<FMT, D, 4, PIECES>(p, stream);
+    }
+    return nt == 2 ? run<FMT, D, 2, PIECES>(p, stream) : MXQ_ERR_SIZE;
 }
 
 template <int FMT, int PIECES>

@@ -59,7 +59,7 @@ struct PartMeta {
     int first, head, r0, rows;                              // first: the row of the tokens' tensors that its sequence begins with
 };
 
-// CTAs that work, of `ctas`: none without a round of keys for its warps, where that leaves enough of them.
+// CTAs that work, of `ctas`: those that there is a tile for.
 __device__ __forceinline__ uint32_t working_ctas(uint32_t total, uint32_t ctas) { return min(ctas, max(total, 1u)); }
 
 __host__ __device__ inline size_t part_bytes(int rows, int dim) { return ((size_t)rows * (dim + 2) * 4 + 31) / 32 * 32; }
