@@ -237,6 +237,33 @@ def test_streams_workspaces_and_captured_graphs():
         assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
 
 
+def test_many_queries_on_two_streams_at_once():
+    rng = np.random.default_rng(16)
+    lengths, counts = [600, 90], [200, 90]
+    cache = cu.Cache(rng, 40, 2, 128, "e2m1", 32, 32)
+    args = (*cache.cuda(), ints(cu.tables(rng, lengths, 32, 40)), ints(lengths), "e2m1")
+    q, starts = plain(rng, (290, 8, 128), BF16), ints(cu.starts_of(counts))
+    want = mxq.cache_attention(q, *args, starts=starts)
+    graphs, outs = [], []
+    for _ in range(2):
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append([mxq.cache_attention(q, *args, starts=starts) for _ in range(3)])
+        graphs.append(g)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        graphs[0].replay()
+        with torch.cuda.stream(side):
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        for out in outs[0] + outs[1]:
+            assert torch.equal(out, want)
+            out.zero_()
+        torch.cuda.synchronize()
+    assert mxq.load_library().mxq_wait_status(0) == 0
+
+
 @pytest.mark.parametrize("counts,lengths", SHAPES + [(None, [9000, 4, 700])])
 def test_results_do_not_depend_on_timing_or_on_what_the_workspace_held(counts, lengths):
     rng = np.random.default_rng(14)
