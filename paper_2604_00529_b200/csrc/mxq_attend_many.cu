@@ -486,11 +486,9 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                 }
                 fence_async();
                 info = __reduce_or_sync(0xFFFFFFFFu, info);
-                if (lane == 0) {
-                    s_info[st][warp - kRowWarps] = info;
-                    mbar_arrive(smem_addr(&bars.v_full[st]));
-                }
-                __syncwarp();
+                if (lane == 0) s_info[st][warp - kRowWarps] = info;
+                __syncwarp();                                // (the reduction orders no stores: the lanes' values and masks stand in front of the arrival)
+                if (lane == 0) mbar_arrive(smem_addr(&bars.v_full[st]));
                 if (j + 1 < count) load(1);
             }
             ok = fine;
