@@ -296,7 +296,8 @@ struct Attend {
         s_lane = (v ? p.cache.vs : p.cache.ks) + rows_before * nb + (v ? lane - nb : lane) * 16;
         to_scales = (v ? S::vs_at + (lane - nb) * 16 : S::ks_at + lane * 16);
     }
-    __device__ __forceinline__ void ask_page(int key, int to)
+    // (Keys are unsigned on the way: those that a warp looks ahead to may lie beyond 2^31, the most that a sequence has.)
+    __device__ __forceinline__ void ask_page(uint32_t key, uint32_t to)
     {
         page_next[0] = ld_int(pages_of + (key >> p.cache.page_shift));
         if constexpr (GROUPS == 2) {
@@ -306,7 +307,7 @@ struct Attend {
     }
 
     // The step of `key`; the next one to be fetched is that of `after`.
-    __device__ __forceinline__ void fetch(uint32_t slot, int key, int after, int to)
+    __device__ __forceinline__ void fetch(uint32_t slot, uint32_t key, uint32_t after, uint32_t to)
     {
         there <<= GROUPS;
         if (key < to) {
@@ -316,9 +317,9 @@ struct Attend {
             if (after < to) ask_page(after, to);
             if constexpr (GROUPS == 2) {
                 // Mostly the step lies in one page and every row of it exists: one place, the rest is in the instructions.
-                if (p.cache.page_shift > 4 && key + S::step <= some_hi && page[0] < (uint32_t)p.cache.pages) {
+                if (p.cache.page_shift > 4 && key + S::step <= (uint32_t)some_hi && page[0] < (uint32_t)p.cache.pages) {
                     there |= 3u;
-                    const uint32_t in_page = (uint32_t)key & ((1u << p.cache.page_shift) - 1u);
+                    const uint32_t in_page = key & ((1u << p.cache.page_shift) - 1u);
                     const uint32_t nb = (uint32_t)D >> p.cache.block_shift;
                     const size_t off = (size_t)page[0] * page_bytes + in_page * S::RB;
                     const uint8_t *k = k_lane + off, *v = v_lane + off;
@@ -339,10 +340,10 @@ struct Attend {
             }
             static_for<GROUPS>([&](auto hc) {
                 constexpr int H = decltype(hc)::value;
-                const int left = some_hi - key - H * kGroup; // rows from here on that exist
+                const int left = (int)((uint32_t)some_hi - key) - H * kGroup;      // rows from here on that exist
                 if (page[H] >= (uint32_t)p.cache.pages || (H > 0 && left <= 0)) return;
                 there |= 1u << H;
-                const uint32_t in_page = (uint32_t)(key + H * kGroup) & ((1u << p.cache.page_shift) - 1u);
+                const uint32_t in_page = (key + H * kGroup) & ((1u << p.cache.page_shift) - 1u);
                 const uint32_t nb = (uint32_t)D >> p.cache.block_shift;
                 const size_t off = (size_t)page[H] * page_bytes + in_page * S::RB;
                 const uint8_t *k = k_lane + off, *v = v_lane + off;
@@ -393,14 +394,14 @@ struct Attend {
     }
 
     template <bool CAREFUL>
-    __device__ __forceinline__ void make_tables(uint32_t slot, int key, uint32_t has)
+    __device__ __forceinline__ void make_tables(uint32_t slot, uint32_t key, uint32_t has)
     {
         uint32_t kw[(HB + 3) / 4], vw[(HB + 3) / 4];
         scale_bytes(slot + S::ks_at, kw);
         scale_bytes(slot + S::vs_at, vw);
-        const int mine = key + lane / LPK;
+        const uint32_t mine = key + lane / LPK;
         // seen by no row, or not there
-        const bool hidden = CAREFUL && (mine < some_lo || mine >= some_hi || !((has >> (lane / LPK / kGroup)) & 1u));
+        const bool hidden = CAREFUL && (mine < (uint32_t)some_lo || mine >= (uint32_t)some_hi || !((has >> (lane / LPK / kGroup)) & 1u));
         uint32_t kb[HB], vb[HB];
         bool rare = false;
 #pragma unroll
@@ -511,7 +512,7 @@ struct Attend {
     }
 
     // Hidden scores of a group become -inf; `seen` gets a one (FP16) for each of the others.
-    __device__ __forceinline__ void hide(int key, float (&sc)[NT][4], uint32_t (&seen)[NT][2]) const
+    __device__ __forceinline__ void hide(uint32_t key, float (&sc)[NT][4], uint32_t (&seen)[NT][2]) const
     {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -519,10 +520,10 @@ struct Attend {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const uint32_t at_column = qs + S::columns_at + (8 * n + 2 * t + j) * 12;
-                const int lo = (int)lds_u32<4>(at_column), hi = (int)lds_u32<8>(at_column);
+                const uint32_t lo = lds_u32<4>(at_column), hi = lds_u32<8>(at_column);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int at = key + g + 8 * h;
+                    const uint32_t at = key + g + 8 * h;
                     const bool on = at >= lo && at < hi;
                     if (!on) sc[n][2 * h + j] = __uint_as_float(0xFF800000u);
                     seen[n][h] |= (on ? 0x3C00u : 0u) << (16 * j);
@@ -580,7 +581,7 @@ struct Attend {
 
     // Groups FIRST ... FIRST + N - 1 of a step.
     template <int FIRST, int N, bool CAREFUL>
-    __device__ __forceinline__ void step(uint32_t slot, int key)
+    __device__ __forceinline__ void step(uint32_t slot, uint32_t key)
     {
         float sc[N][NT][4], x[N][NT][4];                     // scores; times their rows' factors, less m
         uint32_t seen[N][NT][2];
@@ -626,12 +627,13 @@ struct Attend {
     }
 
     // A fetched step: all of it at once where every row sees all of it, else group by group.
-    __device__ __forceinline__ void take(uint32_t slot, int key)
+    __device__ __forceinline__ void take(uint32_t slot, uint32_t key)
     {
         constexpr uint32_t every = (1u << GROUPS) - 1u;
         const uint32_t has = (there >> (GROUPS * (S::stages - 1))) & every;
-        if (!has || key + S::step <= some_lo || key >= some_hi) return;
-        if (has == every && key >= all_lo && key + S::step <= all_hi) {
+        const uint32_t lo = (uint32_t)some_lo, hi = (uint32_t)some_hi;
+        if (!has || key + S::step <= lo || key >= hi) return;
+        if (has == every && key >= (uint32_t)all_lo && key + S::step <= (uint32_t)all_hi) {
             make_tables<false>(slot, key, has);
             __syncwarp();
             step<0, GROUPS, false>(slot, key);
@@ -641,8 +643,8 @@ struct Attend {
         __syncwarp();
         static_for<GROUPS>([&](auto hc) {
             constexpr int H = decltype(hc)::value;
-            const int at = key + H * kGroup;
-            if (((has >> H) & 1u) && at + kGroup > some_lo && at < some_hi) step<H, 1, true>(slot, key);
+            const uint32_t at = key + H * kGroup;
+            if (((has >> H) & 1u) && at + kGroup > lo && at < hi) step<H, 1, true>(slot, key);
         });
     }
 
@@ -845,13 +847,13 @@ struct Attend {
 
     // -- a run of keys [from, to) of the item, from a multiple of a tile on
 
-    __device__ __forceinline__ void run(int from, int to)
+    __device__ __forceinline__ void run(uint32_t from, uint32_t to)
     {
         place(head);
         pages_of = p.batch.table + (size_t)b * p.batch.width;
         there = 0;
-        int key = from + warp * S::step;
-        const int stride = warps * S::step;
+        uint32_t key = from + warp * S::step;
+        const uint32_t stride = warps * S::step;
         if (key < to) ask_page(key, to);
 #pragma unroll
         for (int i = 0; i < S::stages - 1; ++i) fetch(ring + i * S::slot, key + i * stride, key + (i + 1) * stride, to);
@@ -889,7 +891,7 @@ struct Attend {
         for (int j = 0; j < HB; ++j) vref[j] = vlim[j] = -1000;
         int slot = 0, next = S::stages - 1;
         for (; key < to; key += stride) {
-            const int ahead = key + (S::stages - 1) * stride;
+            const uint32_t ahead = key + (S::stages - 1) * stride;
             fetch(ring + next * S::slot, ahead, ahead + stride, to);
             asm volatile("cp.async.wait_group %0;" :: "n"(S::stages - 1) : "memory");
             __syncwarp();
@@ -1088,8 +1090,8 @@ attend_kernel(const __grid_constant__ AttendArgs p)
         const uint32_t end = min(item + tiles, to);
         // (keys are below 2^31, tiles behind the last one reach no further than one tile beyond it)
         const uint32_t key0 = (uint32_t)(a.some_lo >> p.tile_shift << p.tile_shift);
-        const int from_key = (int)min(key0 + ((at - item) << p.tile_shift), (uint32_t)a.some_hi);
-        const int to_key = (int)min(key0 + ((end - item) << p.tile_shift), (uint32_t)a.some_hi);
+        const uint32_t from_key = min(key0 + ((at - item) << p.tile_shift), (uint32_t)a.some_hi);
+        const uint32_t to_key = min(key0 + ((end - item) << p.tile_shift), (uint32_t)a.some_hi);
         a.run(from_key, to_key);
         const bool whole = share || (at == item && end == item + tiles);
         if (first && !share && threadIdx.x == 0) {
@@ -1098,7 +1100,7 @@ attend_kernel(const __grid_constant__ AttendArgs p)
             if (ok) *meta = PartMeta{at, item, item + tiles, plan.total, s.first, a.head, a.row0, a.rows};
         }
         a.finish(reinterpret_cast<float*>(shared), whole, parts + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * part,
-                 min(warps, max((to_key - from_key + S::step - 1) / S::step, 1)), share);
+                 min(warps, max((int)((to_key - from_key + S::step - 1) / S::step), 1)), share);
         if (share) break;
         first = false;
         at = end;

@@ -237,7 +237,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
             it.to = (int)min(key0 + ((end - item) << p.tile_shift), (uint32_t)it.some_hi);
         }
         const bool two = it.rows > kRowTile, whole = at == item && end == item + tiles;
-        const int count = (it.to - it.from + kKeys - 1) / kKeys;       // key tiles, maybe none
+        const int count = (int)(((uint32_t)it.to - (uint32_t)it.from + kKeys - 1) / kKeys);       // key tiles, maybe none
 
         // rows to shared memory, in the order that the keys' elements are widened in; O from zero
         for (int i = threadIdx.x; i < 2 * kRowTile; i += kManyThreads) s_bad[i] = 0;
@@ -359,15 +359,15 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
             uint32_t byte[2][M::chunks];
             uint32_t absent = 0, outside = 0;                // bit per chunk: its key has no page, is seen by no row
             uint32_t row_at[M::chunks], row_page[M::chunks]; // where the tile to come lies
-            auto locate = [&](int k0) {
+            auto locate = [&](uint32_t k0) {                 // (keys of a last tile may lie beyond 2^31: unsigned, here and below)
                 absent = outside = 0;
 #pragma unroll
                 for (int i = 0; i < M::chunks; ++i) {
-                    const int key = k0 + (me + i * kWideners * 32) / M::CPR;
-                    const bool in = key >= it.some_lo && key < it.some_hi;
+                    const uint32_t key = k0 + (me + i * kWideners * 32) / M::CPR;
+                    const bool in = key >= (uint32_t)it.some_lo && key < (uint32_t)it.some_hi;
                     if (!in) outside |= 1u << i;
-                    row_page[i] = (uint32_t)ld_int(pages_of + ((in ? key : it.some_lo) >> p.cache.page_shift));
-                    row_at[i] = (uint32_t)key & ((1u << p.cache.page_shift) - 1u);
+                    row_page[i] = (uint32_t)ld_int(pages_of + ((in ? key : (uint32_t)it.some_lo) >> p.cache.page_shift));
+                    row_at[i] = key & ((1u << p.cache.page_shift) - 1u);
                 }
 #pragma unroll
                 for (int i = 0; i < M::chunks; ++i)
@@ -441,7 +441,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
             }
             for (int j = 0; fine && j < count; ++j) {
                 const uint32_t n = n0 + j, st = n & 1, again = ((n >> 1) & 1) ^ 1;
-                const int k0 = it.from + j * kKeys;
+                const uint32_t k0 = (uint32_t)it.from + j * kKeys, all_lo = (uint32_t)it.all_lo, all_hi = (uint32_t)it.all_hi;
                 if (!(fine = warp_agrees(wait(bars.k_empty[st], again)))) break;
 #pragma unroll
                 for (int i = 0; i < M::chunks; ++i) {
@@ -457,14 +457,14 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                     load(0);
                 }
                 if (!(fine = warp_agrees(wait(bars.v_empty[st], again)))) break;
-                const bool edge = k0 < it.all_lo || k0 + kKeys > it.all_hi;
+                const bool edge = k0 < all_lo || k0 + kKeys > all_hi;
                 uint32_t info = gone ? 1u : 0u;
 #pragma unroll
                 for (int i = 0; i < M::chunks; ++i) {
                     const int id = me + i * kWideners * 32, key = id / M::CPR, c = id % M::CPR;
                     uint32_t zero = 0;                       // elements that are NaN, where a row must not see them
                     if (edge) {
-                        if (k0 + key < it.all_lo || k0 + key >= it.all_hi) {
+                        if (k0 + key < all_lo || k0 + key >= all_hi) {
                             if (byte[1][i] == 255u) zero = M::bits == 4 ? 0xFFFFFFFFu : 0xFFFFu;
                             else if constexpr (W::has_nan) {
                                 const uint32_t words[4] = {code[1][i].x, code[1][i].y, code[1][i].z, code[1][i].w};
@@ -510,7 +510,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
 #pragma unroll
                 for (int w = 0; w < kWideners; ++w) info |= s_info[st][w];
                 const int k0 = it.from + j * kKeys, from = lo - k0, to_key = hi - k0;
-                const bool edge = k0 < it.all_lo || k0 + kKeys > it.all_hi || (info & 1u);
+                const bool edge = k0 < it.all_lo || (uint32_t)k0 + kKeys > (uint32_t)it.all_hi || (info & 1u);
                 const uint8_t* const absent = base_p + M::absent_at + st * kKeys;
                 if (info & 2u) {                             // NaN values that not every row sees: into the sums of those that do
                     uint32_t bad[NB] = {};

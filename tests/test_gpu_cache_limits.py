@@ -1,0 +1,65 @@
+"""The operators over a paged cache of codes at the limits of what their description allows: sequences as long as 32 bits count, many
+sequences in a call, caches beyond 4 GB."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_00529_b200 as mxq
+
+import cache_util as cu
+import product_util as pu
+from test_gpu_cache import BF16, F32, ints, plain
+
+pytestmark = pytest.mark.gpu
+
+LONGEST = (1 << 31) - 1                                      # tokens
+
+
+def repeated(pages):
+    """The table of one sequence of 2^31 tokens in `pages` pages of 256, in turn."""
+    return (torch.arange(1 << 23, device="cuda", dtype=torch.int32) % pages).view(1, -1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("fmt", ["e2m1", "int8"])
+@pytest.mark.parametrize("n", [1, 5, 70])
+def test_the_last_tokens_of_the_longest_sequence(fmt, dtype, n):
+    """Windows at the end of a sequence of 2^31 - 1 tokens: one, a few and many rows of a cache head."""
+    rng = np.random.default_rng(n)
+    cache = cu.Cache(rng, 3, 1, 128, fmt, 32, 256)
+    q = plain(rng, (n, 2, 128), dtype)
+    starts = None if n == 1 else np.array([0, n], np.int32)
+    table = repeated(3)
+    for window in (1, 333):
+        got = mxq.cache_attention(q, *cache.cuda(), table, ints([LONGEST]), fmt, starts=None if n == 1 else ints(starts), window=window)
+        last = 5 * 256 - 1                                   # the same tokens at the end of a sequence of five pages
+        want, _, bound, _ = cu.attention64(pu.to64(q), cache, table[:, -5:].cpu().numpy(), [last], np.array([0, n], np.int32), 128 ** -0.5, True, window, dtype)
+        pu.check(got, want, bound)
+    if n == 1:                                               # and the newest token written and attended by itself
+        bufs = cache.cuda()
+        k, v = plain(rng, (1, 1, 128), dtype), plain(rng, (1, 1, 128), dtype)
+        mxq.cache_write(k, v, *bufs, table, ints([LONGEST]), fmt)
+        got = mxq.cache_attention(q, *bufs, table, ints([LONGEST]), fmt, window=1)
+        page = int(table[0, -1])
+        alone = mxq.cache_read(*bufs, ints([[page]]), ints([0, 255]), 255, fmt, dtype=dtype)[1][254]
+        assert torch.equal(got[0], alone.expand(2, 128))
+        before = cache.cuda()
+        assert sum(int((a != b).any(-1).sum()) for a, b in zip(bufs, before)) <= 4      # one row of each buffer
+
+
+def test_all_tokens_of_the_longest_sequence():
+    rng = np.random.default_rng(3)
+    cache = cu.Cache(rng, 3, 1, 64, "e2m1", 32, 256)
+    q = plain(rng, (1, 2, 64), BF16)
+    lse = torch.empty(1, 2, device="cuda")
+    got = mxq.cache_attention(q, *cache.cuda(), repeated(3), ints([LONGEST]), "e2m1", lse=lse)
+    k64, v64 = (x.transpose(0, 2, 1, 3).reshape(768, 64) for x in cache.values())
+    times = np.full(768, LONGEST // 768)
+    times[:LONGEST % 768] += 1
+    s = pu.to64(q)[0] @ k64.T / 8
+    p = times * np.exp(s - s.max(-1, keepdims=True))
+    total = p.sum(-1, keepdims=True)
+    # each lane adds up to 2^31 / (148 * 128) weights one by one: 2^17 of them, 2^-24 each
+    want, mags = p / total @ v64, p / total @ np.abs(v64)
+    pu.check(got, want[None], (mags * (2.0 ** -11 + 2.0 ** -6) + 2.0 ** -19)[None])
+    assert np.abs(pu.to64(lse)[0] - (s.max(-1) + np.log(total[:, 0]))).max() <= 2.0 ** -6
