@@ -274,6 +274,15 @@ struct Attend {
         all_hi = token_hi(p, s, first);
     }
 
+    // The first key of a tile of the item, none behind its last key.  (Keys are below 2^31, tiles behind the last one reach no further than
+    // one tile beyond it.)
+    __device__ __forceinline__ uint32_t tile_key(uint32_t tile) const
+    {
+        return min((uint32_t)(some_lo >> p.tile_shift << p.tile_shift) + (tile << p.tile_shift), (uint32_t)some_hi);
+    }
+    // Warps that have keys of these; one where there are none.
+    __device__ __forceinline__ int with_keys(uint32_t from, uint32_t to) const { return min(warps, max((int)((to - from + S::step - 1) / S::step), 1)); }
+
     // -- a step's codes and scales on their way to shared memory
 
     // Where the lane's chunks of keys and values and its chunk of scales would lie in page 0, and the bytes from page to page.
@@ -1038,72 +1047,40 @@ attend_kernel(const __grid_constant__ AttendArgs p)
     uint8_t* const parts = p.ws + (size_t)p.ctas * sizeof(PartMeta);
     PartMeta* const meta = reinterpret_cast<PartMeta*>(p.ws) + blockIdx.x;
     const size_t part = part_bytes(p.rows, D);
-    // A run of tiles; or a cluster's item, its tiles by rank, one token per sequence.
+    // A cluster's item, its tiles by rank, one token per sequence; or a run of tiles.
     const int share = NT == 1 ? p.share : 0;
-    uint32_t at, to, seq_at, per_head;
-    int b;
-    Sequence s;
-    bool first = true;
+    bool first = true, whole = true;
+    uint32_t from_key = 0, to_key = 0;
     if (share) {
-        const int item = blockIdx.x / share, rank = share > 1 ? (int)cluster_rank() : 0;
-        b = item / p.cache.heads;
-        s = sequence(p.batch, b, p.cache.page_shift);
-        per_head = sequence_tiles(p, s);
-        seq_at = 0;
-        const uint32_t before = per_head * (item - b * p.cache.heads);
-        at = before + per_head * rank / share;
-        to = before + per_head * (rank + 1) / share;
+        const int item = blockIdx.x / share, rank = share > 1 ? (int)cluster_rank() : 0, b = item / p.cache.heads;
+        const Sequence s = sequence(p.batch, b, p.cache.page_shift);
+        const uint32_t tiles = sequence_tiles(p, s);
         a.item(b, item - b * p.cache.heads, 0, s);
+        from_key = a.tile_key(tiles * rank / share);
+        to_key = a.tile_key(tiles * (rank + 1) / share);
     } else {
         make_plan(p, warps, plan, warp_sum);
-        at = plan.from;
-        to = plan.to;
-        seq_at = plan.base;
-        per_head = plan.per_head;
-        b = plan.b;
-        s = plan.s;
         if (blockIdx.x == 0 && plan.total == 0 && threadIdx.x == 0) *meta = PartMeta{};
     }
-    while (at < to || share) {
-        uint32_t item, tiles = per_head;                     // the item's first tile, and how many
-        if (share) {
-            item = per_head * a.head;
-        } else {
-            if (at - seq_at >= per_head * p.cache.heads) {
-                seq_at += per_head * p.cache.heads;
-                ++b;
-                s = sequence(p.batch, b, p.cache.page_shift);
-                per_head = sequence_tiles(p, s);
-                continue;
-            }
-            const uint32_t head = (at - seq_at) / per_head;
-            item = seq_at + per_head * head;
-            int r0 = 0;
-            if (s.n * p.group > p.rows) {
-                for (;; r0 += p.rows, item += tiles) {
-                    tiles = item_tiles(p, s, r0);
-                    if (at < item + tiles) break;
-                }
-            }
-            a.item(b, (int)head, r0, s);
+    while (share || plan.from < plan.to) {
+        if (!share) {
+            a.item(plan.b, plan.head, plan.r0, plan.s);
+            const uint32_t end = min(plan.item + plan.tiles, plan.to);
+            from_key = a.tile_key(plan.from - plan.item);
+            to_key = a.tile_key(end - plan.item);
+            whole = plan.from == plan.item && end == plan.item + plan.tiles;
         }
-        const uint32_t end = min(item + tiles, to);
-        // (keys are below 2^31, tiles behind the last one reach no further than one tile beyond it)
-        const uint32_t key0 = (uint32_t)(a.some_lo >> p.tile_shift << p.tile_shift);
-        const uint32_t from_key = min(key0 + ((at - item) << p.tile_shift), (uint32_t)a.some_hi);
-        const uint32_t to_key = min(key0 + ((end - item) << p.tile_shift), (uint32_t)a.some_hi);
         a.run(from_key, to_key);
-        const bool whole = share || (at == item && end == item + tiles);
         if (first && !share && threadIdx.x == 0) {
             bool ok = true;
             MXQ_CHECKED(meta, sizeof(PartMeta), ok = false)
-            if (ok) *meta = PartMeta{at, item, item + tiles, plan.total, s.first, a.head, a.row0, a.rows};
+            if (ok) *meta = PartMeta{plan.from, plan.item, plan.item + plan.tiles, plan.total, a.s.first, a.head, a.row0, a.rows};
         }
-        a.finish(reinterpret_cast<float*>(shared), whole, parts + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * part,
-                 min(warps, max((int)((to_key - from_key + S::step - 1) / S::step), 1)), share);
+        a.finish(reinterpret_cast<float*>(shared), whole, parts + ((size_t)blockIdx.x * 2 + (first ? 0 : 1)) * part, a.with_keys(from_key, to_key), share);
         if (share) break;
         first = false;
-        at = end;
+        if (threadIdx.x == 0) next_item(p, plan);
+        __syncthreads();
     }
 }
 

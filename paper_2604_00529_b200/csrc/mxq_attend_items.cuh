@@ -24,19 +24,43 @@ __device__ __forceinline__ uint32_t span_tiles(const AttendArgs& p, int lo, int 
     return (uint32_t)max(tiles, 1);                         // (an item that sees nothing still writes its zeros)
 }
 
-// Tiles of the item that begins with row r0, and of one head of a sequence.
+// Tiles of the item that begins with row r0.
 __device__ __forceinline__ uint32_t item_tiles(const AttendArgs& p, const Sequence& s, int r0)
 {
     const int last = min(r0 + p.rows, s.n * p.group) - 1;
     return span_tiles(p, token_lo(p, s, row_token(p, s, r0)), token_hi(p, s, row_token(p, s, last)));
 }
+
+// The items of one head of a sequence in order, without a division for each: first and last token of an item follow from the item before.
+struct ItemWalk {
+    int r0, first, over, tokens, rest, last_tokens, last_rest;     // over: rows of token `first` that lie in front of r0
+    __device__ __forceinline__ explicit ItemWalk(const AttendArgs& p)
+        : r0(0), first(0), over(0), tokens(p.rows / p.group), rest(p.rows % p.group), last_tokens((p.rows - 1) / p.group), last_rest((p.rows - 1) % p.group) {}
+    __device__ __forceinline__ uint32_t tiles(const AttendArgs& p, const Sequence& s) const
+    {
+        const int last = min(first + last_tokens + (over + last_rest >= p.group), s.n - 1);
+        return span_tiles(p, token_lo(p, s, first), token_hi(p, s, last));
+    }
+    __device__ __forceinline__ void next(const AttendArgs& p)
+    {
+        r0 += p.rows;
+        first += tokens;
+        over += rest;
+        if (over >= p.group) {
+            over -= p.group;
+            ++first;
+        }
+    }
+};
+
+// Tiles of one head of a sequence.
 __device__ __forceinline__ uint32_t sequence_tiles(const AttendArgs& p, const Sequence& s)
 {
     const int rows = s.n * p.group;                         // far below 2^31: the host has seen to that, and to the sum of all tiles
     if (rows == 0) return 0;
     if (rows <= p.rows) return span_tiles(p, token_lo(p, s, 0), token_hi(p, s, s.n - 1));
     uint32_t sum = 0;
-    for (int r = 0; r < rows; r += p.rows) sum += item_tiles(p, s, r);
+    for (ItemWalk w(p); w.r0 < rows; w.next(p)) sum += w.tiles(p, s);
     return sum;
 }
 

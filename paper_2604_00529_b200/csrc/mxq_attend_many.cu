@@ -144,7 +144,6 @@ __host__ __device__ constexpr int widened_place(int e)
 // What all warps know of the item.
 struct ManyItem {
     int b, head, row0, rows, some_lo, some_hi, all_lo, all_hi, from, to;
-    Sequence s;
 };
 
 struct ManyBars {
@@ -193,40 +192,19 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
     PartMeta* const meta = reinterpret_cast<PartMeta*>(p.ws) + blockIdx.x;
     uint8_t* const parts = p.ws + (size_t)p.ctas * sizeof(PartMeta);
     const size_t part = part_bytes(p.rows, D);
-    uint32_t at = plan.from, seq_at = plan.base, per_head = plan.per_head;
-    const uint32_t to = plan.to;
-    int b = plan.b;
-    Sequence s = plan.s;
     bool first = true, ok = true;
     uint32_t n0 = 0, n1 = 0, pieces = 0;                     // tiles that the first and the second row tile have seen, pieces done
     if (blockIdx.x == 0 && plan.total == 0 && threadIdx.x == 0) *meta = PartMeta{};
-    while (at < to) {
-        if (at - seq_at >= per_head * p.cache.heads) {
-            seq_at += per_head * p.cache.heads;
-            ++b;
-            s = sequence(p.batch, b, p.cache.page_shift);
-            per_head = sequence_tiles(p, s);
-            continue;
-        }
+    while (plan.from < plan.to) {
         ManyItem it;
-        uint32_t item, tiles, end;
+        const Sequence s = plan.s;
+        const uint32_t item = plan.item, tiles = plan.tiles, at = plan.from, end = min(item + tiles, plan.to);
         {
-            const uint32_t head = (at - seq_at) / per_head;
-            item = seq_at + per_head * head;
-            tiles = per_head;
-            int r0 = 0;
-            if (s.n * p.group > p.rows) {
-                for (;; r0 += p.rows, item += tiles) {
-                    tiles = item_tiles(p, s, r0);
-                    if (at < item + tiles) break;
-                }
-            }
-            end = min(item + tiles, to);
-            it.b = b;
-            it.head = (int)head;
+            const int r0 = plan.r0;
+            it.b = plan.b;
+            it.head = plan.head;
             it.row0 = r0;
             it.rows = min(p.rows, s.n * p.group - r0);
-            it.s = s;
             const int t0 = row_token(p, s, r0), t1 = row_token(p, s, r0 + it.rows - 1);
             it.some_lo = token_lo(p, s, t0);
             it.some_hi = token_hi(p, s, t1);
@@ -354,7 +332,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
             ok = fine;
         } else if (ok && warp >= kRowWarps && warp < kIssuer) {
             const int me = threadIdx.x - kRowWarps * 32;
-            const int* const pages_of = p.batch.table + (size_t)b * p.batch.width;
+            const int* const pages_of = p.batch.table + (size_t)it.b * p.batch.width;
             uint4 code[2][M::chunks];                        // keys and values of the tile to come
             uint32_t byte[2][M::chunks];
             uint32_t absent = 0, outside = 0;                // bit per chunk: its key has no page, is seen by no row
@@ -650,7 +628,8 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
         if (two) n1 += count;
         ++pieces;
         first = false;
-        at = end;
+        if (threadIdx.x == 0) next_item(p, plan);
+        __syncthreads();
     }
     // A wait that gave up, in whichever warp, may have left products under way: let them end before their memory goes.
     if (s_gave_up) {

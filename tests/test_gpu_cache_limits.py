@@ -8,7 +8,7 @@ import paper_2604_00529_b200 as mxq
 
 import cache_util as cu
 import product_util as pu
-from test_gpu_cache import BF16, F32, ints, plain
+from test_gpu_cache import BF16, F32, attend, ints, plain
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +63,35 @@ def test_all_tokens_of_the_longest_sequence():
     want, mags = p / total @ v64, p / total @ np.abs(v64)
     pu.check(got, want[None], (mags * (2.0 ** -11 + 2.0 ** -6) + 2.0 ** -19)[None])
     assert np.abs(pu.to64(lse)[0] - (s.max(-1) + np.log(total[:, 0]))).max() <= 2.0 ** -6
+
+
+@pytest.mark.parametrize("dtype,dim", [(F32, 64), (F32, 256), (BF16, 256), (BF16, 64)])
+@pytest.mark.parametrize("group,counts,lengths", [(5, [300, 0, 7, 90], [310, 5, 7, 1000]), (3, [1] * 40 + [129], [33] * 40 + [140]), (16, [70, 1], [90, 640])])
+def test_items_of_a_run_are_followed(dtype, dim, group, counts, lengths):
+    """Sequences of many items, groups of heads that do not divide an item's rows, runs over several heads and sequences."""
+    rng = np.random.default_rng(group)
+    cache = cu.Cache(rng, sum(-(-n // 32) for n in lengths) + 1, 2, dim, "int8", 32, 32)
+    for causal, window in ((True, 0), (True, 50), (False, 0)):
+        attend(rng, cache, lengths, counts, group, dtype, causal=causal, window=window)
+
+
+def test_time_grows_like_the_queries():
+    """FP32 queries with a window: four times as many take four times as long (sixteen times, where each item is searched for)."""
+    rng = np.random.default_rng(2)
+    cache = cu.Cache(rng, 2, 1, 64, "int8", 32, 256).cuda()
+    took = []
+    for n in (8192, 32768):
+        q, table = plain(rng, (n, 16, 64), F32), repeated(2)[:, :n // 256].contiguous()
+        args = (q, *cache, table, ints([n]), "int8")
+        mxq.cache_attention(*args, starts=ints([0, n]), window=64)
+        times = []
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            mxq.cache_attention(*args, starts=ints([0, n]), window=64)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        took.append(sorted(times)[2])
+    print("%.3f and %.3f ms" % tuple(took))
+    assert took[1] <= 8 * took[0]
