@@ -456,8 +456,8 @@ int mxq_moe(const mxq_moe_layer *layer, const void *x, int dtype, const float *l
  *   table    [batch, width]  the pages of sequence b in order.  An entry outside [0, pages) is never accessed: what would be written
  *                            there is dropped, its tokens are read as zeros and left out of the attention
  *   lengths  [batch]         tokens of each sequence, the new ones among them; at most width * page count
- *   starts   [batch + 1]     rows starts[b] ... starts[b + 1] - 1 of the tokens' tensors are sequence b's last (newest) tokens, in
- *                            order; rows in front of starts[0] and behind starts[batch] belong to none.  Null: row b is sequence b's one
+ *   starts   [batch + 1]     never decreasing (else results are undefined, and nothing else is accessed): rows starts[b] ... starts[b + 1] - 1
+ *                            of the tokens' tensors are sequence b's last (newest) tokens, in order; rows in front of starts[0] and behind starts[batch] belong to none.  Null: row b is sequence b's one
  *                            newest token, and tokens must equal batch (MXQ_ERR_SIZE)
  * A row that would lie in front of its sequence's first token (a padded slot of length 0) is not written, and attends nothing.
  * Structs are HOST structs, free to reuse when a call returns.  batch, width and tokens are below 2^31 (MXQ_ERR_SIZE).

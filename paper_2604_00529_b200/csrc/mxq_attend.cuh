@@ -1060,7 +1060,11 @@ attend_kernel(const __grid_constant__ AttendArgs p)
         to_key = a.tile_key(tiles * (rank + 1) / share);
     } else {
         make_plan(p, warps, plan, warp_sum);
-        if (blockIdx.x == 0 && plan.total == 0 && threadIdx.x == 0) *meta = PartMeta{};
+        if (plan.from >= plan.to && threadIdx.x == 0) {
+            bool ok = true;
+            MXQ_CHECKED(meta, sizeof(PartMeta), ok = false)
+            if (ok) *meta = PartMeta{0, 0, 0, plan.total, 0, 0, 0, 0};
+        }
     }
     while (share || plan.from < plan.to) {
         if (!share) {

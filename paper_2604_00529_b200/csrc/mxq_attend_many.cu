@@ -194,7 +194,11 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
     const size_t part = part_bytes(p.rows, D);
     bool first = true, ok = true;
     uint32_t n0 = 0, n1 = 0, pieces = 0;                     // tiles that the first and the second row tile have seen, pieces done
-    if (blockIdx.x == 0 && plan.total == 0 && threadIdx.x == 0) *meta = PartMeta{};
+    if (plan.from >= plan.to && threadIdx.x == 0) {
+        bool good = true;
+        MXQ_CHECKED(meta, sizeof(PartMeta), good = false)
+        if (good) *meta = PartMeta{0, 0, 0, plan.total, 0, 0, 0, 0};
+    }
     while (plan.from < plan.to) {
         ManyItem it;
         const Sequence s = plan.s;

@@ -53,6 +53,10 @@ __device__ __noinline__ void next_item(const AttendArgs& p, Plan& plan)
         return;
     }
     do {
+        if (plan.b + 1 >= p.batch.batch) {                   // (only where sums of tiles passed 32 bits: rows that several sequences claim)
+            plan.from = plan.to;
+            return;
+        }
         plan.base += plan.per_head * p.cache.heads;
         ++plan.b;
         plan.s = sequence(p.batch, plan.b, p.cache.page_shift);
@@ -81,6 +85,7 @@ __device__ __forceinline__ void make_plan(const AttendArgs& p, int warps, Plan& 
         if (lane >= o) before += up;
     }
     if (lane == 31) warp_sum[warp] = before;
+    if (threadIdx.x == 0) plan.total = plan.from = plan.to = 0;        // (a run that lies in no sequence, likewise)
     __syncthreads();
     uint32_t sum = lane < warps ? warp_sum[lane] : 0u;
     const uint32_t total = __reduce_add_sync(0xFFFFFFFFu, sum);

@@ -19,13 +19,13 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
     __shared__ float2 weights[kJoinThreads];
     const PartMeta* metas = reinterpret_cast<const PartMeta*>(p.ws);
     const uint32_t c = blockIdx.x + 1;
-    const PartMeta meta = metas[c];                         // (every CTA that works has written its own; read before that is known)
+    const PartMeta meta = metas[c];                         // (every CTA has written its own)
     const uint32_t total = metas[0].total;
     if (c >= working_ctas(total, p.ctas)) return;
     const Runs runs(total, working_ctas(total, p.ctas));
     const uint32_t before = runs.start(c - 1);
     if (meta.from <= meta.item_from || before > meta.item_from) return;
-    const int n = (int)(runs.of(meta.item_to - 1) - (c - 1) + 1);      // runs c - 1 ... have parts of it
+    const int n = (int)(runs.of(min(meta.item_to, total) - 1) - (c - 1) + 1);      // runs c - 1 ... have parts of it
     const size_t part = part_bytes(p.rows, dim) / 4;        // in floats
     const float* const parts = reinterpret_cast<const float*>(p.ws + (size_t)p.ctas * sizeof(PartMeta));
     // the first part is its run's last piece (slot 1), unless the item is that run's first; the others are their runs' first pieces (slot 0)
