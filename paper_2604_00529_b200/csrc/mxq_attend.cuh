@@ -983,10 +983,7 @@ struct Attend {
                 float* const to = reinterpret_cast<float*>(part);
                 MXQ_CHECKED(to + r * D + d, 16, continue)
                 *reinterpret_cast<float4*>(to + r * D + d) = make_float4(v[0], v[1], v[2], v[3]);
-                if (d == 0) {
-                    to[p.rows * D + 2 * r] = top;
-                    to[p.rows * D + 2 * r + 1] = sum;
-                }
+                if (d == 0) write_weight(to + p.rows * D + 2 * r, top, sum);
             }
         }
         if (share > 1) {

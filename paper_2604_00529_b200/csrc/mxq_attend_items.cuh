@@ -86,6 +86,20 @@ struct PartMeta {
 // CTAs that work, of `ctas`: those that there is a tile for.
 __device__ __forceinline__ uint32_t working_ctas(uint32_t total, uint32_t ctas) { return min(ctas, max(total, 1u)); }
 
+// Words of the workspace: what the first kernel leaves of an item's row beside its sums, and what the second one reads.
+__device__ __forceinline__ void write_weight(float* to, float m, float l)
+{
+    MXQ_CHECKED(to, 8, return)
+    to[0] = m;
+    to[1] = l;
+}
+template <class T>
+__device__ __forceinline__ T ld_part(const void* from)
+{
+    MXQ_CHECKED(from, sizeof(T), return T{})
+    return *reinterpret_cast<const T*>(from);
+}
+
 __host__ __device__ inline size_t part_bytes(int rows, int dim) { return ((size_t)rows * (dim + 2) * 4 + 31) / 32 * 32; }
 
 __device__ __forceinline__ float exp2_approx(float v)

@@ -612,10 +612,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                     }
                 }
                 if (mine && whole) write_lse(p, out_row, m, l);
-                if (mine && !whole) {
-                    to_part[p.rows * D + 2 * row] = m;
-                    to_part[p.rows * D + 2 * row + 1] = l;
-                }
+                if (mine && !whole) write_weight(to_part + p.rows * D + 2 * row, m, l);
                 tc_fence_before();
             }
             ok = fine;

@@ -19,8 +19,8 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
     __shared__ float2 weights[kJoinThreads];
     const PartMeta* metas = reinterpret_cast<const PartMeta*>(p.ws);
     const uint32_t c = blockIdx.x + 1;
-    const PartMeta meta = metas[c];                         // (every CTA has written its own)
-    const uint32_t total = metas[0].total;
+    const PartMeta meta = ld_part<PartMeta>(metas + c);    // (every CTA has written its own)
+    const uint32_t total = ld_part<uint32_t>(&metas->total);
     if (c >= working_ctas(total, p.ctas)) return;
     const Runs runs(total, working_ctas(total, p.ctas));
     const uint32_t before = runs.start(c - 1);
@@ -51,7 +51,7 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
 #pragma unroll 4
             for (int i = mine; i < n; i += lanes) {
                 const float* x = i ? part1 + (size_t)(i - 1) * 2 * part : part0;
-                add(*reinterpret_cast<const float2*>(x + p.rows * dim + 2 * r), *reinterpret_cast<const float4*>(x + r * dim + d));
+                add(ld_part<float2>(x + p.rows * dim + 2 * r), ld_part<float4>(x + r * dim + d));
             }
         }
         if (lanes > 1) {

@@ -61,3 +61,16 @@ def test_starts_that_decrease(D, starts, fmt, bits):  # noqa: F811
             assert D.mxq_cache_write(ctypes.byref(b.cache), ctypes.byref(b.batch), ctypes.byref(r), ctypes.byref(r), dtype, tokens, stream) == 0
             assert D.mxq_cache_read(ctypes.byref(b.cache), ctypes.byref(b.batch), tokens, P(kv), P(kv), dtype, stream) == 0
         clean(D, 6)
+
+
+@pytest.mark.parametrize("fmt,bits", [("e4m3", 8), ("e2m1", 4), ("int8", 8), ("int4", 4)])
+@pytest.mark.parametrize("counts,lengths,page,dim,block,heads,group", [
+    ([1], [9000], 64, 128, 32, 2, 4), ([1, 1, 1], [20000, 3, 700], 128, 64, 32, 1, 16), ([3, 2], [3000, 6000], 32, 256, 64, 1, 3),
+    ([300], [5000], 64, 128, 64, 2, 2), ([130, 0, 200], [4000, 9, 210], 16, 64, 64, 3, 1)])
+def test_windows_and_items_in_parts(D, counts, lengths, page, dim, block, heads, group, fmt, bits):  # noqa: F811
+    b = Batch(lengths, [sum(counts[:i]) for i in range(len(counts) + 1)], sum(counts), page, dim, block, heads, fmt, bits)
+    for dtype in (0, 1):
+        for window in (0, 1, 100, 2500):
+            report(D)
+            b.attend(D, dtype, group, window)
+            clean(D, 2)                                      # the items' kernel and the one that joins parts
