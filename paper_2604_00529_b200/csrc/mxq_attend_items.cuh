@@ -16,7 +16,8 @@ __device__ __forceinline__ int row_token(const AttendArgs& p, const Sequence& s,
 
 // The keys [lo, hi) that a new token of a sequence sees.
 __device__ __forceinline__ int token_hi(const AttendArgs& p, const Sequence& s, int i) { return p.causal ? max(s.length - s.n + i + 1, 0) : s.length; }
-__device__ __forceinline__ int token_lo(const AttendArgs& p, const Sequence& s, int i) { return p.window ? max(s.length - s.n + i + 1 - p.window, 0) : 0; }
+// (A token in front of position 0 is taken to be there, so that no window passes 32 bits.)
+__device__ __forceinline__ int token_lo(const AttendArgs& p, const Sequence& s, int i) { return p.window ? max(max(s.length - s.n + i + 1, 0) - p.window, 0) : 0; }
 
 __device__ __forceinline__ uint32_t span_tiles(const AttendArgs& p, int lo, int hi)
 {

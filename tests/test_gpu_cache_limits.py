@@ -95,3 +95,18 @@ def test_time_grows_like_the_queries():
         took.append(sorted(times)[2])
     print("%.3f and %.3f ms" % tuple(took))
     assert took[1] <= 8 * took[0]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("group", [1, 8])
+@pytest.mark.parametrize("counts,lengths", [([8], [5]), ([40, 3], [5, 40]), ([1, 2], [0, 1])])
+def test_a_window_without_limit(dtype, group, counts, lengths):
+    """Windows up to what their type holds, also where sequences bring more queries than they have tokens."""
+    rng = np.random.default_rng(4)
+    cache = cu.Cache(rng, 6, 1, 64, "int8", 32, 16)
+    table = cu.tables(rng, lengths, 16, 6)
+    q = plain(rng, (sum(counts), group, 64), dtype)
+    want = attend(rng, cache, lengths, counts, group, dtype, table=table, q=q)
+    for window in (64, 1 << 30, (1 << 31) - 64, (1 << 31) - 1, 1 << 31, 1 << 40, (1 << 62) + 5):
+        got = mxq.cache_attention(q, *cache.cuda(), ints(table), ints(lengths), "int8", starts=ints(cu.starts_of(counts)), window=window)
+        assert torch.equal(got, want), window
