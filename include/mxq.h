@@ -507,8 +507,9 @@ int mxq_cache_read(const mxq_cache *cache, const mxq_batch *batch, size_t total,
  * window > 0 only the last `window` of them, p included; causal == 0: all tokens (window must be 0, MXQ_ERR_SIZE).  What is not visible
  * has no influence, whatever it holds.  A query that sees nothing gives zeros, and -inf in lse.
  * Sums and the softmax are held in FP32.  Queries enter exactly for BF16 (elements below 2^-31 of a row's largest excepted) and
- * with 22 bits for FP32; the softmax's weights enter the second product with 11 bits for BF16 and 22 for FP32, values of a block of 32
- * dimensions below 2^-24 of the largest there may count as zeros.  BF16 calls of head_dim 64 or 128 with more than 16 rows of a cache head per
+ * with 22 bits for FP32; the softmax's weights enter the second product with 11 bits for BF16 and 22 for FP32, and a key's weight times
+ * the scale of 32 dimensions is off by no more than 2^-20 (FP32: 2^-23) of the row's largest such product, however far the scales of
+ * keys lie apart.  A weight below 2^-120 of a row's largest may count as zero.  BF16 calls of head_dim 64 or 128 with more than 16 rows of a cache head per
  * sequence in the mean (tokens / batch * q_heads / heads) run on other tensor cores: weights enter with 8 bits, every value counts.
  * A NaN or an infinity in a query gives NaN.  Results do not depend on timing.  That kernel waits as those of mxq_matmul do
  * (mxq_wait_status); a wait that runs out leaves an unfinished out.

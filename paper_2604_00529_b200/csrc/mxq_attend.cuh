@@ -10,7 +10,9 @@
 //                   the sum over a block of 32 is multiplied by its scale in FP32
 //   P = 2^(S - m)   m is moved only when a score exceeds it by 2^12; FP16 holds what lies below
 //   O^T += V^T P^T  V^T by the transposing load of shared memory; the scales, which belong to (key, block) here, are multiplied
-//                   into P, relative to the largest seen so far of the block of dimensions
+//                   into P, relative to a reference of the block of dimensions.  A step with a scale that lies too far from it (the products
+//                   would not be FP16 numbers) takes products relative to each row's largest
+//                   instead (far_step), whatever other rows see or what a key weighs
 // FP32 rows enter as two FP16 parts, neighbouring columns of the same step, and so do their P.
 //
 // Bound by HBM for 8-bit codes (64 sequences of 16384 to 32768 tokens, 32 heads over 8 of 128: 6.0 TB/s E4M3, 6.3 INT8), by instructions for 4-bit ones
@@ -34,7 +36,10 @@ constexpr int kGroup = 16;                                  // keys of a matrix 
 constexpr int kStagesMax = 6;
 constexpr float kBias = 8.f;                                // P is held as 2^kBias times itself: more of FP16's range below 1
 constexpr float kSlack = 12.f;                              // m moves when 2^kSlack would be exceeded
-constexpr int kScaleSlack = 3;                              // and a block's reference scale when 2^kScaleSlack would be
+// Scales from 2^-below to 2^kAbove of a block's reference are multiplied into P as they are: what FP16 cuts off is then 2^-21 of a row's largest
+// product of weight and scale for BF16 rows, where a small first token should not cost time, 2^-24 for FP32 ones.
+constexpr int kAbove = 3;
+constexpr int below_of(int pieces) { return pieces == 1 ? 8 : 5; }
 
 // ---- codes to FP16 pairs --------------------------------------------------------------------------------------
 
@@ -220,7 +225,8 @@ struct Shape {
     // a warp's slot: a step's keys, values and scale bytes
     static constexpr int k_at = 0, v_at = step * RB, ks_at = 2 * step * RB, vs_at = ks_at + step * NB, slot = vs_at + step * NB;
     // tables of a warp's step: the keys' scales (FP32), the values' multipliers (FP16, pairs of keys)
-    static constexpr int kf_at = 0, vm_at = step * NB * 4, tables = vm_at + step * NB * 2;
+    static constexpr int kf_at = 0, vm_at = step * NB * 4, far_at = vm_at + step * NB * 2;
+    static constexpr int tables = far_at + NT * NB * 16;    // far_at: units of the sums, 16 bits each (far_step)
     static constexpr int q_row = D * 2 + (bits == 4 ? 16 : 32);       // padded: lanes of a read lie in different banks
     static constexpr int q_bytes = 8 * NT * q_row;
     static constexpr int columns_at = q_bytes;                        // of each column: its factor, the keys that its row sees
@@ -247,13 +253,18 @@ struct Attend {
     using S = Shape<FMT, D, NT>;
     static constexpr int NB = S::NB, MT = S::MT, NP = S::NP, GROUPS = S::groups;
     static constexpr bool has_nan = FMT == MXQ_FP8_E4M3;
+    static constexpr int kBelow = below_of(PIECES);
 
     const AttendArgs& p;
     const int warps, warp, lane, g, t;
     uint32_t ring, tables, qs;                              // shared addresses: the warp's ring and tables, the CTA's rows
     uint32_t twisted;                                       // a lane's part of its matrix loads' addresses
     float acc[MT][NT][4], l[NT][2], m[NT][2], f[NT][2];
-    int vref[NB * S::step / 32], vlim[NB * S::step / 32];   // reference scale bytes of the lane's blocks (make_tables), and what raises them
+    // Of the lane's blocks (make_tables), the smallest scale byte that is multiplied into P as it is: kBelow under the reference, which is the
+    // unit of the block's sums.  kUnset before a key was seen.
+    static constexpr int kUnset = -1000;
+    int low[NB * S::step / 32];
+    bool apart;                                             // the sums have units of their own, by row and block, in shared memory
     uint32_t q[S::q_in_registers ? NT * MT : 1][2];
     // the item
     int b, head, row0, rows;                                // rows: how many of the item are there
@@ -402,8 +413,9 @@ struct Attend {
         }
     }
 
+    // The tables of a step; whether a scale of a value that some row sees lies too far from its block's reference.
     template <bool CAREFUL>
-    __device__ __forceinline__ void make_tables(uint32_t slot, uint32_t key, uint32_t has)
+    __device__ __forceinline__ bool make_tables(uint32_t slot, uint32_t key, uint32_t has)
     {
         uint32_t kw[(HB + 3) / 4], vw[(HB + 3) / 4];
         scale_bytes(slot + S::ks_at, kw);
@@ -417,25 +429,26 @@ struct Attend {
         for (int j = 0; j < HB; ++j) {
             kb[j] = __byte_perm(kw[j / 4], 0, 0x4440 + j % 4);
             vb[j] = __byte_perm(vw[j / 4], 0, 0x4440 + j % 4);
-            rare |= kb[j] == 255u || ((int)vb[j] > vlim[j] && !hidden);
+            rare |= kb[j] == 255u || (vb[j] - (uint32_t)low[j] > (uint32_t)(kBelow + kAbove) && !hidden);
         }
         const bool any_rare = __any_sync(0xFFFFFFFFu, rare);
-        if (any_rare) raise_reference(vb, hidden);
+        bool far = false;
+        if (any_rare) far = settle(vb, hidden);
         float kf[HB], mult[HB];
 #pragma unroll
         for (int j = 0; j < HB; ++j) {
             kf[j] = __uint_as_float(max(kb[j] << 23, 0x00400000u));
-            // (2^-127 and less: nothing; no more than 2^kScaleSlack)
-            mult[j] = __uint_as_float((uint32_t)max((int)vb[j] + 127 - vref[j], 0) << 23);
+            mult[j] = __uint_as_float((vb[j] - (uint32_t)low[j] + (uint32_t)(127 - kBelow)) << 23);
             if (hidden) mult[j] = 0.f;
         }
         uint32_t h[(HB + 1) / 2];
 #pragma unroll
         for (int j = 0; j < HB; j += 2) h[j / 2] = pack_f16(mult[j], j + 1 < HB ? mult[j + 1] : 0.f);
-        if (any_rare) {                                      // poisoned blocks (or just a reference raised)
+        if (any_rare) {                         // poisoned blocks, scales too far away (or just a reference settled)
 #pragma unroll
             for (int j = 0; j < HB; ++j) {
                 if (kb[j] == 255u) kf[j] = __uint_as_float(0x7FC00000u);
+                if (vb[j] - (uint32_t)low[j] > (uint32_t)(kBelow + kAbove)) h[j / 2] &= j & 1 ? 0xFFFFu : 0xFFFF0000u;
                 if (vb[j] == 255u && !hidden) h[j / 2] = j & 1 ? (h[j / 2] & 0xFFFFu) | 0x7E000000u : (h[j / 2] & 0xFFFF0000u) | 0x7E00u;
             }
         }
@@ -457,6 +470,24 @@ struct Attend {
             constexpr int J = decltype(jc)::value;
             sts_u16<S::vm_at + J * 4>(vt, J & 1 ? h[J / 2] >> 16 : h[J / 2]);
         });
+        return far;
+    }
+
+    // References of blocks that have none yet: the largest scale of the step that some row sees (vb: the bytes of the lane's key and blocks;
+    // 251 at most, so that a poisoned block is never near).  Whether a scale lies too far from its block's reference then.
+    __device__ __forceinline__ bool settle(const uint32_t (&vb)[HB], bool hidden)
+    {
+        bool far = false;
+#pragma unroll
+        for (int j = 0; j < HB; ++j) {
+            const bool counts = !hidden && vb[j] != 255u;
+            int top = counts ? (int)min(vb[j], 251u) : kUnset;
+#pragma unroll
+            for (int o = LPK; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            if (low[j] == kUnset && top != kUnset) low[j] = top - kBelow;
+            far |= counts && vb[j] - (uint32_t)low[j] > (uint32_t)(kBelow + kAbove);
+        }
+        return __any_sync(0xFFFFFFFFu, far);
     }
 
     // -- one step
@@ -541,9 +572,9 @@ struct Attend {
         }
     }
 
-    // O^T += V^T P^T of group H, P as matrix operands.
-    template <int H, bool CAREFUL>
-    __device__ __forceinline__ void add_values(uint32_t slot, const uint32_t (&pb)[NT][2], const uint32_t (&seen)[NT][2])
+    // O^T += V^T P^T of group H, P as matrix operands; or (FAR) as the weights of each block, from the scores.
+    template <int H, bool CAREFUL, bool FAR = false>
+    __device__ __forceinline__ void add_values(uint32_t slot, uint32_t (&pb)[NT][2], const uint32_t (&seen)[NT][2], const float (*sc)[4] = nullptr)
     {
         uint32_t vm_lo[NB], vm_hi[NB];                       // keys 2t, 2t + 1 and 2t + 8, 2t + 9
         lds_words<NB, S::vm_at + H * 8 * NB * 4>(tables + t * NB * 4, vm_lo);
@@ -574,9 +605,12 @@ struct Attend {
                 }
                 uint32_t X[NP], Y[NP];
                 value_pairs<FMT>(w[h][0], w[h][1], X, Y);
+                if constexpr (FAR) {
+                    if (S::bits == 4 || h == 0) far_weights<H>(slot, blk, sc, pb);
+                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const uint32_t b0 = mul_f16(pb[n][0], vm_lo[blk]), b1 = mul_f16(pb[n][1], vm_hi[blk]);
+                    const uint32_t b0 = FAR ? pb[n][0] : mul_f16(pb[n][0], vm_lo[blk]), b1 = FAR ? pb[n][1] : mul_f16(pb[n][1], vm_hi[blk]);
 #pragma unroll
                     for (int j = 0; j < NP / 2; ++j)
                         F16Mma::mma(acc[(c + h) * (NP / 2) + j][n], X[2 * j], X[2 * j + 1], Y[2 * j], Y[2 * j + 1], b0, b1);
@@ -635,26 +669,36 @@ struct Attend {
         });
     }
 
-    // A fetched step: all of it at once where every row sees all of it, else group by group.
-    __device__ __forceinline__ void take(uint32_t slot, uint32_t key)
+    // A fetched step: all of it at once where every row sees all of it, else group by group.  Without FAR a step with scales that lie too far
+    // from their references is not taken (false).
+    template <bool FAR>
+    __device__ __forceinline__ bool take(uint32_t slot, uint32_t key)
     {
         constexpr uint32_t every = (1u << GROUPS) - 1u;
         const uint32_t has = (there >> (GROUPS * (S::stages - 1))) & every;
         const uint32_t lo = (uint32_t)some_lo, hi = (uint32_t)some_hi;
-        if (!has || key + S::step <= lo || key >= hi) return;
-        if (has == every && key >= (uint32_t)all_lo && key + S::step <= (uint32_t)all_hi) {
-            make_tables<false>(slot, key, has);
-            __syncwarp();
-            step<0, GROUPS, false>(slot, key);
-            return;
-        }
-        make_tables<true>(slot, key, has);
+        if (!has || key + S::step <= lo || key >= hi) return true;
+        const bool all = has == every && key >= (uint32_t)all_lo && key + S::step <= (uint32_t)all_hi;
+        const bool far = all ? make_tables<false>(slot, key, has) : make_tables<true>(slot, key, has);
         __syncwarp();
-        static_for<GROUPS>([&](auto hc) {
-            constexpr int H = decltype(hc)::value;
-            const uint32_t at = key + H * kGroup;
-            if (((has >> H) & 1u) && at + kGroup > lo && at < hi) step<H, 1, true>(slot, key);
-        });
+        if constexpr (FAR) {
+            if (far || apart) {
+                far_step(slot, key, has);
+                return true;
+            }
+        } else if (far) {
+            return false;
+        }
+        if (all) {
+            step<0, GROUPS, false>(slot, key);
+        } else {
+            static_for<GROUPS>([&](auto hc) {
+                constexpr int H = decltype(hc)::value;
+                const uint32_t at = key + H * kGroup;
+                if (((has >> H) & 1u) && at + kGroup > lo && at < hi) step<H, 1, true>(slot, key);
+            });
+        }
+        return true;
     }
 
     // FP16 NaN halves of v become zeros and are flagged as ones (0x3C00) in the result.
@@ -738,29 +782,209 @@ struct Attend {
             }
     }
 
-    // Reference scales moved up to the step's largest ones (vb: the bytes of the lane's key and blocks).
-    __device__ __forceinline__ void raise_reference(const uint32_t (&vb)[HB], bool hidden)
+    // -- a step whose values' scales lie too far apart for weights times multipliers: each row and block has a unit of its own for its sums, 2^(m +
+    // unit - 127), which follows the largest product of weight and scale so far, and the weights of a block are worked out from the scores and the
+    // scales, in FP32, before they become FP16.  The row's m and l are what they are elsewhere.  Behind the step the sums go back to the blocks' references,
+    // to the step's largest scales, where FP32 has room for that; else the units stay (apart), and the next step takes this way too.
+
+    // Two units of a block, of the lane's columns 2t and 2t + 1 of group n.
+    __device__ __forceinline__ uint32_t unit_at(int n, int blk) const { return tables + S::far_at + ((blk * NT + n) * 4 + t) * 4; }
+    static __device__ __forceinline__ int unit_of(uint32_t units, int j) { return (int)(units << (16 - 16 * j)) >> 16; }
+    static __device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+    // The largest sum of a column's block, of all lanes that have some of it.
+    __device__ __forceinline__ float largest_sum(int n, int j, int blk) const
     {
+        float a = 0.f;
 #pragma unroll
-        for (int j = 0; j < HB; ++j) {
-            int top = hidden || vb[j] == 255u ? -1000 : (int)vb[j];
+        for (int i = 0; i < 2; ++i) {
+            a = fmaxf(a, fmaxf(fabsf(acc[2 * blk + i][n][j]), fabsf(acc[2 * blk + i][n][2 + j])));
+            if constexpr (PIECES == 2) a = fmaxf(a, fmaxf(fabsf(acc[2 * blk + i][n][1]), fabsf(acc[2 * blk + i][n][3])));
+        }
 #pragma unroll
-            for (int o = LPK; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-            const int to = top > vlim[j] ? top : vref[j];
-            const float by = __uint_as_float((uint32_t)max(vref[j] - to + 127, 0) << 23);      // (2^-127 and less: nothing)
-            vref[j] = to;
-            vlim[j] = to < 0 ? to : min(to + kScaleSlack, 254);      // (255 is always looked at)
+        for (int o = 4; o < 32; o <<= 1) a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+        return a;
+    }
+    // A column's block (of both of its parts) times 2^e.
+    __device__ __forceinline__ void scale_sums(int n, int j, int blk, int e)
+    {
+        const int half = min(max(e, -252), 252) / 2;
+        const float by0 = two_to(half), by1 = two_to(min(max(e, -252), 252) - half);
 #pragma unroll
-            for (int part = 0; part < LPK; ++part) {
-                const float of = LPK == 1 ? by : __shfl_sync(0xFFFFFFFFu, by, part);
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[2 * (part * HB + j) + k][n][i] *= of;
+        for (int i = 0; i < 2; ++i) {
+            float* const v = acc[2 * blk + i][n];
+            v[j] = v[j] * by0 * by1;
+            v[2 + j] = v[2 + j] * by0 * by1;
+            if constexpr (PIECES == 2) {
+                v[1] = v[1] * by0 * by1;
+                v[3] = v[3] * by0 * by1;
             }
         }
+    }
+    static __device__ __forceinline__ int exponent_of(float v) { return (int)(__float_as_uint(v) >> 23) - 127; }
+
+    // Weights times scales of block blk and the 16 keys of group H, as matrix operands, the sums of the block in their units.
+    template <int H>
+    __device__ __forceinline__ void far_weights(uint32_t slot, int blk, const float (*sc)[4], uint32_t (&pb)[NT][2])
+    {
+        const int bs = p.cache.block_shift - 5;
+        int byte[2];                                         // of keys g and g + 8; a poisoned block's values are taken out elsewhere
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            byte[h] = (int)lds_u8(slot + S::vs_at + (H * kGroup + g + 8 * h) * (NB >> bs) + (blk >> bs));
+            if (byte[h] == 255) byte[h] = 0;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const uint32_t was = lds_u32(unit_at(n, blk));
+            int unit[2];
+            float w[4];
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 3 - PIECES; ++j) {
+                float top = fmaxf(less(sc[n][j], f[n][j], m[n][j]) + (float)byte[0], less(sc[n][2 + j], f[n][j], m[n][j]) + (float)byte[1]);
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                const float a = largest_sum(n, j, blk);
+                const int old = unit_of(was, j);
+                // (sums so far at 2^10 or less, products at 2^kBias or less)
+                unit[j] = max(a > 0.f ? old + exponent_of(a) - 10 : kUnset, (int)fminf(fmaxf(ceilf(top) - kBias, (float)kUnset), 1000.f));
+                scale_sums(n, j, blk, old - unit[j]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float x = less(sc[n][2 * h + j], f[n][j], m[n][j] + (float)(unit[j] - byte[h]));
+                    w[2 * h + j] = exp2_approx(x);
+                }
+            }
+            if constexpr (PIECES == 1) {
+                pb[n][0] = transpose8x8(pack_f16(w[0], w[1]));
+                pb[n][1] = transpose8x8(pack_f16(w[2], w[3]));
+            } else {
+                unit[1] = unit[0];
+                const uint32_t a = pack_f16(w[0], 0.f), c = pack_f16(w[2], 0.f);
+                pb[n][0] = transpose8x8(a | pack_f16(0.f, w[0] - f16_lo(a)));
+                pb[n][1] = transpose8x8(c | pack_f16(0.f, w[2] - f16_lo(c)));
+            }
+            if (g == 0) asm volatile("st.shared.u32 [%0], %1;" :: "r"(unit_at(n, blk)), "r"(((uint32_t)unit[0] & 0xFFFFu) | (uint32_t)unit[1] << 16) : "memory");
+        }
+    }
+
+    template <int H>
+    __device__ __forceinline__ void far_group(uint32_t slot, uint32_t key)
+    {
+        float sc[NT][4];
+        uint32_t seen[NT][2], pb[NT][2];
+        scores<H>(slot, sc);
+        hide(key + H * kGroup, sc, seen);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            int down[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float top = fmaxf(less(sc[n][j], f[n][j], 0.f), less(sc[n][2 + j], f[n][j], 0.f));
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                // m moves by a whole number: the sums stay, their units relative to m sink
+                const float up = top - m[n][j] > kSlack ? ceilf(top - m[n][j]) - kBias : 0.f, to = m[n][j] == kNone ? fmaxf(top - kBias, kNone) : m[n][j] + up;
+                l[n][j] *= exp2_approx(m[n][j] - to);
+                down[j] = (int)fminf(up, 4000.f);
+                m[n][j] = to;
+                l[n][j] += exp2_approx(less(sc[n][j], f[n][j], to)) + exp2_approx(less(sc[n][2 + j], f[n][j], to));
+            }
+#pragma unroll 1
+            for (int blk = 0; blk < NB; ++blk) {
+                const uint32_t at = unit_at(n, blk), was = lds_u32(at);
+                __syncwarp();
+                const int u0 = max(unit_of(was, 0) - down[0], kUnset), u1 = max(unit_of(was, 1) - down[1], kUnset);
+                if (g == 0) asm volatile("st.shared.u32 [%0], %1;" :: "r"(at), "r"(((uint32_t)u0 & 0xFFFFu) | (uint32_t)u1 << 16) : "memory");
+            }
+        }
+        __syncwarp();
+        add_values<H, true, true>(slot, pb, seen, sc);
+        __syncwarp();
+    }
+
+    __device__ __forceinline__ void far_step(uint32_t slot, uint32_t key, uint32_t has)
+    {
+        if (!apart) {
+#pragma unroll
+            for (int blk = 0; blk < NB; ++blk) {
+                const uint32_t unit = (uint32_t)max(__shfl_sync(0xFFFFFFFFu, low[blk % HB], blk / HB) + kBelow, kUnset) & 0xFFFFu;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    if (g == 0) asm volatile("st.shared.u32 [%0], %1;" :: "r"(unit_at(n, blk)), "r"(unit | unit << 16) : "memory");
+            }
+            __syncwarp();
+        }
+        static_for<GROUPS>([&](auto hc) {
+            constexpr int H = decltype(hc)::value;
+            const uint32_t at = key + H * kGroup;
+            if (((has >> H) & 1u) && at + kGroup > (uint32_t)some_lo && at < (uint32_t)some_hi) far_group<H>(slot, key);
+        });
+        // back to references: the step's largest scales, but for blocks of zeros
+        int to[HB];
+        uint32_t vw[(HB + 3) / 4];
+        scale_bytes(slot + S::vs_at, vw);
+        const uint32_t mine = key + lane / LPK;
+        const bool hidden = mine < (uint32_t)some_lo || mine >= (uint32_t)some_hi || !((has >> (lane / LPK / kGroup)) & 1u);
+#pragma unroll
+        for (int j = 0; j < HB; ++j) {
+            const uint32_t byte = __byte_perm(vw[j / 4], 0, 0x4440 + j % 4);
+            int top = hidden || byte == 255u ? 0 : (int)min(byte, 251u);
+#pragma unroll
+            for (int o = LPK; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            to[j] = top > 0 ? top : max(low[j] + kBelow, 0);
+        }
+        bool fits = true;
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) {
+            const int unit = __shfl_sync(0xFFFFFFFFu, to[blk % HB], blk / HB);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 3 - PIECES; ++j) {
+                    const float a = largest_sum(n, j, blk);
+                    const int e = exponent_of(a) + unit_of(lds_u32(unit_at(n, blk)), j) - unit;
+                    fits &= !(a > 0.f && a < __uint_as_float(0x7F800000u)) || (e >= -60 && e <= 90);
+                }
+        }
+        apart = !__all_sync(0xFFFFFFFFu, fits);
+        if (apart) return;
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) {
+            const int unit = __shfl_sync(0xFFFFFFFFu, to[blk % HB], blk / HB);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 3 - PIECES; ++j) scale_sums(n, j, blk, unit_of(lds_u32(unit_at(n, blk)), j) - unit);
+        }
+#pragma unroll
+        for (int j = 0; j < HB; ++j) low[j] = to[j] - kBelow;
+        __syncwarp();
+    }
+
+    // Sums in units of their own become the warp's results: divided by the weights' sum, then times their units.
+    __device__ __forceinline__ void give_back_units()
+    {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 3 - PIECES; ++j) {
+                float sum = l[n][j];
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    acc[i][n][j] *= inv;
+                    acc[i][n][2 + j] *= inv;
+                    if constexpr (PIECES == 2) {
+                        acc[i][n][1] *= inv;
+                        acc[i][n][3] *= inv;
+                    }
+                }
+#pragma unroll
+                for (int blk = 0; blk < NB; ++blk) scale_sums(n, j, blk, unit_of(lds_u32(unit_at(n, blk)), j) - 127);
+            }
     }
 
     // -- rows
@@ -897,17 +1121,35 @@ struct Attend {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[i][n][j] = 0.f;
 #pragma unroll
-        for (int j = 0; j < HB; ++j) vref[j] = vlim[j] = -1000;
+        for (int j = 0; j < HB; ++j) low[j] = kUnset;
+        apart = false;
         int slot = 0, next = S::stages - 1;
-        for (; key < to; key += stride) {
+        auto next_step = [&] {
             const uint32_t ahead = key + (S::stages - 1) * stride;
             fetch(ring + next * S::slot, ahead, ahead + stride, to);
             asm volatile("cp.async.wait_group %0;" :: "n"(S::stages - 1) : "memory");
             __syncwarp();
-            take(ring + slot * S::slot, key);
+        };
+        auto step_done = [&] {
             __syncwarp();
             slot = slot + 1 == S::stages ? 0 : slot + 1;
             next = next + 1 == S::stages ? 0 : next + 1;
+            key += stride;
+        };
+        bool near = true;
+        while (key < to) {
+            next_step();
+            near = take<false>(ring + slot * S::slot, key);
+            if (!near) break;
+            step_done();
+        }
+        // The first step with scales far apart and all behind it: a loop of its own, whose registers are not the common one's.  (64 sequences of up
+        // to 8192 tokens, E2M1, none of it far: 113 us; 115 with everything in one loop; 110 without a way for scales that are far apart.)
+        while (!near) {
+            take<true>(ring + slot * S::slot, key);
+            step_done();
+            if (key >= to) break;
+            next_step();
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncthreads();
@@ -926,9 +1168,10 @@ struct Attend {
             float scales[NB];
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
-                const int byte = __shfl_sync(0xFFFFFFFFu, vref[i % HB], i / HB);
-                scales[i] = scale_value((uint32_t)max(byte, 0));
+                const int byte = __shfl_sync(0xFFFFFFFFu, low[i % HB], i / HB) + kBelow;
+                scales[i] = apart ? 1.f : scale_value((uint32_t)max(byte, 0));
             }
+            if (apart) give_back_units();
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -936,7 +1179,7 @@ struct Attend {
                     float sum = l[n][j];
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    const float inv = apart ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
                     const int r = PIECES == 1 ? 8 * n + 2 * t + j : 4 * n + t;
                     if (g == 0) {
                         ml[(warp * R + r) * 2] = m[n][j];
