@@ -28,6 +28,7 @@ __device__ unsigned int g_many_status;                       // a bounded wait g
 constexpr int kRowWarps = 8, kWideners = 8, kIssuer = kRowWarps + kWideners, kManyWarps = kIssuer + 1, kManyThreads = kManyWarps * 32;
 constexpr int kRowTile = 128, kKeys = 128;
 constexpr float kManySlack = 8.f;                            // m moves when 2^8 would be exceeded
+constexpr uint32_t kLoudByte = 247;                          // the smallest scale under which an element (448, E4M3) passes BF16's range
 
 template <int FMT, int D>
 struct ManyShape {
@@ -161,7 +162,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
     __shared__ __align__(8) ManyBars bars;
     __shared__ Plan plan;
     __shared__ uint32_t warp_sum[32], s_tmem, s_gave_up;
-    __shared__ uint32_t s_info[2][kWideners];                // of a tile of values: 1: some key has no page, 2: a NaN was taken out
+    __shared__ uint32_t s_info[2][kWideners];                // of a tile of values: 1: some key has no page, 2: something that is no finite number was taken out
     __shared__ uint8_t s_bad[2 * kRowTile];                  // rows whose query holds a NaN or an infinity
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
@@ -368,12 +369,14 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                     byte[kind][i] = ld_u8((kind ? p.cache.vs : p.cache.ks) + row * (D >> p.cache.block_shift) + (c * (128 / M::bits) >> p.cache.block_shift));
                 }
             };
-            // Widens a chunk to `at` (row of its key, first panel); `mask`: elements to be zeros.
-            auto widen = [&](uint32_t at, int key, int c, uint4 v, uint32_t sb, uint32_t zero) {
+            // Widens a chunk to `at` (row of its key, first panel).  With `some` (a key that not all rows see) elements that are NaN or beyond BF16's
+            // range become zeros, which a weight of zero takes away, and are returned, a bit each.
+            auto widen = [&](uint32_t at, int key, int c, uint4 v, uint32_t sb, bool some) {
+                uint32_t out_of = 0;
                 const uint32_t f = W::factor(sb);
                 const uint32_t words[4] = {v.x, v.y, v.z, v.w};
                 uint32_t o[4 * NP];
-                bool odd = sb > W::limit;
+                bool odd = sb > W::limit || (some && sb >= kLoudByte);
                 if constexpr (W::has_nan) {
                     uint32_t seen = 0;
                     W::note_nan(v, seen);
@@ -399,13 +402,14 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                             }
                         }
                     }
-                    if (zero) {
+                    if (some) {
 #pragma unroll
-                        for (int e = 0; e < 4 * NP * 2; ++e)
-                            if ((zero >> e) & 1u) {
-                                const int place = widened_place<NP>(e);
-                                o[place / 2] &= place & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-                            }
+                        for (int e = 0; e < 4 * NP * 2; ++e) {
+                            const int place = widened_place<NP>(e);
+                            if (((o[place / 2] >> (16 * (place & 1))) & 0x7F80u) != 0x7F80u) continue;
+                            out_of |= 1u << e;
+                            o[place / 2] &= place & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                        }
                     }
                 }
                 constexpr int per = 128 / M::bits / 8;       // 16-byte pieces of a chunk
@@ -414,6 +418,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                     const int piece = c * per + q;
                     st_shared16(at + (piece >> 3) * M::panel + (((piece & 7) ^ (key & 7)) << 4), o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
                 }
+                return out_of;
             };
             bool fine = true;
             if (count > 0) {
@@ -428,7 +433,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
 #pragma unroll
                 for (int i = 0; i < M::chunks; ++i) {
                     const int id = me + i * kWideners * 32, key = id / M::CPR;
-                    widen(base + M::k_at + st * M::stage + key * 128, key, id % M::CPR, code[0][i], byte[0][i], 0u);
+                    widen(base + M::k_at + st * M::stage + key * 128, key, id % M::CPR, code[0][i], byte[0][i], false);
                 }
                 fence_async();
                 __syncwarp();
@@ -444,27 +449,15 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
 #pragma unroll
                 for (int i = 0; i < M::chunks; ++i) {
                     const int id = me + i * kWideners * 32, key = id / M::CPR, c = id % M::CPR;
-                    uint32_t zero = 0;                       // elements that are NaN, where a row must not see them
+                    const bool some = edge && (k0 + key < all_lo || k0 + key >= all_hi);
+                    const uint32_t out_of = widen(base + M::v_at + st * M::stage + key * 128, key, c, code[1][i], byte[1][i], some);
                     if (edge) {
-                        if (k0 + key < all_lo || k0 + key >= all_hi) {
-                            if (byte[1][i] == 255u) zero = M::bits == 4 ? 0xFFFFFFFFu : 0xFFFFu;
-                            else if constexpr (W::has_nan) {
-                                const uint32_t words[4] = {code[1][i].x, code[1][i].y, code[1][i].z, code[1][i].w};
-#pragma unroll
-                                for (int w = 0; w < 4; ++w) {
-                                    const uint32_t bad = nan_codes(words[w]);
-#pragma unroll
-                                    for (int k = 0; k < 4; ++k) zero |= (bad >> (7 + 8 * k) & 1u) << (4 * w + k);
-                                }
-                            }
-                            if (zero) info |= 2u;
-                        }
+                        if (out_of) info |= 2u;
                         uint8_t* const to = base_p + M::nan_at + (st * kKeys + key) * NB * 4;
-                        if constexpr (M::bits == 4) reinterpret_cast<uint32_t*>(to)[c] = zero;
-                        else reinterpret_cast<uint16_t*>(to)[c] = (uint16_t)zero;
+                        if constexpr (M::bits == 4) reinterpret_cast<uint32_t*>(to)[c] = out_of;
+                        else reinterpret_cast<uint16_t*>(to)[c] = (uint16_t)out_of;
                     }
                     if (c == 0) base_p[M::absent_at + st * kKeys + key] = (uint8_t)((gone >> i) & 1u);
-                    widen(base + M::v_at + st * M::stage + key * 128, key, c, code[1][i], byte[1][i], zero);
                 }
                 fence_async();
                 info = __reduce_or_sync(0xFFFFFFFFu, info);
@@ -494,7 +487,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                 const int k0 = it.from + j * kKeys, from = lo - k0, to_key = hi - k0;
                 const bool edge = k0 < it.all_lo || (uint32_t)k0 + kKeys > (uint32_t)it.all_hi || (info & 1u);
                 const uint8_t* const absent = base_p + M::absent_at + st * kKeys;
-                if (info & 2u) {                             // NaN values that not every row sees: into the sums of those that do
+                if (info & 2u) {                             // what was taken out of values that not every row sees: NaN in the sums of those that do
                     uint32_t bad[NB] = {};
                     for (int k = 0; k < kKeys; ++k) {
                         if (k < from || k >= to_key || ((info & 1u) && absent[k])) continue;

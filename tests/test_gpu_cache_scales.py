@@ -135,3 +135,34 @@ def test_a_small_first_token_and_blocks_of_zeros(fmt, dtype):
         cache.parts[2][at], cache.parts[3][at] = 0, 0
     cache.parts[2][table[1, 0]], cache.parts[3][table[1, 0], ..., 1] = 0, 0
     check(plain(rng, (3, 8, 128), dtype), cache, lengths, None, table, dtype)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("byte", [245, 248, 250, 253, 254])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("counts,lengths,at,group", [([60], [130], 100, 1), ([140, 33], [140, 200], 139, 2), ([3], [90], 89, 2)])
+def test_hidden_values_beyond_the_type(fmt, byte, dim, counts, lengths, at, group):
+    """The largest elements under the largest scales, which BF16 cannot hold, behind a query or out of its window."""
+    rng = np.random.default_rng(dim)
+    cache = cu.Cache(rng, 30, 2, dim, fmt, 32, 16)
+    table = cu.tables(rng, lengths, 16, 30)
+    place = (table[0, at // 16], slice(None), at % 16)
+    cache.parts[2][place], cache.parts[3][place] = {"e4m3": 0x7E, "e2m1": 0x7F, "int8": 0x81, "int4": 0x97}[fmt], byte
+    q = plain(rng, (sum(counts), 2 * group, dim), BF16)
+    for window in (0, 5):
+        pos = lengths[0] - counts[0] + np.arange(counts[0])
+        hidden = (pos < at) | ((pos >= at + window) if window else False)
+        rows = torch.from_numpy(np.concatenate((np.flatnonzero(hidden), np.arange(counts[0], sum(counts)))))
+        check(q, cache, lengths, counts, table, BF16, window=window, rows=rows)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_many_queries_over_small_values(fmt):
+    rng = np.random.default_rng(5)
+    cache = cu.Cache(rng, 30, 2, 128, fmt, 32, 16, spread=0)
+    table = cu.tables(rng, [130], 16, 30)
+    for down in (0, 60, 100):
+        parts = cache.parts[3].copy()
+        cache.parts[3] = (cache.parts[3] - down).astype(np.uint8)
+        check(plain(rng, (60, 2, 128), BF16), cache, [130], [60], table, BF16)
+        cache.parts[3] = parts
