@@ -265,6 +265,7 @@ struct Attend {
     static constexpr int kUnset = -1000;
     int low[NB * S::step / 32];
     bool apart;                                             // the sums have units of their own, by row and block, in shared memory
+    bool steep;                                             // some row's maximum is beyond kSteep
     uint32_t q[S::q_in_registers ? NT * MT : 1][2];
     // the item
     int b, head, row0, rows;                                // rows: how many of the item are there
@@ -670,7 +671,7 @@ struct Attend {
     }
 
     // A fetched step: all of it at once where every row sees all of it, else group by group.  Without FAR a step with scales that lie too far
-    // from their references is not taken (false).
+    // from their references, or with scores beyond kSteep in front of it, is not taken (false).
     template <bool FAR>
     __device__ __forceinline__ bool take(uint32_t slot, uint32_t key)
     {
@@ -679,10 +680,10 @@ struct Attend {
         const uint32_t lo = (uint32_t)some_lo, hi = (uint32_t)some_hi;
         if (!has || key + S::step <= lo || key >= hi) return true;
         const bool all = has == every && key >= (uint32_t)all_lo && key + S::step <= (uint32_t)all_hi;
-        const bool far = all ? make_tables<false>(slot, key, has) : make_tables<true>(slot, key, has);
+        const bool far = (all ? make_tables<false>(slot, key, has) : make_tables<true>(slot, key, has)) || steep;
         __syncwarp();
         if constexpr (FAR) {
-            if (far || apart) {
+            if (far || apart) {                              // (steep is among what makes `far`)
                 far_step(slot, key, has);
                 return true;
             }
@@ -752,11 +753,14 @@ struct Attend {
 
     // A score less m; hidden ones are -inf, which a factor that is NaN must not make NaN of.
     __device__ __forceinline__ float less(float sc, float f, float m) const { return sc == __uint_as_float(0xFF800000u) ? sc : fmaf(sc, f, -m); }
+    // The same of the rounded score, for maxima of every size.
+    __device__ __forceinline__ float rounded_less(float sc, float f, float m) const { return sc == __uint_as_float(0xFF800000u) ? sc : __fmul_rn(sc, f) - m; }
 
     // The columns' maxima moved up to the step's scores.
     template <int N>
     __device__ __forceinline__ void raise_maximum(const float (&sc)[N][NT][4], float (&x)[N][NT][4])
     {
+        bool high = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -766,8 +770,9 @@ struct Attend {
                 for (int h = 0; h < N; ++h) top = fmaxf(top, fmaxf(less(sc[h][n][j], f[n][j], 0.f), less(sc[h][n][2 + j], f[n][j], 0.f)));
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-                const float to = fmaxf(m[n][j], top - kBias), by = exp2_approx(m[n][j] - to);
+                const float lower = top - kBias, to = fmaxf(m[n][j], top - lower > kSlack ? top : lower), by = exp2_approx(m[n][j] - to);
                 m[n][j] = to;
+                high |= fabsf(to) > kSteep && to != kNone;
                 l[n][j] *= by;
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
@@ -776,10 +781,11 @@ struct Attend {
                 }
 #pragma unroll
                 for (int h = 0; h < N; ++h) {
-                    x[h][n][j] = less(sc[h][n][j], f[n][j], to);
-                    x[h][n][2 + j] = less(sc[h][n][2 + j], f[n][j], to);
+                    x[h][n][j] = rounded_less(sc[h][n][j], f[n][j], to);
+                    x[h][n][2 + j] = rounded_less(sc[h][n][2 + j], f[n][j], to);
                 }
             }
+        steep = __any_sync(0xFFFFFFFFu, high);
     }
 
     // -- a step whose values' scales lie too far apart for weights times multipliers: each row and block has a unit of its own for its sums, 2^(m +
@@ -841,7 +847,8 @@ struct Attend {
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < 3 - PIECES; ++j) {
-                float top = fmaxf(less(sc[n][j], f[n][j], m[n][j]) + (float)byte[0], less(sc[n][2 + j], f[n][j], m[n][j]) + (float)byte[1]);
+                float x[2] = {rounded_less(sc[n][j], f[n][j], m[n][j]), rounded_less(sc[n][2 + j], f[n][j], m[n][j])};
+                float top = fmaxf(x[0] + (float)byte[0], x[1] + (float)byte[1]);
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
                 const float a = largest_sum(n, j, blk);
@@ -850,10 +857,7 @@ struct Attend {
                 unit[j] = max(a > 0.f ? old + exponent_of(a) - 10 : kUnset, (int)fminf(fmaxf(ceilf(top) - kBias, (float)kUnset), 1000.f));
                 scale_sums(n, j, blk, old - unit[j]);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float x = less(sc[n][2 * h + j], f[n][j], m[n][j] + (float)(unit[j] - byte[h]));
-                    w[2 * h + j] = exp2_approx(x);
-                }
+                for (int h = 0; h < 2; ++h) w[2 * h + j] = exp2_approx(x[h] + (float)(byte[h] - unit[j]));
             }
             if constexpr (PIECES == 1) {
                 pb[n][0] = transpose8x8(pack_f16(w[0], w[1]));
@@ -875,6 +879,7 @@ struct Attend {
         uint32_t seen[NT][2], pb[NT][2];
         scores<H>(slot, sc);
         hide(key + H * kGroup, sc, seen);
+        bool high = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             int down[2];
@@ -884,11 +889,12 @@ struct Attend {
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
                 // m moves by a whole number: the sums stay, their units relative to m sink
-                const float up = top - m[n][j] > kSlack ? ceilf(top - m[n][j]) - kBias : 0.f, to = m[n][j] == kNone ? fmaxf(top - kBias, kNone) : m[n][j] + up;
+                const float up = top - m[n][j] > kSlack ? ceilf(top - m[n][j]) - kBias : 0.f, to = m[n][j] == kNone ? fmaxf(top - kBias, kNone) : fminf(m[n][j] + up, fmaxf(top, m[n][j]));
                 l[n][j] *= exp2_approx(m[n][j] - to);
-                down[j] = (int)fminf(up, 4000.f);
+                down[j] = (int)fminf(rintf(to - m[n][j]), 4000.f);
                 m[n][j] = to;
-                l[n][j] += exp2_approx(less(sc[n][j], f[n][j], to)) + exp2_approx(less(sc[n][2 + j], f[n][j], to));
+                high |= fabsf(to) > kSteep && to != kNone;
+                l[n][j] += exp2_approx(rounded_less(sc[n][j], f[n][j], to)) + exp2_approx(rounded_less(sc[n][2 + j], f[n][j], to));
             }
 #pragma unroll 1
             for (int blk = 0; blk < NB; ++blk) {
@@ -898,6 +904,7 @@ struct Attend {
                 if (g == 0) asm volatile("st.shared.u32 [%0], %1;" :: "r"(at), "r"(((uint32_t)u0 & 0xFFFFu) | (uint32_t)u1 << 16) : "memory");
             }
         }
+        steep = __any_sync(0xFFFFFFFFu, high);
         __syncwarp();
         add_values<H, true, true>(slot, pb, seen, sc);
         __syncwarp();
@@ -1122,7 +1129,7 @@ struct Attend {
                 for (int j = 0; j < 4; ++j) acc[i][n][j] = 0.f;
 #pragma unroll
         for (int j = 0; j < HB; ++j) low[j] = kUnset;
-        apart = false;
+        apart = steep = false;
         int slot = 0, next = S::stages - 1;
         auto next_step = [&] {
             const uint32_t ahead = key + (S::stages - 1) * stride;

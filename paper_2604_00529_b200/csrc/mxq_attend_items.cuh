@@ -7,7 +7,9 @@
 namespace mxq {
 namespace {
 
-constexpr float kNone = -1e30f;                             // m of a row that has seen nothing (finite: -inf - kNone is no NaN)
+constexpr float kNone = -3.402823466e38f;                   // m of a row that has seen nothing: no score is less (finite: -inf - kNone is no NaN)
+// Beyond it a maximum differs from the exact product that it was rounded from by one and more: scores are rounded before it is taken from them.
+constexpr float kSteep = 16777216.f;
 
 // ---- items ----------------------------------------------------------------------------------------------------
 

@@ -476,7 +476,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
             const int lo = mine ? token_lo(p, s, token) : 0, hi = mine ? token_hi(p, s, token) : 0;
             const float f = s_bad[row] ? __uint_as_float(0x7FC00000u) : p.scale;
             float m = kNone, l = 0.f;
-            bool fine = true;
+            bool fine = true, steep = false;                 // steep: some row's m is beyond kSteep
             for (int j = 0; fine && j < count; ++j) {
                 const uint32_t st = (n0 + j) & 1;
                 if (!(fine = warp_agrees(wait(bars.v_full[st], ((n0 + j) >> 1) & 1) && wait(bars.s_full[i], (nth + j) & 1)))) break;
@@ -508,11 +508,12 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                         tmem_st_wait();
                     }
                 }
-                // 32 keys at a time: scores less m, P over scores that are read already
-                auto weigh = [&](auto edge_t) {
-                    constexpr bool EDGE = decltype(edge_t)::value;
+                // 32 keys at a time from key c on: scores less m, P over scores that are read already.  Returns where it stopped: in front of keys that
+                // moved some row's m beyond kSteep (STEEP: none).
+                auto weigh = [&](auto edge_t, auto steep_t, int c) {
+                    constexpr bool EDGE = decltype(edge_t)::value, STEEP = decltype(steep_t)::value;
 #pragma unroll 1
-                    for (int c = 0; c < kKeys; c += 32) {
+                    for (; c < kKeys; c += 32) {
                         float2 x[16];
                         auto scores = [&] {                  // less m (or 0, before any key was seen); hidden ones -inf
                             uint32_t v[32];
@@ -521,7 +522,10 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                             const float less = m == kNone ? 0.f : -m;
 #pragma unroll
                             for (int k = 0; k < 16; ++k) {
-                                x[k] = fma2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(f, f), make_float2(less, less));
+                                if constexpr (STEEP)
+                                    x[k] = make_float2(__fmul_rn(__uint_as_float(v[2 * k]), f) + less, __fmul_rn(__uint_as_float(v[2 * k + 1]), f) + less);
+                                else
+                                    x[k] = fma2(make_float2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), make_float2(f, f), make_float2(less, less));
                                 if constexpr (EDGE) {
                                     const int at = c + 2 * k;
                                     if (at < from || at >= to_key || ((info & 1u) && absent[at])) x[k].x = __uint_as_float(0xFF800000u);
@@ -533,7 +537,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                         float top = x[0].x;
 #pragma unroll
                         for (int k = 0; k < 16; ++k) top = max3(top, x[k].x, x[k].y);
-                        if (__any_sync(0xFFFFFFFFu, top > (m == kNone ? -3e38f : kManySlack))) {
+                        if (__any_sync(0xFFFFFFFFu, m == kNone ? top > kNone : top > kManySlack)) {
                             // m moved, by a whole number, so that nothing is rounded again: the sums so far and P so far in this tile
                             const float up = fmaxf(m, ceilf(top + (m == kNone ? 0.f : m))), by = exp2_approx(m - up);
                             m = up;
@@ -550,6 +554,7 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                                 tmem_st16(sc + done, w);
                             }
                             tmem_st_wait();
+                            if (!STEEP && __any_sync(0xFFFFFFFFu, fabsf(m) > kSteep && m != kNone)) return c;
                             scores();
                         }
                         uint32_t o[16];
@@ -563,9 +568,13 @@ attend_many_kernel(const __grid_constant__ AttendArgs p)
                         l += sum.x + sum.y;
                         tmem_st16(sc + c / 2, o);
                     }
+                    return (int)kKeys;
                 };
-                if (edge) weigh(std::true_type{});
-                else weigh(std::false_type{});
+                const int c = steep ? 0 : edge ? weigh(std::true_type{}, std::false_type{}, 0) : weigh(std::false_type{}, std::false_type{}, 0);
+                if (c < kKeys) {
+                    steep = true;
+                    weigh(std::true_type{}, std::true_type{}, c);
+                }
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();

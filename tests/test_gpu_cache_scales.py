@@ -166,3 +166,35 @@ def test_many_queries_over_small_values(fmt):
         cache.parts[3] = (cache.parts[3] - down).astype(np.uint8)
         check(plain(rng, (60, 2, 128), BF16), cache, [130], [60], table, BF16)
         cache.parts[3] = parts
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("counts,lengths", [(None, [70, 129, 1]), ([3, 5], [100, 37]), ([40, 150], [333, 150]), (None, [9000])])
+@pytest.mark.parametrize("scale", [2.0 ** 24, -2.0 ** 28, 2.0 ** 30, 2.0 ** 40, -2.0 ** 70, 1e30, -1e31, 3e35, -3e35])
+def test_scores_of_every_finite_size(fmt, dtype, counts, lengths, scale):
+    """Keys that are all alike weigh alike, however large their scores are; the logarithm of the sum is the score's."""
+    rng = np.random.default_rng(3)
+    cache = cu.Cache(rng, 150, 2, 64, fmt, 32, 64)
+    table = cu.tables(rng, lengths, 64, 150)
+    one = {"e4m3": (0x3A, 127), "e2m1": (0x33, 127), "int8": (0x5B, 121), "int4": (0x55, 125)}[fmt]       # 1.25, 1.5, 91 / 64, 5 / 4
+    cache.parts[0][:], cache.parts[1][:] = one
+    q = torch.empty(sum(counts or [1] * len(lengths)), 4, 64, device="cuda").uniform_(0.5, 1.0, generator=torch.Generator("cuda").manual_seed(1)).to(dtype)
+    starts = cu.starts_of([1] * len(lengths) if counts is None else counts)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    got = mxq.cache_attention(q, *cache.cuda(), ints(table), ints(lengths), fmt, starts=None if counts is None else ints(starts), scale=scale, lse=lse)
+    k64, v64 = cache.values()
+    s = scale * (pu.to64(q) @ k64[0, 0, 0])
+    assert np.isfinite(s.astype(np.float32)).all()
+    g = pu.to64(got)
+    assert np.isfinite(g).all()
+    # a score is off by 2^-17 of itself; weights that are alike are rounded alike
+    assert (np.abs(pu.to64(lse) - s) <= 2.0 ** -17 * np.abs(s) + 16).all()
+    for b, n in enumerate(starts[1:] - starts[:-1]):
+        V = cu.rows_of(v64, table[b], lengths[b], 64)[0]
+        for i in range(n):
+            seen = V[:lengths[b] - n + i + 1]
+            for j in range(4):
+                want, a = seen[:, j // 2].mean(0), np.abs(seen[:, j // 2]).mean(0)
+                # weights: 8, 11 or 22 bits, each the same; sums: as everywhere
+                assert (np.abs(g[starts[b] + i, j] - want) <= (2.0 ** -7 + (lengths[b] / 16 + 64) * 2.0 ** -19) * a + pu.half_step(dtype) * np.abs(want)).all()
