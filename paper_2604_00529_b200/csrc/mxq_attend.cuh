@@ -241,7 +241,8 @@ struct Shape {
     static constexpr int merge = 8 * NT * (D + 2) * 4;                // a warp's results, in the rings' place
     static constexpr int work = ring > merge ? ring : merge;
     static constexpr size_t total(int warps) { return (size_t)warps * (work + tables) + rows_bytes; }
-    static constexpr bool q_in_registers = NT * MT * 2 <= 32;
+    // (Heads of 256 leave no registers for their queries: 32 sequences of up to 4096 E4M3 tokens, 8 heads over one, 27.8 us with them there, 25.8 without.)
+    static constexpr bool q_in_registers = NT * MT * 2 <= 32 && D < 256;
     static_assert(stages >= 2 && (total(kWarps) + 1536) * ctas <= 227 * 1024, "shared memory");
 
     // Chunk c of row r lies at r * RB + (c ^ twist(r)) * 16: the eight rows that a matrix load reads at once are in different banks.
