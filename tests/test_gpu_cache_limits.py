@@ -110,3 +110,39 @@ def test_a_window_without_limit(dtype, group, counts, lengths):
     for window in (64, 1 << 30, (1 << 31) - 64, (1 << 31) - 1, 1 << 31, 1 << 40, (1 << 62) + 5):
         got = mxq.cache_attention(q, *cache.cuda(), ints(table), ints(lengths), "int8", starts=ints(cu.starts_of(counts)), window=window)
         assert torch.equal(got, want), window
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("batch,n,group,dim", [(300, 1, 2, 64), (1100, 1, 1, 128), (200, 2, 3, 256), (600, 3, 8, 64)])
+def test_more_sequences_than_threads(dtype, batch, n, group, dim):
+    """A CTA plans several sequences per thread; some of them are empty, some have no tokens that are new."""
+    rng = np.random.default_rng(batch)
+    lengths = [int(x) for x in rng.integers(0, 60, batch)]
+    counts = [n if n == 1 or b % 7 else 0 for b in range(batch)]
+    cache = cu.Cache(rng, sum(-(-x // 16) for x in lengths), 1, dim, "int8", 32, 16)
+    attend(rng, cache, lengths, None if n == 1 else counts, group, dtype)
+    attend(rng, cache, lengths, counts, group, dtype, window=20)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_pages_beyond_4_gb(dtype):
+    """Tokens in the last pages of a cache of 5.2 GB of codes each for keys and values: the bytes and results of a small cache."""
+    rng = np.random.default_rng(6)
+    pages, page, heads, dim = 80000, 64, 8, 128
+    large = mxq.make_cache(pages, heads, dim, "e4m3", page=page)
+    small = mxq.make_cache(12, heads, dim, "e4m3", page=page)
+    assert large[0].numel() > 1 << 32
+    near = np.array([[0, 5, 11], [3, 7, 2], [10, 1, -1]], np.int32)
+    far = np.where(near < 0, -1, np.where(near % 2, near * 3, pages - 1 - near)).astype(np.int32)
+    lengths, counts = [190, 129, 128], [190, 129, 128]
+    k, v = plain(rng, (sum(counts), heads, dim), dtype), plain(rng, (sum(counts), heads, dim), dtype)
+    got = []
+    for cache, table in ((small, near), (large, far)):
+        starts = ints(cu.starts_of(counts))
+        mxq.cache_write(k, v, *cache, ints(table), ints(lengths), "e4m3", starts=starts)
+        out = [*mxq.cache_read(*cache, ints(table), starts, sum(lengths), "e4m3", dtype=dtype)]
+        for n in (1, 2, 50):
+            q = k[:3 * n].repeat_interleave(2, 1)
+            out.append(mxq.cache_attention(q, *cache, ints(table), ints(lengths), "e4m3", starts=ints([0, n, 2 * n, 3 * n])))
+        got.append(out)
+    assert got[0][0].abs().max() > 1 and all(torch.equal(a, b) for a, b in zip(*got))
