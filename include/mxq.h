@@ -509,7 +509,7 @@ int mxq_cache_read(const mxq_cache *cache, const mxq_batch *batch, size_t total,
  * Sums and the softmax are held in FP32.  Queries enter exactly for BF16 (elements below 2^-31 of a row's largest excepted) and
  * with 22 bits for FP32; the softmax's weights enter the second product with 11 bits for BF16 and 22 for FP32, and a key's weight times
  * the scale of 32 dimensions is off by no more than 2^-20 (FP32: 2^-23) of the row's largest such product, however far the scales of
- * keys lie apart.  A weight below 2^-120 of a row's largest may count as zero.  BF16 calls of head_dim 64 or 128 with more than 16 rows of a cache head per
+ * keys lie apart.  A weight below 2^-120 of a row's largest may count as zero.  BF16 calls of head_dim 64 or 128 with more than 48 rows of a cache head per
  * sequence in the mean (tokens / batch * q_heads / heads) run on other tensor cores: weights enter with 8 bits, every value counts,
  * but is a BF16 number: one of 2^128 or more (scale bytes of 247 and above, which mxq_cache_write does not write) makes infinity or NaN of what sees it.
  * A NaN or an infinity in a query gives NaN.  Results do not depend on timing.  That kernel waits as those of mxq_matmul do

@@ -83,9 +83,14 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
 // ---- launches -------------------------------------------------------------------------------------------------
 
 // How a call is cut up: column groups of its kernel, rows of an item, CTAs and their warps, a tile's keys, bytes of workspace.
-// Columns of a mean sequence, above which its rows are many: 8 sequences of 48 rows over 8192 E2M1 tokens 121 us with four column groups and 90 in
-// tiles of 128 rows; 12 sequences of 16 rows over 4096 INT8 tokens 44 with two column groups, of 32 rows 73 in tiles.
-constexpr size_t kManyColumns = 16;
+// Rows of a cache head in a mean sequence, above which they are many: items of 256 of them in tiles instead of 16 in two column groups.  Both, us, 32 heads
+// over 8 of 128:
+//   rows                                     16        20        32        40        48        64        96
+//   12 sequences of 4096 INT8 tokens      49 / 93   67 / 93   70 / 93   92 / 95   93 / 95   114 / 95  165 / 97
+//   8 of 8192 E2M1                        48 / 95   71 / 95   73 / 93   97 / 96   99 / 96   123 / 95  172 / 98
+//   32 of 2048 E4M3                       55 / 128  86 / 129  90 / 128 117 / 130 119 / 131  153 / 131 216 / 133
+//   1 of 16384 INT8                       48 / 54   43 / 53   46 / 53   49 / 53   50 / 55   55 / 54   68 / 56
+constexpr size_t kManyColumns = 48;
 // Keys per CTA of a cluster, at most: one sequence of 1000 tokens 6.5 us in clusters and 11.8 in runs with the second kernel; 8 of 8000, which
 // would be 4000 keys per CTA, 25 in runs, whose lengths even out.
 constexpr size_t kClusterKeys = 2048;
@@ -105,8 +110,8 @@ Sizes sizes(const mxq_cache* c, const mxq_batch* b, int q_heads, int dtype, size
     // as many column groups as the rows of a mean sequence fill, as registers allow
     const size_t columns = (tokens + b->batch - 1) / b->batch * (size_t)group * (size_t)pieces;
     z.nt = 1;
-    while (z.nt < (dim == 256 ? 2 : 4) && columns > (size_t)8 * z.nt) z.nt *= 2;
-    // Many rows: tiles of 256 of them on the tensor cores that take whole tiles.
+    while (z.nt < (dim == 256 || pieces == 1 ? 2 : 4) && columns > (size_t)8 * z.nt) z.nt *= 2;
+    // Many rows: items of 256 of them on the tensor cores that take whole tiles.
     z.many = dtype == MXQ_BF16 && dim <= 128 && columns > kManyColumns;
     z.rows = z.many ? 256 : 8 * z.nt / pieces;
     const size_t items = (b->starts ? tokens * group / z.rows + b->batch : b->batch * ((size_t)(group + z.rows - 1) / z.rows)) * c->heads, keys = b->width * (size_t)c->page < (size_t)1 << 31 ? b->width * (size_t)c->page : (size_t)1 << 31;     // at most
