@@ -91,8 +91,10 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
 //   32 of 2048 E4M3                       55 / 128  86 / 129  90 / 128 117 / 130 119 / 131  153 / 131 216 / 133
 //   1 of 16384 INT8                       48 / 54   43 / 53   46 / 53   49 / 53   50 / 55   55 / 54   68 / 56
 constexpr size_t kManyColumns = 48;
-// Keys per CTA of a cluster, at most: one sequence of 1000 tokens 6.5 us in clusters and 11.8 in runs with the second kernel; 8 of 8000, which
-// would be 4000 keys per CTA, 25 in runs, whose lengths even out.
+// Keys per CTA of a cluster, at most.  Clusters and runs with the second kernel, us: one sequence of 1000 E2M1 tokens, 8 heads of 128, 7.3 and 10.8, of
+// 16000 15.7 and 20.0; 8 of 2000 11.8 and 19.7; 32 of 2048 to 4096 E4M3 tokens, one head of 256, 22.6 and 33.2.  Lengths are known on the device
+// alone, and a cluster has its sequence to itself: beyond this a long one among short ones would keep the call waiting (8 of 8000, all alike, would
+// still take 25 and 33).
 constexpr size_t kClusterKeys = 2048;
 
 struct Sizes {
