@@ -15,11 +15,11 @@
 //                   instead (far_step), whatever other rows see or what a key weighs
 // FP32 rows enter as two FP16 parts, neighbouring columns of the same step, and so do their P.
 //
-// Bound by HBM for 8-bit codes (64 sequences of 16384 to 32768 tokens, 32 heads over 8 of 128: 6.0 TB/s E4M3, 6.3 INT8), by instructions for 4-bit ones
-// (E2M1 4.5 TB/s, issue slots 63 %, ALU pipe 57 %): widening takes 4 instructions per 8 codes of K and 7 of V, which is transposed on the way, of
+// Bound by HBM for 8-bit codes (64 sequences of 16384 to 32768 tokens, 32 heads over 8 of 128: 6.1 TB/s E4M3, 5.9 INT8), by instructions for 4-bit ones
+// (E2M1 4.5 TB/s; issue slots 56 %, ALU pipe 55 %): widening takes 4 instructions per 8 codes of K and 7 of V, which is transposed on the way, of
 // some 320 per 16 keys of a warp.  Sequences of up to 8192 tokens, E2M1: 147 us as first written (16 keys at a time, every row of a copy asked for by
 // itself, scales worked out by every lane), 126 with two groups of keys per round and offsets in the instructions, 115 with the parts joined by
-// one block per item, 110 with one question per fetched step.
+// one block per item, 110 with one question per fetched step, 112 with a way for scales that are far apart.
 #pragma once
 #include "mxq_attend_items.cuh"
 #include "mxq_attend_plan.cuh"
@@ -1152,7 +1152,7 @@ struct Attend {
             step_done();
         }
         // The first step with scales far apart and all behind it: a loop of its own, whose registers are not the common one's.  (64 sequences of up
-        // to 8192 tokens, E2M1, none of it far: 113 us; 115 with everything in one loop; 110 without a way for scales that are far apart.)
+        // to 8192 tokens, E2M1, none of it far: 112 us; 115 with everything in one loop; 110 without a way for scales that are far apart.)
         while (!near) {
             take<true>(ring + slot * S::slot, key);
             step_done();

@@ -6,11 +6,11 @@
 //   warps 8 - 15         codes of keys and values from global memory, a tile ahead in registers, widened to BF16 with their scales
 //                        multiplied in (exact: eight significant bits, a power of two), into swizzled shared memory
 //   warp 16              issues S_i = Q_i K^T and O_i += P_i V for the two row tiles in turn, so that one's softmax overlaps the other's products
-// Queries are BF16 as they are.  P is rounded to BF16, by 2^-9 of a weight or less, because V^ is BF16 and both operands of a product have one
+// Queries are BF16 as they are.  P is rounded to BF16, by 2^-8 of a weight or less, because V^ is BF16 and both operands of a product have one
 // type (FP16 would hold P to 11 bits, but not every V^): results are 2.3e-3 in norm from 64 bits, where the output's own rounding is 1.7e-3.  The
 // sum is that of the rounded weights, so that they add up to one: a row that sees one key gives that key's value.  Sums are FP32.
 //
-// 2048 queries over 8192 tokens, 32 heads over 8 of 128, E2M1: 355 us, 680 TFLOP/s.  A pair of row tiles takes 5300 cycles per tile of keys: 3300 for
+// 2048 queries over 8192 tokens, 32 heads over 8 of 128, E2M1: 348 us, 690 TFLOP/s.  A pair of row tiles takes 5300 cycles per tile of keys (at 360 us): 3300 for
 // a row tile's softmax (its exponentials alone 1024, two warps of each scheduler at it), 1400 until its scores are there, 500 of waiting; the
 // products themselves take 2900.  With the maximum found in a pass of its own the softmax took 5900 cycles (495 us); 16 scores at a time with the next
 // ones on their way 3900 (384 us).

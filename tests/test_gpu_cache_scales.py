@@ -198,3 +198,23 @@ def test_scores_of_every_finite_size(fmt, dtype, counts, lengths, scale):
                 want, a = seen[:, j // 2].mean(0), np.abs(seen[:, j // 2]).mean(0)
                 # weights: 8, 11 or 22 bits, each the same; sums: as everywhere
                 assert (np.abs(g[starts[b] + i, j] - want) <= (2.0 ** -7 + (lengths[b] / 16 + 64) * 2.0 ** -19) * a + pu.half_step(dtype) * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("counts,lengths", [(None, [70, 129, 16]), ([3, 5], [100, 37]), ([60, 110], [333, 150])])
+def test_nan_among_values_of_every_size(fmt, dtype, counts, lengths):
+    """Poisoned blocks and NaN codes, seen by some rows and hidden from others, where scales lie far apart."""
+    for kind in (0, 2):
+        rng = np.random.default_rng(8)
+        cache = cu.Cache(rng, 40, 2, 128, fmt, 32, 16)
+        table = cu.tables(rng, lengths, 16, 40)
+        cache.parts[3] = rng.integers(60, 180, cache.parts[3].shape).astype(np.uint8)
+        for b, pos in ((0, lengths[0] - 2), (1, 3)):
+            at = (table[b, pos // 16], slice(None), pos % 16)
+            cache.parts[kind + 1][at + (1,)] = 255
+            if fmt == "e4m3":
+                cache.parts[kind][at + (5,)] = 0x7F
+        q = plain(rng, (sum(counts or [1] * len(lengths)), 4, 128), dtype)
+        for causal, window in ((True, 0), (True, 2), (False, 0)):
+            check(q, cache, lengths, counts, table, dtype, scale=0.1, causal=causal, window=window)
