@@ -90,6 +90,8 @@ join_kernel(const __grid_constant__ AttendArgs p, int dim)
 //   8 of 8192 E2M1                        48 / 95   71 / 95   73 / 93   97 / 96   99 / 96   123 / 95  172 / 98
 //   32 of 2048 E4M3                       55 / 128  86 / 129  90 / 128 117 / 130 119 / 131  153 / 131 216 / 133
 //   1 of 16384 INT8                       48 / 54   43 / 53   46 / 53   49 / 53   50 / 55   55 / 54   68 / 56
+// Where one sequence of 64 brings a piece of a prompt and the others one query each, 4096 E2M1 tokens: 256 queries (20 rows in the mean) 236 / 412, 512
+// (36) 338 / 432, 1024 (68) 528 / 482.
 constexpr size_t kManyColumns = 48;
 // Keys per CTA of a cluster, at most.  Clusters and runs with the second kernel, us: one sequence of 1000 E2M1 tokens, 8 heads of 128, 7.3 and 10.8, of
 // 16000 15.7 and 20.0; 8 of 2000 11.8 and 19.7; 32 of 2048 to 4096 E4M3 tokens, one head of 256, 22.6 and 33.2.  Lengths are known on the device
